@@ -20,7 +20,10 @@
  *     see (null pointer, negative size, bad layout).  Errors only the device can see (a block
  *     id out of range, a full table) are accumulated in the per-device status record and read
  *     with aibx_status_fetch.  Nothing aborts, throws or traps.
- *   - All arithmetic is integer; results are defined bit-exactly.
+ *   - Keys, index, routing and block copies: all arithmetic is integer and results are defined
+ *     bit-exactly.  So are the stored bytes of aibx_kv_append and the values of aibx_kv_read (one
+ *     rounding, to the nearest, ties to even).  aibx_attn_paged is the one call with floating
+ *     arithmetic of its own; it states what it rounds.
  *   - Threads: calls on different indexes, pools and streams may come from different host
  *     threads at any time (the few one-time per-device settings - kernel attributes, the address
  *     of the status record - are made under a lock or as single atomic words).  Calls on one
@@ -488,6 +491,124 @@ int32_t aibx_kv_scatter_inner(void* d_pool, const aibx_kv_layout_t* layout, int3
                               int32_t buf_inner, const uint32_t* d_block_ids, int64_t n,
                               const void* d_buf, void* stream);
 
+
+/* ---------------------------------------------------------------------------------------
+ * Tokens in and out of the pool, and attention over it (Section 3.2.5: the cache holds the K and
+ * V an engine computed so that later requests need not compute them again; these are the calls
+ * with which an engine fills the blocks that matching did not find and uses the ones it did).
+ *
+ * Cache: one layer of a pool whose tiles follow `layout` and `inner`, with rows of `type`:
+ *   AIBX_TYPE_BF16 / AIBX_TYPE_FP16   elem_bytes 2
+ *   AIBX_TYPE_E4M3                    elem_bytes 1 and one scale byte s per row of head_dim
+ *                                     elements: element value = e4m3 value * 2^(s - 127)
+ *                                     (s = 255: NaN; s = 0: 2^-127)
+ *   The scale bytes lie in `d_scales` exactly as the rows lie in the pool: it is a pool of the
+ *   same layout with head_dim 1 and elem_bytes 1, so aibx_kv_gather and its kin move it with that
+ *   layout and the same block ids (whenever num_kv_heads * block_tokens is a multiple of 8).
+ * Batch: R requests.  Request r has n_r = d_tok_off[r+1] - d_tok_off[r] tokens in the call, rows
+ *   d_tok_off[r] .. of every per-token tensor; they are the LAST n_r of its kv_len[r] tokens, so
+ *   token i of request r has position kv_len[r] - n_r + i and lives in slot position mod
+ *   block_tokens of block table[r][position / block_tokens].
+ *     d_block_table  uint32 block ids; row r starts at r * table_stride and has table_stride
+ *                    entries, or, when d_blk_off (int64 [R+1]) is given, starts at d_blk_off[r]
+ *                    and ends at d_blk_off[r+1]
+ *     d_tok_off      int64 [R+1], prefix sum of n_r, d_tok_off[0] = 0 (n_r = 0 is fine)
+ *     d_kv_len       int32 [R]
+ *     n_tokens       rows of the per-token tensors; at least d_tok_off[R].  Rows behind the last
+ *                    request are left as they are
+ *     max_new        a bound on n_r that the caller knows (it selects kernels), or 0
+ *   Requests may share blocks that are only read.
+ *   A position whose table entry is AIBX_NO_BLOCK is skipped silently; one whose entry is another
+ *   id >= num_blocks, or that lies behind the row's entries, is skipped and raises RANGE.  A
+ *   negative position (kv_len < n_r) is skipped.
+ * Common errors: INVALID for null pointers (when there is work), negative counts, a layer outside
+ *   the pool, elem_bytes that is not the type's, an unaligned pool; UNSUPPORTED for head_dim > 1024
+ *   or not a multiple of 8, rows that are no multiple of 16 bytes, more than 4096 heads or
+ *   65536 slots per block.  R = 0 or n_tokens = 0 is a no-op.
+ */
+#define AIBX_TYPE_BF16 0
+#define AIBX_TYPE_FP16 1
+#define AIBX_TYPE_FP32 2
+#define AIBX_TYPE_E4M3 3
+
+typedef struct {
+  void* d_pool;
+  uint8_t* d_scales;          /* AIBX_TYPE_E4M3 only */
+  aibx_kv_layout_t layout;
+  int32_t type;
+  int32_t inner;              /* AIBX_INNER_* */
+  int32_t layer;
+} aibx_kv_cache_t;
+
+typedef struct {
+  const uint32_t* d_block_table;
+  const int64_t* d_blk_off;   /* null: rows of table_stride entries */
+  int64_t table_stride;
+  const int64_t* d_tok_off;
+  const int32_t* d_kv_len;
+  int64_t n_tokens;
+  int32_t R;
+  int32_t max_new;
+} aibx_kv_batch_t;
+
+/* append: K and V rows of the call's tokens into their slots.  d_k, d_v: [n_tokens][heads][dim] in
+ *   `type` (BF16, FP16 or FP32), element strides per token and per head given, elements of a row
+ *   adjacent.  16-bit pools: rounded to the pool's type.  E4M3 pools: per row, with a = largest
+ *   finite magnitude, s = 127 + the least e with a <= 448 * 2^e (at least 1; 127 if there is none
+ *   or a = 0); elements rounded to e4m3 after multiplication by 2^(127 - s); NaN and infinities
+ *   become NaN.  Two tokens of a call must not share a slot.
+ * read: the inverse into d_k, d_v of `type`, rounded once.  The same arguments.
+ */
+int32_t aibx_kv_append(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch, const void* d_k,
+                       int64_t k_token_stride, int64_t k_head_stride, const void* d_v,
+                       int64_t v_token_stride, int64_t v_head_stride, int32_t type, void* stream);
+int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch, void* d_k,
+                     int64_t k_token_stride, int64_t k_head_stride, void* d_v,
+                     int64_t v_token_stride, int64_t v_head_stride, int32_t type, void* stream);
+
+/* attn_paged: attention of the call's tokens over their request's cache (which holds the call's own
+ *   K and V already).  Query head h reads KV head h / (num_q_heads / num_kv_heads).  For a query
+ *   at position p the visible keys are the positions j with 0 <= j < kv_len, j <= p (causal only),
+ *   j > p - window (window > 0 only) and a block that is there (see above);
+ *     out = sum_j w_j v_j,   w = softmax_j(scale * q . k_j),   lse = ln sum_j exp(scale * q . k_j).
+ *   A row that sees no key gives out = 0 and lse = -infinity.
+ *   q, out: [n_tokens][num_q_heads][head_dim] of type q_type (BF16 or FP16, the pool's type unless
+ *   the pool is E4M3) with element strides per token and head, 16-byte aligned rows.  d_lse
+ *   (nullable): float [n_tokens][num_q_heads].
+ *   Products are accumulated in fp32; the weights are rounded to q_type (to fp16 over an E4M3
+ *   pool, whose queries are held as fp16 times a power of two per row) before they multiply V; sums
+ *   and maxima of the softmax stay in fp32; the result is rounded once.  Two calls on the same
+ *   inputs give the same bits.
+ *   What lies in slots that no visible position names (stale bytes, NaN) does not matter.  NaN or
+ *   infinite K of a position hidden from a row does not reach it; a NaN or infinite V of a
+ *   position that only some of a request's rows see may reach the others.  Over an E4M3 pool V
+ *   scales below 2^-100 count as 2^-100.
+ * Shapes: head_dim 64 or 128, block_tokens a multiple of 8, at most 128 query heads per KV head:
+ *   UNSUPPORTED otherwise.  INVALID for unaligned q or out, strides that are no multiple of 8
+ *   elements, scale negative or not finite, num_q_heads no multiple of num_kv_heads, a window < 0,
+ *   a workspace that is too small.
+ * Workspace: aibx_attn_workspace_bytes(cache, batch, params) bytes, 16-byte aligned, content
+ *   irrelevant before and after; calls that may overlap on the GPU need separate ones.
+ *   The answer depends on head_dim, num_q_heads / num_kv_heads and max_new alone (0 = arguments
+ *   that attn_paged would refuse).
+ * RANGE is raised at least once for every request with a bad entry among the blocks that it reads,
+ *   and for a request with more than max_new > 0 tokens (whose rows may be left unwritten).
+ */
+typedef struct {
+  int32_t q_type;
+  int32_t num_q_heads;
+  int64_t q_token_stride, q_head_stride;
+  int64_t out_token_stride, out_head_stride;
+  float scale;
+  int32_t causal;
+  int32_t window;
+} aibx_attn_params_t;
+
+uint64_t aibx_attn_workspace_bytes(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
+                                   const aibx_attn_params_t* params);
+int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
+                        const aibx_attn_params_t* params, const void* d_q, void* d_out,
+                        float* d_lse, void* d_workspace, uint64_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
  * Device status of the current device: the most severe (most negative) code recorded by any

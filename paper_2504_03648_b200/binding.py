@@ -21,6 +21,8 @@ ERR_INVALID, ERR_RANGE, ERR_FULL, ERR_CUDA, ERR_UNSUPPORTED, ERR_NOMEM, ERR_TIME
     -1, -2, -3, -4, -5, -6, -7)
 NO_BLOCK = 0xFFFFFFFF
 NO_POD = -1
+TYPE_BF16, TYPE_FP16, TYPE_FP32, TYPE_E4M3 = range(4)
+_TYPE_OF = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16, torch.float32: TYPE_FP32}
 
 
 class AibxError(RuntimeError):
@@ -51,6 +53,24 @@ class KVLayout(C.Structure):
     @property
     def block_bytes(self) -> int:
         return self.num_layers * self.tile_bytes
+
+
+class _CacheC(C.Structure):
+    _fields_ = [("d_pool", C.c_void_p), ("d_scales", C.c_void_p), ("layout", KVLayout),
+                ("type", C.c_int32), ("inner", C.c_int32), ("layer", C.c_int32)]
+
+
+class _BatchC(C.Structure):
+    _fields_ = [("d_block_table", C.c_void_p), ("d_blk_off", C.c_void_p),
+                ("table_stride", C.c_int64), ("d_tok_off", C.c_void_p), ("d_kv_len", C.c_void_p),
+                ("n_tokens", C.c_int64), ("R", C.c_int32), ("max_new", C.c_int32)]
+
+
+class _AttnC(C.Structure):
+    _fields_ = [("q_type", C.c_int32), ("num_q_heads", C.c_int32), ("q_token_stride", C.c_int64),
+                ("q_head_stride", C.c_int64), ("out_token_stride", C.c_int64),
+                ("out_head_stride", C.c_int64), ("scale", C.c_float), ("causal", C.c_int32),
+                ("window", C.c_int32)]
 
 
 class PodMetrics(C.Structure):
@@ -115,6 +135,12 @@ def lib():
             "aibx_kv_scatter_counted": [vp, C.POINTER(KVLayout), vp, i64, vp, vp, vp],
             "aibx_kv_gather_inner": [vp, C.POINTER(KVLayout), i32, i32, vp, i64, vp, vp],
             "aibx_kv_scatter_inner": [vp, C.POINTER(KVLayout), i32, i32, vp, i64, vp, vp],
+            "aibx_kv_append": [C.POINTER(_CacheC), C.POINTER(_BatchC), vp, i64, i64, vp, i64, i64,
+                               i32, vp],
+            "aibx_kv_read": [C.POINTER(_CacheC), C.POINTER(_BatchC), vp, i64, i64, vp, i64, i64,
+                             i32, vp],
+            "aibx_attn_paged": [C.POINTER(_CacheC), C.POINTER(_BatchC), C.POINTER(_AttnC), vp, vp,
+                                vp, vp, u64, vp],
             "aibx_kv_set_tuning": [i32, i32, i32, i32],
             "aibx_kv_set_store_lag": [i32],
             "aibx_kv_get_tuning": [vp, vp, vp, vp, vp],
@@ -126,6 +152,9 @@ def lib():
             fn = getattr(L, name)
             fn.argtypes = args
             fn.restype = i32
+        L.aibx_attn_workspace_bytes.argtypes = [C.POINTER(_CacheC), C.POINTER(_BatchC),
+                                                C.POINTER(_AttnC)]
+        L.aibx_attn_workspace_bytes.restype = u64
         L.aibx_collect_scratch_bytes.argtypes = [u32]
         L.aibx_collect_scratch_bytes.restype = u64
         L.aibx_route_collect_scratch_bytes.argtypes = [u32]
@@ -462,6 +491,137 @@ def kv_scatter_inner(pool, layout: KVLayout, pool_inner: int, buf_inner: int, bl
     _check("aibx_kv_scatter_inner", lib().aibx_kv_scatter_inner(
         _ptr(pool), C.byref(layout), pool_inner, buf_inner, _ptr(block_ids, torch.uint32), n,
         _ptr(buf), _stream()))
+
+
+class KVCache:
+    """One layer of a paged pool whose rows have a type (aibx_kv_cache_t).  `pool` is the pool as
+    kv_gather takes it (any dtype), `scales` the byte pool of an e4m3 one.  Setting `layer` moves
+    the view to another layer."""
+
+    def __init__(self, pool, layout: KVLayout, type: int, scales=None, inner: int = 0,
+                 layer: int = 0):
+        self._keep = (pool, scales)
+        self.device = pool.device
+        _same_device(pool, scales)
+        # a pool that is smaller than its layout says is a fault waiting to happen
+        if pool.numel() * pool.element_size() < layout.num_blocks * layout.block_bytes:
+            raise ValueError("pool of %d bytes, layout of %d" % (
+                pool.numel() * pool.element_size(), layout.num_blocks * layout.block_bytes))
+        if scales is not None and layout.head_dim > 0 and layout.elem_bytes > 0 and scales.numel() < \
+                layout.num_blocks * layout.block_bytes // (layout.head_dim * layout.elem_bytes):
+            raise ValueError("fewer scale bytes than rows")
+        self._c = _CacheC(_ptr(pool), _ptr(scales, torch.uint8), layout, type, inner, layer)
+        self._ref = C.byref(self._c)
+
+    @property
+    def layout(self) -> KVLayout:
+        return self._c.layout
+
+    @property
+    def layer(self) -> int:
+        return self._c.layer
+
+    @layer.setter
+    def layer(self, n: int) -> None:
+        self._c.layer = n
+
+
+class KVBatch:
+    """Which tokens of which requests a call is about (aibx_kv_batch_t): the last
+    tok_off[r+1] - tok_off[r] of request r's kv_len[r] tokens.  block_table: uint32 [R, width], or
+    flat with blk_off (int64 [R+1]).  n_tokens: rows of the per-token tensors.  max_new: a bound on
+    the tokens of one request, if known."""
+
+    def __init__(self, block_table, tok_off, kv_len, n_tokens: int, max_new: int = 0, blk_off=None):
+        R = kv_len.numel()
+        if tok_off.numel() != R + 1 or (blk_off is not None and blk_off.numel() != R + 1):
+            raise ValueError("offsets of %d requests expected" % R)
+        if blk_off is None and (block_table.dim() != 2 or block_table.shape[0] != R):
+            raise ValueError("a block table of %d rows expected" % R)
+        _same_device(block_table, tok_off, kv_len, blk_off)
+        self._keep = (block_table, tok_off, kv_len, blk_off)
+        self.device = kv_len.device
+        self.n_tokens = n_tokens
+        self._c = _BatchC(_ptr(block_table, torch.uint32), _ptr(blk_off, torch.int64),
+                          0 if blk_off is not None else block_table.shape[1],
+                          _ptr(tok_off, torch.int64), _ptr(kv_len, torch.int32), n_tokens, R,
+                          max_new)
+        self._ref = C.byref(self._c)
+
+
+def _same_device(*tensors) -> None:
+    for t in tensors:
+        if t is not None and t.device != tensors[0].device:
+            raise ValueError("tensors on %s and on %s" % (tensors[0].device, t.device))
+
+
+def _rows(t, cache: KVCache, batch: KVBatch, heads=None):
+    """(pointer, token stride, head stride) of a [n_tokens, heads, head_dim] tensor."""
+    if t.dim() != 3 or t.shape[0] != batch.n_tokens or t.shape[2] != cache._c.layout.head_dim or \
+            (heads is not None and t.shape[1] != heads) or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError("rows of [%d, %s, %d] expected, got %s with strides %s" % (
+            batch.n_tokens, heads if heads is not None else "heads", cache._c.layout.head_dim,
+            tuple(t.shape), t.stride()))
+    if not t.is_cuda or t.device != cache.device or t.device != batch.device:
+        raise ValueError("all tensors of a call live on one CUDA device")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _current(cache: KVCache) -> None:
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError("the call works on the current device (%d), the pool is on %s" % (
+            torch.cuda.current_device(), cache.device))
+
+
+def _kv_tokens(name: str, cache: KVCache, batch: KVBatch, k, v) -> None:
+    heads = cache._c.layout.num_kv_heads
+    if k.dtype != v.dtype or k.dtype not in _TYPE_OF:
+        raise ValueError("K and V of one of bfloat16, float16, float32 expected")
+    _current(cache)
+    _check(name, getattr(lib(), name)(
+        cache._ref, batch._ref, *_rows(k, cache, batch, heads), *_rows(v, cache, batch, heads),
+        _TYPE_OF[k.dtype], _stream()))
+
+
+def kv_append(cache: KVCache, batch: KVBatch, k, v) -> None:
+    """Write the batch's tokens (k, v: [n_tokens, kv_heads, head_dim], rows adjacent, other strides
+    free) into their slots, quantised where the pool is e4m3."""
+    _kv_tokens("aibx_kv_append", cache, batch, k, v)
+
+
+def kv_read(cache: KVCache, batch: KVBatch, k, v) -> None:
+    """Read the batch's tokens back into k, v (bfloat16, float16 or float32)."""
+    _kv_tokens("aibx_kv_read", cache, batch, k, v)
+
+
+def attn_paged(cache: KVCache, batch: KVBatch, q, out, lse=None, scale=None, causal: bool = True,
+               window: int = 0, workspace=None) -> None:
+    """Attention of the batch's tokens over their requests' cached keys.  q, out: [n_tokens,
+    q_heads, head_dim]; lse: float32 [n_tokens, q_heads] or None; scale: 1/sqrt(head_dim) if None.
+    workspace: uint8 tensor of attn_workspace_bytes(...) bytes, allocated here if None."""
+    if q.dtype != out.dtype or q.dtype not in _TYPE_OF:
+        raise ValueError("queries and output of one type expected")
+    heads = q.shape[1] if q.dim() == 3 else 0
+    qp, qt, qh = _rows(q, cache, batch, heads)
+    op, ot, oh = _rows(out, cache, batch, heads)
+    if lse is not None and (lse.shape != q.shape[:2] or lse.device != q.device):
+        raise ValueError("lse of [n_tokens, q_heads] expected")
+    _current(cache)
+    prm = _AttnC(_TYPE_OF[q.dtype], heads, qt, qh, ot, oh,
+                 cache._c.layout.head_dim ** -0.5 if scale is None else scale, bool(causal), window)
+    L = lib()
+    if workspace is None:
+        need = L.aibx_attn_workspace_bytes(cache._ref, batch._ref, prm)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    _check("aibx_attn_paged", L.aibx_attn_paged(
+        cache._ref, batch._ref, prm, qp, op, _ptr(lse, torch.float32), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream()))
+
+
+def attn_workspace_bytes(cache: KVCache, batch: KVBatch, q) -> int:
+    """Workspace of attn_paged for queries shaped like q; 0 where attn_paged would refuse."""
+    prm = _AttnC(_TYPE_OF.get(q.dtype, -1), q.shape[1], 8, 8, 8, 8, 1.0, 1, 0)
+    return int(lib().aibx_attn_workspace_bytes(cache._ref, batch._ref, prm))
 
 
 def kv_set_tuning(mode: int = -1, chunk_bytes: int = 0, stages: int = 0,

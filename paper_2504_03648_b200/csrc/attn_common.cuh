@@ -1,0 +1,214 @@
+// What the two kernels of attn_paged share: the call's arguments, how its work is cut and handed
+// out, the tensor map of the pool, and the kernel that joins cut rows.
+//
+// Work is a line of KV tiles: request by request, KV head by KV head, (row block by row block,)
+// tile by tile.  CTA c of the persistent grid takes the c-th equal piece of that line, whatever
+// the requests' lengths are: no CTA waits for a long request, and the host needs to know no
+// length.  A piece that begins or ends inside a (request, head, row block) leaves unnormalised
+// sums with their maximum in one of the CTA's two workspace slots; attn_join_kernel adds those
+// up in line order, so the result does not depend on timing.
+#pragma once
+
+#include "kv_paged.cuh"
+
+namespace aibx {
+
+struct AttnArgs {
+  PagedPool pool;
+  PagedBatch b;
+  const char* q;
+  char* out;
+  float* lse;
+  long long q_tok, q_head, o_tok, o_head;   // element strides
+  float scale_log2;                         // scale * log2(e): scores in powers of two
+  int G;                                    // query heads per KV head
+  int causal, window;
+  int box;                                  // tokens one tensor-map box covers
+  int check_bound;                          // report requests this call has no kernel for
+  float* slots;
+};
+
+constexpr int kRowsMax = 16;                // rows (tokens * G) the row kernel takes per request
+
+struct AttnRequest {
+  long long tok0;     // first row of the per-token tensors
+  int n;              // new tokens
+  int len;            // tokens in the cache
+  int keys;           // of them, those the table has entries for
+};
+
+__device__ __forceinline__ AttnRequest attn_request(const PagedBatch& b, int T, int r) {
+  AttnRequest q;
+  q.tok0 = __ldg(b.tok_off + r);
+  long long n = __ldg(b.tok_off + r + 1) - q.tok0;
+  if (q.tok0 < 0) n = 0;
+  if (n > b.n_tokens - q.tok0) n = b.n_tokens - q.tok0;
+  q.n = n > 0 ? (int)n : 0;
+  q.len = max(__ldg(b.kv_len + r), 0);
+  const uint32_t* row;
+  long long entries;
+  table_row(b, r, row, entries);
+  const long long cap = entries * T;
+  q.keys = cap < q.len ? (int)max(cap, 0LL) : q.len;
+  return q;
+}
+
+// Block-wide sum and exclusive prefix of one value per thread (N threads, scratch[33]).
+template <int N>
+__device__ __forceinline__ long long block_prefix(long long v, long long* scratch, long long& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long inc = v;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long up = (long long)shfl_up64((uint64_t)inc, d);
+    if (lane >= d) inc += up;
+  }
+  if (lane == 31) scratch[warp] = inc;
+  __syncthreads();
+  long long before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < N / 32; ++w) {
+    const long long s = scratch[w];
+    if (w < warp) before += s;
+    all += s;
+  }
+  __syncthreads();
+  total = all;
+  return before + inc - v;
+}
+
+struct WorkStart {
+  long long total;      // tiles of the whole line
+  long long base;       // first position of request r's part of the line
+  int r;                // request in which this CTA's piece begins
+};
+
+// Finds the request that holds position `index * per` of the line, per = ceil(total / pieces).
+// cost(r) = tiles of request r over all heads.  All N threads take part.
+template <int N, typename Cost>
+__device__ __forceinline__ WorkStart locate_piece(int R, unsigned int index, unsigned int pieces,
+                                                  long long* scratch, WorkStart* shared,
+                                                  const Cost& cost) {
+  const int tid = threadIdx.x;
+  const bool one = R <= N;                 // every request has a thread: one look at each
+  long long mine = 0, total, base = 0;
+  for (int r = tid; r < R; r += N) mine += cost(r);
+  long long before = block_prefix<N>(mine, scratch, total);
+  const long long per = (total + pieces - 1) / pieces;
+  const long long target = per * index;
+  if (tid == 0) {
+    shared->total = total;
+    shared->base = 0;
+    shared->r = -1;                        // past the end: nothing to do
+  }
+  __syncthreads();
+  if (target < total) {
+    if (one) {
+      if (mine > 0 && before <= target && target < before + mine) {
+        shared->base = before;
+        shared->r = tid;
+      }
+    } else {
+      for (int r0 = 0; r0 < R; r0 += N) {
+        const long long v = r0 + tid < R ? cost(r0 + tid) : 0;
+        long long sum;
+        before = base + block_prefix<N>(v, scratch, sum);
+        if (v > 0 && before <= target && target < before + v) {
+          shared->base = before;
+          shared->r = r0 + tid;
+        }
+        base += sum;
+        if (base > target) break;
+      }
+    }
+  }
+  __syncthreads();
+  return *shared;
+}
+
+// ------------------------------------------------------------------------------------------
+// tensor map of a pool's layer: (element, slot, head, block, K/V)
+
+__device__ __forceinline__ void tensor_load_5d(unsigned int dst, const CUtensorMap* map,
+                                               unsigned int bar, int x, int slot, int head,
+                                               int block, int kv) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(slot), "r"(head), "r"(block), "r"(kv)
+      : "memory");
+}
+
+// 16-bit rows are cut into 128-byte columns whose 16-byte pieces are XORed with the row's place
+// among eight (128-byte swizzle); so is a 128-byte e4m3 row.  64-byte rows stay as they are.
+inline int32_t pool_tensor_map(const PagedPool& p, int type, int box, CUtensorMap* map) {
+  const EncodeTiledFn encode = encode_tiled_fn();
+  if (!encode) return AIBX_ERR_CUDA;
+  const int size = type_bytes(type);
+  const int col = p.D * size < 128 ? p.D * size : 128;
+  const cuuint64_t dims[5] = {(cuuint64_t)p.D, (cuuint64_t)p.T, (cuuint64_t)p.H,
+                              (cuuint64_t)p.num_blocks, 2};
+  const cuuint64_t strides[4] = {(cuuint64_t)p.slot, (cuuint64_t)p.head, (cuuint64_t)p.block,
+                                 (cuuint64_t)p.kv};
+  const cuuint32_t bx[5] = {(cuuint32_t)(col / size), (cuuint32_t)box, 1, 1, 1};
+  const cuuint32_t es[5] = {1, 1, 1, 1, 1};
+  const CUtensorMapDataType dt = type == AIBX_TYPE_BF16   ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                 : type == AIBX_TYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                          : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+  if (encode(map, dt, 5, p.base, dims, strides, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             col == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return AIBX_ERR_UNSUPPORTED;
+  return AIBX_OK;
+}
+
+inline int gcd_int(int a, int b) {
+  while (b) {
+    const int t = a % b;
+    a = b;
+    b = t;
+  }
+  return a;
+}
+
+// ------------------------------------------------------------------------------------------
+// numbers
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <typename T>
+struct Bits16;
+template <>
+struct Bits16<__nv_bfloat16> {
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) {
+    return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w));
+  }
+};
+template <>
+struct Bits16<__half> {
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) {
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  }
+};
+
+// 2^-k and 2^k for the power k that brings a magnitude into [1, 2); k = 0 for 0, kept in range.
+__device__ __forceinline__ void power_scale(float amax, float& down, float& up) {
+  int k = (int)(__float_as_uint(amax) >> 23) - 127;
+  if (!(amax > 0.0f)) k = 0;
+  k = max(-120, min(k, 120));
+  down = __uint_as_float((unsigned int)(127 - k) << 23);
+  up = __uint_as_float((unsigned int)(127 + k) << 23);
+}
+
+}  // namespace aibx

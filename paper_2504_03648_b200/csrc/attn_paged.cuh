@@ -1,0 +1,64 @@
+// Host side of attn_paged: checks, the choice of kernels and the workspace.
+#pragma once
+
+#include <math.h>
+
+#include "attn_rows.cuh"
+
+namespace aibx {
+
+struct AttnPlan {
+  int G = 0;
+  bool rows = false, tiles = false;      // which kernels run
+  uint64_t rows_bytes = 0, workspace = 0;
+};
+
+// The row kernel alone where no request can have more than kRowsMax rows; the tile kernel alone
+// for a single request; both for a batch, each taking the requests of its kind.
+inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
+                         const aibx_attn_params_t* p, AttnPlan& plan) {
+  PagedPool pool;
+  PagedBatch batch;
+  bool work;
+  const int32_t rc = paged_views(c, b, pool, batch, work);
+  if (rc != AIBX_OK) return rc;
+  if (!p) return AIBX_ERR_INVALID;
+  const aibx_kv_layout_t& L = c->layout;
+  if (p->q_type != AIBX_TYPE_BF16 && p->q_type != AIBX_TYPE_FP16) return AIBX_ERR_INVALID;
+  if (p->num_q_heads <= 0 || p->num_q_heads % L.num_kv_heads != 0 || p->window < 0 ||
+      !(p->scale >= 0.0f) || !isfinite(p->scale))
+    return AIBX_ERR_INVALID;
+  const long long strides[4] = {p->q_token_stride, p->q_head_stride, p->out_token_stride,
+                                p->out_head_stride};
+  for (long long s : strides)
+    if (s < 0 || s % 8 != 0) return AIBX_ERR_INVALID;
+  if (c->type != AIBX_TYPE_E4M3 && c->type != p->q_type) return AIBX_ERR_UNSUPPORTED;
+  if ((L.head_dim != 64 && L.head_dim != 128) || L.block_tokens % 8 != 0) return AIBX_ERR_UNSUPPORTED;
+  plan.G = p->num_q_heads / L.num_kv_heads;
+  if (plan.G > 128) return AIBX_ERR_UNSUPPORTED;
+  const long long bound = b->max_new > 0 ? b->max_new : (1LL << 31);
+  plan.tiles = bound * plan.G > kRowsMax;
+  plan.rows = !plan.tiles;
+  plan.rows_bytes = 2ull * sm_count() * kRowsMax * (L.head_dim + 2) * sizeof(float);
+  plan.workspace = plan.rows_bytes;
+  return AIBX_OK;
+}
+
+template <int D>
+inline int32_t launch_attn_dim(const AttnArgs& a, int type, int q_type, const AttnPlan& plan,
+                               cudaStream_t st) {
+  if (plan.tiles) return AIBX_ERR_UNSUPPORTED;
+  if (type == AIBX_TYPE_E4M3)
+    return q_type == AIBX_TYPE_BF16 ? launch_attn_rows<D, true, __nv_bfloat16>(a, type, st)
+                                    : launch_attn_rows<D, true, __half>(a, type, st);
+  return q_type == AIBX_TYPE_BF16 ? launch_attn_rows<D, false, __nv_bfloat16>(a, type, st)
+                                  : launch_attn_rows<D, false, __half>(a, type, st);
+}
+
+inline int32_t launch_attn(const AttnArgs& a, int type, int q_type, const AttnPlan& plan,
+                           cudaStream_t st) {
+  return a.pool.D == 64 ? launch_attn_dim<64>(a, type, q_type, plan, st)
+                        : launch_attn_dim<128>(a, type, q_type, plan, st);
+}
+
+}  // namespace aibx

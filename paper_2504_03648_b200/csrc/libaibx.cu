@@ -7,10 +7,12 @@
 #include "aibx.h"
 #include "aibx_tuning.h"
 #include "aibx_common.cuh"
+#include "attn_paged.cuh"
 #include "collect_blocks.cuh"
 #include "hash_blocks.cuh"
 #include "index.cuh"
 #include "kv_copy.cuh"
+#include "kv_paged.cuh"
 #include "kv_permute.cuh"
 #include "selftest.cuh"
 #include "route_head.cuh"
@@ -875,6 +877,63 @@ int32_t aibx_kv_scatter_inner(void* d_pool, const aibx_kv_layout_t* layout, int3
   AIBX_CALL_RANGE();
   return launch_kv_permute(d_pool, layout, pool_inner, buf_inner, d_block_ids, n, d_buf, 1,
                            as_stream(stream));
+}
+
+int32_t aibx_kv_append(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch, const void* d_k,
+                       int64_t k_token_stride, int64_t k_head_stride, const void* d_v,
+                       int64_t v_token_stride, int64_t v_head_stride, int32_t type, void* stream) {
+  AIBX_CALL_RANGE();
+  return kv_tokens<true>(cache, batch, d_k, k_token_stride, k_head_stride, d_v, v_token_stride,
+                         v_head_stride, type, as_stream(stream));
+}
+
+int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch, void* d_k,
+                     int64_t k_token_stride, int64_t k_head_stride, void* d_v,
+                     int64_t v_token_stride, int64_t v_head_stride, int32_t type, void* stream) {
+  AIBX_CALL_RANGE();
+  return kv_tokens<false>(cache, batch, d_k, k_token_stride, k_head_stride, d_v, v_token_stride,
+                          v_head_stride, type, as_stream(stream));
+}
+
+uint64_t aibx_attn_workspace_bytes(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
+                                   const aibx_attn_params_t* params) {
+  AttnPlan plan;
+  if (attn_plan(cache, batch, params, plan) != AIBX_OK) return 0;
+  return plan.workspace;
+}
+
+int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
+                        const aibx_attn_params_t* params, const void* d_q, void* d_out,
+                        float* d_lse, void* d_workspace, uint64_t workspace_bytes, void* stream) {
+  AIBX_CALL_RANGE();
+  AttnPlan plan;
+  int32_t rc = attn_plan(cache, batch, params, plan);
+  if (rc != AIBX_OK) return rc;
+  AttnArgs a;
+  bool work;
+  rc = paged_views(cache, batch, a.pool, a.b, work);
+  if (rc != AIBX_OK || !work) return rc;
+  if (!d_q || !d_out || !d_workspace) return AIBX_ERR_INVALID;
+  if ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_out) |
+       reinterpret_cast<uintptr_t>(d_workspace)) & 15)
+    return AIBX_ERR_INVALID;
+  if ((reinterpret_cast<uintptr_t>(d_lse) & 3) || workspace_bytes < plan.workspace)
+    return AIBX_ERR_INVALID;
+  a.q = static_cast<const char*>(d_q);
+  a.out = static_cast<char*>(d_out);
+  a.lse = d_lse;
+  a.q_tok = params->q_token_stride;
+  a.q_head = params->q_head_stride;
+  a.o_tok = params->out_token_stride;
+  a.o_head = params->out_head_stride;
+  a.scale_log2 = params->scale * 1.4426950408889634f;
+  a.G = plan.G;
+  a.causal = params->causal != 0;
+  a.window = params->window;
+  a.box = 0;
+  a.check_bound = !plan.tiles;
+  a.slots = static_cast<float*>(d_workspace);
+  return launch_attn(a, cache->type, params->q_type, plan, as_stream(stream));
 }
 
 int32_t aibx_kv_set_tuning(int32_t mode, int32_t chunk_bytes, int32_t stages,
