@@ -582,10 +582,10 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  *   What lies in slots that no visible position names (stale bytes, NaN) does not matter.  NaN or
  *   infinite K of a position hidden from a row does not reach it; a NaN or infinite V of a
  *   position that only some of a request's rows see may reach the others.  Over an E4M3 pool V
- *   scales below 2^-100 count as 2^-100.
- * Shapes: head_dim 64 or 128, block_tokens a multiple of 8, at most 128 query heads per KV head:
- *   UNSUPPORTED otherwise.  INVALID for unaligned q or out, strides that are no multiple of 8
- *   elements, scale negative or not finite, num_q_heads no multiple of num_kv_heads, a window < 0,
+ *   scales below 2^-100 may count as 2^-100 (an error below 2^-91).
+ * Shapes: head_dim 64 or 128, block_tokens a multiple of 8, at most 128 query heads per KV head,
+ *   num_blocks below 2^31: UNSUPPORTED otherwise.  INVALID for unaligned q or out, strides that are no multiple of 8
+ *   elements, a scale that is not positive and finite, num_q_heads no multiple of num_kv_heads, a window < 0,
  *   a workspace that is too small.
  * Workspace: aibx_attn_workspace_bytes(cache, batch, params) bytes, 16-byte aligned, content
  *   irrelevant before and after; calls that may overlap on the GPU need separate ones.

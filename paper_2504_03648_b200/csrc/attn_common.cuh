@@ -25,6 +25,7 @@ struct AttnArgs {
   int causal, window;
   int box;                                  // tokens one tensor-map box covers
   int check_bound;                          // report requests this call has no kernel for
+  int rows_too;                             // the row kernel runs in this call as well
   float* slots;
 };
 
@@ -124,6 +125,34 @@ __device__ __forceinline__ WorkStart locate_piece(int R, unsigned int index, uns
   }
   __syncthreads();
   return *shared;
+}
+
+// Waits for a phase of an mbarrier, at most two seconds; then (or once another warp has given up)
+// the CTA's abort flag is set, TIMEOUT is in the device status, and every later wait returns at
+// once: roles run to their end on whatever is in memory, and nobody is left at a barrier.
+__device__ __forceinline__ bool ring_wait(unsigned int bar, unsigned int parity, volatile int* abort_flag) {
+  if (mbar_try_wait(bar, parity)) return true;
+  unsigned long long t0 = 0;
+  for (unsigned int spins = 1;; ++spins) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((spins & 63u) == 0) {
+      if (*abort_flag) return false;
+      unsigned long long now;
+      asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+      if (t0 == 0) t0 = now;
+      if (now - t0 > 2000000000ull) {
+        if (!*abort_flag) raise_status(AIBX_ERR_TIMEOUT);
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+}
+
+// The same for copies that must have landed before a CTA ends.
+__device__ __forceinline__ void ring_drain(unsigned int bar, unsigned int parity) {
+  for (unsigned int spins = 0; spins < (1u << 14) && !mbar_try_wait(bar, parity); ++spins) {
+  }
 }
 
 // ------------------------------------------------------------------------------------------

@@ -3,7 +3,7 @@
 
 #include <math.h>
 
-#include "attn_rows.cuh"
+#include "attn_tiles.cuh"
 
 namespace aibx {
 
@@ -26,7 +26,7 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
   const aibx_kv_layout_t& L = c->layout;
   if (p->q_type != AIBX_TYPE_BF16 && p->q_type != AIBX_TYPE_FP16) return AIBX_ERR_INVALID;
   if (p->num_q_heads <= 0 || p->num_q_heads % L.num_kv_heads != 0 || p->window < 0 ||
-      !(p->scale >= 0.0f) || !isfinite(p->scale))
+      !(p->scale > 0.0f) || !isfinite(p->scale))
     return AIBX_ERR_INVALID;
   const long long strides[4] = {p->q_token_stride, p->q_head_stride, p->out_token_stride,
                                 p->out_head_stride};
@@ -35,24 +35,34 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
   if (c->type != AIBX_TYPE_E4M3 && c->type != p->q_type) return AIBX_ERR_UNSUPPORTED;
   if ((L.head_dim != 64 && L.head_dim != 128) || L.block_tokens % 8 != 0) return AIBX_ERR_UNSUPPORTED;
   plan.G = p->num_q_heads / L.num_kv_heads;
-  if (plan.G > 128) return AIBX_ERR_UNSUPPORTED;
+  if (plan.G > 128 || L.num_blocks > 0x7fffffffu) return AIBX_ERR_UNSUPPORTED;
   const long long bound = b->max_new > 0 ? b->max_new : (1LL << 31);
   plan.tiles = bound * plan.G > kRowsMax;
-  plan.rows = !plan.tiles;
+  plan.rows = !plan.tiles || b->R > 1;
   plan.rows_bytes = 2ull * sm_count() * kRowsMax * (L.head_dim + 2) * sizeof(float);
-  plan.workspace = plan.rows_bytes;
+  plan.workspace = plan.rows ? plan.rows_bytes : 0;
+  if (plan.tiles) plan.workspace += 2ull * sm_count() * 2 * kTileRows * (L.head_dim + 2) * sizeof(float);
   return AIBX_OK;
+}
+
+template <int D, bool F8, typename QT>
+inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cudaStream_t st) {
+  if (plan.rows) {
+    const int32_t rc = launch_attn_rows<D, F8, QT>(a, type, st);
+    if (rc != AIBX_OK) return rc;
+    a.slots += plan.rows_bytes / sizeof(float);
+  }
+  return plan.tiles ? launch_attn_tiles<D, F8, QT>(a, type, st) : AIBX_OK;
 }
 
 template <int D>
 inline int32_t launch_attn_dim(const AttnArgs& a, int type, int q_type, const AttnPlan& plan,
                                cudaStream_t st) {
-  if (plan.tiles) return AIBX_ERR_UNSUPPORTED;
   if (type == AIBX_TYPE_E4M3)
-    return q_type == AIBX_TYPE_BF16 ? launch_attn_rows<D, true, __nv_bfloat16>(a, type, st)
-                                    : launch_attn_rows<D, true, __half>(a, type, st);
-  return q_type == AIBX_TYPE_BF16 ? launch_attn_rows<D, false, __nv_bfloat16>(a, type, st)
-                                  : launch_attn_rows<D, false, __half>(a, type, st);
+    return q_type == AIBX_TYPE_BF16 ? launch_attn_kind<D, true, __nv_bfloat16>(a, type, plan, st)
+                                    : launch_attn_kind<D, true, __half>(a, type, plan, st);
+  return q_type == AIBX_TYPE_BF16 ? launch_attn_kind<D, false, __nv_bfloat16>(a, type, plan, st)
+                                  : launch_attn_kind<D, false, __half>(a, type, plan, st);
 }
 
 inline int32_t launch_attn(const AttnArgs& a, int type, int q_type, const AttnPlan& plan,

@@ -215,11 +215,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
                                    walk.span.hi, walk.head == 0, valid_next, slot_next);
         const int s = (int)(it % kRowStages);
         const unsigned int bar = smem_u32(&s_full[s]);
-        if (it >= kRowStages &&
-            !bounded_wait(smem_u32(&s_empty[s]), (unsigned int)((it / kRowStages - 1) & 1), abort_flag)) {
-          if (!*abort_flag && lane == 0) raise_status(AIBX_ERR_TIMEOUT);
-          *abort_flag = 1;
-        }
+        if (it >= kRowStages) ring_wait(smem_u32(&s_empty[s]), (it / kRowStages - 1) & 1u, abort_flag);
         __syncwarp();
         if (*abort_flag) valid = false;
         const unsigned int mask = __ballot_sync(0xffffffffu, valid);
@@ -246,12 +242,8 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       }
     }
     // what is still in flight targets this CTA's shared memory: wait for it before leaving
-    for (unsigned int i = it > kRowStages ? it - kRowStages : 0; i < it; ++i) {
-      unsigned int spins = 0;
-      while (!mbar_try_wait(smem_u32(&s_full[i % kRowStages]), (unsigned int)((i / kRowStages) & 1)) &&
-             ++spins < kWaitSpins) {
-      }
-    }
+    for (unsigned int i = it > kRowStages ? it - kRowStages : 0; i < it; ++i)
+      ring_drain(smem_u32(&s_full[i % kRowStages]), (i / kRowStages) & 1u);
     return;
   }
   if (F8 && warp > kRowWarps) {
@@ -292,11 +284,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           }
         }
         const int s = (int)(it % kRowStages);
-        if (it >= kRowStages &&
-            !bounded_wait(smem_u32(&s_empty[s]), (unsigned int)((it / kRowStages - 1) & 1), abort_flag)) {
-          if (!*abort_flag && lane == 0) raise_status(AIBX_ERR_TIMEOUT);
-          *abort_flag = 1;
-        }
+        if (it >= kRowStages) ring_wait(smem_u32(&s_empty[s]), (it / kRowStages - 1) & 1u, abort_flag);
         uint32_t* dst = reinterpret_cast<uint32_t*>(s_scale + s * 2 * TOK);
         if (kPer == 8) {
           dst[2 * lane] = kb;
@@ -386,10 +374,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 
     for (int t = walk.t0; t < walk.t1; ++t, ++it) {
       const int s = (int)(it % kRowStages);
-      if (!bounded_wait(smem_u32(&s_full[s]), (unsigned int)((it / kRowStages) & 1), abort_flag)) {
-        if (!*abort_flag && lane == 0) raise_status(AIBX_ERR_TIMEOUT);
-        *abort_flag = 1;
-      }
+      ring_wait(smem_u32(&s_full[s]), (it / kRowStages) & 1u, abort_flag);
       __syncwarp();
       const unsigned int boxmask = s_mask[s];
       // the 16-token tasks of all stages go round the warps in turn
@@ -695,10 +680,10 @@ attn_rows_join_kernel(const __grid_constant__ AttnArgs a) {
 // ------------------------------------------------------------------------------------------
 
 template <typename Kernel>
-inline int32_t launch_after(Kernel kernel, unsigned int grid, unsigned int threads, cudaStream_t st,
+inline int32_t launch_after(Kernel kernel, dim3 grid, unsigned int threads, cudaStream_t st,
                             const AttnArgs& a) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -726,7 +711,7 @@ inline int32_t launch_attn_rows(AttnArgs a, int type, cudaStream_t st) {
   attn_rows_kernel<D, F8, QT><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
   const int32_t rc2 = launch_status();
   if (rc2 != AIBX_OK) return rc2;
-  return launch_after(attn_rows_join_kernel<D, F8, QT>, grid, 256, st, a);
+  return launch_after(attn_rows_join_kernel<D, F8, QT>, dim3(grid), 256, st, a);
 }
 
 }  // namespace aibx

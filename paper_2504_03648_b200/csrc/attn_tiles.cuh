@@ -1,0 +1,819 @@
+// Attention of chunks of new tokens over a paged cache on the 5th-generation tensor cores.
+//
+// A CTA works on a block of 256 query rows of one (request, KV head) - row = token * G + query
+// head of the group, so that the heads which share K and V share their tiles - as two tiles of
+// 128 rows, against KV tiles of 128 positions:
+//   S = Q K^T          tcgen05.mma, Q and K from shared memory, S in tensor memory (fp32)
+//   P = 2^(S c - m)    one thread per row: S to registers, running maximum m (moved only when it
+//                      grows by more than 2^8, so that O is rarely rescaled), P to tensor memory
+//                      over S, as 16-bit
+//   O += P V           tcgen05.mma, P from tensor memory, V from shared memory as it lies in the
+//                      pool ([position][dim], the operand's N-major form), O in tensor memory
+// Roles: two softmax warpgroups (one per tile), one warp that issues all MMAs, one that feeds a
+// ring of K and V tiles with tensor-map boxes (one box = the slots of one block and head that
+// fall into the tile).  While one tile's rows are exponentiated the other tile's two MMAs run.
+// MMAs complete in issue order, and S of step j + 1 is issued behind PV of step j: seeing S(j + 1)
+// is therefore also seeing O(j), and no further barrier guards O.
+//
+// Over an e4m3 pool a warpgroup more turns each raw tile into fp16 as it arrives: element times
+// 2^(e - E), e its row's exponent and E the tile's largest, which is exact down to 2^-24 of the
+// tile's range; 2^E then joins the scale of the scores (K) or the exponent of the weights (V: m
+// covers S c + E, and l takes the sum of the weights times 2^-E).  Queries become fp16 scaled to
+// [1, 2) per row.
+//
+// Bound: the tensor pipe (1024 cycles per KV tile and 128 rows at D = 128, both products) and the
+// special function unit (128 * 128 exponentials at 16 a cycle: 1024 cycles too).
+#pragma once
+
+#include "attn_rows.cuh"
+
+namespace aibx {
+
+constexpr int kTileRows = 128;
+constexpr int kTileKeys = 128;
+constexpr int kInfoRing = 16;        // per-step facts the softmax reads: far deeper than the rings
+
+template <int D, bool F8>
+struct TileShape {
+  static constexpr int kThreads = F8 ? 512 : 384;
+  static constexpr int kBuf = kTileKeys * D * 2;           // one K or V tile as MMA operand
+  static constexpr int kBufs = D == 64 ? 8 : (F8 ? 3 : 5);
+  static constexpr int kRawBuf = kTileKeys * D;
+  static constexpr int kRaws = F8 ? 3 : 0;
+  static constexpr int kFactorRing = 4;
+  static constexpr int kCols = D / 64;                     // 128-byte columns of an operand row
+  static constexpr int kColBytes = 128 * 128;
+  static constexpr int kQ = kTileRows * D * 2;
+  static constexpr int kSmem = 2 * kQ + kBufs * kBuf + kRaws * kRawBuf +
+                               (F8 ? kFactorRing * 2 * kTileKeys * 2 + 2 * kTileRows * 4 : 0) + 1024;
+  static constexpr int kSlot = 2 * kTileRows * (D + 2);    // floats per workspace slot
+  static constexpr int kRegsSoftmax = F8 ? 208 : 224;      // launch: 128 (512 threads), 168 (384)
+  static constexpr int kRegsOther = F8 ? 48 : 56;          // 2 * 208 + 2 * 48 = 4 * 128; 2 * 224 + 56 = 3 * 168
+};
+
+// ------------------------------------------------------------------------------------------
+// tensor-core wrappers
+
+__device__ __forceinline__ uint64_t operand_desc(unsigned int addr, unsigned int lbo, unsigned int sbo) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) |
+         (1ull << 46) | (2ull << 61);                      // version 1, 128-byte swizzle
+}
+
+// fp32 accumulator, M = 128; `half` operands or bfloat16; B as it lies (K-major) or N-major
+__host__ __device__ constexpr unsigned int mma_desc(bool half, int n, bool b_n_major) {
+  return (1u << 4) | ((half ? 0u : 1u) << 7) | ((half ? 0u : 1u) << 10) | ((b_n_major ? 1u : 0u) << 16) |
+         ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+__device__ __forceinline__ void mma_smem(unsigned int d, uint64_t a, uint64_t b, unsigned int idesc, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((unsigned int)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_tmem(unsigned int d, unsigned int a, uint64_t b, unsigned int idesc, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((unsigned int)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(unsigned int bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_ld32(unsigned int addr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st32(unsigned int addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+      "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
+      "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(unsigned int addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(
+          r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+      : "memory");
+}
+
+// ------------------------------------------------------------------------------------------
+// the line of work
+
+// KV tiles of one block of 256 rows: the positions [lo, hi) that some row of it sees.
+struct TileSpan {
+  int lo, hi, tile0, tiles;
+};
+
+__device__ __forceinline__ TileSpan tile_span(const AttnArgs& a, const AttnRequest& q, int block) {
+  const int rows = q.n * a.G;
+  const int r0 = block * 2 * kTileRows, r1 = min(r0 + 2 * kTileRows, rows) - 1;
+  const long long first = (long long)q.len - q.n;
+  TileSpan s;
+  long long hi = a.causal ? first + r1 / a.G + 1 : q.keys;
+  hi = hi < 0 ? 0 : hi > q.keys ? q.keys : hi;
+  long long lo = a.window > 0 ? first + r0 / a.G - a.window + 1 : 0;
+  lo = lo < 0 ? 0 : lo > hi ? hi : lo;
+  s.hi = (int)hi;
+  s.lo = (int)lo;
+  s.tile0 = s.lo / kTileKeys;
+  s.tiles = max(1, (s.hi + kTileKeys - 1) / kTileKeys - s.tile0);
+  return s;
+}
+
+struct TileCost {
+  const AttnArgs& a;
+  // tiles of request r for one head, and its blocks of rows (0: not this kernel's)
+  __device__ __forceinline__ long long head_tiles(const AttnRequest& q, int& blocks) const {
+    blocks = 0;
+    const long long rows = (long long)q.n * a.G;
+    if (rows == 0 || (a.rows_too && rows <= kRowsMax)) return 0;
+    blocks = (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
+    long long sum = 0;
+    for (int b = 0; b < blocks; ++b) sum += tile_span(a, q, b).tiles;
+    return sum;
+  }
+  __device__ __forceinline__ long long operator()(int r) const {
+    int blocks;
+    return head_tiles(attn_request(a.b, a.pool.T, r), blocks) * a.pool.H;
+  }
+};
+
+struct TileWalk {
+  const AttnArgs& a;
+  long long pos, end;
+  int r, head, block, blocks, t0, t1;
+  AttnRequest q;
+  TileSpan span;
+  bool fresh;                        // block not yet entered
+
+  __device__ __forceinline__ TileWalk(const AttnArgs& args, const WorkStart& w, unsigned int index,
+                                      unsigned int pieces)
+      : a(args) {
+    const long long per = (w.total + pieces - 1) / pieces;
+    pos = per * index;
+    end = min(pos + per, w.total);
+    r = w.r;
+    if (r < 0) pos = end = 0;
+    if (pos >= end) return;
+    q = attn_request(a.b, a.pool.T, r);
+    const TileCost cost{a};
+    const long long per_head = cost.head_tiles(q, blocks);
+    long long off = pos - w.base;
+    head = (int)(off / per_head);
+    off -= (long long)head * per_head;
+    block = 0;
+    span = tile_span(a, q, 0);
+    while (off >= span.tiles) {
+      off -= span.tiles;
+      span = tile_span(a, q, ++block);
+    }
+    t1 = (int)off;                   // where next() goes on
+    fresh = false;
+  }
+  __device__ __forceinline__ bool next() {
+    if (pos >= end) return false;
+    if (fresh) {
+      if (++block == blocks) {
+        block = 0;
+        if (++head == a.pool.H) {
+          head = 0;
+          do {
+            ++r;
+            q = attn_request(a.b, a.pool.T, r);
+            const long long rows = (long long)q.n * a.G;
+            blocks = rows == 0 || (a.rows_too && rows <= kRowsMax)
+                         ? 0
+                         : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
+          } while (blocks == 0);
+        }
+      }
+      span = tile_span(a, q, block);
+      t1 = 0;
+    }
+    t0 = t1;
+    const long long left = end - pos;
+    t1 = left < span.tiles - t0 ? t0 + (int)left : span.tiles;
+    pos += t1 - t0;
+    fresh = true;
+    return true;
+  }
+  __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == span.tiles; }
+  __device__ __forceinline__ int rows() const { return min(q.n * a.G - block * 2 * kTileRows, 2 * kTileRows); }
+};
+
+template <int REGS>
+__device__ __forceinline__ void regs_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS));
+}
+template <int REGS>
+__device__ __forceinline__ void regs_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS));
+}
+
+template <int D, bool F8, typename QT>
+__global__ void __launch_bounds__(TileShape<D, F8>::kThreads, 1)
+attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a) {
+  using S = TileShape<D, F8>;
+  using MT = typename std::conditional<F8, __half, QT>::type;
+  extern __shared__ unsigned char s_raw[];
+  __shared__ __align__(8) unsigned long long s_kv_full[S::kBufs], s_kv_empty[S::kBufs];
+  __shared__ __align__(8) unsigned long long s_raw_full[F8 ? S::kRaws : 1], s_raw_empty[F8 ? S::kRaws : 1];
+  __shared__ __align__(8) unsigned long long s_fac_full[S::kFactorRing], s_fac_empty[S::kFactorRing];
+  __shared__ __align__(8) unsigned long long s_q_full[2], s_s_full[2], s_p_full[2], s_o_full[2];
+  __shared__ unsigned int s_mask[kInfoRing];
+  __shared__ float s_kscale[kInfoRing], s_vexp[kInfoRing];
+  __shared__ long long s_scan[33];
+  __shared__ WorkStart s_start;
+  __shared__ unsigned int s_tmem;
+  __shared__ int s_abort;
+
+  const unsigned int smem0 = (smem_u32(s_raw) + 1023u) & ~1023u;
+  unsigned char* base = s_raw + (smem0 - smem_u32(s_raw));
+  unsigned char* raws = base + 2 * S::kQ + S::kBufs * S::kBuf;
+  __half* factors = reinterpret_cast<__half*>(raws + S::kRaws * S::kRawBuf);
+  float* s_qup = reinterpret_cast<float*>(factors + S::kFactorRing * 2 * kTileKeys);
+  const unsigned int kv0 = smem0 + 2 * S::kQ;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  volatile int* abort_flag = &s_abort;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S::kBufs; ++i) {
+      mbar_init(smem_u32(&s_kv_full[i]), F8 ? 128u : 1u);
+      mbar_init(smem_u32(&s_kv_empty[i]), 1u);
+    }
+    for (int i = 0; i < S::kRaws; ++i) {
+      mbar_init(smem_u32(&s_raw_full[i]), 1u);
+      mbar_init(smem_u32(&s_raw_empty[i]), 4u);
+    }
+    for (int i = 0; i < S::kFactorRing; ++i) {
+      mbar_init(smem_u32(&s_fac_full[i]), 1u);
+      mbar_init(smem_u32(&s_fac_empty[i]), 4u);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(smem_u32(&s_q_full[t]), 128u);
+      mbar_init(smem_u32(&s_s_full[t]), 1u);
+      mbar_init(smem_u32(&s_p_full[t]), 4u);
+      mbar_init(smem_u32(&s_o_full[t]), 1u);
+    }
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    tmem_before();
+  }
+  const TileCost cost{a};
+  const WorkStart w = locate_piece<S::kThreads>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
+  tmem_after();                                            // (locate_piece synchronises the block)
+  const unsigned int tmem = s_tmem;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  TileWalk walk(a, w, blockIdx.x, gridDim.x);
+
+  if (warp < 8) {
+    // ================================================================ softmax: thread = row
+    regs_up<S::kRegsSoftmax>();
+    const int t = warp >> 2;                               // tile
+    const int row = threadIdx.x & 127;
+    const unsigned int lanes = (unsigned int)(warp & 3) << 21;
+    const unsigned int tm_s = tmem + lanes + t * 128;
+    const unsigned int tm_o = tmem + lanes + 256 + t * D;
+    unsigned int s_phase = 0, o_phase = 0, step = 0;
+    while (walk.next()) {
+      const int rows_here = walk.rows() - t * kTileRows;   // rows of this tile (<= 0: none)
+      const int steps = walk.t1 - walk.t0;
+      if (rows_here <= 0) {
+        step += steps;
+        continue;
+      }
+      const int row0 = walk.block * 2 * kTileRows + t * kTileRows;   // in the request's rows
+      // ---- queries into shared memory
+      {
+        constexpr int kChunks = D / 8;                     // 16-byte pieces of a row
+        const int c = row % kChunks;
+        unsigned char* dst = base + t * S::kQ + (c >> 3) * S::kColBytes;
+        for (int i = row / kChunks; i < kTileRows; i += 128 / kChunks) {
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (i < rows_here) {
+            const int ti = (row0 + i) / a.G, gi = row0 + i - ti * a.G;
+            v = *reinterpret_cast<const uint4*>(reinterpret_cast<const QT*>(a.q) + (walk.q.tok0 + ti) * a.q_tok +
+                                                (long long)(walk.head * a.G + gi) * a.q_head + c * 8);
+          }
+          if constexpr (F8) {
+            uint32_t x[4] = {v.x, v.y, v.z, v.w};
+            float amax = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = Bits16<QT>::unpack(x[e]);
+              amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+            }
+#pragma unroll
+            for (int m = 1; m < kChunks; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
+            float down, up;
+            power_scale(amax, down, up);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = Bits16<QT>::unpack(x[e]);
+              x[e] = Bits16<MT>::pack(f.x * down, f.y * down);
+            }
+            v = make_uint4(x[0], x[1], x[2], x[3]);
+            if (c == 0) s_qup[t * kTileRows + i] = up;
+          }
+          *reinterpret_cast<uint4*>(dst + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = v;
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(smem_u32(&s_q_full[t]));
+        if (F8) asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
+      }
+      const float c0 = F8 ? a.scale_log2 * s_qup[t * kTileRows + row] : a.scale_log2;
+      const int tok = (row0 + min(row, rows_here - 1)) / a.G;
+      const long long p = (long long)walk.q.len - walk.q.n + tok;      // this row's position
+      // positions [vis0, vis1) this row sees (of those that are there)
+      const int vis1 = (int)max(0LL, a.causal ? min(p + 1, (long long)walk.span.hi) : (long long)walk.span.hi);
+      const int vis0 = a.window > 0 ? (int)max((long long)walk.span.lo, p - a.window + 1) : walk.span.lo;
+      float m = -INFINITY, l = 0.0f;
+      for (int j = 0; j < steps; ++j, ++step) {
+        ring_wait(smem_u32(&s_s_full[t]), s_phase, abort_flag);
+        s_phase ^= 1u;
+        __syncwarp();
+        tmem_after();
+        const int key0 = (walk.span.tile0 + walk.t0 + j) * kTileKeys;
+        const unsigned int mask = s_mask[step % kInfoRing];
+        float c = c0, shift = 0.0f;
+        if constexpr (F8) {
+          c *= s_kscale[step % kInfoRing];
+          shift = s_vexp[step % kInfoRing];
+        }
+        uint32_t s[128];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tmem_ld32(tm_s + k * 32, s + k * 32);
+        tmem_wait_ld();
+        // ---- hide what this row does not see
+        if (mask != 0xffffffffu) {                         // blocks that are not there: rare
+#pragma unroll
+          for (int k = 0; k < 128; ++k)
+            if (!((mask >> (k / a.box)) & 1u)) s[k] = 0xff800000u;
+        }
+        if (key0 + kTileKeys > vis1 || key0 < vis0) {
+          const int b0 = vis0 - key0, b1 = vis1 - key0;
+#pragma unroll
+          for (int k = 0; k < 128; ++k)
+            if (k < b0 || k >= b1) s[k] = 0xff800000u;
+        }
+        // ---- maximum
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int k = 0; k < 128; k += 4)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], __uint_as_float(s[k + e]));
+        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c + shift;
+        if (__any_sync(0xffffffffu, mt > m + 8.0f)) {
+          const float mn = fmaxf(m, mt);
+          const float al = mn == -INFINITY ? 1.0f : exp2_fast(m - mn);
+          m = mn;
+          l *= al;
+          if (j > 0) {
+#pragma unroll
+            for (int k = 0; k < D; k += 32) {
+              uint32_t o[32];
+              tmem_ld32(tm_o + k, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
+              tmem_st32(tm_o + k, o);
+            }
+          }
+        }
+        const float off = (m == -INFINITY ? 0.0f : m) - shift;
+        // ---- weights
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < 128; k += 32) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float p0 = exp2_fast(fmaf(__uint_as_float(s[k + e]), c, -off));
+            const float p1 = exp2_fast(fmaf(__uint_as_float(s[k + e + 1]), c, -off));
+            sum[(e >> 1) & 3] += p0 + p1;
+            pk[e >> 1] = Bits16<MT>::pack(p0, p1);
+          }
+          tmem_st16(tm_s + (k >> 1), pk);
+        }
+        const float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        l += F8 ? total * exp2_fast(-shift) : total;
+        tmem_wait_st();
+        tmem_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_p_full[t]));
+      }
+      // ---- O out of tensor memory
+      ring_wait(smem_u32(&s_o_full[t]), o_phase, abort_flag);
+      o_phase ^= 1u;
+      __syncwarp();
+      tmem_after();
+      const bool whole = walk.whole();
+      const bool at_start = walk.pos - steps == (w.total + gridDim.x - 1) / gridDim.x * blockIdx.x;
+      float* slot = a.slots + ((long long)blockIdx.x * 2 + (at_start ? 0 : 1)) * S::kSlot;
+      const int srow = t * kTileRows + row;
+      const bool on = row < rows_here;
+      const long long otok = walk.q.tok0 + tok;
+      const int qh = walk.head * a.G + (row0 + row - tok * a.G);
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      QT* dst = reinterpret_cast<QT*>(a.out) + otok * a.o_tok + (long long)qh * a.o_head;
+#pragma unroll
+      for (int k = 0; k < D; k += 32) {
+        uint32_t o[32];
+        __syncwarp();
+        tmem_ld32(tm_o + k, o);
+        tmem_wait_ld();
+        if (on && whole) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            uint4 v;
+            v.x = Bits16<QT>::pack(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+            v.y = Bits16<QT>::pack(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+            v.z = Bits16<QT>::pack(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv);
+            v.w = Bits16<QT>::pack(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv);
+            *reinterpret_cast<uint4*>(dst + k + e) = v;
+          }
+        } else if (on) {
+          float* to = slot + 4 * kTileRows + (long long)srow * D + k;
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<uint4*>(to + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        }
+      }
+      if (on) {
+        if (!whole) {
+          slot[srow] = m;
+          slot[2 * kTileRows + srow] = l;
+        } else if (a.lse) {
+          a.lse[otok * (a.pool.H * a.G) + qh] = l == 0.0f ? -INFINITY : 0.69314718056f * (m + log2f(l));
+        }
+      }
+      tmem_before();
+    }
+  } else if (warp < 12) {
+    regs_down<S::kRegsOther>();
+    if (warp == 8) {
+      // ============================================================== MMA warp
+      constexpr bool kHalf = std::is_same<MT, __half>::value;
+      constexpr unsigned int kQK = mma_desc(kHalf, kTileKeys, false), kPV = mma_desc(kHalf, D, true);
+      unsigned int buf = 0, buf_phase = 0;                 // next buffer of the ring to be read
+      unsigned int q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      unsigned int last_buf = 0, last_phase = 1;           // (a fresh barrier passes for phase 1)
+      auto advance = [&]() {
+        if (++buf == S::kBufs) {
+          buf = 0;
+          buf_phase ^= 1u;
+        }
+      };
+      auto qk = [&](int t, unsigned int kbuf) {
+        if (lane == 0) {
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const unsigned int off = (k >> 2) * S::kColBytes + (k & 3) * 32;
+            mma_smem(tmem + t * 128, operand_desc(smem0 + t * S::kQ + off, 16, 1024),
+                     operand_desc(kv0 + kbuf * S::kBuf + off, 16, 1024), kQK, k > 0);
+          }
+          mma_commit(smem_u32(&s_s_full[t]));
+        }
+        __syncwarp();
+      };
+      while (walk.next()) {
+        const int steps = walk.t1 - walk.t0;
+        const int tiles = walk.rows() > kTileRows ? 2 : 1;
+        ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
+        for (int t = 0; t < tiles; ++t) {
+          ring_wait(smem_u32(&s_q_full[t]), q_phase[t], abort_flag);
+          q_phase[t] ^= 1u;
+          tmem_after();
+          qk(t, buf);
+        }
+        if (lane == 0) mma_commit(smem_u32(&s_kv_empty[buf]));
+        __syncwarp();
+        advance();
+        for (int j = 0; j < steps; ++j) {
+          const unsigned int vbuf = buf;
+          last_buf = buf;
+          last_phase = buf_phase;
+          ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
+          advance();
+          if (!F8) {
+            // V rows of positions nobody in the block sees: whatever the pool holds there
+            // (0 * NaN is NaN) becomes zero
+            const int key0 = (walk.span.tile0 + walk.t0 + j) * kTileKeys;
+            const int z0 = min(max(walk.span.lo - key0, 0), kTileKeys), z1 = max(min(walk.span.hi - key0, kTileKeys), 0);
+            if (z0 > 0 || z1 < kTileKeys) {
+              unsigned char* v = base + 2 * S::kQ + vbuf * S::kBuf;
+              for (int x = lane; x < kTileKeys * 8; x += 32) {
+                const int rr = x >> 3;
+                if (rr < z0 || rr >= z1) {
+#pragma unroll
+                  for (int cc = 0; cc < S::kCols; ++cc)
+                    *reinterpret_cast<uint4*>(v + cc * S::kColBytes + rr * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+                }
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+            }
+          }
+          const bool more = j + 1 < steps;
+          const unsigned int kbuf = buf;
+          if (more) {
+            ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
+            advance();
+          }
+          for (int t = 0; t < tiles; ++t) {
+            ring_wait(smem_u32(&s_p_full[t]), p_phase[t], abort_flag);
+            p_phase[t] ^= 1u;
+            tmem_after();
+            if (lane == 0) {
+#pragma unroll
+              for (int k = 0; k < kTileKeys / 16; ++k)
+                mma_tmem(tmem + 256 + t * D, tmem + t * 128 + k * 8,
+                         operand_desc(kv0 + vbuf * S::kBuf + k * 2048, S::kColBytes, 1024), kPV, j > 0 || k > 0);
+              if (!more) mma_commit(smem_u32(&s_o_full[t]));
+            }
+            __syncwarp();
+            if (more) qk(t, kbuf);
+          }
+          if (lane == 0) {
+            if (more) mma_commit(smem_u32(&s_kv_empty[kbuf]));
+            mma_commit(smem_u32(&s_kv_empty[vbuf]));
+          }
+          __syncwarp();
+        }
+      }
+      // the last commit has to arrive while its barrier is still this CTA's
+      ring_wait(smem_u32(&s_kv_empty[last_buf]), last_phase, abort_flag);
+    } else if (warp == 9) {
+      // ============================================================== loader warp
+      constexpr int kRing = F8 ? S::kRaws : S::kBufs;
+      constexpr unsigned int kBytes = F8 ? S::kRawBuf : S::kBuf;
+      constexpr int kRow = F8 ? D : 128;
+      const unsigned int ring0 = F8 ? smem_u32(raws) : kv0;
+      unsigned long long* full = F8 ? s_raw_full : s_kv_full;
+      unsigned long long* empty = F8 ? s_raw_empty : s_kv_empty;
+      const int boxes = kTileKeys / a.box;
+      unsigned int buf = 0, phase = 1, issued = 0, step = 0;
+      while (walk.next()) {
+        const uint32_t* row;
+        long long entries;
+        table_row(a.b, walk.r, row, entries);
+        if (walk.q.keys < walk.q.len && walk.head == 0 && walk.block == 0 && walk.t0 == 0 && lane == 0)
+          raise_status(AIBX_ERR_RANGE);                    // tokens the table has no entry for
+        for (int j = walk.t0; j < walk.t1; ++j, ++step) {
+          bool valid;
+          int slot;
+          const uint32_t id = box_block<kTileKeys>(a, row, walk.span.tile0 + j, lane, boxes, walk.span.lo,
+                                                   walk.span.hi, walk.head == 0, valid, slot);
+          // a box that is not there, or that holds no visible key, comes as zeros from beyond the pool
+          const int block = valid ? (int)id : (int)a.pool.num_blocks;
+          const int tok = (walk.span.tile0 + j) * kTileKeys + lane * a.box;
+          const bool missing = lane < boxes && tok < walk.span.hi && tok + a.box > walk.span.lo && !valid;
+          const unsigned int gone = __ballot_sync(0xffffffffu, missing);
+          if (lane == 0) s_mask[step % kInfoRing] = ~gone;
+          for (int kv = 0; kv < 2; ++kv) {
+            ring_wait(smem_u32(&empty[buf]), phase, abort_flag);
+            __syncwarp();
+            const unsigned int bar = smem_u32(&full[buf]);
+            if (__any_sync(0xffffffffu, *abort_flag)) {
+              if (lane == 0) mbar_arrive(bar);
+            } else {
+              if (lane == 0) mbar_arrive_expect_tx(bar, kBytes);
+              __syncwarp();
+              if (lane < boxes) {
+                const unsigned int dst = ring0 + buf * kBytes + lane * a.box * kRow;
+#pragma unroll
+                for (int cc = 0; cc < (F8 ? 1 : S::kCols); ++cc)
+                  tensor_load_5d(dst + cc * S::kColBytes, &map, bar, cc * 64, slot, walk.head, block, kv);
+              }
+            }
+            __syncwarp();
+            ++issued;
+            if (++buf == (unsigned int)kRing) {
+              buf = 0;
+              phase ^= 1u;
+            }
+          }
+        }
+      }
+      // nothing may still be on its way into this CTA's shared memory when it ends
+      for (unsigned int i = issued > (unsigned int)kRing ? issued - kRing : 0; i < issued; ++i)
+        ring_drain(smem_u32(&full[i % kRing]), (i / kRing) & 1u);
+    } else if constexpr (F8) {
+      // ============================================================== scale warps (10, 11)
+      // Per step: the factor 2^(e - E) of every position of the K and of the V tile, and E.  The
+      // chain table -> scale byte is long: the two warps take turns and run ahead.
+      unsigned int step = 0;
+      while (walk.next()) {
+        const uint32_t* row;
+        long long entries;
+        table_row(a.b, walk.r, row, entries);
+        for (int j = walk.t0; j < walk.t1; ++j, ++step) {
+          if ((step & 1u) != (unsigned int)(warp - 10)) continue;
+          const int tok = (walk.span.tile0 + j) * kTileKeys + lane * 4;   // four slots of one block
+          int byte[2][4];
+          unsigned int there = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            byte[0][i] = byte[1][i] = 0;
+            if (tok + i >= walk.span.lo && tok + i < walk.span.hi) there |= 1u << i;
+          }
+          if (there) {
+            const int at = tok / a.pool.T;
+            const uint32_t id = __ldg(row + at);
+            if (id < a.pool.num_blocks) {
+              const unsigned char* src = a.pool.scales + (long long)id * a.pool.s_block +
+                                         (long long)walk.head * a.pool.s_head +
+                                         (long long)(tok - at * a.pool.T) * a.pool.s_slot;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                byte[0][i] = __ldg(src + i * a.pool.s_slot);
+                byte[1][i] = __ldg(src + a.pool.s_kv + i * a.pool.s_slot);
+              }
+            } else {
+              there = 0;
+            }
+          }
+          const unsigned int f = step % S::kFactorRing;
+          ring_wait(smem_u32(&s_fac_empty[f]), ((step / S::kFactorRing) & 1u) ^ 1u, abort_flag);
+          __syncwarp();
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            int top = 27;                                  // exponents from -100: 2^-E stays finite
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (((there >> i) & 1u) && byte[kv][i] != 255) top = max(top, byte[kv][i]);
+            top = __reduce_max_sync(0xffffffffu, top);
+            __half out[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float x = byte[kv][i] == 255 ? NAN : exp2f((float)(byte[kv][i] - top));
+              if (!((there >> i) & 1u)) x = 0.0f;
+              out[i] = __float2half(x);
+            }
+            *reinterpret_cast<uint2*>(factors + (f * 2 + kv) * kTileKeys + lane * 4) = *reinterpret_cast<uint2*>(out);
+            if (lane == 0) {
+              if (kv == 0) s_kscale[step % kInfoRing] = power_of_byte(top);
+              else s_vexp[step % kInfoRing] = (float)(top - 127);
+            }
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&s_fac_full[f]));
+        }
+      }
+    }
+  } else if constexpr (F8) {
+    // ================================================================ converter warps (12 .. 15)
+    regs_down<S::kRegsOther>();
+    const int tid = threadIdx.x - 384;
+    constexpr int kChunks = D / 16;                        // 16-byte pieces of a raw row
+    const int c = tid % kChunks;
+    unsigned int raw = 0, raw_phase = 0, buf = 0, buf_phase = 1, step = 0;
+    while (walk.next()) {
+      const int steps = walk.t1 - walk.t0;
+      for (int j = 0; j < steps; ++j, ++step) {
+        const unsigned int f = step % S::kFactorRing;
+        ring_wait(smem_u32(&s_fac_full[f]), (step / S::kFactorRing) & 1u, abort_flag);
+        for (int kv = 0; kv < 2; ++kv) {
+          ring_wait(smem_u32(&s_raw_full[raw]), raw_phase, abort_flag);
+          ring_wait(smem_u32(&s_kv_empty[buf]), buf_phase, abort_flag);
+          __syncwarp();
+          const unsigned char* src = raws + raw * S::kRawBuf;
+          unsigned char* dst = base + 2 * S::kQ + buf * S::kBuf + (c >> 2) * S::kColBytes;
+          const __half* fac = factors + (f * 2 + kv) * kTileKeys;
+#pragma unroll 4
+          for (int i = tid / kChunks; i < kTileKeys; i += 128 / kChunks) {
+            const uint4 v = *reinterpret_cast<const uint4*>(src + i * D + ((D == 128 ? c ^ (i & 7) : c) << 4));
+            const __half x = fac[i];
+            const bool none = __half_as_ushort(x) == 0;    // not there, or too small to show
+            const __half2 x2 = __half2half2(x);
+            const uint32_t wv[4] = {v.x, v.y, v.z, v.w};
+            uint32_t o[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const __half2 lo = __hmul2(halves_of_e4m3(wv[e] & 0xffffu), x2);
+              const __half2 hi = __hmul2(halves_of_e4m3(wv[e] >> 16), x2);
+              o[2 * e] = none ? 0u : *reinterpret_cast<const uint32_t*>(&lo);
+              o[2 * e + 1] = none ? 0u : *reinterpret_cast<const uint32_t*>(&hi);
+            }
+            const int p0 = (2 * c) & 7;
+            *reinterpret_cast<uint4*>(dst + i * 128 + ((p0 ^ (i & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(dst + i * 128 + (((p0 + 1) ^ (i & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          mbar_arrive(smem_u32(&s_kv_full[buf]));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&s_raw_empty[raw]));
+          if (++raw == S::kRaws) {
+            raw = 0;
+            raw_phase ^= 1u;
+          }
+          if (++buf == S::kBufs) {
+            buf = 0;
+            buf_phase ^= 1u;
+          }
+        }
+        if (lane == 0) mbar_arrive(smem_u32(&s_fac_empty[f]));
+      }
+    }
+  }
+  tmem_before();
+  __syncthreads();
+  if (warp == 8) {
+    tmem_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// Joins a block of rows that was cut, as attn_rows_join_kernel does; blockIdx.y takes 32 rows.
+template <int D, bool F8, typename QT>
+__global__ void __launch_bounds__(256)
+attn_tiles_join_kernel(const __grid_constant__ AttnArgs a) {
+  using S = TileShape<D, F8>;
+  __shared__ long long s_scan[33];
+  __shared__ WorkStart s_start;
+  const TileCost cost{a};
+  const WorkStart w = locate_piece<256>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  TileWalk walk(a, w, blockIdx.x, gridDim.x);
+  if (!walk.next() || walk.t0 == 0 || walk.t1 != walk.span.tiles) return;
+  const long long per = (w.total + gridDim.x - 1) / gridDim.x;
+  const long long p0 = walk.pos - walk.t1;                 // first position of the block
+  const int c0 = (int)(p0 / per), c1 = (int)blockIdx.x;
+  const int rows = walk.rows();
+  for (int x = threadIdx.x; x < 32 * (D / 4); x += 256) {
+    const int i = blockIdx.y * 32 + x / (D / 4), d = (x % (D / 4)) * 4;
+    if (i >= rows) continue;
+    float top = -INFINITY, sum = 0.0f;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int c = c0; c <= c1; ++c) {
+      const float* slot = a.slots + ((long long)c * 2 + (c == c0 && p0 != c0 * per ? 1 : 0)) * S::kSlot;
+      const float mc = slot[i];
+      const float4 o = *reinterpret_cast<const float4*>(slot + 4 * kTileRows + (long long)i * D + d);
+      const float tn = fmaxf(top, mc);
+      const float safe = tn == -INFINITY ? 0.0f : tn;
+      const float f0 = exp2_fast(top - safe), f1 = exp2_fast(mc - safe);
+      sum = sum * f0 + slot[2 * kTileRows + i] * f1;
+      v.x = v.x * f0 + o.x * f1;
+      v.y = v.y * f0 + o.y * f1;
+      v.z = v.z * f0 + o.z * f1;
+      v.w = v.w * f0 + o.w * f1;
+      top = tn;
+    }
+    const int ri = walk.block * 2 * kTileRows + i, ti = ri / a.G;
+    const long long tok = walk.q.tok0 + ti;
+    const int qh = walk.head * a.G + (ri - ti * a.G);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    QT* dst = reinterpret_cast<QT*>(a.out) + tok * a.o_tok + (long long)qh * a.o_head + d;
+    *reinterpret_cast<uint2*>(dst) = make_uint2(Bits16<QT>::pack(v.x * inv, v.y * inv),
+                                                Bits16<QT>::pack(v.z * inv, v.w * inv));
+    if (a.lse && d == 0)
+      a.lse[tok * (a.pool.H * a.G) + qh] = sum == 0.0f ? -INFINITY : 0.69314718056f * (top + log2f(sum));
+  }
+}
+
+template <int D, bool F8, typename QT>
+inline int32_t launch_attn_tiles(AttnArgs a, int type, cudaStream_t st) {
+  using S = TileShape<D, F8>;
+  a.box = gcd_int(a.pool.T, kTileKeys);
+  CUtensorMap map;
+  const int32_t rc = pool_tensor_map(a.pool, type, a.box, &map);
+  if (rc != AIBX_OK) return rc;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return AIBX_ERR_CUDA;
+  static size_t configured[64] = {0};
+  static std::mutex lock;
+  if (!ensure_dynamic_smem(attn_tiles_kernel<D, F8, QT>, S::kSmem, dev, configured, lock))
+    return AIBX_ERR_CUDA;
+  const unsigned int grid = (unsigned int)sm_count();
+  attn_tiles_kernel<D, F8, QT><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
+  const int32_t rc2 = launch_status();
+  if (rc2 != AIBX_OK) return rc2;
+  return launch_after(attn_tiles_join_kernel<D, F8, QT>, dim3(grid, 2 * kTileRows / 32), 256, st, a);
+}
+
+}  // namespace aibx

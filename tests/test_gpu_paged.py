@@ -268,3 +268,27 @@ def test_attention_few_rows(G, new, causal, window, pool, io):
     b = Batch(np.random.default_rng(G), s, new, lens, ragged=G == 7)
     st, _, _ = check_attention(s, b, io, G=G, causal=causal, window=window, seed=window)
     assert st == (0, 0)
+
+
+@pytest.mark.parametrize("pool,io", POOLS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("layout,inner,T", [(0, 0, 16), (1, 1, 8), (2, 0, 24), (2, 1, 256)])
+def test_attention_chunks(pool, io, D, layout, inner, T):
+    new = [17, 0, 64, 130, 5, 33]
+    lens = [n + c for n, c in zip(new, (0, 40, 300, 1, 128, 95))]
+    s = Shape(H=2, D=D, T=T, layout=layout, inner=inner, pool=pool, blocks=sum(-(-x // T) for x in lens) + 2)
+    b = Batch(np.random.default_rng(T), s, new, lens, pad=3, ragged=T == 24)
+    st, _, _ = check_attention(s, b, io, G=4, seed=D + T, spread=2.0)
+    assert st == (0, 0)
+
+
+@pytest.mark.parametrize("G", [1, 3, 7, 40, 128])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 5), (False, 0), (False, 70), (True, 200)])
+@pytest.mark.parametrize("pool,io", [("bf16", "bf16"), ("e4m3", "bf16")])
+def test_attention_one_chunk(G, causal, window, pool, io):
+    """One request: the tile kernel alone, whatever its length."""
+    for n, c in ((1, 0), (2, 131), (40, 400), (300 if G < 4 else 9, 77)):
+        s = Shape(H=1, D=128, T=16, layout=1, pool=pool, blocks=90)
+        b = Batch(np.random.default_rng(G), s, [n], [n + c])
+        st, _, _ = check_attention(s, b, io, G=G, causal=causal, window=window, seed=window, max_new=0)
+        assert st == (0, 0)
