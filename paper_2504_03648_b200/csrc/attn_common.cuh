@@ -23,13 +23,13 @@ struct AttnArgs {
   float scale_log2;                         // scale * log2(e): scores in powers of two
   int G;                                    // query heads per KV head
   int causal, window;
-  int box;                                  // tokens one tensor-map box covers
+  int box, box_log;                         // tokens one tensor-map box covers: a power of two
+  int row_limit;                            // requests of up to so many rows (tokens * G) are the
+                                            // row kernel's, 0: none
   int check_bound;                          // report requests this call has no kernel for
-  int rows_too;                             // the row kernel runs in this call as well
   float* slots;
 };
 
-constexpr int kRowsMax = 16;                // rows (tokens * G) the row kernel takes per request
 
 struct AttnRequest {
   long long tok0;     // first row of the per-token tensors
@@ -169,25 +169,43 @@ __device__ __forceinline__ void tensor_load_5d(unsigned int dst, const CUtensorM
 
 // 16-bit rows are cut into 128-byte columns whose 16-byte pieces are XORed with the row's place
 // among eight (128-byte swizzle); so is a 128-byte e4m3 row.  64-byte rows stay as they are.
-inline int32_t pool_tensor_map(const PagedPool& p, int type, int box, CUtensorMap* map) {
+// dims: element of a column, slot, then three of {column, head, block, K/V}.
+inline int32_t encode_pool_map(const PagedPool& p, int type, const void* base, const cuuint64_t* dims,
+                               const cuuint64_t* strides, const cuuint32_t* box, CUtensorMap* map) {
   const EncodeTiledFn encode = encode_tiled_fn();
   if (!encode) return AIBX_ERR_CUDA;
-  const int size = type_bytes(type);
-  const int col = p.D * size < 128 ? p.D * size : 128;
-  const cuuint64_t dims[5] = {(cuuint64_t)p.D, (cuuint64_t)p.T, (cuuint64_t)p.H,
-                              (cuuint64_t)p.num_blocks, 2};
-  const cuuint64_t strides[4] = {(cuuint64_t)p.slot, (cuuint64_t)p.head, (cuuint64_t)p.block,
-                                 (cuuint64_t)p.kv};
-  const cuuint32_t bx[5] = {(cuuint32_t)(col / size), (cuuint32_t)box, 1, 1, 1};
   const cuuint32_t es[5] = {1, 1, 1, 1, 1};
   const CUtensorMapDataType dt = type == AIBX_TYPE_BF16   ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                  : type == AIBX_TYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                                           : CU_TENSOR_MAP_DATA_TYPE_UINT8;
-  if (encode(map, dt, 5, p.base, dims, strides, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             col == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+  if (encode(map, dt, 5, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             p.D * type_bytes(type) >= 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return AIBX_ERR_UNSUPPORTED;
   return AIBX_OK;
+}
+
+inline int column_elems(const PagedPool& p, int type) {
+  const int size = type_bytes(type);
+  return p.D * size < 128 ? p.D : 128 / size;
+}
+
+// (element, slot, head, block, K/V): a box is one column of `box` slots.
+inline int32_t pool_tensor_map(const PagedPool& p, int type, int box, CUtensorMap* map) {
+  const cuuint64_t dims[5] = {(cuuint64_t)p.D, (cuuint64_t)p.T, (cuuint64_t)p.H, (cuuint64_t)p.num_blocks, 2};
+  const cuuint64_t strides[4] = {(cuuint64_t)p.slot, (cuuint64_t)p.head, (cuuint64_t)p.block, (cuuint64_t)p.kv};
+  const cuuint32_t bx[5] = {(cuuint32_t)column_elems(p, type), (cuuint32_t)box, 1, 1, 1};
+  return encode_pool_map(p, type, p.base, dims, strides, bx, map);
+}
+
+// (element, slot, column, head, block) of K or of V: a box is `box` whole rows, column by column.
+inline int32_t plane_tensor_map(const PagedPool& p, int type, int box, int kv, CUtensorMap* map) {
+  const int col = column_elems(p, type);
+  const cuuint64_t dims[5] = {(cuuint64_t)col, (cuuint64_t)p.T, (cuuint64_t)(p.D / col), (cuuint64_t)p.H,
+                              (cuuint64_t)p.num_blocks};
+  const cuuint64_t strides[4] = {(cuuint64_t)p.slot, 128, (cuuint64_t)p.head, (cuuint64_t)p.block};
+  const cuuint32_t bx[5] = {(cuuint32_t)col, (cuuint32_t)box, (cuuint32_t)(p.D / col), 1, 1};
+  return encode_pool_map(p, type, p.base + kv * p.kv, dims, strides, bx, map);
 }
 
 inline int gcd_int(int a, int b) {
@@ -197,6 +215,12 @@ inline int gcd_int(int a, int b) {
     b = t;
   }
   return a;
+}
+
+inline int log2_int(int power) {
+  int k = 0;
+  while ((1 << k) < power) ++k;
+  return k;
 }
 
 // ------------------------------------------------------------------------------------------

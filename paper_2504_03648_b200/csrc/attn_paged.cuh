@@ -9,12 +9,15 @@ namespace aibx {
 
 struct AttnPlan {
   int G = 0;
+  int row_limit = 0;                     // rows up to which a request is the row kernel's
   bool rows = false, tiles = false;      // which kernels run
   uint64_t rows_bytes = 0, workspace = 0;
 };
 
-// The row kernel alone where no request can have more than kRowsMax rows; the tile kernel alone
-// for a single request; both for a batch, each taking the requests of its kind.
+// The row kernel alone where no request can have more than 16 rows; the tile kernel alone for a
+// single request; both for a batch, each taking the requests of its kind.  The row kernel comes
+// for 8 rows and for 16; beside the tile kernel it is the one for 8 where that holds a request's
+// single token.
 inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
                          const aibx_attn_params_t* p, AttnPlan& plan) {
   PagedPool pool;
@@ -37,9 +40,10 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
   plan.G = p->num_q_heads / L.num_kv_heads;
   if (plan.G > 128 || L.num_blocks > 0x7fffffffu) return AIBX_ERR_UNSUPPORTED;
   const long long bound = b->max_new > 0 ? b->max_new : (1LL << 31);
-  plan.tiles = bound * plan.G > kRowsMax;
-  plan.rows = !plan.tiles || b->R > 1;
-  plan.rows_bytes = 2ull * sm_count() * kRowsMax * (L.head_dim + 2) * sizeof(float);
+  plan.tiles = bound * plan.G > 16;
+  plan.rows = !plan.tiles || (b->R > 1 && plan.G <= 16);
+  if (plan.rows) plan.row_limit = (plan.tiles ? plan.G : bound * plan.G) <= 8 ? 8 : 16;
+  plan.rows_bytes = 2ull * sm_count() * plan.row_limit * (L.head_dim + 2) * sizeof(float);
   plan.workspace = plan.rows ? plan.rows_bytes : 0;
   if (plan.tiles) plan.workspace += 2ull * sm_count() * 2 * kTileRows * (L.head_dim + 2) * sizeof(float);
   return AIBX_OK;
@@ -48,7 +52,8 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
 template <int D, bool F8, typename QT>
 inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cudaStream_t st) {
   if (plan.rows) {
-    const int32_t rc = launch_attn_rows<D, F8, QT>(a, type, st);
+    const int32_t rc = plan.row_limit == 8 ? launch_attn_rows<D, F8, QT, 8>(a, type, st)
+                                           : launch_attn_rows<D, F8, QT, 16>(a, type, st);
     if (rc != AIBX_OK) return rc;
     a.slots += plan.rows_bytes / sizeof(float);
   }

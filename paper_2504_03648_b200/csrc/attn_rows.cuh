@@ -17,32 +17,36 @@
 // of one block and head), 160 KB per SM outstanding, and runs ahead over the seams between
 // requests, so that the memory never idles; eight warps consume, 16 tokens each at a time, with
 // their own m, l and O, joined once per (request, head).
-// Fragments are read from shared memory without transposition: the order of the contraction index
-// is free as long as both operands agree.  For Q K^T a lane's 16-byte piece of a K row serves as
-// the k-indices of two MMAs; for P V a lane reads the same 16-byte column piece of its four
-// tokens and pairs tokens with byte permutes.
+// The keys are the MMA's M dimension and the query rows its N of 8: S^T = K Q^T and O^T = V^T P^T,
+// so that 8 rows (7 or 8 query heads of one token) waste nothing.  Fragments are read from shared
+// memory without transposition: the order of the contraction index is free as long as both
+// operands agree.  For K Q^T a lane's 16-byte piece of a K row serves as the k-indices of two MMAs;
+// for V^T P^T a lane reads the same 16-byte column piece of its four tokens and pairs tokens with
+// byte permutes; P^T goes from accumulator to operand layout with movmatrix.
 #pragma once
 
 #include "attn_common.cuh"
 
 namespace aibx {
 
-constexpr int kRowWarps = 8;
 constexpr int kRowStages = 5;
 constexpr int kRowHalfStage = 16384;                       // bytes of K (and of V) per stage
-constexpr int kScaleWarps = 3;                            // 12 warps in all: 168 registers each
+constexpr int kScaleWarps = 3;
 
-template <int D, bool F8>
+template <int D, bool F8, int ROWS>
 struct RowShape {
+  static constexpr int kWarps = 8;                           // consumers (16 of them, at 96 registers
+                                                             // each: 297 us against 215)
+  static constexpr int kNQ = ROWS / 8;                       // MMAs across the rows
   static constexpr int kElem = F8 ? 1 : 2;
   static constexpr int kTok = kRowHalfStage / (D * kElem);   // tokens per stage
   static constexpr int kRowBytes = F8 ? D : 128;             // bytes of a shared-memory row
   static constexpr int kCols = F8 ? 1 : D / 64;              // 128-byte columns of a 16-bit row
   static constexpr int kTasks = kTok / 16;
-  static constexpr int kThreads = 32 * (kRowWarps + 1 + (F8 ? kScaleWarps : 0));
-  static constexpr int kSmem = kRowStages * 2 * kRowHalfStage + kRowWarps / 2 * kRowsMax * D * 4 +
+  static constexpr int kThreads = 32 * (kWarps + 1 + (F8 ? kScaleWarps : 0));
+  static constexpr int kSmem = kRowStages * 2 * kRowHalfStage + kWarps / 2 * ROWS * D * 4 +
                                (F8 ? kRowStages * 2 * kTok : 0) + 1024;
-  static constexpr int kSlot = kRowsMax * (D + 2);           // floats per workspace slot
+  static constexpr int kSlot = ROWS * (D + 2);               // floats per workspace slot
 };
 
 __device__ __forceinline__ void mma_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1,
@@ -58,6 +62,18 @@ __device__ __forceinline__ void mma_16816(float* c, const uint32_t* a, uint32_t 
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Transposes an 8x8 matrix of 16-bit numbers held as an MMA fragment.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint32_t e4m3_bits(uint32_t pair) {
+  const __half2 h = halves_of_e4m3(pair);
+  return *reinterpret_cast<const uint32_t*>(&h);
 }
 
 // The tiles of request r: first tile and how many (at least one, so that empty rows are written).
@@ -81,7 +97,7 @@ struct RowCost {
   const AttnArgs& a;
   __device__ __forceinline__ long long operator()(int r) const {
     const AttnRequest q = attn_request(a.b, a.pool.T, r);
-    if (q.n == 0 || (long long)q.n * a.G > kRowsMax) return 0;
+    if (q.n == 0 || (long long)q.n * a.G > a.row_limit) return 0;
     return (long long)row_span<TOK>(a, q).tiles * a.pool.H;
   }
 };
@@ -119,7 +135,7 @@ struct RowWalk {
       do {
         ++r;
         q = attn_request(a.b, a.pool.T, r);
-      } while (q.n == 0 || (long long)q.n * a.G > kRowsMax);
+      } while (q.n == 0 || (long long)q.n * a.G > a.row_limit);
       span = row_span<TOK>(a, q);
       off = pos - base;
     }
@@ -133,37 +149,68 @@ struct RowWalk {
   __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == span.tiles; }
 };
 
-// Block ids of a tile's boxes, one per lane; `valid` where the box is there and holds keys.
+// Block ids of the boxes of a segment's tiles, in order.  A lane fetches the id of one box, 32
+// boxes at a time, and the next 32 are under way while these are used: the loader never waits for
+// the table (looking at an id as soon as it was asked for cost the latency of the load per tile:
+// 302 instead of 285 us for 64 single tokens over 292,000 cached ones).
 template <int TOK>
-__device__ __forceinline__ uint32_t box_block(const AttnArgs& a, const uint32_t* row, int tile,
-                                              int lane, int boxes, int lo, int hi, bool tell,
-                                              bool& valid, int& slot) {
-  const int tok = tile * TOK + lane * a.box;
-  valid = lane < boxes && tok < hi && tok + a.box > lo;
-  slot = 0;
-  uint32_t id = 0;
-  if (valid) {
-    const int at = tok / a.pool.T;
-    slot = tok - at * a.pool.T;
-    id = __ldg(row + at);
-    if (id >= a.pool.num_blocks) {
-      if (id != AIBX_NO_BLOCK && tell) raise_status(AIBX_ERR_RANGE);
-      valid = false;
-    }
-  }
-  return id;
-}
+struct BoxIds {
+  const AttnArgs& a;
+  const uint32_t* row;
+  int lane, boxes, per;          // boxes per tile (a power of two), tiles per 32 boxes
+  int tile, end, lo, hi;         // next tile to be asked for
+  uint32_t id, id_next;
+  int used;                      // tiles of the current 32 boxes already given out
+  int slot, slot_step;           // this lane's first slot in the next tile, and its way per tile
 
-template <int D, bool F8, typename QT>
-__global__ void __launch_bounds__(RowShape<D, F8>::kThreads, 1)
-attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a) {
-  using S = RowShape<D, F8>;
+  __device__ __forceinline__ BoxIds(const AttnArgs& args, const uint32_t* table, int tile0, int tile1,
+                                    int lo_, int hi_)
+      : a(args), row(table), lane(threadIdx.x & 31), boxes(TOK >> args.box_log), per(32 / boxes), tile(tile0),
+        end(tile1), lo(lo_), hi(hi_), id(0), used(0) {
+    id_next = ask();
+    used = per;
+    slot = (int)(((long long)tile0 * TOK + lane * a.box) % a.pool.T);
+    slot_step = TOK % a.pool.T;
+  }
+  __device__ __forceinline__ void step_slot() {
+    slot += slot_step;
+    if (slot >= a.pool.T) slot -= a.pool.T;
+  }
+  __device__ __forceinline__ uint32_t ask() {
+    const int t = tile + lane / boxes;
+    const long long tok = (long long)t * TOK + (lane & (boxes - 1)) * a.box;
+    tile += per;
+    return t < end && tok < hi && tok + a.box > lo ? __ldg(row + (int)tok / a.pool.T) : AIBX_NO_BLOCK;
+  }
+  // The next tile's box of this lane (lanes below `boxes`): its block, and whether it is there.
+  __device__ __forceinline__ bool give(uint32_t& block, bool tell) {
+    if (used == per) {
+      id = id_next;
+      id_next = ask();
+      used = 0;
+    }
+    block = __shfl_sync(0xffffffffu, id, (used * boxes + lane) & 31);
+    ++used;
+    if (lane >= boxes || block == AIBX_NO_BLOCK) return false;
+    if (block >= a.pool.num_blocks) {
+      if (tell) raise_status(AIBX_ERR_RANGE);
+      return false;
+    }
+    return true;
+  }
+};
+
+template <int D, bool F8, typename QT, int ROWS>
+__global__ void __launch_bounds__(RowShape<D, F8, ROWS>::kThreads, 1)
+attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                 const __grid_constant__ AttnArgs a) {
+  using S = RowShape<D, F8, ROWS>;
   using MT = typename std::conditional<F8, __half, QT>::type;   // operand type of the MMAs
-  constexpr int TOK = S::kTok, RB = S::kRowBytes;
+  constexpr int TOK = S::kTok, RB = S::kRowBytes, kRowWarps = S::kWarps;
   extern __shared__ unsigned char s_raw[];
   __shared__ __align__(8) unsigned long long s_full[kRowStages], s_empty[kRowStages];
   __shared__ unsigned int s_mask[kRowStages];
-  __shared__ float s_m[2][kRowWarps][kRowsMax], s_l[2][kRowWarps][kRowsMax];
+  __shared__ float s_m[2][kRowWarps][ROWS], s_l[2][kRowWarps][ROWS];
   __shared__ long long s_scan[33];
   __shared__ WorkStart s_start;
   __shared__ int s_abort;
@@ -171,7 +218,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   const unsigned int smem0 = (smem_u32(s_raw) + 1023u) & ~1023u;
   unsigned char* ring = s_raw + (smem0 - smem_u32(s_raw));
   float* merge = reinterpret_cast<float*>(ring + kRowStages * 2 * kRowHalfStage);
-  unsigned char* s_scale = reinterpret_cast<unsigned char*>(merge + kRowWarps / 2 * kRowsMax * D);
+  unsigned char* s_scale = reinterpret_cast<unsigned char*>(merge + kRowWarps / 2 * ROWS * D);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 
   if (threadIdx.x == 0) {
@@ -186,63 +233,54 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   if (a.check_bound && blockIdx.x == 0)
     for (int r = threadIdx.x; r < a.b.R; r += S::kThreads) {
       const AttnRequest q = attn_request(a.b, a.pool.T, r);
-      if ((long long)q.n * a.G > kRowsMax) raise_status(AIBX_ERR_RANGE);
+      if ((long long)q.n * a.G > a.row_limit) raise_status(AIBX_ERR_RANGE);
     }
   const RowCost<TOK> cost{a};
   const WorkStart w = locate_piece<S::kThreads>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   RowWalk<TOK> walk(a, w, blockIdx.x, gridDim.x);
   volatile int* abort_flag = &s_abort;
-  const int boxes = TOK / a.box;
 
   if (warp == kRowWarps) {
     // ---------------------------------------------------------------- loader warp
-    unsigned int it = 0;
+    // Its instructions per tile are what a tile takes at least: counters instead of divisions.
+    unsigned int issued = 0, s = 0, phase = 1;               // (a fresh barrier passes for phase 1)
+    const unsigned int box_bytes = (unsigned int)a.box * D * S::kElem;
     while (walk.next()) {
       const uint32_t* row;
       long long entries;
       table_row(a.b, walk.r, row, entries);
       if (walk.q.keys < walk.q.len && walk.head == 0 && walk.t0 == 0 && lane == 0)
         raise_status(AIBX_ERR_RANGE);                      // tokens the table has no entry for
-      bool valid, valid_next = false;
-      int slot, slot_next = 0;
-      uint32_t id = box_block<TOK>(a, row, walk.span.tile0 + walk.t0, lane, boxes, walk.span.lo,
-                                   walk.span.hi, walk.head == 0, valid, slot);
-      for (int t = walk.t0; t < walk.t1; ++t, ++it) {
-        uint32_t id_next = 0;
-        if (t + 1 < walk.t1)
-          id_next = box_block<TOK>(a, row, walk.span.tile0 + t + 1, lane, boxes, walk.span.lo,
-                                   walk.span.hi, walk.head == 0, valid_next, slot_next);
-        const int s = (int)(it % kRowStages);
+      BoxIds<TOK> ids(a, row, walk.span.tile0 + walk.t0, walk.span.tile0 + walk.t1, walk.span.lo, walk.span.hi);
+      for (int t = walk.t0; t < walk.t1; ++t, ++issued) {
+        uint32_t id;
+        bool valid = ids.give(id, walk.head == 0);
         const unsigned int bar = smem_u32(&s_full[s]);
-        if (it >= kRowStages) ring_wait(smem_u32(&s_empty[s]), (it / kRowStages - 1) & 1u, abort_flag);
-        __syncwarp();
-        if (*abort_flag) valid = false;
+        if (!ring_wait(smem_u32(&s_empty[s]), phase, abort_flag)) valid = false;
         const unsigned int mask = __ballot_sync(0xffffffffu, valid);
         if (lane == 0) {
           s_mask[s] = mask;
           if (mask)
-            mbar_arrive_expect_tx(bar, (unsigned int)__popc(mask) * 2u * a.box * D * S::kElem);
+            mbar_arrive_expect_tx(bar, (unsigned int)__popc(mask) * 2u * box_bytes);
           else
             mbar_arrive(bar);
         }
         __syncwarp();
         if (valid) {
-          const unsigned int dst = smem0 + s * 2 * kRowHalfStage + lane * a.box * RB;
-#pragma unroll
-          for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-            for (int c = 0; c < S::kCols; ++c)
-              tensor_load_5d(dst + kv * kRowHalfStage + c * TOK * RB, &map, bar, c * 64, slot,
-                             walk.head, (int)id, kv);
+          const unsigned int dst = smem0 + s * 2 * kRowHalfStage + lane * box_bytes;
+          tensor_load_5d(dst, &map_k, bar, 0, ids.slot, 0, walk.head, (int)id);
+          tensor_load_5d(dst + kRowHalfStage, &map_v, bar, 0, ids.slot, 0, walk.head, (int)id);
         }
-        id = id_next;
-        valid = valid_next;
-        slot = slot_next;
+        ids.step_slot();
+        if (++s == kRowStages) {
+          s = 0;
+          phase ^= 1u;
+        }
       }
     }
     // what is still in flight targets this CTA's shared memory: wait for it before leaving
-    for (unsigned int i = it > kRowStages ? it - kRowStages : 0; i < it; ++i)
+    for (unsigned int i = issued > kRowStages ? issued - kRowStages : 0; i < issued; ++i)
       ring_drain(smem_u32(&s_full[i % kRowStages]), (i / kRowStages) & 1u);
     return;
   }
@@ -304,23 +342,30 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 
   // ------------------------------------------------------------------ consumer warps
   const int g = lane >> 2, t4 = lane & 3;
-  constexpr int kNT = D / 8;                               // n-tiles of O
+  constexpr int NQ = S::kNQ;
+  constexpr int kMT = D / 16;                              // 16-dim tiles of O^T
   constexpr int kPiece = F8 ? 16 : 8;                      // elements of a lane's piece of a K row
   constexpr int kPieces = D / (4 * kPiece);
   constexpr int kSteps = kPiece / 4;                       // MMAs per piece
-  unsigned int it = 0;
-  int seg = 0;
+  // a box lies column by column, `box` rows of RB bytes each; 16 tokens are two runs of 8 rows
+  const int boxes = TOK >> a.box_log;
+  const int col_stride = a.box * RB;
+  const int run_stride = a.box >= 16 ? 8 * RB : col_stride * S::kCols;
+  int stage = 0, seg = 0;
+  unsigned int phase = 0;
+  int turn = warp;                                         // first task of the next stage that is this warp's
+  const unsigned int all_boxes = boxes == 32 ? 0xffffffffu : (1u << boxes) - 1u;
   while (walk.next()) {
     const int n_rows = walk.q.n * a.G;
     const int first = walk.q.len - walk.q.n;
-    uint32_t qf[kPieces][kSteps][4];
-    float qscale[2];
-    int prow[2];
+    // ---- queries: row x * 8 + g as the operand's column g; their scale for columns 2 t4, 2 t4 + 1
+    uint32_t qf[NQ][kPieces][kSteps][2];
+    float qscale[NQ][2];
+    int prow[NQ][2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int i = g + 8 * h;
+    for (int x = 0; x < NQ; ++x) {
+      const int i = x * 8 + g;
       const int ti = min(i, n_rows - 1) / a.G;
-      prow[h] = first + ti;
       const QT* src = reinterpret_cast<const QT*>(a.q) + (walk.q.tok0 + ti) * a.q_tok +
                       (long long)(walk.head * a.G + (i - ti * a.G)) * a.q_head;
       uint32_t raw[kPieces][kPiece / 2];
@@ -336,7 +381,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           raw[p][4 * e + 3] = v.w;
         }
       float down = 1.0f, up = 1.0f;
-      if (F8) {
+      if constexpr (F8) {
         float amax = 0.0f;
 #pragma unroll
         for (int p = 0; p < kPieces; ++p)
@@ -356,242 +401,297 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             raw[p][e] = Bits16<MT>::pack(f.x * down, f.y * down);
           }
       }
-      qscale[h] = up * a.scale_log2;
 #pragma unroll
       for (int p = 0; p < kPieces; ++p)
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
-          qf[p][s][h] = raw[p][2 * s];
-          qf[p][s][2 + h] = raw[p][2 * s + 1];
+          qf[x][p][s][0] = raw[p][2 * s];
+          qf[x][p][s][1] = raw[p][2 * s + 1];
         }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        qscale[x][h] = __shfl_sync(0xffffffffu, up, (2 * t4 + h) * 4) * a.scale_log2;
+        prow[x][h] = first + min(x * 8 + 2 * t4 + h, n_rows - 1) / a.G;
+      }
     }
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-    float o[kNT][4];
+    float m[NQ][2], l[NQ][2], o[NQ][kMT][4];
 #pragma unroll
-    for (int j = 0; j < kNT; ++j)
+    for (int x = 0; x < NQ; ++x) {
+      m[x][0] = m[x][1] = -INFINITY;
+      l[x][0] = l[x][1] = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[j][e] = 0.0f;
+      for (int j = 0; j < kMT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[x][j][e] = 0.0f;
+    }
 
-    for (int t = walk.t0; t < walk.t1; ++t, ++it) {
-      const int s = (int)(it % kRowStages);
-      ring_wait(smem_u32(&s_full[s]), (it / kRowStages) & 1u, abort_flag);
-      __syncwarp();
-      const unsigned int boxmask = s_mask[s];
-      // the 16-token tasks of all stages go round the warps in turn
-      for (int task = (int)(((unsigned int)warp - it * S::kTasks) & (kRowWarps - 1)); task < S::kTasks; task += kRowWarps) {
-        const int key0 = (walk.span.tile0 + t) * TOK + task * 16;
-        if (key0 >= walk.span.hi || key0 + 15 < walk.span.lo) continue;
-        const int b0 = task * 16 / a.box, b1 = (task * 16 + 15) / a.box;
-        const unsigned int want = ((2u << (b1 - b0)) - 1u) << b0;
-        if ((boxmask & want) == 0) continue;
-        // all 16 keys seen by all rows: the rows' positions run from `first` to len - 1
-        const bool open = (boxmask & want) == want && key0 + 15 < walk.span.hi &&
-                          (!a.causal || key0 + 15 <= first) &&
-                          (a.window <= 0 || key0 > (long long)walk.q.len - 1 - a.window);
-        const unsigned char* kbase = ring + s * 2 * kRowHalfStage + task * 16 * RB;
-        const unsigned char* vbase = kbase + kRowHalfStage;
-        float c[2][4];
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) c[nt][e] = 0.0f;
-          const int row = nt * 8 + g;
-#pragma unroll
-          for (int p = 0; p < kPieces; ++p) {
-            if constexpr (F8) {
-              const int piece = p * 4 + t4;
-              const unsigned char* src = kbase + row * RB + ((RB == 128 ? piece ^ (row & 7) : piece) << 4);
-              const uint4 v = *reinterpret_cast<const uint4*>(src);
-              const uint32_t wv[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-              for (int st = 0; st < 4; ++st) {
-                const __half2 lo = halves_of_e4m3(wv[st] & 0xffffu), hi = halves_of_e4m3(wv[st] >> 16);
-                mma_16816(c[nt], qf[p][st], *reinterpret_cast<const uint32_t*>(&lo),
-                          *reinterpret_cast<const uint32_t*>(&hi), MT());
-              }
-            } else {
-              const int piece = (p & 1) * 4 + t4;
-              const unsigned char* src = kbase + (p >> 1) * TOK * 128 + row * 128 + ((piece ^ (row & 7)) << 4);
-              const uint4 v = *reinterpret_cast<const uint4*>(src);
-              mma_16816(c[nt], qf[p][0], v.x, v.y, MT());
-              mma_16816(c[nt], qf[p][1], v.z, v.w, MT());
-            }
-          }
-        }
-        // ---- scores in powers of two; over e4m3 with the V exponent of each key added
-        float unshift[2][2];                                // 2^-b_j
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float kf = 1.0f, vexp = 0.0f;
-            if constexpr (F8) {
-              const unsigned char* sc = s_scale + s * 2 * TOK + task * 16 + nt * 8 + 2 * t4 + e;
-              const int kb = sc[0], vb = sc[TOK];
-              kf = kb == 255 ? NAN : power_of_byte(kb);
-              const int ve = max(vb - 127, -100);
-              vexp = vb == 255 ? NAN : (float)ve;
-              unshift[nt][e] = __uint_as_float((unsigned int)(127 - min(ve, 126)) << 23);
-            }
-            c[nt][e] = fmaf(c[nt][e] * kf, qscale[0], vexp);
-            c[nt][2 + e] = fmaf(c[nt][2 + e] * kf, qscale[1], vexp);
-          }
-        unsigned int seen = 0xfu;                           // this lane's four tokens: V rows that count
-        if (!open) {
-          seen = 0;
-#pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int rel = nt * 8 + 2 * t4 + e;
-              const int key = key0 + rel;
-              const bool here = key >= walk.span.lo && key < walk.span.hi &&
-                                ((boxmask >> ((task * 16 + rel) / a.box)) & 1u);
-              if (here) seen |= 1u << (nt * 2 + e);
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const bool ok = here && (!a.causal || key <= prow[h]) &&
-                                (a.window <= 0 || (long long)key > (long long)prow[h] - a.window);
-                if (!ok) c[nt][2 * h + e] = -INFINITY;
-              }
-            }
-        }
-        // ---- running maximum, moved only when it grows by more than 2^8
-        float mt[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float x = fmaxf(fmaxf(c[0][2 * h], c[0][2 * h + 1]), fmaxf(c[1][2 * h], c[1][2 * h + 1]));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-          mt[h] = x;
-        }
-        const bool grow = mt[0] > m[0] + 8.0f || mt[1] > m[1] + 8.0f;   // also from -infinity
-        if (__any_sync(0xffffffffu, grow)) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float mn = fmaxf(m[h], mt[h]);
-            const float al = mn == -INFINITY ? 1.0f : exp2_fast(m[h] - mn);
-            m[h] = mn;
-            l[h] *= al;
-#pragma unroll
-            for (int j = 0; j < kNT; ++j) {
-              o[j][2 * h] *= al;
-              o[j][2 * h + 1] *= al;
-            }
-          }
-        }
-        const float ms[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
-        uint32_t pa[4];
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float p0 = exp2_fast(c[nt][2 * h] - ms[h]), p1 = exp2_fast(c[nt][2 * h + 1] - ms[h]);
-            if constexpr (F8)
-              l[h] += p0 * unshift[nt][0] + p1 * unshift[nt][1];
-            else
-              l[h] += p0 + p1;
-            pa[nt * 2 + h] = Bits16<MT>::pack(p0, p1);
-          }
-        // ---- O += P V
-        const int r0 = 2 * t4;
-        if constexpr (F8) {
-          constexpr int kW = D / 32;                        // words of a lane's piece of a V row
-          uint32_t v[4][kW];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int row = (e >> 1) * 8 + r0 + (e & 1);
-            if constexpr (RB == 128) {
-              const uint4 x = *reinterpret_cast<const uint4*>(vbase + row * 128 + ((g ^ (row & 7)) << 4));
-              v[e][0] = x.x; v[e][1] = x.y; v[e][2] = x.z; v[e][3] = x.w;
-            } else {
-              const uint2 x = *reinterpret_cast<const uint2*>(vbase + row * RB + g * 8);
-              v[e][0] = x.x; v[e][1] = x.y;
-            }
-            if (!((seen >> e) & 1u)) {
-#pragma unroll
-              for (int q = 0; q < kW; ++q) v[e][q] = 0;
-            }
-          }
-#pragma unroll
-          for (int q = 0; q < kW; ++q) {
-            uint32_t b[2][4];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const uint32_t lo = __byte_perm(v[2 * half][q], v[2 * half + 1][q], 0x5140);
-              const uint32_t hi = __byte_perm(v[2 * half][q], v[2 * half + 1][q], 0x7362);
-              const __half2 x0 = halves_of_e4m3(lo & 0xffffu), x1 = halves_of_e4m3(lo >> 16);
-              const __half2 x2 = halves_of_e4m3(hi & 0xffffu), x3 = halves_of_e4m3(hi >> 16);
-              b[half][0] = *reinterpret_cast<const uint32_t*>(&x0);
-              b[half][1] = *reinterpret_cast<const uint32_t*>(&x1);
-              b[half][2] = *reinterpret_cast<const uint32_t*>(&x2);
-              b[half][3] = *reinterpret_cast<const uint32_t*>(&x3);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mma_16816(o[4 * q + e], pa, b[0][e], b[1][e], MT());
-          }
-        } else {
-#pragma unroll
-          for (int hh = 0; hh < S::kCols; ++hh) {
-            uint32_t v[4][4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int row = (e >> 1) * 8 + r0 + (e & 1);
-              const uint4 x = *reinterpret_cast<const uint4*>(vbase + hh * TOK * 128 + row * 128 +
-                                                              ((g ^ (row & 7)) << 4));
-              v[e][0] = x.x; v[e][1] = x.y; v[e][2] = x.z; v[e][3] = x.w;
-              if (!((seen >> e) & 1u)) v[e][0] = v[e][1] = v[e][2] = v[e][3] = 0;
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              mma_16816(o[hh * 8 + 2 * q], pa, __byte_perm(v[0][q], v[1][q], 0x5410),
-                        __byte_perm(v[2][q], v[3][q], 0x5410), MT());
-              mma_16816(o[hh * 8 + 2 * q + 1], pa, __byte_perm(v[0][q], v[1][q], 0x7632),
-                        __byte_perm(v[2][q], v[3][q], 0x7632), MT());
-            }
-          }
-        }
+    // the rows' positions run from `first` to len - 1: keys from open_lo to open_hi - 1 all see
+    const int open_hi = a.causal ? min(walk.span.hi, first + 1) : walk.span.hi;
+    const int open_lo = max(walk.span.lo, a.window > 0 ? walk.q.len - a.window : 0);
+    for (int t = walk.t0; t < walk.t1; ++t) {
+      // Every warp waits for every stage and hands every stage back, its own or not: a phase bit
+      // tells a stage from the next one in its place only to a warp that misses none.
+      const int s = stage;
+      ring_wait(smem_u32(&s_full[s]), phase, abort_flag);
+      if (++stage == kRowStages) {
+        stage = 0;
+        phase ^= 1u;
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&s_empty[s]));
+      const unsigned int boxmask = s_mask[s];
+      bool handed = false;
+      const int tile_key0 = (walk.span.tile0 + t) * TOK;
+      // the 16-token tasks of all stages go round the warps in turn
+      for (int task = turn; task < S::kTasks; task += kRowWarps) {
+        const int key0 = tile_key0 + task * 16;
+        const int b0 = (task * 16) >> a.box_log;
+        // all 16 keys there, and seen by all rows
+        const bool open = boxmask == all_boxes && key0 >= open_lo && key0 + 16 <= open_hi;
+        if (!open) {
+          const int b1 = (task * 16 + 15) >> a.box_log;
+          const unsigned int want = ((2u << (b1 - b0)) - 1u) << b0;
+          if ((boxmask & want) == 0 || key0 >= walk.span.hi || key0 + 15 < walk.span.lo) continue;
+        }
+        const unsigned char* kbase =
+            ring + s * 2 * kRowHalfStage + ((b0 * S::kCols) << a.box_log) * RB + (task * 16 - (b0 << a.box_log)) * RB;
+        const unsigned char* vbase = kbase + kRowHalfStage;
+        // ---- everything the task needs, into registers; then the stage goes back to the loader
+        // (held until the task was done, it was missing from the copies in flight: 215 us)
+        uint4 kr[kPieces][2];
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+          const int piece = F8 ? p * 4 + t4 : (p & 1) * 4 + t4;
+          const unsigned char* src = kbase + (F8 ? 0 : (p >> 1) * col_stride) + g * RB +
+                                     ((RB == 128 ? piece ^ g : piece) << 4);
+          kr[p][0] = *reinterpret_cast<const uint4*>(src);
+          kr[p][1] = *reinterpret_cast<const uint4*>(src + run_stride);
+        }
+        // V: the pieces of this lane's four tokens
+        constexpr int kW = F8 ? D / 32 : 4;                  // words of a piece
+        constexpr int kVC = F8 ? 1 : S::kCols;
+        uint32_t v[kVC][4][kW];
+#pragma unroll
+        for (int cc = 0; cc < kVC; ++cc)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r8 = 2 * t4 + (e & 1);
+            const unsigned char* src = vbase + cc * col_stride + (e >> 1) * run_stride + r8 * RB;
+            if constexpr (RB == 128) {
+              const uint4 y = *reinterpret_cast<const uint4*>(src + ((g ^ r8) << 4));
+              v[cc][e][0] = y.x; v[cc][e][1] = y.y; v[cc][e][2] = y.z; v[cc][e][3] = y.w;
+            } else {
+              const uint2 y = *reinterpret_cast<const uint2*>(src + g * 8);
+              v[cc][e][0] = y.x; v[cc][e][1] = y.y;
+            }
+          }
+        int kbyte[2] = {127, 127}, vbyte[2] = {127, 127};
+        if constexpr (F8) {
+          const unsigned char* sc = s_scale + s * 2 * TOK + task * 16 + g;
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            kbyte[r] = sc[r * 8];
+            vbyte[r] = sc[TOK + r * 8];
+          }
+        }
+        if (task + kRowWarps >= S::kTasks) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&s_empty[s]));
+          handed = true;
+        }
+        // ---- S^T = K Q^T, in two chains
+        float c[NQ][4], c2[NQ][4];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[x][e] = c2[x][e] = 0.0f;
+#pragma unroll
+        for (int p = 0; p < kPieces; ++p) {
+          const uint4 lo = kr[p][0], hi = kr[p][1];
+          if constexpr (F8) {
+            const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+            for (int st = 0; st < 4; ++st) {
+              const uint32_t af[4] = {e4m3_bits(wl[st] & 0xffffu), e4m3_bits(wh[st] & 0xffffu),
+                                      e4m3_bits(wl[st] >> 16), e4m3_bits(wh[st] >> 16)};
+#pragma unroll
+              for (int x = 0; x < NQ; ++x)
+                mma_16816((st & 1) ? c2[x] : c[x], af, qf[x][p][st][0], qf[x][p][st][1], MT());
+            }
+          } else {
+            const uint32_t a0[4] = {lo.x, hi.x, lo.y, hi.y}, a1[4] = {lo.z, hi.z, lo.w, hi.w};
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) {
+              mma_16816(c[x], a0, qf[x][p][0][0], qf[x][p][0][1], MT());
+              mma_16816(c2[x], a1, qf[x][p][1][0], qf[x][p][1][1], MT());
+            }
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) c[x][e] += c2[x][e];
+        // ---- scores in powers of two; over e4m3 with the V exponent of each key added
+        float unshift[2];                                   // 2^-b_j
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float kf = 1.0f, vexp = 0.0f;
+          if constexpr (F8) {
+            const int kb = kbyte[r], vb = vbyte[r];
+            kf = kb == 255 ? NAN : power_of_byte(kb);
+            const int ve = max(vb - 127, -100);
+            vexp = vb == 255 ? NAN : (float)ve;
+            unshift[r] = __uint_as_float((unsigned int)(127 - min(ve, 126)) << 23);
+          }
+#pragma unroll
+          for (int x = 0; x < NQ; ++x)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float& z = c[x][2 * r + h];
+              z = F8 ? fmaf(z * kf, qscale[x][h], vexp) : z * qscale[x][h];
+            }
+        }
+        if (!open) {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const int rel = r * 8 + g, key = key0 + rel;
+            const bool here = key >= walk.span.lo && key < walk.span.hi && ((boxmask >> ((task * 16 + rel) >> a.box_log)) & 1u);
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const bool ok = here && (!a.causal || key <= prow[x][h]) &&
+                                (a.window <= 0 || (long long)key > (long long)prow[x][h] - a.window);
+                if (!ok) c[x][2 * r + h] = -INFINITY;
+              }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {                      // V rows nobody sees may hold anything
+            const int rel = (e >> 1) * 8 + 2 * t4 + (e & 1), key = key0 + rel;
+            const bool here = key >= walk.span.lo && key < walk.span.hi && ((boxmask >> ((task * 16 + rel) >> a.box_log)) & 1u);
+            if (!here) {
+#pragma unroll
+              for (int cc = 0; cc < kVC; ++cc)
+#pragma unroll
+                for (int w4 = 0; w4 < kW; ++w4) v[cc][e][w4] = 0;
+            }
+          }
+        }
+        // ---- running maximum, moved only when it grows by more than 2^8
+        float mt[NQ][2];
+        bool grow = false;
+#pragma unroll
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float y = fmaxf(c[x][h], c[x][2 + h]);
+            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 4));
+            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
+            y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
+            mt[x][h] = y;
+            grow |= y > m[x][h] + 8.0f;                     // also from -infinity
+          }
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+          for (int x = 0; x < NQ; ++x)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float mn = fmaxf(m[x][h], mt[x][h]);
+              const float al = mn == -INFINITY ? 1.0f : exp2_fast(m[x][h] - mn);
+              m[x][h] = mn;
+              l[x][h] *= al;
+#pragma unroll
+              for (int j = 0; j < kMT; ++j) {
+                o[x][j][h] *= al;
+                o[x][j][2 + h] *= al;
+              }
+            }
+        }
+        uint32_t pb[NQ][2];
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+          const float m0 = m[x][0] == -INFINITY ? 0.0f : m[x][0], m1 = m[x][1] == -INFINITY ? 0.0f : m[x][1];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float p0 = exp2_fast(c[x][2 * r] - m0), p1 = exp2_fast(c[x][2 * r + 1] - m1);
+            l[x][0] += F8 ? p0 * unshift[r] : p0;
+            l[x][1] += F8 ? p1 * unshift[r] : p1;
+            pb[x][r] = transpose8(Bits16<MT>::pack(p0, p1));
+          }
+        }
+        // ---- O^T += V^T P^T
+#pragma unroll
+        for (int cc = 0; cc < kVC; ++cc)
+#pragma unroll
+          for (int w4 = 0; w4 < kW; ++w4) {
+            if constexpr (F8) {
+              const uint32_t lo0 = __byte_perm(v[cc][0][w4], v[cc][1][w4], 0x5140);
+              const uint32_t hi0 = __byte_perm(v[cc][0][w4], v[cc][1][w4], 0x7362);
+              const uint32_t lo1 = __byte_perm(v[cc][2][w4], v[cc][3][w4], 0x5140);
+              const uint32_t hi1 = __byte_perm(v[cc][2][w4], v[cc][3][w4], 0x7362);
+              const uint32_t a0[4] = {e4m3_bits(lo0 & 0xffffu), e4m3_bits(lo0 >> 16), e4m3_bits(lo1 & 0xffffu),
+                                      e4m3_bits(lo1 >> 16)};
+              const uint32_t a1[4] = {e4m3_bits(hi0 & 0xffffu), e4m3_bits(hi0 >> 16), e4m3_bits(hi1 & 0xffffu),
+                                      e4m3_bits(hi1 >> 16)};
+#pragma unroll
+              for (int x = 0; x < NQ; ++x) {
+                mma_16816(o[x][2 * w4], a0, pb[x][0], pb[x][1], MT());
+                mma_16816(o[x][2 * w4 + 1], a1, pb[x][0], pb[x][1], MT());
+              }
+            } else {
+              const uint32_t a0[4] = {
+                  __byte_perm(v[cc][0][w4], v[cc][1][w4], 0x5410), __byte_perm(v[cc][0][w4], v[cc][1][w4], 0x7632),
+                  __byte_perm(v[cc][2][w4], v[cc][3][w4], 0x5410), __byte_perm(v[cc][2][w4], v[cc][3][w4], 0x7632)};
+#pragma unroll
+              for (int x = 0; x < NQ; ++x) mma_16816(o[x][cc * 4 + w4], a0, pb[x][0], pb[x][1], MT());
+            }
+          }
+      }
+      turn = (turn - S::kTasks % kRowWarps + kRowWarps) % kRowWarps;
+      if (!handed) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_empty[s]));
+      }
     }
 
-    // ---- join the eight warps
+    // ---- join the warps
     const int par = seg & 1;
     ++seg;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-      if (t4 == 0) {
-        s_m[par][warp][g + 8 * h] = m[h];
-        s_l[par][warp][g + 8 * h] = l[h];
-      }
-    }
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * kRowWarps) : "memory");
-    // the upper four warps hand their O to the lower four, whose sums meet in shared memory
-#pragma unroll
-    for (int turn = 0; turn < 2; ++turn) {
-      const bool upper = warp >= kRowWarps / 2;
+    for (int x = 0; x < NQ; ++x)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int i = g + 8 * h;
-        if (i >= n_rows || upper != (turn == 0)) continue;
-        float top = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < kRowWarps; ++x) top = fmaxf(top, s_m[par][x][i]);
-        const float f = top == -INFINITY ? 0.0f : exp2_fast(m[h] - top);
-        float* dst = merge + ((warp & (kRowWarps / 2 - 1)) * kRowsMax + i) * D;
-#pragma unroll
-        for (int j = 0; j < kNT; ++j)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int n = 2 * t4 + e;
-            const int d = F8 ? n * (D / 8) + j : (j >> 3) * 64 + n * 8 + (j & 7);
-            const float x = o[j][2 * h + e] * f;
-            dst[d] = turn == 0 ? x : dst[d] + x;
-          }
+        for (int d = 4; d < 32; d <<= 1) l[x][h] += __shfl_xor_sync(0xffffffffu, l[x][h], d);
+        if (g == 0) {
+          s_m[par][warp][x * 8 + 2 * t4 + h] = m[x][h];
+          s_l[par][warp][x * 8 + 2 * t4 + h] = l[x][h];
+        }
       }
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * kRowWarps) : "memory");
+    // the upper half of the warps hands its O to the lower half, whose sums meet in shared memory
+#pragma unroll
+    for (int go = 0; go < 2; ++go) {
+      const bool upper = warp >= kRowWarps / 2;
+#pragma unroll
+      for (int x = 0; x < NQ; ++x)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int i = x * 8 + 2 * t4 + h;
+          if (i >= n_rows || upper != (go == 0)) continue;
+          float top = -INFINITY;
+#pragma unroll
+          for (int y = 0; y < kRowWarps; ++y) top = fmaxf(top, s_m[par][y][i]);
+          const float f = top == -INFINITY ? 0.0f : exp2_fast(m[x][h] - top);
+          float* dst = merge + ((warp % (kRowWarps / 2)) * ROWS + i) * D;
+#pragma unroll
+          for (int j = 0; j < kMT; ++j)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const int d = F8 ? g * (D / 8) + 2 * j + r : (j >> 2) * 64 + g * 8 + (j & 3) * 2 + r;
+              const float y = o[x][j][2 * r + h] * f;
+              dst[d] = go == 0 ? y : dst[d] + y;
+            }
+        }
       asm volatile("bar.sync 1, %0;" ::"n"(32 * kRowWarps) : "memory");
     }
     const bool whole = walk.whole();
@@ -609,7 +709,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       for (int y = 0; y < kRowWarps; ++y) sum += s_l[par][y][i] * exp2_fast(s_m[par][y][i] - safe);
 #pragma unroll
       for (int y = 0; y < kRowWarps / 2; ++y) {
-        const float2 p = *reinterpret_cast<const float2*>(merge + (y * kRowsMax + i) * D + d);
+        const float2 p = *reinterpret_cast<const float2*>(merge + (y * ROWS + i) * D + d);
         v0 += p.x;
         v1 += p.y;
       }
@@ -623,10 +723,10 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         if (a.lse && d == 0)
           a.lse[tok * (a.pool.H * a.G) + qh] = sum == 0.0f ? -INFINITY : 0.69314718056f * (top + log2f(sum));
       } else {
-        *reinterpret_cast<float2*>(slot + 2 * kRowsMax + i * D + d) = make_float2(v0, v1);
+        *reinterpret_cast<float2*>(slot + 2 * ROWS + i * D + d) = make_float2(v0, v1);
         if (d == 0) {
           slot[i] = top;
-          slot[kRowsMax + i] = sum;
+          slot[ROWS + i] = sum;
         }
       }
     }
@@ -635,10 +735,10 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 
 // Joins a (request, head) that was cut: block c takes the one whose last tile lies in CTA c and
 // whose first tile lies in an earlier CTA.
-template <int D, bool F8, typename QT>
+template <int D, bool F8, typename QT, int ROWS>
 __global__ void __launch_bounds__(256)
 attn_rows_join_kernel(const __grid_constant__ AttnArgs a) {
-  using S = RowShape<D, F8>;
+  using S = RowShape<D, F8, ROWS>;
   constexpr int TOK = S::kTok;
   __shared__ long long s_scan[33];
   __shared__ WorkStart s_start;
@@ -657,11 +757,11 @@ attn_rows_join_kernel(const __grid_constant__ AttnArgs a) {
     for (int c = c0; c <= c1; ++c) {
       const float* slot = a.slots + ((long long)c * 2 + (c == c0 && p0 != c0 * per ? 1 : 0)) * S::kSlot;
       const float mc = slot[i];
-      const float2 p = *reinterpret_cast<const float2*>(slot + 2 * kRowsMax + i * D + d);
+      const float2 p = *reinterpret_cast<const float2*>(slot + 2 * ROWS + i * D + d);
       const float tn = fmaxf(top, mc);
       const float safe = tn == -INFINITY ? 0.0f : tn;
       const float f0 = exp2_fast(top - safe), f1 = exp2_fast(mc - safe);
-      sum = sum * f0 + slot[kRowsMax + i] * f1;
+      sum = sum * f0 + slot[ROWS + i] * f1;
       v0 = v0 * f0 + p.x * f1;
       v1 = v1 * f0 + p.y * f1;
       top = tn;
@@ -694,24 +794,26 @@ inline int32_t launch_after(Kernel kernel, dim3 grid, unsigned int threads, cuda
   return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? AIBX_OK : AIBX_ERR_CUDA;
 }
 
-template <int D, bool F8, typename QT>
+template <int D, bool F8, typename QT, int ROWS>
 inline int32_t launch_attn_rows(AttnArgs a, int type, cudaStream_t st) {
-  using S = RowShape<D, F8>;
+  using S = RowShape<D, F8, ROWS>;
   a.box = gcd_int(a.pool.T, S::kTok);
-  CUtensorMap map;
-  const int32_t rc = pool_tensor_map(a.pool, type, a.box, &map);
+  a.box_log = log2_int(a.box);
+  CUtensorMap map_k, map_v;
+  int32_t rc = plane_tensor_map(a.pool, type, a.box, 0, &map_k);
+  if (rc == AIBX_OK) rc = plane_tensor_map(a.pool, type, a.box, 1, &map_v);
   if (rc != AIBX_OK) return rc;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return AIBX_ERR_CUDA;
   static size_t configured[64] = {0};
   static std::mutex lock;
-  if (!ensure_dynamic_smem(attn_rows_kernel<D, F8, QT>, S::kSmem, dev, configured, lock))
+  if (!ensure_dynamic_smem(attn_rows_kernel<D, F8, QT, ROWS>, S::kSmem, dev, configured, lock))
     return AIBX_ERR_CUDA;
   const unsigned int grid = (unsigned int)sm_count();
-  attn_rows_kernel<D, F8, QT><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
+  attn_rows_kernel<D, F8, QT, ROWS><<<grid, S::kThreads, S::kSmem, st>>>(map_k, map_v, a);
   const int32_t rc2 = launch_status();
   if (rc2 != AIBX_OK) return rc2;
-  return launch_after(attn_rows_join_kernel<D, F8, QT>, dim3(grid), 256, st, a);
+  return launch_after(attn_rows_join_kernel<D, F8, QT, ROWS>, dim3(grid), 256, st, a);
 }
 
 }  // namespace aibx

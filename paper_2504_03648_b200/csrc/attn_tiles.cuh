@@ -146,7 +146,7 @@ struct TileCost {
   __device__ __forceinline__ long long head_tiles(const AttnRequest& q, int& blocks) const {
     blocks = 0;
     const long long rows = (long long)q.n * a.G;
-    if (rows == 0 || (a.rows_too && rows <= kRowsMax)) return 0;
+    if (rows <= a.row_limit) return 0;
     blocks = (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
     long long sum = 0;
     for (int b = 0; b < blocks; ++b) sum += tile_span(a, q, b).tiles;
@@ -201,9 +201,7 @@ struct TileWalk {
             ++r;
             q = attn_request(a.b, a.pool.T, r);
             const long long rows = (long long)q.n * a.G;
-            blocks = rows == 0 || (a.rows_too && rows <= kRowsMax)
-                         ? 0
-                         : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
+            blocks = rows <= a.row_limit ? 0 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
           } while (blocks == 0);
         }
       }
@@ -373,7 +371,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         if (mask != 0xffffffffu) {                         // blocks that are not there: rare
 #pragma unroll
           for (int k = 0; k < 128; ++k)
-            if (!((mask >> (k / a.box)) & 1u)) s[k] = 0xff800000u;
+            if (!((mask >> (k >> a.box_log)) & 1u)) s[k] = 0xff800000u;
         }
         if (key0 + kTileKeys > vis1 || key0 < vis0) {
           const int b0 = vis0 - key0, b1 = vis1 - key0;
@@ -576,7 +574,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       const unsigned int ring0 = F8 ? smem_u32(raws) : kv0;
       unsigned long long* full = F8 ? s_raw_full : s_kv_full;
       unsigned long long* empty = F8 ? s_raw_empty : s_kv_empty;
-      const int boxes = kTileKeys / a.box;
+      const int boxes = kTileKeys >> a.box_log;
       unsigned int buf = 0, phase = 1, issued = 0, step = 0;
       while (walk.next()) {
         const uint32_t* row;
@@ -584,11 +582,13 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         table_row(a.b, walk.r, row, entries);
         if (walk.q.keys < walk.q.len && walk.head == 0 && walk.block == 0 && walk.t0 == 0 && lane == 0)
           raise_status(AIBX_ERR_RANGE);                    // tokens the table has no entry for
+        BoxIds<kTileKeys> ids(a, row, walk.span.tile0 + walk.t0, walk.span.tile0 + walk.t1, walk.span.lo,
+                              walk.span.hi);
         for (int j = walk.t0; j < walk.t1; ++j, ++step) {
-          bool valid;
-          int slot;
-          const uint32_t id = box_block<kTileKeys>(a, row, walk.span.tile0 + j, lane, boxes, walk.span.lo,
-                                                   walk.span.hi, walk.head == 0, valid, slot);
+          uint32_t id;
+          const bool valid = ids.give(id, walk.head == 0);
+          const int slot = ids.slot;
+          ids.step_slot();
           // a box that is not there, or that holds no visible key, comes as zeros from beyond the pool
           const int block = valid ? (int)id : (int)a.pool.num_blocks;
           const int tok = (walk.span.tile0 + j) * kTileKeys + lane * a.box;
@@ -800,6 +800,7 @@ template <int D, bool F8, typename QT>
 inline int32_t launch_attn_tiles(AttnArgs a, int type, cudaStream_t st) {
   using S = TileShape<D, F8>;
   a.box = gcd_int(a.pool.T, kTileKeys);
+  a.box_log = log2_int(a.box);
   CUtensorMap map;
   const int32_t rc = pool_tensor_map(a.pool, type, a.box, &map);
   if (rc != AIBX_OK) return rc;
