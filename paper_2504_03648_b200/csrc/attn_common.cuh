@@ -13,6 +13,14 @@
 
 namespace aibx {
 
+// Division of a row number below 2^31 by a small divisor, as a multiplication: with
+// m = ceil(2^40 / d), d <= 2^8, n * m / 2^40 exceeds n / d by less than n / 2^40 < 1 / d.
+struct SmallDivisor {
+  unsigned long long m;
+  __device__ __forceinline__ int div(int n) const { return (int)(((unsigned long long)n * m) >> 40); }
+};
+inline SmallDivisor small_divisor(int d) { return SmallDivisor{((1ull << 40) + d - 1) / d}; }
+
 struct AttnArgs {
   PagedPool pool;
   PagedBatch b;
@@ -22,12 +30,13 @@ struct AttnArgs {
   long long q_tok, q_head, o_tok, o_head;   // element strides
   float scale_log2;                         // scale * log2(e): scores in powers of two
   int G;                                    // query heads per KV head
+  SmallDivisor by_g;
   int causal, window;
   int box, box_log;                         // tokens one tensor-map box covers: a power of two
   int row_limit;                            // requests of up to so many rows (tokens * G) are the
                                             // row kernel's, 0: none
   int check_bound;                          // report requests this call has no kernel for
-  float* slots;
+  float* slots;                             // two per CTA, then a JoinRecord per CTA
 };
 
 
@@ -81,19 +90,19 @@ __device__ __forceinline__ long long block_prefix(long long v, long long* scratc
 struct WorkStart {
   long long total;      // tiles of the whole line
   long long base;       // first position of request r's part of the line
-  int r;                // request in which this CTA's piece begins
+  int r;                // request in which this CTA's piece begins (-1: it is empty)
+  int head, block, off; // and there: head, block of rows, tiles of it that belong to earlier pieces
 };
 
 // Finds the request that holds position `index * per` of the line, per = ceil(total / pieces).
-// cost(r) = tiles of request r over all heads.  All N threads take part.
+// cost(r, on) = tiles of request r over all heads, asked by whole warps.  All N threads take part.
 template <int N, typename Cost>
-__device__ __forceinline__ WorkStart locate_piece(int R, unsigned int index, unsigned int pieces,
-                                                  long long* scratch, WorkStart* shared,
-                                                  const Cost& cost) {
+__device__ __forceinline__ void locate_piece(int R, unsigned int index, unsigned int pieces, long long* scratch,
+                                             WorkStart* shared, const Cost& cost) {
   const int tid = threadIdx.x;
   const bool one = R <= N;                 // every request has a thread: one look at each
   long long mine = 0, total, base = 0;
-  for (int r = tid; r < R; r += N) mine += cost(r);
+  for (int r0 = 0; r0 < R; r0 += N) mine += cost(r0 + tid, r0 + tid < R);
   long long before = block_prefix<N>(mine, scratch, total);
   const long long per = (total + pieces - 1) / pieces;
   const long long target = per * index;
@@ -111,7 +120,7 @@ __device__ __forceinline__ WorkStart locate_piece(int R, unsigned int index, uns
       }
     } else {
       for (int r0 = 0; r0 < R; r0 += N) {
-        const long long v = r0 + tid < R ? cost(r0 + tid) : 0;
+        const long long v = cost(r0 + tid, r0 + tid < R);
         long long sum;
         before = base + block_prefix<N>(v, scratch, sum);
         if (v > 0 && before <= target && target < before + v) {
@@ -124,8 +133,25 @@ __device__ __forceinline__ WorkStart locate_piece(int R, unsigned int index, uns
     }
   }
   __syncthreads();
-  return *shared;
 }
+
+// What a CTA leaves for the join, beside its two slots: whether its first piece ends rows that an
+// earlier CTA began, and which.  (Working this out again would cost the join what it cost here.)
+struct alignas(16) JoinRecord {
+  long long tok0;               // first token of the request
+  int rows;                     // rows to join; 0: none
+  int row0;                     // the first of them among the request's rows
+  int head;
+  int first_cta, first_slot;    // the CTA that holds the rows' first tiles, and its slot
+  int pad;
+};
+
+// Joins rows that were cut: block c those that end in CTA c.  Slot of CTA x: 2 x for the piece it
+// begins with, 2 x + 1 for the one it ends with, each holding `cap` maxima, `cap` sums and cap x D
+// unnormalised outputs.  blockIdx.y takes 16 rows.
+template <int D, typename QT>
+__global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnArgs a, const float* slots,
+                                                        const JoinRecord* records, int cap);
 
 // Waits for a phase of an mbarrier, at most two seconds; then (or once another warp has given up)
 // the CTA's abort flag is set, TIMEOUT is in the device status, and every later wait returns at
@@ -262,6 +288,64 @@ __device__ __forceinline__ void power_scale(float amax, float& down, float& up) 
   k = max(-120, min(k, 120));
   down = __uint_as_float((unsigned int)(127 - k) << 23);
   up = __uint_as_float((unsigned int)(127 + k) << 23);
+}
+
+}  // namespace aibx
+
+namespace aibx {
+
+template <int D, typename QT>
+__global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnArgs a, const float* slots,
+                                                        const JoinRecord* records, int cap) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const JoinRecord rec = records[blockIdx.x];
+  const int c1 = (int)blockIdx.x;
+  const size_t size = (size_t)cap * (D + 2);
+  for (int x = threadIdx.x; x < 16 * (D / 4); x += 256) {
+    const int i = blockIdx.y * 16 + x / (D / 4), d = (x % (D / 4)) * 4;
+    if (i >= rec.rows) break;
+    float top = -INFINITY, sum = 0.0f;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int c = rec.first_cta; c <= c1; ++c) {
+      const float* slot = slots + (size_t)(2 * c + (c == rec.first_cta ? rec.first_slot : 0)) * size;
+      const float mc = slot[i], lc = slot[cap + i];
+      const float4 o = *reinterpret_cast<const float4*>(slot + 2 * cap + (size_t)i * D + d);
+      const float tn = fmaxf(top, mc);
+      const float safe = tn == -INFINITY ? 0.0f : tn;
+      const float f0 = exp2_fast(top - safe), f1 = exp2_fast(mc - safe);
+      sum = sum * f0 + lc * f1;
+      v.x = v.x * f0 + o.x * f1;
+      v.y = v.y * f0 + o.y * f1;
+      v.z = v.z * f0 + o.z * f1;
+      v.w = v.w * f0 + o.w * f1;
+      top = tn;
+    }
+    const int ri = rec.row0 + i, ti = a.by_g.div(ri);
+    const long long tok = rec.tok0 + ti;
+    const int qh = rec.head * a.G + (ri - ti * a.G);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    QT* dst = reinterpret_cast<QT*>(a.out) + tok * a.o_tok + (long long)qh * a.o_head + d;
+    *reinterpret_cast<uint2*>(dst) =
+        make_uint2(Bits16<QT>::pack(v.x * inv, v.y * inv), Bits16<QT>::pack(v.z * inv, v.w * inv));
+    if (a.lse && d == 0)
+      a.lse[tok * (a.pool.H * a.G) + qh] = sum == 0.0f ? -INFINITY : 0.69314718056f * (top + log2f(sum));
+  }
+}
+
+template <int D, typename QT>
+inline int32_t launch_join(const AttnArgs& a, const float* slots, const JoinRecord* records, int cap,
+                           unsigned int grid, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid, (cap + 15) / 16);
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, attn_join_kernel<D, QT>, a, slots, records, cap) == cudaSuccess ? AIBX_OK
+                                                                                                : AIBX_ERR_CUDA;
 }
 
 }  // namespace aibx

@@ -14,6 +14,11 @@ struct AttnPlan {
   uint64_t rows_bytes = 0, workspace = 0;
 };
 
+// Two slots of `rows` rows and one record per CTA.
+inline uint64_t slot_bytes(int rows, int dim) {
+  return (uint64_t)sm_count() * (2ull * rows * (dim + 2) * sizeof(float) + sizeof(JoinRecord));
+}
+
 // The row kernel alone where no request can have more than 16 rows; the tile kernel alone for a
 // single request; both for a batch, each taking the requests of its kind.  The row kernel comes
 // for 8 rows and for 16; beside the tile kernel it is the one for 8 where that holds a request's
@@ -43,9 +48,8 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
   plan.tiles = bound * plan.G > 16;
   plan.rows = !plan.tiles || (b->R > 1 && plan.G <= 16);
   if (plan.rows) plan.row_limit = (plan.tiles ? plan.G : bound * plan.G) <= 8 ? 8 : 16;
-  plan.rows_bytes = 2ull * sm_count() * plan.row_limit * (L.head_dim + 2) * sizeof(float);
-  plan.workspace = plan.rows ? plan.rows_bytes : 0;
-  if (plan.tiles) plan.workspace += 2ull * sm_count() * 2 * kTileRows * (L.head_dim + 2) * sizeof(float);
+  plan.rows_bytes = plan.rows ? slot_bytes(plan.row_limit, L.head_dim) : 0;
+  plan.workspace = plan.rows_bytes + (plan.tiles ? slot_bytes(2 * kTileRows, L.head_dim) : 0);
   return AIBX_OK;
 }
 

@@ -95,7 +95,8 @@ __device__ __forceinline__ RowSpan row_span(const AttnArgs& a, const AttnRequest
 template <int TOK>
 struct RowCost {
   const AttnArgs& a;
-  __device__ __forceinline__ long long operator()(int r) const {
+  __device__ __forceinline__ long long operator()(int r, bool on) const {
+    if (!on) return 0;
     const AttnRequest q = attn_request(a.b, a.pool.T, r);
     if (q.n == 0 || (long long)q.n * a.G > a.row_limit) return 0;
     return (long long)row_span<TOK>(a, q).tiles * a.pool.H;
@@ -236,10 +237,26 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       if ((long long)q.n * a.G > a.row_limit) raise_status(AIBX_ERR_RANGE);
     }
   const RowCost<TOK> cost{a};
-  const WorkStart w = locate_piece<S::kThreads>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
+  locate_piece<S::kThreads>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
+  const WorkStart w = s_start;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   RowWalk<TOK> walk(a, w, blockIdx.x, gridDim.x);
   volatile int* abort_flag = &s_abort;
+
+  if (threadIdx.x == 0) {
+    RowWalk<TOK> look = walk;
+    JoinRecord rec = {};
+    if (look.next() && look.t0 > 0 && look.t1 == look.span.tiles) {
+      const long long per = (w.total + gridDim.x - 1) / gridDim.x;
+      const long long p0 = look.pos - look.t1;             // position of the rows' first tile
+      rec.tok0 = look.q.tok0;
+      rec.rows = look.q.n * a.G;
+      rec.head = look.head;
+      rec.first_cta = (int)(p0 / per);
+      rec.first_slot = p0 != rec.first_cta * per;
+    }
+    reinterpret_cast<JoinRecord*>(a.slots + 2ull * gridDim.x * S::kSlot)[blockIdx.x] = rec;
+  }
 
   if (warp == kRowWarps) {
     // ---------------------------------------------------------------- loader warp
@@ -365,7 +382,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       const int i = x * 8 + g;
-      const int ti = min(i, n_rows - 1) / a.G;
+      const int ti = a.by_g.div(min(i, n_rows - 1));
       const QT* src = reinterpret_cast<const QT*>(a.q) + (walk.q.tok0 + ti) * a.q_tok +
                       (long long)(walk.head * a.G + (i - ti * a.G)) * a.q_head;
       uint32_t raw[kPieces][kPiece / 2];
@@ -411,7 +428,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         qscale[x][h] = __shfl_sync(0xffffffffu, up, (2 * t4 + h) * 4) * a.scale_log2;
-        prow[x][h] = first + min(x * 8 + 2 * t4 + h, n_rows - 1) / a.G;
+        prow[x][h] = first + a.by_g.div(min(x * 8 + 2 * t4 + h, n_rows - 1));
       }
     }
     float m[NQ][2], l[NQ][2], o[NQ][kMT][4];
@@ -714,7 +731,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         v1 += p.y;
       }
       if (whole) {
-        const int ti = i / a.G;
+        const int ti = a.by_g.div(i);
         const long long tok = walk.q.tok0 + ti;
         const int qh = walk.head * a.G + (i - ti * a.G);
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -731,67 +748,6 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
     }
   }
-}
-
-// Joins a (request, head) that was cut: block c takes the one whose last tile lies in CTA c and
-// whose first tile lies in an earlier CTA.
-template <int D, bool F8, typename QT, int ROWS>
-__global__ void __launch_bounds__(256)
-attn_rows_join_kernel(const __grid_constant__ AttnArgs a) {
-  using S = RowShape<D, F8, ROWS>;
-  constexpr int TOK = S::kTok;
-  __shared__ long long s_scan[33];
-  __shared__ WorkStart s_start;
-  const RowCost<TOK> cost{a};
-  const WorkStart w = locate_piece<256>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  RowWalk<TOK> walk(a, w, blockIdx.x, gridDim.x);
-  if (!walk.next() || walk.t0 == 0 || walk.t1 != walk.span.tiles) return;
-  const long long per = (w.total + gridDim.x - 1) / gridDim.x;
-  const long long p0 = walk.base + (long long)walk.head * walk.span.tiles;   // its first position
-  const int c0 = (int)(p0 / per), c1 = (int)blockIdx.x;
-  const int n_rows = walk.q.n * a.G;
-  for (int x = threadIdx.x; x < n_rows * (D / 2); x += 256) {
-    const int i = x / (D / 2), d = (x - i * (D / 2)) * 2;
-    float top = -INFINITY, sum = 0.0f, v0 = 0.0f, v1 = 0.0f;
-    for (int c = c0; c <= c1; ++c) {
-      const float* slot = a.slots + ((long long)c * 2 + (c == c0 && p0 != c0 * per ? 1 : 0)) * S::kSlot;
-      const float mc = slot[i];
-      const float2 p = *reinterpret_cast<const float2*>(slot + 2 * ROWS + i * D + d);
-      const float tn = fmaxf(top, mc);
-      const float safe = tn == -INFINITY ? 0.0f : tn;
-      const float f0 = exp2_fast(top - safe), f1 = exp2_fast(mc - safe);
-      sum = sum * f0 + slot[ROWS + i] * f1;
-      v0 = v0 * f0 + p.x * f1;
-      v1 = v1 * f0 + p.y * f1;
-      top = tn;
-    }
-    const int ti = i / a.G;
-    const long long tok = walk.q.tok0 + ti;
-    const int qh = walk.head * a.G + (i - ti * a.G);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    QT* dst = reinterpret_cast<QT*>(a.out) + tok * a.o_tok + (long long)qh * a.o_head + d;
-    *reinterpret_cast<uint32_t*>(dst) = Bits16<QT>::pack(v0 * inv, v1 * inv);
-    if (a.lse && d == 0)
-      a.lse[tok * (a.pool.H * a.G) + qh] = sum == 0.0f ? -INFINITY : 0.69314718056f * (top + log2f(sum));
-  }
-}
-
-// ------------------------------------------------------------------------------------------
-
-template <typename Kernel>
-inline int32_t launch_after(Kernel kernel, dim3 grid, unsigned int threads, cudaStream_t st,
-                            const AttnArgs& a) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, a) == cudaSuccess ? AIBX_OK : AIBX_ERR_CUDA;
 }
 
 template <int D, bool F8, typename QT, int ROWS>
@@ -813,7 +769,8 @@ inline int32_t launch_attn_rows(AttnArgs a, int type, cudaStream_t st) {
   attn_rows_kernel<D, F8, QT, ROWS><<<grid, S::kThreads, S::kSmem, st>>>(map_k, map_v, a);
   const int32_t rc2 = launch_status();
   if (rc2 != AIBX_OK) return rc2;
-  return launch_after(attn_rows_join_kernel<D, F8, QT, ROWS>, dim3(grid), 256, st, a);
+  return launch_join<D, QT>(a, a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot), ROWS,
+                            grid, st);
 }
 
 }  // namespace aibx

@@ -47,16 +47,19 @@ struct TileShape {
   static constexpr int kSmem = 2 * kQ + kBufs * kBuf + kRaws * kRawBuf +
                                (F8 ? kFactorRing * 2 * kTileKeys * 2 + 2 * kTileRows * 4 : 0) + 1024;
   static constexpr int kSlot = 2 * kTileRows * (D + 2);    // floats per workspace slot
-  static constexpr int kRegsSoftmax = F8 ? 208 : 224;      // launch: 128 (512 threads), 168 (384)
-  static constexpr int kRegsOther = F8 ? 48 : 56;          // 2 * 208 + 2 * 48 = 4 * 128; 2 * 224 + 56 = 3 * 168
+  static constexpr int kRegsSoftmax = F8 ? 200 : 208;      // launch: 128 (512 threads), 168 (384)
+  static constexpr int kRegsOther = F8 ? 56 : 88;          // 2 * 200 + 2 * 56 = 4 * 128; 2 * 208 + 88 = 3 * 168
 };
 
 // ------------------------------------------------------------------------------------------
 // tensor-core wrappers
 
-__device__ __forceinline__ uint64_t operand_desc(unsigned int addr, unsigned int lbo, unsigned int sbo) {
-  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) |
-         (1ull << 46) | (2ull << 61);                      // version 1, 128-byte swizzle
+// Shared-memory operand: 128-byte swizzle, groups of 8 rows 1024 bytes apart; `lbo` bytes between
+// 64-element columns (N-major operands).
+__device__ __forceinline__ uint64_t operand_desc(unsigned int addr, unsigned int lbo) {
+  const unsigned int lo = (addr >> 4) | ((lbo >> 4) << 16);
+  constexpr unsigned int hi = (1024u >> 4) | (1u << 14) | (2u << 29);      // version 1 at bit 46
+  return ((uint64_t)hi << 32) | lo;
 }
 
 // fp32 accumulator, M = 128; `half` operands or bfloat16; B as it lies (K-major) or N-major
@@ -65,22 +68,31 @@ __host__ __device__ constexpr unsigned int mma_desc(bool half, int n, bool b_n_m
          ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-__device__ __forceinline__ void mma_smem(unsigned int d, uint64_t a, uint64_t b, unsigned int idesc, bool add) {
+// MMAs and commits run convergent, with a predicate for the one lane that issues: everything that
+// goes into a descriptor stays warp-uniform and needs no detour through vector registers (issued
+// inside `if (lane == 0)` an MMA took 120 cycles to issue and 64 to execute).
+__device__ __forceinline__ void mma_smem(unsigned int d, uint64_t a, uint64_t b, unsigned int idesc,
+                                         unsigned int add, unsigned int leader) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((unsigned int)add)
+      "{\n.reg .pred p, q;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(add), "r"(leader)
       : "memory");
 }
-__device__ __forceinline__ void mma_tmem(unsigned int d, unsigned int a, uint64_t b, unsigned int idesc, bool add) {
+__device__ __forceinline__ void mma_tmem(unsigned int d, unsigned int a, uint64_t b, unsigned int idesc,
+                                         unsigned int add, unsigned int leader) {
   asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((unsigned int)add)
+      "{\n.reg .pred p, q;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(add), "r"(leader)
       : "memory");
 }
-__device__ __forceinline__ void mma_commit(unsigned int bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void mma_commit(unsigned int bar, unsigned int leader) {
+  asm volatile(
+      "{\n.reg .pred q;\nsetp.ne.u32 q, %1, 0;\n"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar),
+      "r"(leader)
+      : "memory");
 }
 __device__ __forceinline__ void tmem_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -116,6 +128,31 @@ __device__ __forceinline__ void tmem_st16(unsigned int addr, const uint32_t* r) 
       : "memory");
 }
 
+// Two fp32 operations in one instruction, and the maximum of three.
+__device__ __forceinline__ uint64_t pair2(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void split2(uint64_t v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // ------------------------------------------------------------------------------------------
 // the line of work
 
@@ -129,9 +166,9 @@ __device__ __forceinline__ TileSpan tile_span(const AttnArgs& a, const AttnReque
   const int r0 = block * 2 * kTileRows, r1 = min(r0 + 2 * kTileRows, rows) - 1;
   const long long first = (long long)q.len - q.n;
   TileSpan s;
-  long long hi = a.causal ? first + r1 / a.G + 1 : q.keys;
+  long long hi = a.causal ? first + a.by_g.div(r1) + 1 : q.keys;
   hi = hi < 0 ? 0 : hi > q.keys ? q.keys : hi;
-  long long lo = a.window > 0 ? first + r0 / a.G - a.window + 1 : 0;
+  long long lo = a.window > 0 ? first + a.by_g.div(r0) - a.window + 1 : 0;
   lo = lo < 0 ? 0 : lo > hi ? hi : lo;
   s.hi = (int)hi;
   s.lo = (int)lo;
@@ -140,57 +177,100 @@ __device__ __forceinline__ TileSpan tile_span(const AttnArgs& a, const AttnReque
   return s;
 }
 
+// Tiles of a request for one head.  Requests of many blocks of rows are summed by the whole warp,
+// 32 blocks at a time (one thread over 128 blocks took tens of microseconds before the first load).
 struct TileCost {
   const AttnArgs& a;
-  // tiles of request r for one head, and its blocks of rows (0: not this kernel's)
-  __device__ __forceinline__ long long head_tiles(const AttnRequest& q, int& blocks) const {
-    blocks = 0;
+  __device__ __forceinline__ int blocks(const AttnRequest& q) const {
     const long long rows = (long long)q.n * a.G;
-    if (rows <= a.row_limit) return 0;
-    blocks = (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
-    long long sum = 0;
-    for (int b = 0; b < blocks; ++b) sum += tile_span(a, q, b).tiles;
-    return sum;
+    return rows <= a.row_limit ? 0 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
   }
-  __device__ __forceinline__ long long operator()(int r) const {
-    int blocks;
-    return head_tiles(attn_request(a.b, a.pool.T, r), blocks) * a.pool.H;
+  __device__ __forceinline__ long long operator()(int r, bool on) const {
+    AttnRequest q = {};
+    if (on) q = attn_request(a.b, a.pool.T, r);
+    const int n = on ? blocks(q) : 0;
+    long long sum = 0;
+    if (n <= 4)
+      for (int b = 0; b < n; ++b) sum += tile_span(a, q, b).tiles;
+    for (unsigned int many = __ballot_sync(0xffffffffu, n > 4); many; many &= many - 1) {
+      const int src = __ffs(many) - 1, lane = threadIdx.x & 31;
+      AttnRequest w;
+      w.n = __shfl_sync(0xffffffffu, q.n, src);
+      w.len = __shfl_sync(0xffffffffu, q.len, src);
+      w.keys = __shfl_sync(0xffffffffu, q.keys, src);
+      const int wn = blocks(w);
+      long long part = 0;
+      for (int b = lane; b < wn; b += 32) part += tile_span(a, w, b).tiles;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) part += (long long)shfl_xor64(0xffffffffu, (uint64_t)part, d);
+      if (lane == src) sum = part;
+    }
+    return sum * a.pool.H;
   }
 };
 
+// By one warp: where in its request a piece begins.
+__device__ __forceinline__ void locate_block(const AttnArgs& a, unsigned int index, unsigned int pieces, WorkStart* w) {
+  if (w->r < 0) return;
+  const int lane = threadIdx.x & 31;
+  const AttnRequest q = attn_request(a.b, a.pool.T, w->r);
+  const TileCost cost{a};
+  const int n = cost.blocks(q);
+  long long per_head = 0;
+  for (int b = lane; b < n; b += 32) per_head += tile_span(a, q, b).tiles;
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) per_head += (long long)shfl_xor64(0xffffffffu, (uint64_t)per_head, d);
+  long long off = (w->total + pieces - 1) / pieces * index - w->base;
+  const int head = (int)(off / per_head);
+  off -= (long long)head * per_head;
+  for (int b0 = 0; b0 < n; b0 += 32) {
+    const int tiles = b0 + lane < n ? tile_span(a, q, b0 + lane).tiles : 0;
+    int upto = tiles;                                        // tiles of the blocks up to this one
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += up;
+    }
+    const unsigned int past = __ballot_sync(0xffffffffu, off < upto);
+    if (past) {
+      const int at = __ffs(past) - 1;
+      if (lane == at) {
+        w->head = head;
+        w->block = b0 + at;
+        w->off = (int)(off - (upto - tiles));
+      }
+      break;
+    }
+    off -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+}
+
+// Walks a CTA's piece of the line, one (request, head, block of rows) at a time.  Each warp keeps
+// its own in shared memory, moved on by its first lane: as registers of 16 warps it cost the
+// softmax warps spills.
 struct TileWalk {
-  const AttnArgs& a;
-  long long pos, end;
+  long long pos, start, end;
   int r, head, block, blocks, t0, t1;
   AttnRequest q;
   TileSpan span;
-  bool fresh;                        // block not yet entered
+  int fresh;                         // block not yet entered
 
-  __device__ __forceinline__ TileWalk(const AttnArgs& args, const WorkStart& w, unsigned int index,
-                                      unsigned int pieces)
-      : a(args) {
+  __device__ void init(const AttnArgs& a, const WorkStart& w, unsigned int index, unsigned int pieces) {
     const long long per = (w.total + pieces - 1) / pieces;
-    pos = per * index;
+    pos = start = per * index;
     end = min(pos + per, w.total);
     r = w.r;
     if (r < 0) pos = end = 0;
     if (pos >= end) return;
     q = attn_request(a.b, a.pool.T, r);
-    const TileCost cost{a};
-    const long long per_head = cost.head_tiles(q, blocks);
-    long long off = pos - w.base;
-    head = (int)(off / per_head);
-    off -= (long long)head * per_head;
-    block = 0;
-    span = tile_span(a, q, 0);
-    while (off >= span.tiles) {
-      off -= span.tiles;
-      span = tile_span(a, q, ++block);
-    }
-    t1 = (int)off;                   // where next() goes on
-    fresh = false;
+    blocks = TileCost{a}.blocks(q);
+    head = w.head;
+    block = w.block;
+    span = tile_span(a, q, block);
+    t1 = w.off;                      // where next() goes on
+    fresh = 0;
   }
-  __device__ __forceinline__ bool next() {
+  __device__ bool next(const AttnArgs& a) {
     if (pos >= end) return false;
     if (fresh) {
       if (++block == blocks) {
@@ -200,8 +280,7 @@ struct TileWalk {
           do {
             ++r;
             q = attn_request(a.b, a.pool.T, r);
-            const long long rows = (long long)q.n * a.G;
-            blocks = rows <= a.row_limit ? 0 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
+            blocks = TileCost{a}.blocks(q);
           } while (blocks == 0);
         }
       }
@@ -212,11 +291,20 @@ struct TileWalk {
     const long long left = end - pos;
     t1 = left < span.tiles - t0 ? t0 + (int)left : span.tiles;
     pos += t1 - t0;
-    fresh = true;
+    fresh = 1;
     return true;
   }
+  // by a whole warp
+  __device__ __forceinline__ bool next_warp(const AttnArgs& a) {
+    __syncwarp();
+    int more = 0;
+    if ((threadIdx.x & 31) == 0) more = next(a);
+    return __shfl_sync(0xffffffffu, more, 0) != 0;
+  }
   __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == span.tiles; }
-  __device__ __forceinline__ int rows() const { return min(q.n * a.G - block * 2 * kTileRows, 2 * kTileRows); }
+  __device__ __forceinline__ int rows(const AttnArgs& a) const {
+    return min(q.n * a.G - block * 2 * kTileRows, 2 * kTileRows);
+  }
 };
 
 template <int REGS>
@@ -237,11 +325,12 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   __shared__ __align__(8) unsigned long long s_kv_full[S::kBufs], s_kv_empty[S::kBufs];
   __shared__ __align__(8) unsigned long long s_raw_full[F8 ? S::kRaws : 1], s_raw_empty[F8 ? S::kRaws : 1];
   __shared__ __align__(8) unsigned long long s_fac_full[S::kFactorRing], s_fac_empty[S::kFactorRing];
-  __shared__ __align__(8) unsigned long long s_q_full[2], s_s_full[2], s_p_full[2], s_o_full[2];
+  __shared__ __align__(8) unsigned long long s_q_full[2], s_s_full[2], s_h_full[2], s_p_full[2], s_o_full[2];
   __shared__ unsigned int s_mask[kInfoRing];
   __shared__ float s_kscale[kInfoRing], s_vexp[kInfoRing];
   __shared__ long long s_scan[33];
   __shared__ WorkStart s_start;
+  __shared__ TileWalk s_walk[S::kThreads / 32];
   __shared__ unsigned int s_tmem;
   __shared__ int s_abort;
 
@@ -270,6 +359,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&s_q_full[t]), 128u);
       mbar_init(smem_u32(&s_s_full[t]), 1u);
+      mbar_init(smem_u32(&s_h_full[t]), 4u);
       mbar_init(smem_u32(&s_p_full[t]), 4u);
       mbar_init(smem_u32(&s_o_full[t]), 1u);
     }
@@ -283,11 +373,34 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     tmem_before();
   }
   const TileCost cost{a};
-  const WorkStart w = locate_piece<S::kThreads>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
-  tmem_after();                                            // (locate_piece synchronises the block)
+  locate_piece<S::kThreads>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
+  if (warp == 0) {
+    locate_block(a, blockIdx.x, gridDim.x, &s_start);
+    __syncwarp();
+    if (lane == 0) {
+      TileWalk look;
+      look.init(a, s_start, blockIdx.x, gridDim.x);
+      JoinRecord rec = {};
+      if (look.next(a) && look.t0 > 0 && look.t1 == look.span.tiles) {
+        const long long per = (s_start.total + gridDim.x - 1) / gridDim.x;
+        const long long p0 = look.pos - look.t1;           // position of the rows' first tile
+        rec.tok0 = look.q.tok0;
+        rec.rows = look.rows(a);
+        rec.row0 = look.block * 2 * kTileRows;
+        rec.head = look.head;
+        rec.first_cta = (int)(p0 / per);
+        rec.first_slot = p0 != rec.first_cta * per;
+      }
+      reinterpret_cast<JoinRecord*>(a.slots + 2ull * gridDim.x * S::kSlot)[blockIdx.x] = rec;
+    }
+  }
+  __syncthreads();
+  tmem_after();
   const unsigned int tmem = s_tmem;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  TileWalk walk(a, w, blockIdx.x, gridDim.x);
+  TileWalk& walk = s_walk[warp];
+  if (lane == 0) walk.init(a, s_start, blockIdx.x, gridDim.x);
+  __syncwarp();
 
   if (warp < 8) {
     // ================================================================ softmax: thread = row
@@ -298,8 +411,8 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     const unsigned int tm_s = tmem + lanes + t * 128;
     const unsigned int tm_o = tmem + lanes + 256 + t * D;
     unsigned int s_phase = 0, o_phase = 0, step = 0;
-    while (walk.next()) {
-      const int rows_here = walk.rows() - t * kTileRows;   // rows of this tile (<= 0: none)
+    while (walk.next_warp(a)) {
+      const int rows_here = walk.rows(a) - t * kTileRows;   // rows of this tile (<= 0: none)
       const int steps = walk.t1 - walk.t0;
       if (rows_here <= 0) {
         step += steps;
@@ -311,12 +424,13 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         constexpr int kChunks = D / 8;                     // 16-byte pieces of a row
         const int c = row % kChunks;
         unsigned char* dst = base + t * S::kQ + (c >> 3) * S::kColBytes;
+#pragma unroll 8
         for (int i = row / kChunks; i < kTileRows; i += 128 / kChunks) {
           uint4 v = make_uint4(0, 0, 0, 0);
           if (i < rows_here) {
-            const int ti = (row0 + i) / a.G, gi = row0 + i - ti * a.G;
-            v = *reinterpret_cast<const uint4*>(reinterpret_cast<const QT*>(a.q) + (walk.q.tok0 + ti) * a.q_tok +
-                                                (long long)(walk.head * a.G + gi) * a.q_head + c * 8);
+            const int ti = a.by_g.div(row0 + i), gi = row0 + i - ti * a.G;
+            v = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const QT*>(a.q) + (walk.q.tok0 + ti) * a.q_tok +
+                                                     (long long)(walk.head * a.G + gi) * a.q_head + c * 8));
           }
           if constexpr (F8) {
             uint32_t x[4] = {v.x, v.y, v.z, v.w};
@@ -345,18 +459,19 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         if (F8) asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
       }
       const float c0 = F8 ? a.scale_log2 * s_qup[t * kTileRows + row] : a.scale_log2;
-      const int tok = (row0 + min(row, rows_here - 1)) / a.G;
+      const int tok = a.by_g.div(row0 + min(row, rows_here - 1));
       const long long p = (long long)walk.q.len - walk.q.n + tok;      // this row's position
       // positions [vis0, vis1) this row sees (of those that are there)
       const int vis1 = (int)max(0LL, a.causal ? min(p + 1, (long long)walk.span.hi) : (long long)walk.span.hi);
       const int vis0 = a.window > 0 ? (int)max((long long)walk.span.lo, p - a.window + 1) : walk.span.lo;
+      const int key_first = (walk.span.tile0 + walk.t0) * kTileKeys;
       float m = -INFINITY, l = 0.0f;
       for (int j = 0; j < steps; ++j, ++step) {
         ring_wait(smem_u32(&s_s_full[t]), s_phase, abort_flag);
         s_phase ^= 1u;
         __syncwarp();
         tmem_after();
-        const int key0 = (walk.span.tile0 + walk.t0 + j) * kTileKeys;
+        const int key0 = key_first + j * kTileKeys;
         const unsigned int mask = s_mask[step % kInfoRing];
         float c = c0, shift = 0.0f;
         if constexpr (F8) {
@@ -382,10 +497,11 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         // ---- maximum
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int k = 0; k < 128; k += 4)
+        for (int k = 0; k < 128; k += 8)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], __uint_as_float(s[k + e]));
-        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c + shift;
+          for (int e = 0; e < 4; ++e)
+            mx[e] = max3(mx[e], __uint_as_float(s[k + 2 * e]), __uint_as_float(s[k + 2 * e + 1]));
+        const float mt = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * c + shift;
         if (__any_sync(0xffffffffu, mt > m + 8.0f)) {
           const float mn = fmaxf(m, mt);
           const float al = mn == -INFINITY ? 1.0f : exp2_fast(m - mn);
@@ -405,20 +521,31 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
         const float off = (m == -INFINITY ? 0.0f : m) - shift;
         // ---- weights
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const uint64_t c2 = pair2(c, c), off2 = pair2(-off, -off);
+        uint64_t sum2[2] = {0, 0};                         // two zeros each
 #pragma unroll
         for (int k = 0; k < 128; k += 32) {
           uint32_t pk[16];
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            const float p0 = exp2_fast(fmaf(__uint_as_float(s[k + e]), c, -off));
-            const float p1 = exp2_fast(fmaf(__uint_as_float(s[k + e + 1]), c, -off));
-            sum[(e >> 1) & 3] += p0 + p1;
+            float p0, p1;
+            split2(fma2(pair2(__uint_as_float(s[k + e]), __uint_as_float(s[k + e + 1])), c2, off2), p0, p1);
+            p0 = exp2_fast(p0);
+            p1 = exp2_fast(p1);
+            sum2[(e >> 1) & 1] = add2(sum2[(e >> 1) & 1], pair2(p0, p1));
             pk[e >> 1] = Bits16<MT>::pack(p0, p1);
           }
           tmem_st16(tm_s + (k >> 1), pk);
+          if (k == 32) {                                   // the first half may be multiplied already
+            tmem_wait_st();
+            tmem_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_h_full[t]));
+          }
         }
-        const float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        float total, other;
+        split2(add2(sum2[0], sum2[1]), total, other);
+        total += other;
         l += F8 ? total * exp2_fast(-shift) : total;
         tmem_wait_st();
         tmem_before();
@@ -431,7 +558,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       __syncwarp();
       tmem_after();
       const bool whole = walk.whole();
-      const bool at_start = walk.pos - steps == (w.total + gridDim.x - 1) / gridDim.x * blockIdx.x;
+      const bool at_start = walk.pos - steps == walk.start;
       float* slot = a.slots + ((long long)blockIdx.x * 2 + (at_start ? 0 : 1)) * S::kSlot;
       const int srow = t * kTileRows + row;
       const bool on = row < rows_here;
@@ -487,30 +614,34 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           buf_phase ^= 1u;
         }
       };
+      const unsigned int leader = lane == 0;
+      const unsigned int tmu = __shfl_sync(0xffffffffu, tmem, 0), smu = __shfl_sync(0xffffffffu, smem0, 0);
+      auto uniform = [](unsigned int x) { return __shfl_sync(0xffffffffu, x, 0); };
       auto qk = [&](int t, unsigned int kbuf) {
-        if (lane == 0) {
+        const unsigned int kaddr = uniform(kv0 + kbuf * S::kBuf);
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const unsigned int off = (k >> 2) * S::kColBytes + (k & 3) * 32;
-            mma_smem(tmem + t * 128, operand_desc(smem0 + t * S::kQ + off, 16, 1024),
-                     operand_desc(kv0 + kbuf * S::kBuf + off, 16, 1024), kQK, k > 0);
-          }
-          mma_commit(smem_u32(&s_s_full[t]));
+        for (int k = 0; k < D / 16; ++k) {
+          const unsigned int off = (k >> 2) * S::kColBytes + (k & 3) * 32;
+          mma_smem(tmu + t * 128, operand_desc(smu + t * S::kQ + off, 16), operand_desc(kaddr + off, 16), kQK, k > 0,
+                   leader);
         }
-        __syncwarp();
+        mma_commit(smem_u32(&s_s_full[t]), leader);
       };
-      while (walk.next()) {
+      while (walk.next_warp(a)) {
         const int steps = walk.t1 - walk.t0;
-        const int tiles = walk.rows() > kTileRows ? 2 : 1;
+        const int tiles = walk.rows(a) > kTileRows ? 2 : 1;
+        const int key_first = (walk.span.tile0 + walk.t0) * kTileKeys, lo = walk.span.lo, hi = walk.span.hi;
         ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
-        for (int t = 0; t < tiles; ++t) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (t >= tiles) break;
           ring_wait(smem_u32(&s_q_full[t]), q_phase[t], abort_flag);
+          __syncwarp();
           q_phase[t] ^= 1u;
           tmem_after();
           qk(t, buf);
         }
-        if (lane == 0) mma_commit(smem_u32(&s_kv_empty[buf]));
-        __syncwarp();
+        mma_commit(smem_u32(&s_kv_empty[buf]), leader);
         advance();
         for (int j = 0; j < steps; ++j) {
           const unsigned int vbuf = buf;
@@ -521,8 +652,8 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           if (!F8) {
             // V rows of positions nobody in the block sees: whatever the pool holds there
             // (0 * NaN is NaN) becomes zero
-            const int key0 = (walk.span.tile0 + walk.t0 + j) * kTileKeys;
-            const int z0 = min(max(walk.span.lo - key0, 0), kTileKeys), z1 = max(min(walk.span.hi - key0, kTileKeys), 0);
+            const int key0 = key_first + j * kTileKeys;
+            const int z0 = min(max(lo - key0, 0), kTileKeys), z1 = max(min(hi - key0, kTileKeys), 0);
             if (z0 > 0 || z1 < kTileKeys) {
               unsigned char* v = base + 2 * S::kQ + vbuf * S::kBuf;
               for (int x = lane; x < kTileKeys * 8; x += 32) {
@@ -543,25 +674,28 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
             advance();
           }
-          for (int t = 0; t < tiles; ++t) {
-            ring_wait(smem_u32(&s_p_full[t]), p_phase[t], abort_flag);
-            p_phase[t] ^= 1u;
-            tmem_after();
-            if (lane == 0) {
+          const unsigned int vaddr = uniform(kv0 + vbuf * S::kBuf), old = uniform(j > 0);
 #pragma unroll
-              for (int k = 0; k < kTileKeys / 16; ++k)
-                mma_tmem(tmem + 256 + t * D, tmem + t * 128 + k * 8,
-                         operand_desc(kv0 + vbuf * S::kBuf + k * 2048, S::kColBytes, 1024), kPV, j > 0 || k > 0);
-              if (!more) mma_commit(smem_u32(&s_o_full[t]));
+          for (int t = 0; t < 2; ++t) {
+            if (t >= tiles) break;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              ring_wait(smem_u32(half ? &s_p_full[t] : &s_h_full[t]), p_phase[t], abort_flag);
+              __syncwarp();
+              tmem_after();
+#pragma unroll
+              for (int k = half * 4; k < half * 4 + 4; ++k)
+                mma_tmem(tmu + 256 + t * D, tmu + t * 128 + k * 8, operand_desc(vaddr + k * 2048, S::kColBytes), kPV,
+                         k > 0 ? 1u : old, leader);
             }
-            __syncwarp();
-            if (more) qk(t, kbuf);
+            p_phase[t] ^= 1u;
+            if (more)
+              qk(t, kbuf);
+            else
+              mma_commit(smem_u32(&s_o_full[t]), leader);
           }
-          if (lane == 0) {
-            if (more) mma_commit(smem_u32(&s_kv_empty[kbuf]));
-            mma_commit(smem_u32(&s_kv_empty[vbuf]));
-          }
-          __syncwarp();
+          if (more) mma_commit(smem_u32(&s_kv_empty[kbuf]), leader);
+          mma_commit(smem_u32(&s_kv_empty[vbuf]), leader);
         }
       }
       // the last commit has to arrive while its barrier is still this CTA's
@@ -576,7 +710,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       unsigned long long* empty = F8 ? s_raw_empty : s_kv_empty;
       const int boxes = kTileKeys >> a.box_log;
       unsigned int buf = 0, phase = 1, issued = 0, step = 0;
-      while (walk.next()) {
+      while (walk.next_warp(a)) {
         const uint32_t* row;
         long long entries;
         table_row(a.b, walk.r, row, entries);
@@ -584,15 +718,16 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           raise_status(AIBX_ERR_RANGE);                    // tokens the table has no entry for
         BoxIds<kTileKeys> ids(a, row, walk.span.tile0 + walk.t0, walk.span.tile0 + walk.t1, walk.span.lo,
                               walk.span.hi);
-        for (int j = walk.t0; j < walk.t1; ++j, ++step) {
+        const int head = walk.head, tile0 = walk.span.tile0, lo = walk.span.lo, hi = walk.span.hi, t1 = walk.t1;
+        for (int j = walk.t0; j < t1; ++j, ++step) {
           uint32_t id;
-          const bool valid = ids.give(id, walk.head == 0);
+          const bool valid = ids.give(id, head == 0);
           const int slot = ids.slot;
           ids.step_slot();
           // a box that is not there, or that holds no visible key, comes as zeros from beyond the pool
           const int block = valid ? (int)id : (int)a.pool.num_blocks;
-          const int tok = (walk.span.tile0 + j) * kTileKeys + lane * a.box;
-          const bool missing = lane < boxes && tok < walk.span.hi && tok + a.box > walk.span.lo && !valid;
+          const int tok = (tile0 + j) * kTileKeys + lane * a.box;
+          const bool missing = lane < boxes && tok < hi && tok + a.box > lo && !valid;
           const unsigned int gone = __ballot_sync(0xffffffffu, missing);
           if (lane == 0) s_mask[step % kInfoRing] = ~gone;
           for (int kv = 0; kv < 2; ++kv) {
@@ -608,7 +743,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
                 const unsigned int dst = ring0 + buf * kBytes + lane * a.box * kRow;
 #pragma unroll
                 for (int cc = 0; cc < (F8 ? 1 : S::kCols); ++cc)
-                  tensor_load_5d(dst + cc * S::kColBytes, &map, bar, cc * 64, slot, walk.head, block, kv);
+                  tensor_load_5d(dst + cc * S::kColBytes, &map, bar, cc * 64, slot, head, block, kv);
               }
             }
             __syncwarp();
@@ -628,26 +763,27 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       // Per step: the factor 2^(e - E) of every position of the K and of the V tile, and E.  The
       // chain table -> scale byte is long: the two warps take turns and run ahead.
       unsigned int step = 0;
-      while (walk.next()) {
+      while (walk.next_warp(a)) {
         const uint32_t* row;
         long long entries;
         table_row(a.b, walk.r, row, entries);
-        for (int j = walk.t0; j < walk.t1; ++j, ++step) {
+        const int head = walk.head, tile0 = walk.span.tile0, lo = walk.span.lo, hi = walk.span.hi, t1 = walk.t1;
+        for (int j = walk.t0; j < t1; ++j, ++step) {
           if ((step & 1u) != (unsigned int)(warp - 10)) continue;
-          const int tok = (walk.span.tile0 + j) * kTileKeys + lane * 4;   // four slots of one block
+          const int tok = (tile0 + j) * kTileKeys + lane * 4;   // four slots of one block
           int byte[2][4];
           unsigned int there = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             byte[0][i] = byte[1][i] = 0;
-            if (tok + i >= walk.span.lo && tok + i < walk.span.hi) there |= 1u << i;
+            if (tok + i >= lo && tok + i < hi) there |= 1u << i;
           }
           if (there) {
             const int at = tok / a.pool.T;
             const uint32_t id = __ldg(row + at);
             if (id < a.pool.num_blocks) {
               const unsigned char* src = a.pool.scales + (long long)id * a.pool.s_block +
-                                         (long long)walk.head * a.pool.s_head +
+                                         (long long)head * a.pool.s_head +
                                          (long long)(tok - at * a.pool.T) * a.pool.s_slot;
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
@@ -693,7 +829,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     constexpr int kChunks = D / 16;                        // 16-byte pieces of a raw row
     const int c = tid % kChunks;
     unsigned int raw = 0, raw_phase = 0, buf = 0, buf_phase = 1, step = 0;
-    while (walk.next()) {
+    while (walk.next_warp(a)) {
       const int steps = walk.t1 - walk.t0;
       for (int j = 0; j < steps; ++j, ++step) {
         const unsigned int f = step % S::kFactorRing;
@@ -749,53 +885,6 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   }
 }
 
-// Joins a block of rows that was cut, as attn_rows_join_kernel does; blockIdx.y takes 32 rows.
-template <int D, bool F8, typename QT>
-__global__ void __launch_bounds__(256)
-attn_tiles_join_kernel(const __grid_constant__ AttnArgs a) {
-  using S = TileShape<D, F8>;
-  __shared__ long long s_scan[33];
-  __shared__ WorkStart s_start;
-  const TileCost cost{a};
-  const WorkStart w = locate_piece<256>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  TileWalk walk(a, w, blockIdx.x, gridDim.x);
-  if (!walk.next() || walk.t0 == 0 || walk.t1 != walk.span.tiles) return;
-  const long long per = (w.total + gridDim.x - 1) / gridDim.x;
-  const long long p0 = walk.pos - walk.t1;                 // first position of the block
-  const int c0 = (int)(p0 / per), c1 = (int)blockIdx.x;
-  const int rows = walk.rows();
-  for (int x = threadIdx.x; x < 32 * (D / 4); x += 256) {
-    const int i = blockIdx.y * 32 + x / (D / 4), d = (x % (D / 4)) * 4;
-    if (i >= rows) continue;
-    float top = -INFINITY, sum = 0.0f;
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int c = c0; c <= c1; ++c) {
-      const float* slot = a.slots + ((long long)c * 2 + (c == c0 && p0 != c0 * per ? 1 : 0)) * S::kSlot;
-      const float mc = slot[i];
-      const float4 o = *reinterpret_cast<const float4*>(slot + 4 * kTileRows + (long long)i * D + d);
-      const float tn = fmaxf(top, mc);
-      const float safe = tn == -INFINITY ? 0.0f : tn;
-      const float f0 = exp2_fast(top - safe), f1 = exp2_fast(mc - safe);
-      sum = sum * f0 + slot[2 * kTileRows + i] * f1;
-      v.x = v.x * f0 + o.x * f1;
-      v.y = v.y * f0 + o.y * f1;
-      v.z = v.z * f0 + o.z * f1;
-      v.w = v.w * f0 + o.w * f1;
-      top = tn;
-    }
-    const int ri = walk.block * 2 * kTileRows + i, ti = ri / a.G;
-    const long long tok = walk.q.tok0 + ti;
-    const int qh = walk.head * a.G + (ri - ti * a.G);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    QT* dst = reinterpret_cast<QT*>(a.out) + tok * a.o_tok + (long long)qh * a.o_head + d;
-    *reinterpret_cast<uint2*>(dst) = make_uint2(Bits16<QT>::pack(v.x * inv, v.y * inv),
-                                                Bits16<QT>::pack(v.z * inv, v.w * inv));
-    if (a.lse && d == 0)
-      a.lse[tok * (a.pool.H * a.G) + qh] = sum == 0.0f ? -INFINITY : 0.69314718056f * (top + log2f(sum));
-  }
-}
-
 template <int D, bool F8, typename QT>
 inline int32_t launch_attn_tiles(AttnArgs a, int type, cudaStream_t st) {
   using S = TileShape<D, F8>;
@@ -814,7 +903,8 @@ inline int32_t launch_attn_tiles(AttnArgs a, int type, cudaStream_t st) {
   attn_tiles_kernel<D, F8, QT><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
   const int32_t rc2 = launch_status();
   if (rc2 != AIBX_OK) return rc2;
-  return launch_after(attn_tiles_join_kernel<D, F8, QT>, dim3(grid, 2 * kTileRows / 32), 256, st, a);
+  return launch_join<D, QT>(a, a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot),
+                            2 * kTileRows, grid, st);
 }
 
 }  // namespace aibx

@@ -928,6 +928,7 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
   a.o_head = params->out_head_stride;
   a.scale_log2 = params->scale * 1.4426950408889634f;
   a.G = plan.G;
+  a.by_g = small_divisor(plan.G);
   a.causal = params->causal != 0;
   a.window = params->window;
   a.box = 0;
