@@ -47,8 +47,8 @@ struct TileShape {
   static constexpr int kSmem = 2 * kQ + kBufs * kBuf + kRaws * kRawBuf +
                                (F8 ? kFactorRing * 2 * kTileKeys * 2 + 2 * kTileRows * 4 : 0) + 1024;
   static constexpr int kSlot = 2 * kTileRows * (D + 2);    // floats per workspace slot
-  static constexpr int kRegsSoftmax = F8 ? 200 : 208;      // launch: 128 (512 threads), 168 (384)
-  static constexpr int kRegsOther = F8 ? 56 : 88;          // 2 * 200 + 2 * 56 = 4 * 128; 2 * 208 + 88 = 3 * 168
+  static constexpr int kRegsSoftmax = F8 ? 176 : 200;      // launch: 128 (512 threads), 168 (384)
+  static constexpr int kRegsOther = F8 ? 80 : 104;          // 2 * 176 + 2 * 80 = 4 * 128; 2 * 200 + 104 = 3 * 168
 };
 
 // ------------------------------------------------------------------------------------------
@@ -56,8 +56,10 @@ struct TileShape {
 
 // Shared-memory operand: 128-byte swizzle, groups of 8 rows 1024 bytes apart; `lbo` bytes between
 // 64-element columns (N-major operands).
-__device__ __forceinline__ uint64_t operand_desc(unsigned int addr, unsigned int lbo) {
-  const unsigned int lo = (addr >> 4) | ((lbo >> 4) << 16);
+__device__ __forceinline__ unsigned int operand_low(unsigned int addr, unsigned int lbo) {
+  return (addr >> 4) | ((lbo >> 4) << 16);
+}
+__device__ __forceinline__ uint64_t operand_desc(unsigned int lo) {
   constexpr unsigned int hi = (1024u >> 4) | (1u << 14) | (2u << 29);      // version 1 at bit 46
   return ((uint64_t)hi << 32) | lo;
 }
@@ -128,7 +130,7 @@ __device__ __forceinline__ void tmem_st16(unsigned int addr, const uint32_t* r) 
       : "memory");
 }
 
-// Two fp32 operations in one instruction, and the maximum of three.
+// Two fp32 operations in one instruction, and the maximum of three (NaN if one is).
 __device__ __forceinline__ uint64_t pair2(float lo, float hi) {
   uint64_t d;
   asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
@@ -149,7 +151,7 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
 
@@ -340,7 +342,9 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   __half* factors = reinterpret_cast<__half*>(raws + S::kRaws * S::kRawBuf);
   float* s_qup = reinterpret_cast<float*>(factors + S::kFactorRing * 2 * kTileKeys);
   const unsigned int kv0 = smem0 + 2 * S::kQ;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  // the same in all lanes, and known to be: role code may keep it in uniform registers
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   volatile int* abort_flag = &s_abort;
 
   if (threadIdx.x == 0) {
@@ -424,14 +428,21 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         constexpr int kChunks = D / 8;                     // 16-byte pieces of a row
         const int c = row % kChunks;
         unsigned char* dst = base + t * S::kQ + (c >> 3) * S::kColBytes;
-#pragma unroll 8
-        for (int i = row / kChunks; i < kTileRows; i += 128 / kChunks) {
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (i < rows_here) {
-            const int ti = a.by_g.div(row0 + i), gi = row0 + i - ti * a.G;
-            v = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const QT*>(a.q) + (walk.q.tok0 + ti) * a.q_tok +
-                                                     (long long)(walk.head * a.G + gi) * a.q_head + c * 8));
+        constexpr int kBatch = 8;                          // rows on their way at once
+        for (int i0 = row / kChunks; i0 < kTileRows; i0 += kBatch * (128 / kChunks)) {
+          uint4 batch[kBatch];
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            const int ri = row0 + min(i0 + u * (128 / kChunks), rows_here - 1);
+            const int ti = a.by_g.div(ri), gi = ri - ti * a.G;
+            batch[u] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const QT*>(a.q) +
+                                                            (walk.q.tok0 + ti) * a.q_tok +
+                                                            (long long)(walk.head * a.G + gi) * a.q_head + c * 8));
           }
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+          const int i = i0 + u * (128 / kChunks);
+          uint4 v = i < rows_here ? batch[u] : make_uint4(0, 0, 0, 0);
           if constexpr (F8) {
             uint32_t x[4] = {v.x, v.y, v.z, v.w};
             float amax = 0.0f;
@@ -453,6 +464,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             if (c == 0) s_qup[t * kTileRows + i] = up;
           }
           *reinterpret_cast<uint4*>(dst + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = v;
+          }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         mbar_arrive(smem_u32(&s_q_full[t]));
@@ -478,30 +490,54 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           c *= s_kscale[step % kInfoRing];
           shift = s_vexp[step % kInfoRing];
         }
-        uint32_t s[128];
+        const int b0 = vis0 - key0, b1 = vis1 - key0;
+        const bool hide = mask != 0xffffffffu || b1 < kTileKeys || b0 > 0;
+        auto hide_keys = [&](uint32_t* x, int k0) {         // what this row does not see
 #pragma unroll
-        for (int k = 0; k < 4; ++k) tmem_ld32(tm_s + k * 32, s + k * 32);
-        tmem_wait_ld();
-        // ---- hide what this row does not see
-        if (mask != 0xffffffffu) {                         // blocks that are not there: rare
-#pragma unroll
-          for (int k = 0; k < 128; ++k)
-            if (!((mask >> (k >> a.box_log)) & 1u)) s[k] = 0xff800000u;
-        }
-        if (key0 + kTileKeys > vis1 || key0 < vis0) {
-          const int b0 = vis0 - key0, b1 = vis1 - key0;
-#pragma unroll
-          for (int k = 0; k < 128; ++k)
-            if (k < b0 || k >= b1) s[k] = 0xff800000u;
-        }
-        // ---- maximum
+          for (int k = 0; k < 64; ++k)
+            if (k0 + k < b0 || k0 + k >= b1 || !((mask >> ((k0 + k) >> a.box_log)) & 1u)) x[k] = 0xff800000u;
+        };
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto raise_max = [&](const uint32_t* x) {
 #pragma unroll
-        for (int k = 0; k < 128; k += 8)
+          for (int e = 0; e < 64; e += 8)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            mx[e] = max3(mx[e], __uint_as_float(s[k + 2 * e]), __uint_as_float(s[k + 2 * e + 1]));
-        const float mt = max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]) * c + shift;
+            for (int y = 0; y < 4; ++y)
+              mx[y] = max3(mx[y], __uint_as_float(x[e + 2 * y]), __uint_as_float(x[e + 2 * y + 1]));
+        };
+        const uint64_t c2 = pair2(c, c);
+        uint64_t off2, sum2;
+        auto weights = [&](const uint32_t* x, uint32_t* pk) {   // of 64 scores, packed
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) {
+            float p0, p1;
+            const uint64_t z = fma2(pair2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, off2);
+            split2(z, p0, p1);
+            p0 = exp2_fast(p0);
+            p1 = exp2_fast(p1);
+            sum2 = add2(sum2, pair2(p0, p1));
+            pk[e >> 1] = Bits16<MT>::pack(p0, p1);
+          }
+        };
+        uint32_t s[128], pk[32];
+        tmem_ld32(tm_s, s);
+        tmem_ld32(tm_s + 32, s + 32);
+        tmem_wait_ld();
+        tmem_ld32(tm_s + 64, s + 64);
+        tmem_ld32(tm_s + 96, s + 96);
+        // The first half's weights are taken with the maximum so far while the second half arrives
+        // and the new maximum forms; it hardly ever moves, and then they are taken again.
+        if (hide) hide_keys(s, 0);
+        float off = (m == -INFINITY ? 0.0f : m) - shift;
+        off2 = pair2(-off, -off);
+        sum2 = 0;                                          // two zeros
+        weights(s, pk);
+        raise_max(s);
+        tmem_wait_ld();
+        if (hide) hide_keys(s + 64, 64);
+        raise_max(s + 64);
+        const float mt = max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[3]) * c + shift;
+        if (!(mt < INFINITY)) l = NAN;                     // a NaN or infinite score: so is the row's result
         if (__any_sync(0xffffffffu, mt > m + 8.0f)) {
           const float mn = fmaxf(m, mt);
           const float al = mn == -INFINITY ? 1.0f : exp2_fast(m - mn);
@@ -518,33 +554,24 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
               tmem_st32(tm_o + k, o);
             }
           }
+          tmem_ld32(tm_s, s);
+          tmem_ld32(tm_s + 32, s + 32);
+          tmem_wait_ld();
+          if (hide) hide_keys(s, 0);
+          off = (m == -INFINITY ? 0.0f : m) - shift;
+          off2 = pair2(-off, -off);
+          sum2 = 0;
+          weights(s, pk);
         }
-        const float off = (m == -INFINITY ? 0.0f : m) - shift;
-        // ---- weights
-        const uint64_t c2 = pair2(c, c), off2 = pair2(-off, -off);
-        uint64_t sum2[2] = {0, 0};                         // two zeros each
-#pragma unroll
-        for (int k = 0; k < 128; k += 32) {
-          uint32_t pk[16];
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            float p0, p1;
-            split2(fma2(pair2(__uint_as_float(s[k + e]), __uint_as_float(s[k + e + 1])), c2, off2), p0, p1);
-            p0 = exp2_fast(p0);
-            p1 = exp2_fast(p1);
-            sum2[(e >> 1) & 1] = add2(sum2[(e >> 1) & 1], pair2(p0, p1));
-            pk[e >> 1] = Bits16<MT>::pack(p0, p1);
-          }
-          tmem_st16(tm_s + (k >> 1), pk);
-          if (k == 32) {                                   // the first half may be multiplied already
-            tmem_wait_st();
-            tmem_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_h_full[t]));
-          }
-        }
+        tmem_st32(tm_s, pk);
+        tmem_wait_st();
+        tmem_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_h_full[t]));   // the first half may be multiplied already
+        weights(s + 64, pk);
+        tmem_st32(tm_s + 32, pk);
         float total, other;
-        split2(add2(sum2[0], sum2[1]), total, other);
+        split2(sum2, total, other);
         total += other;
         l += F8 ? total * exp2_fast(-shift) : total;
         tmem_wait_st();
@@ -564,6 +591,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       const bool on = row < rows_here;
       const long long otok = walk.q.tok0 + tok;
       const int qh = walk.head * a.G + (row0 + row - tok * a.G);
+      if (m == -INFINITY) l = l == l ? 0.0f : l;           // a row that has seen no key
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       QT* dst = reinterpret_cast<QT*>(a.out) + otok * a.o_tok + (long long)qh * a.o_head;
 #pragma unroll
@@ -615,22 +643,26 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
       };
       const unsigned int leader = lane == 0;
-      const unsigned int tmu = __shfl_sync(0xffffffffu, tmem, 0), smu = __shfl_sync(0xffffffffu, smem0, 0);
       auto uniform = [](unsigned int x) { return __shfl_sync(0xffffffffu, x, 0); };
+      const unsigned int tmu = uniform(tmem);
+      // low words of the operands' descriptors; the rest of them is constant
+      const unsigned int q_low = uniform(operand_low(smem0, 16)), k_low = uniform(operand_low(kv0, 16));
+      const unsigned int v_low = uniform(operand_low(kv0, S::kColBytes));
       auto qk = [&](int t, unsigned int kbuf) {
-        const unsigned int kaddr = uniform(kv0 + kbuf * S::kBuf);
+        const unsigned int low = k_low + kbuf * (S::kBuf >> 4);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const unsigned int off = (k >> 2) * S::kColBytes + (k & 3) * 32;
-          mma_smem(tmu + t * 128, operand_desc(smu + t * S::kQ + off, 16), operand_desc(kaddr + off, 16), kQK, k > 0,
+          const unsigned int off = ((k >> 2) * S::kColBytes + (k & 3) * 32) >> 4;
+          mma_smem(tmu + t * 128, operand_desc(q_low + t * (S::kQ >> 4) + off), operand_desc(low + off), kQK, k > 0,
                    leader);
         }
         mma_commit(smem_u32(&s_s_full[t]), leader);
       };
       while (walk.next_warp(a)) {
-        const int steps = walk.t1 - walk.t0;
-        const int tiles = walk.rows(a) > kTileRows ? 2 : 1;
-        const int key_first = (walk.span.tile0 + walk.t0) * kTileKeys, lo = walk.span.lo, hi = walk.span.hi;
+        const int steps = (int)uniform(walk.t1 - walk.t0);
+        const int tiles = uniform(walk.rows(a) > kTileRows) ? 2 : 1;
+        const int key_first = (int)uniform((walk.span.tile0 + walk.t0) * kTileKeys);
+        const int lo = (int)uniform(walk.span.lo), hi = (int)uniform(walk.span.hi);
         ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -674,7 +706,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
             advance();
           }
-          const unsigned int vaddr = uniform(kv0 + vbuf * S::kBuf), old = uniform(j > 0);
+          const unsigned int low = v_low + vbuf * (S::kBuf >> 4), old = j > 0;
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             if (t >= tiles) break;
@@ -685,7 +717,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
               tmem_after();
 #pragma unroll
               for (int k = half * 4; k < half * 4 + 4; ++k)
-                mma_tmem(tmu + 256 + t * D, tmu + t * 128 + k * 8, operand_desc(vaddr + k * 2048, S::kColBytes), kPV,
+                mma_tmem(tmu + 256 + t * D, tmu + t * 128 + k * 8, operand_desc(low + k * (2048 >> 4)), kPV,
                          k > 0 ? 1u : old, leader);
             }
             p_phase[t] ^= 1u;
@@ -843,9 +875,9 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           const __half* fac = factors + (f * 2 + kv) * kTileKeys;
 #pragma unroll 4
           for (int i = tid / kChunks; i < kTileKeys; i += 128 / kChunks) {
-            const uint4 v = *reinterpret_cast<const uint4*>(src + i * D + ((D == 128 ? c ^ (i & 7) : c) << 4));
+            uint4 v = *reinterpret_cast<const uint4*>(src + i * D + ((D == 128 ? c ^ (i & 7) : c) << 4));
             const __half x = fac[i];
-            const bool none = __half_as_ushort(x) == 0;    // not there, or too small to show
+            if (__half_as_ushort(x) == 0) v = make_uint4(0, 0, 0, 0);   // not there, or too small to show
             const __half2 x2 = __half2half2(x);
             const uint32_t wv[4] = {v.x, v.y, v.z, v.w};
             uint32_t o[8];
@@ -853,8 +885,8 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             for (int e = 0; e < 4; ++e) {
               const __half2 lo = __hmul2(halves_of_e4m3(wv[e] & 0xffffu), x2);
               const __half2 hi = __hmul2(halves_of_e4m3(wv[e] >> 16), x2);
-              o[2 * e] = none ? 0u : *reinterpret_cast<const uint32_t*>(&lo);
-              o[2 * e + 1] = none ? 0u : *reinterpret_cast<const uint32_t*>(&hi);
+              o[2 * e] = *reinterpret_cast<const uint32_t*>(&lo);
+              o[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&hi);
             }
             const int p0 = (2 * c) & 7;
             *reinterpret_cast<uint4*>(dst + i * 128 + ((p0 ^ (i & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
