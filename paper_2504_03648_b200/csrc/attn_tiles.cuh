@@ -36,15 +36,16 @@ constexpr int kInfoRing = 16;        // per-step facts the softmax reads: far de
 template <int D, bool F8>
 struct TileShape {
   static constexpr int kThreads = F8 ? 512 : 384;
-  static constexpr int kBuf = kTileKeys * D * 2;           // one K or V tile as MMA operand
-  static constexpr int kBufs = D == 64 ? 8 : (F8 ? 3 : 5);
-  static constexpr int kRawBuf = kTileKeys * D;
-  static constexpr int kRaws = F8 ? 3 : 0;
+  static constexpr int kRaw = kTileKeys * D;               // a tile's e4m3 rows, as they arrive
+  // One K or V tile as MMA operand.  Raw rows arrive 16 KB into the buffer: at D = 128 that is the
+  // second column, and every 128-byte raw row lies where the second half of its own fp16 row goes.
+  static constexpr int kBuf = kTileKeys * D * 2 + (F8 && D == 64 ? kRaw : 0);
+  static constexpr int kBufs = D == 64 ? (F8 ? 6 : 8) : (F8 ? 4 : 5);
   static constexpr int kFactorRing = 4;
   static constexpr int kCols = D / 64;                     // 128-byte columns of an operand row
   static constexpr int kColBytes = 128 * 128;
   static constexpr int kQ = kTileRows * D * 2;
-  static constexpr int kSmem = 2 * kQ + kBufs * kBuf + kRaws * kRawBuf +
+  static constexpr int kSmem = 2 * kQ + kBufs * kBuf +
                                (F8 ? kFactorRing * 2 * kTileKeys * 2 + 2 * kTileRows * 4 : 0) + 1024;
   static constexpr int kSlot = 2 * kTileRows * (D + 2);    // floats per workspace slot
   static constexpr int kRegsSoftmax = F8 ? 176 : 200;      // launch: 128 (512 threads), 168 (384)
@@ -325,7 +326,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   using MT = typename std::conditional<F8, __half, QT>::type;
   extern __shared__ unsigned char s_raw[];
   __shared__ __align__(8) unsigned long long s_kv_full[S::kBufs], s_kv_empty[S::kBufs];
-  __shared__ __align__(8) unsigned long long s_raw_full[F8 ? S::kRaws : 1], s_raw_empty[F8 ? S::kRaws : 1];
+  __shared__ __align__(8) unsigned long long s_raw_full[S::kBufs];
   __shared__ __align__(8) unsigned long long s_fac_full[S::kFactorRing], s_fac_empty[S::kFactorRing];
   __shared__ __align__(8) unsigned long long s_q_full[2], s_s_full[2], s_h_full[2], s_p_full[2], s_o_full[2];
   __shared__ unsigned int s_mask[kInfoRing];
@@ -338,8 +339,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
 
   const unsigned int smem0 = (smem_u32(s_raw) + 1023u) & ~1023u;
   unsigned char* base = s_raw + (smem0 - smem_u32(s_raw));
-  unsigned char* raws = base + 2 * S::kQ + S::kBufs * S::kBuf;
-  __half* factors = reinterpret_cast<__half*>(raws + S::kRaws * S::kRawBuf);
+  __half* factors = reinterpret_cast<__half*>(base + 2 * S::kQ + S::kBufs * S::kBuf);
   float* s_qup = reinterpret_cast<float*>(factors + S::kFactorRing * 2 * kTileKeys);
   const unsigned int kv0 = smem0 + 2 * S::kQ;
   const int lane = threadIdx.x & 31;
@@ -351,10 +351,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     for (int i = 0; i < S::kBufs; ++i) {
       mbar_init(smem_u32(&s_kv_full[i]), F8 ? 128u : 1u);
       mbar_init(smem_u32(&s_kv_empty[i]), 1u);
-    }
-    for (int i = 0; i < S::kRaws; ++i) {
       mbar_init(smem_u32(&s_raw_full[i]), 1u);
-      mbar_init(smem_u32(&s_raw_empty[i]), 4u);
     }
     for (int i = 0; i < S::kFactorRing; ++i) {
       mbar_init(smem_u32(&s_fac_full[i]), 1u);
@@ -492,10 +489,24 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
         const int b0 = vis0 - key0, b1 = vis1 - key0;
         const bool hide = mask != 0xffffffffu || b1 < kTileKeys || b0 > 0;
-        auto hide_keys = [&](uint32_t* x, int k0) {         // what this row does not see
+        // what this row sees of the tile, a bit per key
+        uint32_t vis[4];
+        if (hide) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int lo = min(max(b0 - 32 * x, 0), 32), hi = min(max(b1 - 32 * x, 0), 32);
+            vis[x] = (uint32_t)((1ull << hi) - 1) & ~(uint32_t)((1ull << lo) - 1);
+          }
+          if (mask != 0xffffffffu) {                       // blocks that are not there
+            for (int k = 0; k < kTileKeys >> a.box_log; ++k)
+              if (!((mask >> k) & 1u))
+                for (int e = 0; e < a.box; e += 8) vis[((k << a.box_log) + e) >> 5] &= ~(0xffu << (((k << a.box_log) + e) & 31));
+          }
+        }
+        auto hide_keys = [&](uint32_t* x, int w) {
 #pragma unroll
           for (int k = 0; k < 64; ++k)
-            if (k0 + k < b0 || k0 + k >= b1 || !((mask >> ((k0 + k) >> a.box_log)) & 1u)) x[k] = 0xff800000u;
+            if (!(vis[w + (k >> 5)] & (1u << (k & 31)))) x[k] = 0xff800000u;
         };
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
         auto raise_max = [&](const uint32_t* x) {
@@ -534,7 +545,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         weights(s, pk);
         raise_max(s);
         tmem_wait_ld();
-        if (hide) hide_keys(s + 64, 64);
+        if (hide) hide_keys(s + 64, 2);
         raise_max(s + 64);
         const float mt = max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[3]) * c + shift;
         if (!(mt < INFINITY)) l = NAN;                     // a NaN or infinite score: so is the row's result
@@ -734,12 +745,10 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       ring_wait(smem_u32(&s_kv_empty[last_buf]), last_phase, abort_flag);
     } else if (warp == 9) {
       // ============================================================== loader warp
-      constexpr int kRing = F8 ? S::kRaws : S::kBufs;
-      constexpr unsigned int kBytes = F8 ? S::kRawBuf : S::kBuf;
+      constexpr unsigned int kBytes = F8 ? S::kRaw : S::kBuf;
       constexpr int kRow = F8 ? D : 128;
-      const unsigned int ring0 = F8 ? smem_u32(raws) : kv0;
+      const unsigned int ring0 = F8 ? kv0 + S::kColBytes : kv0;
       unsigned long long* full = F8 ? s_raw_full : s_kv_full;
-      unsigned long long* empty = F8 ? s_raw_empty : s_kv_empty;
       const int boxes = kTileKeys >> a.box_log;
       unsigned int buf = 0, phase = 1, issued = 0, step = 0;
       while (walk.next_warp(a)) {
@@ -763,7 +772,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           const unsigned int gone = __ballot_sync(0xffffffffu, missing);
           if (lane == 0) s_mask[step % kInfoRing] = ~gone;
           for (int kv = 0; kv < 2; ++kv) {
-            ring_wait(smem_u32(&empty[buf]), phase, abort_flag);
+            ring_wait(smem_u32(&s_kv_empty[buf]), phase, abort_flag);
             __syncwarp();
             const unsigned int bar = smem_u32(&full[buf]);
             if (__any_sync(0xffffffffu, *abort_flag)) {
@@ -772,7 +781,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
               if (lane == 0) mbar_arrive_expect_tx(bar, kBytes);
               __syncwarp();
               if (lane < boxes) {
-                const unsigned int dst = ring0 + buf * kBytes + lane * a.box * kRow;
+                const unsigned int dst = ring0 + buf * S::kBuf + lane * a.box * kRow;
 #pragma unroll
                 for (int cc = 0; cc < (F8 ? 1 : S::kCols); ++cc)
                   tensor_load_5d(dst + cc * S::kColBytes, &map, bar, cc * 64, slot, head, block, kv);
@@ -780,7 +789,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             }
             __syncwarp();
             ++issued;
-            if (++buf == (unsigned int)kRing) {
+            if (++buf == S::kBufs) {
               buf = 0;
               phase ^= 1u;
             }
@@ -788,8 +797,8 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         }
       }
       // nothing may still be on its way into this CTA's shared memory when it ends
-      for (unsigned int i = issued > (unsigned int)kRing ? issued - kRing : 0; i < issued; ++i)
-        ring_drain(smem_u32(&full[i % kRing]), (i / kRing) & 1u);
+      for (unsigned int i = issued > S::kBufs ? issued - S::kBufs : 0; i < issued; ++i)
+        ring_drain(smem_u32(&full[i % S::kBufs]), (i / S::kBufs) & 1u);
     } else if constexpr (F8) {
       // ============================================================== scale warps (10, 11)
       // Per step: the factor 2^(e - E) of every position of the K and of the V tile, and E.  The
@@ -857,54 +866,73 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   } else if constexpr (F8) {
     // ================================================================ converter warps (12 .. 15)
     regs_down<S::kRegsOther>();
+    // A thread takes one 16-byte piece of kRows neighbouring rows, half of them at a time; a row's
+    // pieces are one warp's, which has read them all before it writes over them.
     const int tid = threadIdx.x - 384;
     constexpr int kChunks = D / 16;                        // 16-byte pieces of a raw row
-    const int c = tid % kChunks;
-    unsigned int raw = 0, raw_phase = 0, buf = 0, buf_phase = 1, step = 0;
+    constexpr int kRows = kTileKeys * kChunks / 128;
+    const int c = tid % kChunks, i0 = tid / kChunks * kRows;
+    unsigned int buf = 0, phase = 0, step = 0;
     while (walk.next_warp(a)) {
       const int steps = walk.t1 - walk.t0;
       for (int j = 0; j < steps; ++j, ++step) {
         const unsigned int f = step % S::kFactorRing;
         ring_wait(smem_u32(&s_fac_full[f]), (step / S::kFactorRing) & 1u, abort_flag);
         for (int kv = 0; kv < 2; ++kv) {
-          ring_wait(smem_u32(&s_raw_full[raw]), raw_phase, abort_flag);
-          ring_wait(smem_u32(&s_kv_empty[buf]), buf_phase, abort_flag);
-          __syncwarp();
-          const unsigned char* src = raws + raw * S::kRawBuf;
-          unsigned char* dst = base + 2 * S::kQ + buf * S::kBuf + (c >> 2) * S::kColBytes;
-          const __half* fac = factors + (f * 2 + kv) * kTileKeys;
-#pragma unroll 4
-          for (int i = tid / kChunks; i < kTileKeys; i += 128 / kChunks) {
-            uint4 v = *reinterpret_cast<const uint4*>(src + i * D + ((D == 128 ? c ^ (i & 7) : c) << 4));
-            const __half x = fac[i];
-            if (__half_as_ushort(x) == 0) v = make_uint4(0, 0, 0, 0);   // not there, or too small to show
-            const __half2 x2 = __half2half2(x);
-            const uint32_t wv[4] = {v.x, v.y, v.z, v.w};
-            uint32_t o[8];
+          __half x[kRows];
+          const __half* fac = factors + (f * 2 + kv) * kTileKeys + i0;
+          if constexpr (kRows == 8)
+            *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(fac);
+          else
+            *reinterpret_cast<uint2*>(x) = *reinterpret_cast<const uint2*>(fac);
+          bool gone = false;                               // rows that are not there, or too small to show
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const __half2 lo = __hmul2(halves_of_e4m3(wv[e] & 0xffffu), x2);
-              const __half2 hi = __hmul2(halves_of_e4m3(wv[e] >> 16), x2);
-              o[2 * e] = *reinterpret_cast<const uint32_t*>(&lo);
-              o[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&hi);
+          for (int u = 0; u < kRows; ++u) gone |= __half_as_ushort(x[u]) == 0;
+          ring_wait(smem_u32(&s_raw_full[buf]), phase, abort_flag);
+          __syncwarp();
+          unsigned char* out = base + 2 * S::kQ + buf * S::kBuf + (c >> 2) * S::kColBytes;
+          const unsigned char* src = base + 2 * S::kQ + buf * S::kBuf + S::kColBytes;
+          constexpr int kTurn = kRows / 2;
+#pragma unroll
+          for (int u0 = 0; u0 < kRows; u0 += kTurn) {
+            uint4 v[kTurn];
+#pragma unroll
+            for (int u = 0; u < kTurn; ++u) {
+              const int i = i0 + u0 + u;
+              v[u] = *reinterpret_cast<const uint4*>(src + i * D + ((D == 128 ? c ^ (i & 7) : c) << 4));
             }
-            const int p0 = (2 * c) & 7;
-            *reinterpret_cast<uint4*>(dst + i * 128 + ((p0 ^ (i & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<uint4*>(dst + i * 128 + (((p0 + 1) ^ (i & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+            if (gone) {
+#pragma unroll
+              for (int u = 0; u < kTurn; ++u)
+                if (__half_as_ushort(x[u0 + u]) == 0) v[u] = make_uint4(0, 0, 0, 0);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < kTurn; ++u) {
+              const int i = i0 + u0 + u;
+              const __half2 x2 = __half2half2(x[u0 + u]);
+              const uint32_t wv[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+              uint32_t o[8];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const __half2 lo = __hmul2(halves_of_e4m3(wv[e] & 0xffffu), x2);
+                const __half2 hi = __hmul2(halves_of_e4m3(wv[e] >> 16), x2);
+                o[2 * e] = *reinterpret_cast<const uint32_t*>(&lo);
+                o[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&hi);
+              }
+              const int p0 = (2 * c) & 7;
+              *reinterpret_cast<uint4*>(out + i * 128 + ((p0 ^ (i & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+              *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + 1) ^ (i & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+            }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           mbar_arrive(smem_u32(&s_kv_full[buf]));
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&s_raw_empty[raw]));
-          if (++raw == S::kRaws) {
-            raw = 0;
-            raw_phase ^= 1u;
-          }
           if (++buf == S::kBufs) {
             buf = 0;
-            buf_phase ^= 1u;
+            phase ^= 1u;
           }
         }
+        __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_fac_empty[f]));
       }
     }
