@@ -11,11 +11,13 @@
 //   every type it can go to.
 // read: the same places, the other way round.
 //
-// One warp takes one token (or, with few tokens, a part of its 2 * heads rows, so that a decoding
-// step's handful of tokens still spreads over the machine); `lanes per row` lanes hold a row in
-// 8-element pieces, reduce its maximum by shuffles and store it with one access per lane.  Each
-// byte crosses the memory system once in each direction: bound by HBM bandwidth for long inputs
-// and by the chain offsets -> length -> table -> pool of dependent loads for short ones.
+// A warp takes up to 32 neighbouring tokens and some of their 2 * heads planes (K or V of a head).
+// Finding a token's request, length, block and slot is a chain of dependent loads; the lanes walk
+// it once for all the warp's tokens together and hand the places on by shuffles, so that what is
+// left per row is an address and 16 pool bytes per lane.  (A warp per token, searching for itself,
+// spent 620 instructions on 1 KB: 444 us for 464,000 tokens of 4 e4m3 heads.)  With few tokens the
+// groups shrink, down to one step of rows per warp.  Every byte crosses the memory system once in
+// each direction: bound by HBM for long inputs, by the chain of loads for short ones.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -78,91 +80,76 @@ __device__ __forceinline__ int warp_find_request(const int64_t* tok_off, int R, 
 }
 
 // ------------------------------------------------------------------------------------------
-// eight elements of a row
+// elements of a row in registers
 
-template <typename T>
-struct Row8;
-
+template <typename X>
+struct Elems;
 template <>
-struct Row8<float> {
-  static constexpr int kBytes = 32;
-  static __device__ __forceinline__ void load(const float* p, bool vec, float* x) {
-    if (vec) {
-      const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-      x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = p[i];
-    }
-  }
-  static __device__ __forceinline__ void store(float* p, bool vec, const float* x) {
-    if (vec) {
-      *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-      *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = x[i];
-    }
+struct Elems<float> {
+  static __device__ __forceinline__ float get(const uint32_t* w, int e) { return __uint_as_float(w[e]); }
+  static __device__ __forceinline__ void put(uint32_t* w, int e, float a, float b) {
+    w[e] = __float_as_uint(a);
+    w[e + 1] = __float_as_uint(b);
   }
 };
-
-template <typename T2>
-struct Half8 {
-  static __device__ __forceinline__ void unpack(uint4 v, float* x) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const T2 h = *reinterpret_cast<const T2*>(&w[i]);
-      const float2 f = to_float2(h);
-      x[2 * i] = f.x;
-      x[2 * i + 1] = f.y;
-    }
+template <>
+struct Elems<__nv_bfloat16> {
+  static __device__ __forceinline__ float get(const uint32_t* w, int e) {
+    return __uint_as_float((e & 1) ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
   }
-  static __device__ __forceinline__ float2 to_float2(__nv_bfloat162 h) { return __bfloat1622float2(h); }
-  static __device__ __forceinline__ float2 to_float2(__half2 h) { return __half22float2(h); }
-  static __device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat162*) {
+  static __device__ __forceinline__ void put(uint32_t* w, int e, float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
+    w[e >> 1] = *reinterpret_cast<const uint32_t*>(&h);
   }
-  static __device__ __forceinline__ uint32_t pack2(float a, float b, __half2*) {
+};
+template <>
+struct Elems<__half> {
+  static __device__ __forceinline__ float get(const uint32_t* w, int e) {
+    const __half2 h = *reinterpret_cast<const __half2*>(w + (e >> 1));
+    return (e & 1) ? __high2float(h) : __low2float(h);
+  }
+  static __device__ __forceinline__ void put(uint32_t* w, int e, float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-  static __device__ __forceinline__ uint4 pack(const float* x) {
-    T2* tag = nullptr;
-    return make_uint4(pack2(x[0], x[1], tag), pack2(x[2], x[3], tag), pack2(x[4], x[5], tag),
-                      pack2(x[6], x[7], tag));
+    w[e >> 1] = *reinterpret_cast<const uint32_t*>(&h);
   }
 };
 
-template <typename T, typename T2>
-struct Row8Half {
-  static constexpr int kBytes = 16;
-  static __device__ __forceinline__ void load(const T* p, bool vec, float* x) {
-    if (vec) {
-      Half8<T2>::unpack(*reinterpret_cast<const uint4*>(p), x);
-    } else {
+// N words from or to memory; element by element where the caller's rows are not 16-byte aligned.
+template <typename X, int N>
+__device__ __forceinline__ void load_words(const X* p, bool vec, uint32_t* w) {
+  if (vec) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = (float)p[i];
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<uint4*>(w + i) = __ldg(reinterpret_cast<const uint4*>(p) + i / 4);
+  } else {
+    constexpr int kPer = 4 / sizeof(X);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (kPer == 1)
+        w[i] = *reinterpret_cast<const uint32_t*>(p + i);
+      else
+        w[i] = (uint32_t)*reinterpret_cast<const uint16_t*>(p + 2 * i) |
+               ((uint32_t)*reinterpret_cast<const uint16_t*>(p + 2 * i + 1) << 16);
     }
   }
-  static __device__ __forceinline__ void store(T* p, bool vec, const float* x) {
-    const uint4 v = Half8<T2>::pack(x);
-    if (vec) {
-      *reinterpret_cast<uint4*>(p) = v;
-    } else {
-      const T* h = reinterpret_cast<const T*>(&v);
+}
+template <typename X, int N>
+__device__ __forceinline__ void store_words(X* p, bool vec, const uint32_t* w) {
+  if (vec) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = h[i];
+    for (int i = 0; i < N; i += 4) *(reinterpret_cast<uint4*>(p) + i / 4) = *reinterpret_cast<const uint4*>(w + i);
+  } else {
+    constexpr int kPer = 4 / sizeof(X);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (kPer == 1) {
+        *reinterpret_cast<uint32_t*>(p + i) = w[i];
+      } else {
+        *reinterpret_cast<uint16_t*>(p + 2 * i) = (uint16_t)w[i];
+        *reinterpret_cast<uint16_t*>(p + 2 * i + 1) = (uint16_t)(w[i] >> 16);
+      }
     }
   }
-};
-
-template <>
-struct Row8<__nv_bfloat16> : Row8Half<__nv_bfloat16, __nv_bfloat162> {};
-template <>
-struct Row8<__half> : Row8Half<__half, __half2> {};
+}
 
 struct E4M3 {};   // tag of a pool of e4m3 rows with scale bytes
 
@@ -185,10 +172,33 @@ __device__ __forceinline__ float finite_abs(float x) {
   return a < INFINITY ? a : 0.0f;
 }
 
-// Two e4m3 numbers; infinities become NaN (the format has none).
-__device__ __forceinline__ uint32_t e4m3_pair(float a, float b) {
-  a = fabsf(a) < INFINITY ? a : NAN;
-  b = fabsf(b) < INFINITY ? b : NAN;
+// Bits of the largest magnitude among 2 or 1 numbers a word holds: magnitudes order as their bits
+// do, infinities and NaN above all finite ones.
+template <typename X>
+__device__ __forceinline__ uint32_t max_bits(uint32_t m, uint32_t w) {
+  if constexpr (sizeof(X) == 2) return __vmaxu2(m, w & 0x7fff7fffu);
+  return max(m, w & 0x7fffffffu);
+}
+// The magnitude itself; `finite`: whether it is one.
+template <typename X>
+__device__ __forceinline__ float magnitude(uint32_t m, bool& finite) {
+  if constexpr (sizeof(X) == 2) {
+    m = max(m >> 16, m & 0xffffu);
+    const uint32_t w[1] = {m};
+    const float a = Elems<X>::get(w, 0);
+    finite = a < INFINITY;
+    return a;
+  }
+  finite = m < 0x7f800000u;
+  return __uint_as_float(m);
+}
+
+// Two e4m3 numbers; where not all are finite (`odd`) infinities become NaN: the format has none.
+__device__ __forceinline__ uint32_t e4m3_pair(float a, float b, bool odd) {
+  if (odd) {
+    a = fabsf(a) < INFINITY ? a : NAN;
+    b = fabsf(b) < INFINITY ? b : NAN;
+  }
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
 
@@ -201,135 +211,170 @@ struct PagedIO {
   char* k;
   char* v;
   long long k_tok, k_head, v_tok, v_head;   // strides in elements
-  int lanes;                                // lanes per row, a power of two
-  int parts;                                // warps per token
+  int lane_log;                             // log2 of the lanes that hold a row
+  int tokens;                               // per warp: a power of two up to 32, at least 32 >> lane_log
+  int parts;                                // warps that share a group's planes
   int vec;                                  // every row 16-byte aligned
 };
 
-// Where row `row` (K rows of all heads, then V rows) of a token lies.
-template <typename X>
-__device__ __forceinline__ X* io_row(const PagedIO& io, long long i, int row, int H) {
-  const bool is_v = row >= H;
-  const int h = is_v ? row - H : row;
-  X* b = reinterpret_cast<X*>(is_v ? io.v : io.k);
-  return b + i * (is_v ? io.v_tok : io.k_tok) + h * (is_v ? io.v_head : io.k_head);
-}
-
 constexpr int kPagedThreads = 256;
-constexpr int kPagedUnroll = 4;      // rows in flight per lane
 
 // TO_POOL: append; else read.  P: pool element (E4M3 tag, __half, __nv_bfloat16), X: the caller's.
-// PIECES: 8-element pieces of a row per lane (1 up to D = 256, 4 up to 1024).
+// PIECES: 16-byte pool pieces of a row per lane (with 8 bytes of an e4m3 row a lane stores 16-bit rows
+// in whole sectors, but does everything else twice: 286 instead of 264 us).
 template <bool TO_POOL, typename P, typename X, int PIECES>
-__global__ void __launch_bounds__(kPagedThreads)
+__global__ void __launch_bounds__(kPagedThreads, TO_POOL ? 4 : 6)
 kv_token_kernel(PagedPool pool, PagedBatch b, PagedIO io) {
   constexpr bool kQuant = std::is_same<P, E4M3>::value;
-  constexpr int kUnroll = PIECES == 1 ? kPagedUnroll : 1;
+  constexpr bool kCopy = std::is_same<P, X>::value;       // nothing to convert
+  constexpr int kN = kQuant ? 16 : 8;                     // elements of a piece
+  constexpr int kWords = kN * (int)sizeof(X) / 4;         // of the caller's side
+  constexpr int kUnroll = PIECES > 1 ? 1 : 2;   // rows in flight per lane
   const long long unit = ((long long)blockIdx.x * kPagedThreads + threadIdx.x) >> 5;
-  const long long i = unit / io.parts;
-  const int part = (int)(unit - i * io.parts);
-  if (i >= b.n_tokens) return;
+  const long long group = unit / io.parts;
+  const int part = (int)(unit - group * io.parts);
+  const long long i0 = group * io.tokens;
+  if (i0 >= b.n_tokens) return;
   const int lane = threadIdx.x & 31;
-  const int r = warp_find_request(b.tok_off, b.R, i);
-  if (r < 0) return;                                     // padding behind the last request
-  const long long pos = (long long)__ldg(b.kv_len + r) - (__ldg(b.tok_off + r + 1) - i);
-  if (pos < 0) return;
-  const uint32_t* row;
-  long long entries;
-  table_row(b, r, row, entries);
-  const long long at = pos / pool.T;
-  const int slot = (int)(pos - at * pool.T);
-  const uint32_t id = at < entries ? __ldg(row + at) : pool.num_blocks;
-  if (id >= pool.num_blocks) {
-    if (id != AIBX_NO_BLOCK && part == 0 && lane == 0) raise_status(AIBX_ERR_RANGE);
-    return;
-  }
-  char* base = pool.base + (long long)id * pool.block + (long long)slot * pool.slot;
-  unsigned char* sbase =
-      kQuant ? pool.scales + (long long)id * pool.s_block + (long long)slot * pool.s_slot : nullptr;
 
-  const int rows = 2 * pool.H;
-  const int per_step = 32 / io.lanes;                     // rows a warp holds at once
-  const int sub = lane / io.lanes, col = (lane - sub * io.lanes) * 8;
-  const int per_part = (rows + io.parts - 1) / io.parts;
-  const int row0 = part * per_part, row1 = min(row0 + per_part, rows);
-  for (int r0 = row0; r0 < row1; r0 += per_step * kUnroll) {
-    float x[kUnroll][PIECES][8];
-    int byte[kUnroll];
+  // ---- lane t: where token i0 + t lives
+  const int r0 = warp_find_request(b.tok_off, b.R, i0);
+  if (r0 < 0) return;                                     // padding behind the last request
+  const int t = lane & (io.tokens - 1);
+  const long long i = i0 + t;
+  const int behind = (int)min(__ldg(b.tok_off + min(r0 + 1 + lane, b.R)) - i0, (long long)(1 << 20));
+  int r = 0;                                              // requests that end at or before i
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int rr = r0 + u * per_step + sub;
-      byte[u] = 127;
-#pragma unroll
-      for (int p = 0; p < PIECES; ++p) {
-        const int d = col + p * io.lanes * 8;
-        const bool on = rr < row1 && d < pool.D;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[u][p][e] = 0.0f;
-        if (!on) continue;
-        if (TO_POOL) {
-          Row8<X>::load(io_row<const X>(io, i, rr, pool.H) + d, io.vec, x[u][p]);
-        } else {
-          const int kv = rr >= pool.H, h = rr - kv * pool.H;
-          const char* src = base + kv * pool.kv + h * pool.head;
-          if constexpr (kQuant) {
-            const uint2 w = *reinterpret_cast<const uint2*>(src + d);
-            byte[u] = sbase[kv * pool.s_kv + h * pool.s_head];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t pair = ((e < 2 ? w.x : w.y) >> (16 * (e & 1))) & 0xffffu;
-              const float2 f = __half22float2(halves_of_e4m3(pair));
-              x[u][p][2 * e] = f.x;
-              x[u][p][2 * e + 1] = f.y;
-            }
-          } else {
-            Row8<P>::load(reinterpret_cast<const P*>(src) + d, true, x[u][p]);
-          }
-        }
+  for (int d = 16; d > 0; d >>= 1)
+    if (__shfl_sync(0xffffffffu, behind, r + d - 1) <= t) r += d;
+  const int last = __shfl_sync(0xffffffffu, behind, 31);
+  if (r == 31 && last <= t) r = 32;
+  r += r0;
+  while (r < b.R && __ldg(b.tok_off + r + 1) <= i) ++r;   // only past 32 requests without tokens
+  long long place = -1, splace = 0;
+  if (r < b.R && i < b.n_tokens) {
+    const long long pos = (long long)__ldg(b.kv_len + r) - (__ldg(b.tok_off + r + 1) - i);
+    if (pos >= 0) {
+      const uint32_t* row;
+      long long entries;
+      table_row(b, r, row, entries);
+      const int at = (int)pos / pool.T, slot = (int)pos - at * pool.T;
+      const uint32_t id = at < entries ? __ldg(row + at) : pool.num_blocks;
+      if (id < pool.num_blocks) {
+        place = (long long)id * pool.block + (long long)slot * pool.slot;
+        if (kQuant) splace = (long long)id * pool.s_block + (long long)slot * pool.s_slot;
+      } else if (id != AIBX_NO_BLOCK && part == 0 && lane < io.tokens) {
+        raise_status(AIBX_ERR_RANGE);
       }
     }
+  }
+
+  // ---- rows: `step` tokens at a time, a plane after the other
+  const int lanes = 1 << io.lane_log, step = 32 >> io.lane_log;
+  const int sub = lane >> io.lane_log, col = (lane & (lanes - 1)) * kN;
+  const int planes = 2 * pool.H, per_part = (planes + io.parts - 1) / io.parts;
+  const int y1 = min(part * per_part + per_part, planes);
+  for (int y = part * per_part; y < y1; ++y) {
+    const bool is_v = y >= pool.H;
+    const int h = is_v ? y - pool.H : y;
+    char* base = pool.base + (is_v ? pool.kv : 0) + h * pool.head;
+    unsigned char* sbase = kQuant ? pool.scales + (is_v ? pool.s_kv : 0) + h * pool.s_head : nullptr;
+    const long long x_tok = is_v ? io.v_tok : io.k_tok;
+    X* x0 = reinterpret_cast<X*>(is_v ? io.v : io.k) + (long long)h * (is_v ? io.v_head : io.k_head) + i0 * x_tok;
+    for (int t0 = 0; t0 < io.tokens; t0 += step * kUnroll) {
+      uint32_t w[kUnroll][PIECES][kWords];
+      uint4 q[kUnroll][PIECES];                           // the pool's side
+      long long at[kUnroll], sat[kUnroll];
+      int byte[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int rr = r0 + u * per_step + sub;
-      float f = 1.0f;
-      if constexpr (kQuant) {
-        if (TO_POOL) {
-          float a = 0.0f;
+      for (int u = 0; u < kUnroll; ++u) {
+        const int tt = t0 + u * step + sub;
+        at[u] = (long long)shfl64(0xffffffffu, (uint64_t)place, tt & 31);
+        if (kQuant) sat[u] = (long long)shfl64(0xffffffffu, (uint64_t)splace, tt & 31);
+        if (tt >= io.tokens) at[u] = -1;
+        byte[u] = 127;
 #pragma unroll
-          for (int p = 0; p < PIECES; ++p)
+        for (int p = 0; p < PIECES; ++p) {
+          const int d = col + p * lanes * kN;
+          const bool on = at[u] >= 0 && d < pool.D;
+          if (TO_POOL) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a = fmaxf(a, finite_abs(x[u][p][e]));
-          for (int m = io.lanes >> 1; m > 0; m >>= 1)
-            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, m));
-          byte[u] = scale_byte(a);
-          f = power_of_byte(254 - byte[u]);
-        } else {
-          f = byte[u] == 255 ? NAN : power_of_byte(byte[u]);
+            for (int e = 0; e < kWords; ++e) w[u][p][e] = 0;
+            if (on) load_words<X, kWords>(x0 + tt * x_tok + d, io.vec, w[u][p]);
+          } else if (on) {
+            q[u][p] = __ldg(reinterpret_cast<const uint4*>(base + at[u] + d * (kQuant ? 1 : 2)));
+            if (kQuant) byte[u] = __ldg(sbase + sat[u]);
+          }
         }
       }
-      if (rr >= row1) continue;
-      const int kv = rr >= pool.H, h = rr - kv * pool.H;
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) {
-        const int d = col + p * io.lanes * 8;
-        if (d >= pool.D) continue;
+      for (int u = 0; u < kUnroll; ++u) {
+        const int tt = t0 + u * step + sub;
+        float f = 1.0f;
+        bool odd = false;                                  // somewhere in the warp's rows: not a finite number
         if constexpr (kQuant) {
+          if (TO_POOL) {
+            uint32_t top = 0;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[u][p][e] *= f;
-        }
-        if (TO_POOL) {
-          char* dst = base + kv * pool.kv + h * pool.head;
-          if constexpr (kQuant) {
-            uint2 w;
-            w.x = e4m3_pair(x[u][p][0], x[u][p][1]) | (e4m3_pair(x[u][p][2], x[u][p][3]) << 16);
-            w.y = e4m3_pair(x[u][p][4], x[u][p][5]) | (e4m3_pair(x[u][p][6], x[u][p][7]) << 16);
-            *reinterpret_cast<uint2*>(dst + d) = w;
-            if (p == 0 && col == 0) sbase[kv * pool.s_kv + h * pool.s_head] = (unsigned char)byte[u];
+            for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+              for (int e = 0; e < kWords; ++e) top = max_bits<X>(top, w[u][p][e]);
+            bool finite;
+            float a = magnitude<X>(top, finite);
+            odd = __any_sync(0xffffffffu, !finite);
+            if (odd) {
+              a = 0.0f;
+#pragma unroll
+              for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+                for (int e = 0; e < kN; ++e) a = fmaxf(a, finite_abs(Elems<X>::get(w[u][p], e)));
+            }
+            for (int m = lanes >> 1; m > 0; m >>= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, m));
+            byte[u] = scale_byte(a);
+            f = power_of_byte(254 - byte[u]);
           } else {
-            Row8<P>::store(reinterpret_cast<P*>(dst) + d, true, x[u][p]);
+            f = byte[u] == 255 ? NAN : power_of_byte(byte[u]);
           }
-        } else {
-          Row8<X>::store(io_row<X>(io, i, rr, pool.H) + d, io.vec, x[u][p]);
+        }
+        if (at[u] < 0) continue;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+          const int d = col + p * lanes * kN;
+          if (d >= pool.D) continue;
+          if (TO_POOL) {
+            uint32_t* out = reinterpret_cast<uint32_t*>(&q[u][p]);
+            if constexpr (kQuant) {
+#pragma unroll
+              for (int e = 0; e < kN; e += 4)
+                out[e / 4] = e4m3_pair(Elems<X>::get(w[u][p], e) * f, Elems<X>::get(w[u][p], e + 1) * f, odd) |
+                             (e4m3_pair(Elems<X>::get(w[u][p], e + 2) * f, Elems<X>::get(w[u][p], e + 3) * f, odd) << 16);
+              if (p == 0 && col == 0) sbase[sat[u]] = (unsigned char)byte[u];
+            } else if constexpr (kCopy) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) out[e] = w[u][p][e];
+            } else {
+#pragma unroll
+              for (int e = 0; e < kN; e += 2)
+                Elems<P>::put(out, e, Elems<X>::get(w[u][p], e), Elems<X>::get(w[u][p], e + 1));
+            }
+            *reinterpret_cast<uint4*>(base + at[u] + d * (kQuant ? 1 : 2)) = q[u][p];
+          } else {
+            const uint32_t* in = reinterpret_cast<const uint32_t*>(&q[u][p]);
+            if constexpr (kQuant) {
+#pragma unroll
+              for (int e = 0; e < kN; e += 2) {
+                const float2 y2 = __half22float2(halves_of_e4m3((in[e / 4] >> (16 * ((e >> 1) & 1))) & 0xffffu));
+                Elems<X>::put(w[u][p], e, y2.x * f, y2.y * f);
+              }
+            } else if constexpr (kCopy) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) w[u][p][e] = in[e];
+            } else {
+#pragma unroll
+              for (int e = 0; e < kN; e += 2) Elems<X>::put(w[u][p], e, Elems<P>::get(in, e), Elems<P>::get(in, e + 1));
+            }
+            store_words<X, kWords>(x0 + tt * x_tok + d, io.vec, w[u][p]);
+          }
         }
       }
     }
@@ -405,22 +450,26 @@ inline int32_t paged_views(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b, P
 template <bool TO_POOL, typename P, typename X>
 inline int32_t launch_kv_token(const PagedPool& pool, const PagedBatch& b, PagedIO io,
                                cudaStream_t st) {
-  const int pieces = pool.D / 8;
-  int lanes = 1;
-  while (lanes < pieces && lanes < 32) lanes *= 2;
-  io.lanes = lanes;
-  // One warp per token once there are tokens for four warps on every scheduler; with fewer, a
-  // token's rows are shared out down to one step of the warp's rows.
-  const int steps = (2 * pool.H + 32 / lanes - 1) / (32 / lanes);
-  long long parts = (long long)sm_count() * 16 / b.n_tokens;
-  io.parts = (int)(parts < 1 ? 1 : parts > steps ? steps : parts);
-  const long long warps = b.n_tokens * io.parts;
+  constexpr int kN = std::is_same<P, E4M3>::value ? 16 : 8;
+  const int pieces = pool.D / kN;
+  io.lane_log = 0;
+  while ((1 << io.lane_log) < pieces && io.lane_log < 5) ++io.lane_log;
+  // Groups of 32 tokens, one warp per plane, once that gives every scheduler eight warps to switch
+  // between; with fewer tokens smaller groups, down to one step of rows.
+  const long long enough = (long long)sm_count() * 32;
+  io.tokens = 32;
+  while (io.tokens > (32 >> io.lane_log) && (b.n_tokens + io.tokens - 1) / io.tokens * 2 * pool.H < enough)
+    io.tokens /= 2;
+  const long long groups = (b.n_tokens + io.tokens - 1) / io.tokens;
+  io.parts = 2 * pool.H;
+  while (io.parts > 1 && groups * io.parts >= 64 * enough) io.parts = (io.parts + 1) / 2;
+  const long long warps = groups * io.parts;
   const long long blocks = (warps + kPagedThreads / 32 - 1) / (kPagedThreads / 32);
   if (blocks >= (1LL << 31)) return AIBX_ERR_UNSUPPORTED;
   if (pieces <= 32)
     kv_token_kernel<TO_POOL, P, X, 1><<<(unsigned int)blocks, kPagedThreads, 0, st>>>(pool, b, io);
   else
-    kv_token_kernel<TO_POOL, P, X, 4><<<(unsigned int)blocks, kPagedThreads, 0, st>>>(pool, b, io);
+    kv_token_kernel<TO_POOL, P, X, 32 / kN><<<(unsigned int)blocks, kPagedThreads, 0, st>>>(pool, b, io);
   return launch_status();
 }
 
