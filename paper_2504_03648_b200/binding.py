@@ -135,12 +135,9 @@ def lib():
             "aibx_kv_scatter_counted": [vp, C.POINTER(KVLayout), vp, i64, vp, vp, vp],
             "aibx_kv_gather_inner": [vp, C.POINTER(KVLayout), i32, i32, vp, i64, vp, vp],
             "aibx_kv_scatter_inner": [vp, C.POINTER(KVLayout), i32, i32, vp, i64, vp, vp],
-            "aibx_kv_append": [C.POINTER(_CacheC), C.POINTER(_BatchC), vp, i64, i64, vp, i64, i64,
-                               i32, vp],
-            "aibx_kv_read": [C.POINTER(_CacheC), C.POINTER(_BatchC), vp, i64, i64, vp, i64, i64,
-                             i32, vp],
-            "aibx_attn_paged": [C.POINTER(_CacheC), C.POINTER(_BatchC), C.POINTER(_AttnC), vp, vp,
-                                vp, vp, u64, vp],
+            "aibx_kv_append": [vp, vp, vp, i64, i64, vp, i64, i64, i32, vp],
+            "aibx_kv_read": [vp, vp, vp, i64, i64, vp, i64, i64, i32, vp],
+            "aibx_attn_paged": [vp, vp, vp, vp, vp, vp, vp, u64, vp],
             "aibx_kv_set_tuning": [i32, i32, i32, i32],
             "aibx_kv_set_store_lag": [i32],
             "aibx_kv_get_tuning": [vp, vp, vp, vp, vp],
@@ -152,8 +149,7 @@ def lib():
             fn = getattr(L, name)
             fn.argtypes = args
             fn.restype = i32
-        L.aibx_attn_workspace_bytes.argtypes = [C.POINTER(_CacheC), C.POINTER(_BatchC),
-                                                C.POINTER(_AttnC)]
+        L.aibx_attn_workspace_bytes.argtypes = [vp, vp, vp]
         L.aibx_attn_workspace_bytes.restype = u64
         L.aibx_collect_scratch_bytes.argtypes = [u32]
         L.aibx_collect_scratch_bytes.restype = u64
@@ -168,7 +164,8 @@ def lib():
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # the handle itself: a torch Stream object around it costs as much as a launch (3 us)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _ptr(t, dtype=None):
@@ -501,17 +498,17 @@ class KVCache:
     def __init__(self, pool, layout: KVLayout, type: int, scales=None, inner: int = 0,
                  layer: int = 0):
         self._keep = (pool, scales)
-        self.device = pool.device
-        _same_device(pool, scales)
+        self.device = pool.get_device()
+        self.heads, self.head_dim = layout.num_kv_heads, layout.head_dim
         # a pool that is smaller than its layout says is a fault waiting to happen
-        if pool.numel() * pool.element_size() < layout.num_blocks * layout.block_bytes:
-            raise ValueError("pool of %d bytes, layout of %d" % (
-                pool.numel() * pool.element_size(), layout.num_blocks * layout.block_bytes))
-        if scales is not None and layout.head_dim > 0 and layout.elem_bytes > 0 and scales.numel() < \
-                layout.num_blocks * layout.block_bytes // (layout.head_dim * layout.elem_bytes):
-            raise ValueError("fewer scale bytes than rows")
+        rows = layout.num_blocks * layout.num_layers * 2 * layout.num_kv_heads * layout.block_tokens
+        if pool.nbytes < rows * layout.head_dim * layout.elem_bytes:
+            raise ValueError("pool of %d bytes, layout of %d rows of %d elements of %d bytes" % (
+                pool.nbytes, rows, layout.head_dim, layout.elem_bytes))
+        if scales is not None and (scales.get_device() != self.device or scales.numel() < rows):
+            raise ValueError("%d scale bytes on the pool's device expected" % rows)
         self._c = _CacheC(_ptr(pool), _ptr(scales, torch.uint8), layout, type, inner, layer)
-        self._ref = C.byref(self._c)
+        self._ref = C.addressof(self._c)
 
     @property
     def layout(self) -> KVLayout:
@@ -538,49 +535,46 @@ class KVBatch:
             raise ValueError("offsets of %d requests expected" % R)
         if blk_off is None and (block_table.dim() != 2 or block_table.shape[0] != R):
             raise ValueError("a block table of %d rows expected" % R)
-        _same_device(block_table, tok_off, kv_len, blk_off)
         self._keep = (block_table, tok_off, kv_len, blk_off)
-        self.device = kv_len.device
+        self.device = kv_len.get_device()
+        if block_table.get_device() != self.device or tok_off.get_device() != self.device or \
+                (blk_off is not None and blk_off.get_device() != self.device):
+            raise ValueError("all tensors of a batch live on one CUDA device")
         self.n_tokens = n_tokens
         self._c = _BatchC(_ptr(block_table, torch.uint32), _ptr(blk_off, torch.int64),
                           0 if blk_off is not None else block_table.shape[1],
                           _ptr(tok_off, torch.int64), _ptr(kv_len, torch.int32), n_tokens, R,
                           max_new)
-        self._ref = C.byref(self._c)
+        self._ref = C.addressof(self._c)
 
 
-def _same_device(*tensors) -> None:
-    for t in tensors:
-        if t is not None and t.device != tensors[0].device:
-            raise ValueError("tensors on %s and on %s" % (tensors[0].device, t.device))
-
-
-def _rows(t, cache: KVCache, batch: KVBatch, heads=None):
+def _rows(t, cache: KVCache, batch: KVBatch, heads: int):
     """(pointer, token stride, head stride) of a [n_tokens, heads, head_dim] tensor."""
-    if t.dim() != 3 or t.shape[0] != batch.n_tokens or t.shape[2] != cache._c.layout.head_dim or \
-            (heads is not None and t.shape[1] != heads) or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError("rows of [%d, %s, %d] expected, got %s with strides %s" % (
-            batch.n_tokens, heads if heads is not None else "heads", cache._c.layout.head_dim,
-            tuple(t.shape), t.stride()))
-    if not t.is_cuda or t.device != cache.device or t.device != batch.device:
+    st = t.stride()
+    if tuple(t.shape) != (batch.n_tokens, heads, cache.head_dim) or (st[2] != 1 and cache.head_dim > 1):
+        raise ValueError("rows of [%d, %d, %d] expected, got %s with strides %s" % (
+            batch.n_tokens, heads, cache.head_dim, tuple(t.shape), st))
+    if t.get_device() != cache.device:
         raise ValueError("all tensors of a call live on one CUDA device")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), st[0], st[1]
 
 
-def _current(cache: KVCache) -> None:
-    if cache.device.index != torch.cuda.current_device():
-        raise ValueError("the call works on the current device (%d), the pool is on %s" % (
-            torch.cuda.current_device(), cache.device))
+def _here(cache: KVCache, batch: KVBatch) -> int:
+    """The current stream, once it is sure that everything lives on the current device."""
+    if cache.device != batch.device or cache.device != torch._C._cuda_getDevice():
+        raise ValueError("the call works on the current device (%d); pool on %d, batch on %d" % (
+            torch._C._cuda_getDevice(), cache.device, batch.device))
+    return torch._C._cuda_getCurrentRawStream(cache.device)
 
 
 def _kv_tokens(name: str, cache: KVCache, batch: KVBatch, k, v) -> None:
-    heads = cache._c.layout.num_kv_heads
     if k.dtype != v.dtype or k.dtype not in _TYPE_OF:
         raise ValueError("K and V of one of bfloat16, float16, float32 expected")
-    _current(cache)
-    _check(name, getattr(lib(), name)(
-        cache._ref, batch._ref, *_rows(k, cache, batch, heads), *_rows(v, cache, batch, heads),
-        _TYPE_OF[k.dtype], _stream()))
+    stream = _here(cache, batch)
+    kp, kt, kh = _rows(k, cache, batch, cache.heads)
+    vp, vt, vh = _rows(v, cache, batch, cache.heads)
+    _check(name, getattr(lib(), name)(cache._ref, batch._ref, kp, kt, kh, vp, vt, vh,
+                                      _TYPE_OF[k.dtype], stream))
 
 
 def kv_append(cache: KVCache, batch: KVBatch, k, v) -> None:
@@ -599,29 +593,35 @@ def attn_paged(cache: KVCache, batch: KVBatch, q, out, lse=None, scale=None, cau
     """Attention of the batch's tokens over their requests' cached keys.  q, out: [n_tokens,
     q_heads, head_dim]; lse: float32 [n_tokens, q_heads] or None; scale: 1/sqrt(head_dim) if None.
     workspace: uint8 tensor of attn_workspace_bytes(...) bytes, allocated here if None."""
-    if q.dtype != out.dtype or q.dtype not in _TYPE_OF:
-        raise ValueError("queries and output of one type expected")
-    heads = q.shape[1] if q.dim() == 3 else 0
+    if q.dtype != out.dtype or q.dtype not in _TYPE_OF or q.dim() != 3:
+        raise ValueError("queries and output of one type and [n_tokens, q_heads, head_dim] expected")
+    stream = _here(cache, batch)
+    heads = q.shape[1]
     qp, qt, qh = _rows(q, cache, batch, heads)
     op, ot, oh = _rows(out, cache, batch, heads)
-    if lse is not None and (lse.shape != q.shape[:2] or lse.device != q.device):
-        raise ValueError("lse of [n_tokens, q_heads] expected")
-    _current(cache)
+    lp = None
+    if lse is not None:
+        if lse.shape != q.shape[:2] or lse.dtype != torch.float32 or not lse.is_contiguous() or \
+                lse.get_device() != cache.device:
+            raise ValueError("lse of float32 [n_tokens, q_heads], contiguous, expected")
+        lp = lse.data_ptr()
     prm = _AttnC(_TYPE_OF[q.dtype], heads, qt, qh, ot, oh,
-                 cache._c.layout.head_dim ** -0.5 if scale is None else scale, bool(causal), window)
+                 cache.head_dim ** -0.5 if scale is None else scale, bool(causal), window)
+    ref = C.addressof(prm)
     L = lib()
     if workspace is None:
-        need = L.aibx_attn_workspace_bytes(cache._ref, batch._ref, prm)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
-    _check("aibx_attn_paged", L.aibx_attn_paged(
-        cache._ref, batch._ref, prm, qp, op, _ptr(lse, torch.float32), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream()))
+        workspace = torch.empty(max(L.aibx_attn_workspace_bytes(cache._ref, batch._ref, ref), 16),
+                                dtype=torch.uint8, device=q.device)
+    elif workspace.get_device() != cache.device or not workspace.is_contiguous():
+        raise ValueError("a contiguous workspace on the pool's device expected")
+    _check("aibx_attn_paged", L.aibx_attn_paged(cache._ref, batch._ref, ref, qp, op, lp,
+                                                workspace.data_ptr(), workspace.nbytes, stream))
 
 
 def attn_workspace_bytes(cache: KVCache, batch: KVBatch, q) -> int:
     """Workspace of attn_paged for queries shaped like q; 0 where attn_paged would refuse."""
     prm = _AttnC(_TYPE_OF.get(q.dtype, -1), q.shape[1], 8, 8, 8, 8, 1.0, 1, 0)
-    return int(lib().aibx_attn_workspace_bytes(cache._ref, batch._ref, prm))
+    return int(lib().aibx_attn_workspace_bytes(cache._ref, batch._ref, C.addressof(prm)))
 
 
 def kv_set_tuning(mode: int = -1, chunk_bytes: int = 0, stages: int = 0,
