@@ -573,7 +573,8 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  *     out = sum_j w_j v_j,   w = softmax_j(scale * q . k_j),   lse = ln sum_j exp(scale * q . k_j).
  *   A row that sees no key gives out = 0 and lse = -infinity.
  *   q, out: [n_tokens][num_q_heads][head_dim] of type q_type (BF16 or FP16, the pool's type unless
- *   the pool is E4M3) with element strides per token and head, 16-byte aligned rows.  d_lse
+ *   the pool is E4M3) with element strides per token and head, 16-byte aligned rows; out must not
+ *   overlap q.  d_lse
  *   (nullable): float [n_tokens][num_q_heads].
  *   Products are accumulated in fp32; the weights are rounded to q_type (to fp16 over an E4M3
  *   pool, whose queries are held as fp16 times a power of two per row) before they multiply V; sums
@@ -581,10 +582,11 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  *   inputs give the same bits.
  *   What lies in slots that no visible position names (stale bytes, NaN) does not matter.  NaN or
  *   infinite K of a position hidden from a row does not reach it; a NaN or infinite V of a
- *   position that only some of a request's rows see may reach the others.  Over an E4M3 pool V
+ *   position that only some of a request's rows see may reach the others.  Over an E4M3 pool
+ *   a cached element may be off by 2^-34 of the largest magnitude among its 128 positions, and V
  *   scales below 2^-100 may count as 2^-100 (an error below 2^-91).
  * Shapes: head_dim 64 or 128, block_tokens a multiple of 8, at most 128 query heads per KV head,
- *   num_blocks below 2^31: UNSUPPORTED otherwise.  INVALID for unaligned q or out, strides that are no multiple of 8
+ *   num_blocks and n_tokens * that number below 2^31: UNSUPPORTED otherwise.  INVALID for unaligned q or out, strides that are no multiple of 8
  *   elements, a scale that is not positive and finite, num_q_heads no multiple of num_kv_heads, a window < 0,
  *   a workspace that is too small.
  * Workspace: aibx_attn_workspace_bytes(cache, batch, params) bytes, 16-byte aligned, content

@@ -484,7 +484,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         const unsigned int mask = s_mask[step % kInfoRing];
         float c = c0, shift = 0.0f;
         if constexpr (F8) {
-          c *= s_kscale[step % kInfoRing];
+          c = fmaxf(c * s_kscale[step % kInfoRing], 1.2e-38f);   // (0 would make NaN of a hidden key's -infinity)
           shift = s_vexp[step % kInfoRing];
         }
         const int b0 = vis0 - key0, b1 = vis1 - key0;
