@@ -574,8 +574,7 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  *   A row that sees no key gives out = 0 and lse = -infinity.
  *   q, out: [n_tokens][num_q_heads][head_dim] of type q_type (BF16 or FP16, the pool's type unless
  *   the pool is E4M3) with element strides per token and head, 16-byte aligned rows; out must not
- *   overlap q.  d_lse
- *   (nullable): float [n_tokens][num_q_heads].
+ *   overlap q.  d_lse (nullable): float [n_tokens][num_q_heads].
  *   Products are accumulated in fp32; the weights are rounded to q_type (to fp16 over an E4M3
  *   pool, whose queries are held as fp16 times a power of two per row) before they multiply V; sums
  *   and maxima of the softmax stay in fp32; the result is rounded once.  Two calls on the same
@@ -586,13 +585,13 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  *   a cached element may be off by 2^-34 of the largest magnitude among its 128 positions, and V
  *   scales below 2^-100 may count as 2^-100 (an error below 2^-91).
  * Shapes: head_dim 64 or 128, block_tokens a multiple of 8, at most 128 query heads per KV head,
- *   num_blocks and n_tokens * that number below 2^31: UNSUPPORTED otherwise.  INVALID for unaligned q or out, strides that are no multiple of 8
- *   elements, a scale that is not positive and finite, num_q_heads no multiple of num_kv_heads, a window < 0,
- *   a workspace that is too small.
+ *   num_blocks and n_tokens * that number below 2^31: UNSUPPORTED otherwise.  INVALID for
+ *   unaligned q or out, strides that are no multiple of 8 elements, a scale that is not positive
+ *   and finite, num_q_heads no multiple of num_kv_heads, a window < 0, a workspace that is too small.
  * Workspace: aibx_attn_workspace_bytes(cache, batch, params) bytes, 16-byte aligned, content
  *   irrelevant before and after; calls that may overlap on the GPU need separate ones.
- *   The answer depends on head_dim, num_q_heads / num_kv_heads and max_new alone (0 = arguments
- *   that attn_paged would refuse).
+ *   The answer depends on head_dim, num_q_heads / num_kv_heads, max_new and on whether R is 1, on
+ *   nothing else (0 = arguments that attn_paged would refuse).
  * RANGE is raised at least once for every request with a bad entry among the blocks that it reads,
  *   and for a request with more than max_new > 0 tokens (whose rows may be left unwritten).
  */

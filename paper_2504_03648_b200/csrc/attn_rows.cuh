@@ -456,7 +456,6 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
       __syncwarp();
       const unsigned int boxmask = s_mask[s];
-      bool handed = false;
       const int tile_key0 = (walk.span.tile0 + t) * TOK;
       // the 16-token tasks of all stages go round the warps in turn
       for (int task = turn; task < S::kTasks; task += kRowWarps) {
@@ -472,8 +471,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const unsigned char* kbase =
             ring + s * 2 * kRowHalfStage + ((b0 * S::kCols) << a.box_log) * RB + (task * 16 - (b0 << a.box_log)) * RB;
         const unsigned char* vbase = kbase + kRowHalfStage;
-        // ---- everything the task needs, into registers; then the stage goes back to the loader
-        // (held until the task was done, it was missing from the copies in flight: 215 us)
+        // ---- everything the task needs, into registers
         uint4 kr[kPieces][2];
 #pragma unroll
         for (int p = 0; p < kPieces; ++p) {
@@ -509,11 +507,6 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             kbyte[r] = sc[r * 8];
             vbyte[r] = sc[TOK + r * 8];
           }
-        }
-        if (task + kRowWarps >= S::kTasks) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&s_empty[s]));
-          handed = true;
         }
         // ---- S^T = K Q^T, in two chains
         float c[NQ][4], c2[NQ][4];
@@ -664,10 +657,8 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           }
       }
       turn = (turn - S::kTasks % kRowWarps + kRowWarps) % kRowWarps;
-      if (!handed) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_empty[s]));
-      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s_empty[s]));
     }
 
     // ---- join the warps
