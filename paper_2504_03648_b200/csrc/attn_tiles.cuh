@@ -328,7 +328,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   __shared__ __align__(8) unsigned long long s_kv_full[S::kBufs], s_kv_empty[S::kBufs];
   __shared__ __align__(8) unsigned long long s_raw_full[S::kBufs];
   __shared__ __align__(8) unsigned long long s_fac_full[S::kFactorRing], s_fac_empty[S::kFactorRing];
-  __shared__ __align__(8) unsigned long long s_q_full[2], s_s_full[2], s_h_full[2], s_p_full[2], s_o_full[2];
+  __shared__ __align__(8) unsigned long long s_q_full[2], s_s_full[2], s_h_full[2], s_p_full[2], s_o_full[2], s_turn[2];
   __shared__ unsigned int s_mask[kInfoRing];
   __shared__ float s_kscale[kInfoRing], s_vexp[kInfoRing];
   __shared__ long long s_scan[33];
@@ -350,7 +350,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kBufs; ++i) {
       mbar_init(smem_u32(&s_kv_full[i]), F8 ? 128u : 1u);
-      mbar_init(smem_u32(&s_kv_empty[i]), 1u);
+      mbar_init(smem_u32(&s_kv_empty[i]), 2u);
       mbar_init(smem_u32(&s_raw_full[i]), 1u);
     }
     for (int i = 0; i < S::kFactorRing; ++i) {
@@ -363,6 +363,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       mbar_init(smem_u32(&s_h_full[t]), 4u);
       mbar_init(smem_u32(&s_p_full[t]), 4u);
       mbar_init(smem_u32(&s_o_full[t]), 1u);
+      mbar_init(smem_u32(&s_turn[t]), 1u);
     }
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -640,12 +641,17 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     }
   } else if (warp < 12) {
     regs_down<S::kRegsOther>();
-    if (warp == 8) {
-      // ============================================================== MMA warp
+    if (warp == 8 || warp == 10) {
+      // ============================================================== MMA warps, one per tile
+      // Issuing an MMA and looking at a barrier take one warp 60 and more than 100 cycles each: while
+      // one of the two looks, the other's MMAs run.
+      const int t = warp == 10 ? 1 : 0;
       constexpr bool kHalf = std::is_same<MT, __half>::value;
       constexpr unsigned int kQK = mma_desc(kHalf, kTileKeys, false), kPV = mma_desc(kHalf, D, true);
       unsigned int buf = 0, buf_phase = 0;                 // next buffer of the ring to be read
-      unsigned int q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+      unsigned int q_phase = 0, p_phase = 0;
+      unsigned int turn_phase = t == 0;                    // (the first turn is tile 0's: a fresh barrier passes for phase 1)
+      constexpr bool kTurns = true;
       unsigned int last_buf = 0, last_phase = 1;           // (a fresh barrier passes for phase 1)
       auto advance = [&]() {
         if (++buf == S::kBufs) {
@@ -659,7 +665,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       // low words of the operands' descriptors; the rest of them is constant
       const unsigned int q_low = uniform(operand_low(smem0, 16)), k_low = uniform(operand_low(kv0, 16));
       const unsigned int v_low = uniform(operand_low(kv0, S::kColBytes));
-      auto qk = [&](int t, unsigned int kbuf) {
+      auto qk = [&](unsigned int kbuf) {
         const unsigned int low = k_low + kbuf * (S::kBuf >> 4);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
@@ -671,18 +677,17 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       };
       while (walk.next_warp(a)) {
         const int steps = (int)uniform(walk.t1 - walk.t0);
-        const int tiles = uniform(walk.rows(a) > kTileRows) ? 2 : 1;
+        const bool turns = kTurns && uniform(walk.rows(a) > kTileRows);     // two tiles at work
+        const bool active = uniform(walk.rows(a) > t * kTileRows);   // the tile has rows; else only hands buffers on
         const int key_first = (int)uniform((walk.span.tile0 + walk.t0) * kTileKeys);
         const int lo = (int)uniform(walk.span.lo), hi = (int)uniform(walk.span.hi);
         ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (t >= tiles) break;
-          ring_wait(smem_u32(&s_q_full[t]), q_phase[t], abort_flag);
+        if (active) {
+          ring_wait(smem_u32(&s_q_full[t]), q_phase, abort_flag);
           __syncwarp();
-          q_phase[t] ^= 1u;
+          q_phase ^= 1u;
           tmem_after();
-          qk(t, buf);
+          qk(buf);
         }
         mma_commit(smem_u32(&s_kv_empty[buf]), leader);
         advance();
@@ -694,7 +699,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           advance();
           if (!F8) {
             // V rows of positions nobody in the block sees: whatever the pool holds there
-            // (0 * NaN is NaN) becomes zero
+            // (0 * NaN is NaN) becomes zero; both warps see to it, each before its own MMAs
             const int key0 = key_first + j * kTileKeys;
             const int z0 = min(max(lo - key0, 0), kTileKeys), z1 = max(min(hi - key0, kTileKeys), 0);
             if (z0 > 0 || z1 < kTileKeys) {
@@ -718,12 +723,15 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             advance();
           }
           const unsigned int low = v_low + vbuf * (S::kBuf >> 4), old = j > 0;
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if (t >= tiles) break;
+          if (active) {
+            ring_wait(smem_u32(&s_h_full[t]), p_phase, abort_flag);
+            if (turns) {
+              ring_wait(smem_u32(&s_turn[t]), turn_phase, abort_flag);
+              turn_phase ^= 1u;
+            }
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              ring_wait(smem_u32(half ? &s_p_full[t] : &s_h_full[t]), p_phase[t], abort_flag);
+              if (half) ring_wait(smem_u32(&s_p_full[t]), p_phase, abort_flag);
               __syncwarp();
               tmem_after();
 #pragma unroll
@@ -731,14 +739,16 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
                 mma_tmem(tmu + 256 + t * D, tmu + t * 128 + k * 8, operand_desc(low + k * (2048 >> 4)), kPV,
                          k > 0 ? 1u : old, leader);
             }
-            p_phase[t] ^= 1u;
+            p_phase ^= 1u;
             if (more)
-              qk(t, kbuf);
+              qk(kbuf);
             else
               mma_commit(smem_u32(&s_o_full[t]), leader);
+            if (turns && lane == 0) mbar_arrive(smem_u32(&s_turn[1 - t]));
+            __syncwarp();
           }
-          if (more) mma_commit(smem_u32(&s_kv_empty[kbuf]), leader);
           mma_commit(smem_u32(&s_kv_empty[vbuf]), leader);
+          if (more) mma_commit(smem_u32(&s_kv_empty[kbuf]), leader);
         }
       }
       // the last commit has to arrive while its barrier is still this CTA's
@@ -799,10 +809,10 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       // nothing may still be on its way into this CTA's shared memory when it ends
       for (unsigned int i = issued > S::kBufs ? issued - S::kBufs : 0; i < issued; ++i)
         ring_drain(smem_u32(&full[i % S::kBufs]), (i / S::kBufs) & 1u);
-    } else if constexpr (F8) {
-      // ============================================================== scale warps (10, 11)
+    } else if (F8 && warp == 11) {
+      // ============================================================== scale warp (11)
       // Per step: the factor 2^(e - E) of every position of the K and of the V tile, and E.  The
-      // chain table -> scale byte is long: the two warps take turns and run ahead.
+      // chain table -> scale byte is long: it runs ahead.
       unsigned int step = 0;
       while (walk.next_warp(a)) {
         const uint32_t* row;
@@ -810,7 +820,6 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         table_row(a.b, walk.r, row, entries);
         const int head = walk.head, tile0 = walk.span.tile0, lo = walk.span.lo, hi = walk.span.hi, t1 = walk.t1;
         for (int j = walk.t0; j < t1; ++j, ++step) {
-          if ((step & 1u) != (unsigned int)(warp - 10)) continue;
           const int tok = (tile0 + j) * kTileKeys + lane * 4;   // four slots of one block
           int byte[2][4];
           unsigned int there = 0;
