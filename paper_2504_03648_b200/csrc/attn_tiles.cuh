@@ -9,11 +9,13 @@
 //                      over S, as 16-bit
 //   O += P V           tcgen05.mma, P from tensor memory, V from shared memory as it lies in the
 //                      pool ([position][dim], the operand's N-major form), O in tensor memory
-// Roles: two softmax warpgroups (one per tile), one warp that issues all MMAs, one that feeds a
-// ring of K and V tiles with tensor-map boxes (one box = the slots of one block and head that
-// fall into the tile).  While one tile's rows are exponentiated the other tile's two MMAs run.
-// MMAs complete in issue order, and S of step j + 1 is issued behind PV of step j: seeing S(j + 1)
-// is therefore also seeing O(j), and no further barrier guards O.
+// Roles: two softmax warpgroups (one per tile), a warp per tile that issues its MMAs, one warp that
+// feeds a ring of K and V tiles with tensor-map boxes (one box = the slots of one block and head that
+// fall into the tile).  The MMA warps take turns, PV(j) and S(j + 1) of one tile, then of the other:
+// while one tile's rows are exponentiated the other tile's MMAs run (without turns both tiles fall
+// into step, softmax with softmax: 948 instead of 805 us for six chunks over cached prefixes).  A
+// tile's MMAs complete in issue order, and S of step j + 1 is issued behind PV of step j: seeing
+// S(j + 1) is therefore also seeing O(j), and no further barrier guards O.
 //
 // Over an e4m3 pool a warpgroup more turns each raw tile into fp16 as it arrives: element times
 // 2^(e - E), e its row's exponent and E the tile's largest, which is exact down to 2^-24 of the
@@ -22,7 +24,11 @@
 // [1, 2) per row.
 //
 // Bound: the tensor pipe (1024 cycles per KV tile and 128 rows at D = 128, both products) and the
-// special function unit (128 * 128 exponentials at 16 a cycle: 1024 cycles too).
+// special function unit (128 * 128 exponentials at 16 a cycle: 1024 cycles too), neither of them
+// busy all the time: a step of both tiles takes about 3,500 cycles, 2,400 of a tile's softmax and
+// 1,050 from its last weights to its next scores.  Six chunks of 8,505 tokens over prefixes of 1k to
+// 8k (16-bit, 32 query heads on 8): 805 us, 950 TFLOP/s; a 1,023-token chunk over 130k e4m3 positions:
+// 2,200 us, 870 TFLOP/s.
 #pragma once
 
 #include "attn_rows.cuh"
