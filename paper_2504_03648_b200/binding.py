@@ -507,18 +507,20 @@ class KVCache:
                  layer: int = 0):
         self._keep = (pool, scales)
         self.device = pool.get_device()
-        self.heads, self.head_dim = layout.num_kv_heads, layout.head_dim
+        self.layout = layout
+        kind, layers, heads, slots, dim, size, blocks = (
+            layout.layout, layout.num_layers, layout.num_kv_heads, layout.block_tokens, layout.head_dim,
+            layout.elem_bytes, layout.num_blocks)
+        self.heads, self.head_dim = heads, dim
         # a pool that is smaller than its layout says is a fault waiting to happen
-        rows = layout.num_blocks * layout.num_layers * 2 * layout.num_kv_heads * layout.block_tokens
-        if pool.nbytes < rows * layout.head_dim * layout.elem_bytes:
+        rows = blocks * layers * 2 * heads * slots
+        if pool.nbytes < rows * dim * size:
             raise ValueError("pool of %d bytes, layout of %d rows of %d elements of %d bytes" % (
-                pool.nbytes, rows, layout.head_dim, layout.elem_bytes))
+                pool.nbytes, rows, dim, size))
         if scales is not None and (scales.get_device() != self.device or scales.numel() < rows):
             raise ValueError("%d scale bytes on the pool's device expected" % rows)
-        self.layout = layout
-        self._fields = [_ptr(pool), _ptr(scales, torch.uint8) or 0, layout.layout, layout.num_layers,
-                        layout.num_kv_heads, layout.block_tokens, layout.head_dim, layout.elem_bytes,
-                        layout.num_blocks, type, inner, layer]
+        self._fields = [_ptr(pool), 0 if scales is None else _ptr(scales, torch.uint8), kind, layers, heads, slots,
+                        dim, size, blocks, type, inner, layer]
         self._ref = _CACHE_BYTES.pack(*self._fields)
 
     @property
@@ -550,7 +552,7 @@ class KVBatch:
             raise ValueError("all tensors of a batch live on one CUDA device")
         self.n_tokens = n_tokens
         self._ref = _BATCH_BYTES.pack(
-            _ptr(block_table, torch.uint32), _ptr(blk_off, torch.int64) or 0,
+            _ptr(block_table, torch.uint32), 0 if blk_off is None else _ptr(blk_off, torch.int64),
             0 if blk_off is not None else block_table.shape[1], _ptr(tok_off, torch.int64),
             _ptr(kv_len, torch.int32), n_tokens, R, max_new)
 

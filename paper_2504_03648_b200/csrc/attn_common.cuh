@@ -146,12 +146,13 @@ struct alignas(16) JoinRecord {
   int pad;
 };
 
-// Joins rows that were cut: block c those that end in CTA c.  Slot of CTA x: 2 x for the piece it
-// begins with, 2 x + 1 for the one it ends with, each holding `cap` maxima, `cap` sums and cap x D
-// unnormalised outputs.  blockIdx.y takes 16 rows.
-template <int D, typename QT>
-__global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnArgs a, const float* slots,
-                                                        const JoinRecord* records, int cap);
+// What one kernel leaves to be joined.  Slot of CTA x: 2 x for the piece it begins with, 2 x + 1 for
+// the one it ends with, each holding `cap` maxima, `cap` sums and cap x D unnormalised outputs.
+struct JoinSet {
+  const float* slots;
+  const JoinRecord* records;
+  int cap;
+};
 
 // Waits for a phase of an mbarrier, at most two seconds; then (or once another warp has given up)
 // the CTA's abort flag is set, TIMEOUT is in the device status, and every later wait returns at
@@ -294,15 +295,21 @@ __device__ __forceinline__ void power_scale(float amax, float& down, float& up) 
 
 namespace aibx {
 
+// Joins rows that were cut: block c those that end in CTA c.  blockIdx.y takes 16 rows: the first
+// y_rows of them of the row kernel's set, the others of the tile kernel's.
 template <int D, typename QT>
-__global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ AttnArgs a, const float* slots,
-                                                        const JoinRecord* records, int cap) {
+__global__ void __launch_bounds__(256)
+attn_join_kernel(const __grid_constant__ AttnArgs a, JoinSet rows, JoinSet tiles, int y_rows) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const JoinRecord rec = records[blockIdx.x];
+  const bool of_rows = (int)blockIdx.y < y_rows;
+  const int y = of_rows ? (int)blockIdx.y : (int)blockIdx.y - y_rows;
+  const float* slots = of_rows ? rows.slots : tiles.slots;
+  const int cap = of_rows ? rows.cap : tiles.cap;
+  const JoinRecord rec = (of_rows ? rows.records : tiles.records)[blockIdx.x];
   const int c1 = (int)blockIdx.x;
   const size_t size = (size_t)cap * (D + 2);
   for (int x = threadIdx.x; x < 16 * (D / 4); x += 256) {
-    const int i = blockIdx.y * 16 + x / (D / 4), d = (x % (D / 4)) * 4;
+    const int i = y * 16 + x / (D / 4), d = (x % (D / 4)) * 4;
     if (i >= rec.rows) break;
     float top = -INFINITY, sum = 0.0f;
     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -333,10 +340,10 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
 }
 
 template <int D, typename QT>
-inline int32_t launch_join(const AttnArgs& a, const float* slots, const JoinRecord* records, int cap,
-                           unsigned int grid, cudaStream_t st) {
+inline int32_t launch_join(const AttnArgs& a, const JoinSet& rows, const JoinSet& tiles, cudaStream_t st) {
+  const int y_rows = (rows.cap + 15) / 16, y_tiles = (tiles.cap + 15) / 16;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid, (cap + 15) / 16);
+  cfg.gridDim = dim3((unsigned int)sm_count(), (unsigned int)(y_rows + y_tiles));
   cfg.blockDim = dim3(256);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
@@ -344,7 +351,7 @@ inline int32_t launch_join(const AttnArgs& a, const float* slots, const JoinReco
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attn_join_kernel<D, QT>, a, slots, records, cap) == cudaSuccess ? AIBX_OK
+  return cudaLaunchKernelEx(&cfg, attn_join_kernel<D, QT>, a, rows, tiles, y_rows) == cudaSuccess ? AIBX_OK
                                                                                                 : AIBX_ERR_CUDA;
 }
 

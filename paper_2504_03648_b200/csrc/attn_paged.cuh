@@ -55,13 +55,18 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
 
 template <int D, bool F8, typename QT>
 inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cudaStream_t st) {
+  JoinSet rows = {nullptr, nullptr, 0}, tiles = rows;
   if (plan.rows) {
-    const int32_t rc = plan.row_limit == 8 ? launch_attn_rows<D, F8, QT, 8>(a, type, st)
-                                           : launch_attn_rows<D, F8, QT, 16>(a, type, st);
+    const int32_t rc = plan.row_limit == 8 ? launch_attn_rows<D, F8, QT, 8>(a, type, rows, st)
+                                           : launch_attn_rows<D, F8, QT, 16>(a, type, rows, st);
     if (rc != AIBX_OK) return rc;
     a.slots += plan.rows_bytes / sizeof(float);
   }
-  return plan.tiles ? launch_attn_tiles<D, F8, QT>(a, type, st) : AIBX_OK;
+  if (plan.tiles) {
+    const int32_t rc = launch_attn_tiles<D, F8, QT>(a, type, tiles, st);
+    if (rc != AIBX_OK) return rc;
+  }
+  return launch_join<D, QT>(a, rows, tiles, st);
 }
 
 template <int D>

@@ -743,7 +743,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 }
 
 template <int D, bool F8, typename QT, int ROWS>
-inline int32_t launch_attn_rows(AttnArgs a, int type, cudaStream_t st) {
+inline int32_t launch_attn_rows(AttnArgs a, int type, JoinSet& join, cudaStream_t st) {
   using S = RowShape<D, F8, ROWS>;
   a.box = gcd_int(a.pool.T, S::kTok);
   a.box_log = log2_int(a.box);
@@ -759,10 +759,8 @@ inline int32_t launch_attn_rows(AttnArgs a, int type, cudaStream_t st) {
     return AIBX_ERR_CUDA;
   const unsigned int grid = (unsigned int)sm_count();
   attn_rows_kernel<D, F8, QT, ROWS><<<grid, S::kThreads, S::kSmem, st>>>(map_k, map_v, a);
-  const int32_t rc2 = launch_status();
-  if (rc2 != AIBX_OK) return rc2;
-  return launch_join<D, QT>(a, a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot), ROWS,
-                            grid, st);
+  join = JoinSet{a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot), ROWS};
+  return launch_status();
 }
 
 }  // namespace aibx

@@ -961,7 +961,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
 }
 
 template <int D, bool F8, typename QT>
-inline int32_t launch_attn_tiles(AttnArgs a, int type, cudaStream_t st) {
+inline int32_t launch_attn_tiles(AttnArgs a, int type, JoinSet& join, cudaStream_t st) {
   using S = TileShape<D, F8>;
   a.box = gcd_int(a.pool.T, kTileKeys);
   a.box_log = log2_int(a.box);
@@ -976,10 +976,8 @@ inline int32_t launch_attn_tiles(AttnArgs a, int type, cudaStream_t st) {
     return AIBX_ERR_CUDA;
   const unsigned int grid = (unsigned int)sm_count();
   attn_tiles_kernel<D, F8, QT><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
-  const int32_t rc2 = launch_status();
-  if (rc2 != AIBX_OK) return rc2;
-  return launch_join<D, QT>(a, a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot),
-                            2 * kTileRows, grid, st);
+  join = JoinSet{a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot), 2 * kTileRows};
+  return launch_status();
 }
 
 }  // namespace aibx
