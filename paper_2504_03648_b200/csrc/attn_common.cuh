@@ -1,8 +1,8 @@
 // What the two kernels of attn_paged share: the call's arguments, how its work is cut and handed
 // out, the tensor map of the pool, and the kernel that joins cut rows.
 //
-// Work is a line of KV tiles: request by request, KV head by KV head, (row block by row block,)
-// tile by tile.  CTA c of the persistent grid takes the c-th equal piece of that line, whatever
+// Work is a line of KV tiles: request by request, (KV head, row block) by (KV head, row block), tile
+// by tile.  CTA c of the persistent grid takes the c-th equal piece of that line, whatever
 // the requests' lengths are: no CTA waits for a long request, and the host needs to know no
 // length.  A piece that begins or ends inside a (request, head, row block) leaves unnormalised
 // sums with their maximum in one of the CTA's two workspace slots; attn_join_kernel adds those
@@ -92,6 +92,7 @@ struct WorkStart {
   long long base;       // first position of request r's part of the line
   int r;                // request in which this CTA's piece begins (-1: it is empty)
   int head, block, off; // and there: head, block of rows, tiles of it that belong to earlier pieces
+  int cls, g;           // and where that stands in the request's order
 };
 
 // Finds the request that holds position `index * per` of the line, per = ceil(total / pieces).
