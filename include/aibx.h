@@ -585,7 +585,7 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  *   a cached element may be off by 2^-34 of the largest magnitude among its 128 positions, and V
  *   scales below 2^-100 may count as 2^-100 (an error below 2^-91).
  * Shapes: head_dim 64 or 128, block_tokens a multiple of 8, at most 128 query heads per KV head,
- *   num_blocks and n_tokens * that number below 2^31: UNSUPPORTED otherwise.  INVALID for
+ *   num_blocks below 2^31, n_tokens below 2^24: UNSUPPORTED otherwise.  INVALID for
  *   unaligned q or out, strides that are no multiple of 8 elements, a scale that is not positive
  *   and finite, num_q_heads no multiple of num_kv_heads, a window < 0, a workspace that is too small.
  * Workspace: aibx_attn_workspace_bytes(cache, batch, params) bytes, 16-byte aligned, content

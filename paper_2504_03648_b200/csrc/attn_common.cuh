@@ -13,8 +13,8 @@
 
 namespace aibx {
 
-// Division of a row number below 2^31 by a small divisor, as a multiplication: with
-// m = ceil(2^40 / d), d <= 2^8, n * m / 2^40 exceeds n / d by less than n / 2^40 < 1 / d.
+// Division of a row number n < 2^24 d by a small divisor d <= 128, as a multiplication: with
+// m = ceil(2^40 / d), n m < 2^64, and n m / 2^40 exceeds n / d by less than n / 2^40 < 1 / d.
 struct SmallDivisor {
   unsigned long long m;
   __device__ __forceinline__ int div(int n) const { return (int)(((unsigned long long)n * m) >> 40); }

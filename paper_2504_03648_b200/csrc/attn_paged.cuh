@@ -43,7 +43,7 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
   if (c->type != AIBX_TYPE_E4M3 && c->type != p->q_type) return AIBX_ERR_UNSUPPORTED;
   if ((L.head_dim != 64 && L.head_dim != 128) || L.block_tokens % 8 != 0) return AIBX_ERR_UNSUPPORTED;
   plan.G = p->num_q_heads / L.num_kv_heads;
-  if (plan.G > 128 || L.num_blocks > 0x7fffffffu || b->n_tokens > 0x7fffffff / plan.G) return AIBX_ERR_UNSUPPORTED;
+  if (plan.G > 128 || L.num_blocks > 0x7fffffffu || b->n_tokens >= (1 << 24)) return AIBX_ERR_UNSUPPORTED;
   const long long bound = b->max_new > 0 ? b->max_new : (1LL << 31);
   plan.tiles = bound * plan.G > 16;
   plan.rows = !plan.tiles || (b->R > 1 && plan.G <= 16);

@@ -117,7 +117,7 @@ def test_attention_shapes_and_pointers(lib):
         assert attn(lib, cache(**kw), batch(), params()) == aibx.ERR_UNSUPPORTED, kw
     assert attn(lib, cache(num_kv_heads=1), batch(), params(num_q_heads=129)) == aibx.ERR_UNSUPPORTED
     assert attn(lib, cache(), batch(), params(q_type=aibx.TYPE_FP16)) == aibx.ERR_UNSUPPORTED
-    assert attn(lib, cache(), batch(n_tokens=1 << 30), params()) == aibx.ERR_UNSUPPORTED
+    assert attn(lib, cache(), batch(n_tokens=1 << 24), params()) == aibx.ERR_UNSUPPORTED
     for kw in (dict(q=None), dict(out=None), dict(ws=None), dict(q=FAKE + 8), dict(out=FAKE + 2), dict(ws=FAKE + 4),
                dict(lse=FAKE + 2), dict(size=1000)):
         assert attn(lib, cache(), batch(), params(), **kw) == aibx.ERR_INVALID, kw
