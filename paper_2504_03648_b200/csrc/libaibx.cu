@@ -913,7 +913,8 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
   bool work;
   rc = paged_views(cache, batch, a.pool, a.b, work);
   if (rc != AIBX_OK || !work) return rc;
-  if (!d_q || !d_out || !d_workspace) return AIBX_ERR_INVALID;
+  // a piece may still read queries of a row that another has written
+  if (!d_q || !d_out || !d_workspace || d_q == d_out) return AIBX_ERR_INVALID;
   if ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_out) |
        reinterpret_cast<uintptr_t>(d_workspace)) & 15)
     return AIBX_ERR_INVALID;

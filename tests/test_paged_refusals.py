@@ -49,7 +49,7 @@ def tokens(lib, name, c, b, k=FAKE, v=FAKE, strides=(512, 128, 512, 128), type=a
                               strides[0], strides[1], v, strides[2], strides[3], type, None)
 
 
-def attn(lib, c, b, p, q=FAKE, out=FAKE, lse=None, ws=FAKE, size=1 << 40):
+def attn(lib, c, b, p, q=FAKE, out=FAKE + 4096, lse=None, ws=FAKE, size=1 << 40):
     return lib.aibx_attn_paged(C.addressof(c) if c is not None else None, C.addressof(b) if b is not None else None,
                                C.addressof(p) if p is not None else None, q, out, lse, ws, size, None)
 
@@ -131,3 +131,7 @@ def test_workspace_depends_on_the_shape_of_the_work_alone(lib):
     few = size(cache(), batch(max_new=1), params())
     assert 0 < few == size(cache(num_blocks=500, layout=2), batch(max_new=1, n_tokens=900, R=900), params())
     assert few < size(cache(), batch(max_new=100), params()) == size(cache(), batch(max_new=0, R=7), params())
+
+
+def test_output_in_place_of_queries(lib):
+    assert attn(lib, cache(), batch(), params(), q=FAKE, out=FAKE) == aibx.ERR_INVALID
