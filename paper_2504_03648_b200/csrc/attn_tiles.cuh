@@ -381,6 +381,7 @@ struct TileWalk {
       int more = 0;
       if ((threadIdx.x & 31) == 0) more = next(a);
       more = __shfl_sync(0xffffffffu, more, 0);
+      __syncwarp();                  // (a shuffle orders no memory: the other lanes read what next() wrote)
       if (more != 2) return more != 0;
       enter(a, per);
     }

@@ -1,0 +1,57 @@
+"""GPU tests of the paged token and attention calls where numbers, lengths and bounds are at their
+edges: scales far apart, rows of zeros, scale bytes at the ends of their range, positions near 2^31,
+more tokens than promised, many short segments."""
+import numpy as np
+import pytest
+import torch
+
+from paged_ref import DTYPE, HALF_STEP, Batch, Shape, attention, pool_values, tolerance
+from paper_2504_03648_b200 import binding as aibx
+from test_gpu_paged import POOLS, check_attention, dev, make_batch, make_cache, make_pool
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _clean_status():
+    aibx.status_fetch()
+    yield
+
+
+def run(cache, batch, q, **kw):
+    out = torch.empty_like(q)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    aibx.attn_paged(cache, batch, q, out, lse=lse, **kw)
+    return out, lse
+
+
+def same(a, b):
+    return all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("pool,io", POOLS)
+def test_many_short_segments(pool, io):
+    """Chunks of one to three tiles, several to a CTA: every warp of a CTA has to move from segment to
+    segment with the others.  Right, and the same bits every time."""
+    R = 700
+    s = Shape(H=2, D=64, T=16, pool=pool, blocks=R * 12, layers=1, layer=0)
+    rng = np.random.default_rng(21)
+    new = [int(x) for x in rng.integers(20, 40, R)]
+    b = Batch(rng, s, new, [n + int(c) for n, c in zip(new, rng.integers(0, 140, R))])
+    p, sc = make_pool(rng, s)
+    cache, batch = make_cache(s, p, sc), make_batch(b)
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2, s.D))).to(DTYPE[io])
+    want = run(cache, batch, q.cuda())
+    for _ in range(20):
+        assert same(run(cache, batch, q.cuda()), want)
+    few = Batch.__new__(Batch)                                  # the plain form of some of them
+    few.__dict__.update(b.__dict__)
+    pick = list(range(0, R, 29))
+    few.new, few.length = [b.new[r] for r in pick], [b.length[r] for r in pick]
+    few.table = b.table[pick]
+    few.tok_off = np.concatenate([[0], np.cumsum(few.new)]).astype(np.int64)
+    few.n_tokens = int(few.tok_off[-1])
+    rows = np.concatenate([np.arange(b.tok_off[r], b.tok_off[r + 1]) for r in pick])
+    out, lse, mag, slack = attention(s, few, pool_values(s, p, sc), q[rows].double().numpy(), s.D ** -0.5, True, 0)
+    assert (np.abs(want[0][rows].double().cpu().numpy() - out) <= tolerance(s, io, out, mag, slack)).all()
+    assert aibx.status_fetch() == (0, 0)
