@@ -35,7 +35,7 @@ struct AttnArgs {
   int box, box_log;                         // tokens one tensor-map box covers: a power of two
   int row_limit;                            // requests of up to so many rows (tokens * G) are the
                                             // row kernel's, 0: none
-  int check_bound;                          // report requests this call has no kernel for
+  int max_new;                              // bound on a request's tokens, 0: none given
   float* slots;                             // two per CTA, then a JoinRecord per CTA
 };
 
@@ -301,6 +301,11 @@ namespace aibx {
 template <int D, typename QT>
 __global__ void __launch_bounds__(256)
 attn_join_kernel(const __grid_constant__ AttnArgs a, JoinSet rows, JoinSet tiles, int y_rows) {
+  // Requests with more tokens than the caller's bound: looked for here, beside the kernel before,
+  // where it costs the call nothing.
+  if (a.max_new > 0 && blockIdx.x == 0 && blockIdx.y == 0)
+    for (int r = threadIdx.x; r < a.b.R; r += 256)
+      if (attn_request(a.b, a.pool.T, r).n > a.max_new) raise_status(AIBX_ERR_RANGE);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const bool of_rows = (int)blockIdx.y < y_rows;
   const int y = of_rows ? (int)blockIdx.y : (int)blockIdx.y - y_rows;

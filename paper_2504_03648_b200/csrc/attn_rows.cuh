@@ -232,11 +232,6 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (a.check_bound && blockIdx.x == 0)
-    for (int r = threadIdx.x; r < a.b.R; r += S::kThreads) {
-      const AttnRequest q = attn_request(a.b, a.pool.T, r);
-      if ((long long)q.n * a.G > a.row_limit) raise_status(AIBX_ERR_RANGE);
-    }
   const RowCost<TOK> cost{a};
   locate_piece<S::kThreads>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
   const WorkStart w = s_start;

@@ -933,7 +933,7 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
   a.causal = params->causal != 0;
   a.window = params->window;
   a.box = 0;
-  a.check_bound = !plan.tiles;
+  a.max_new = batch->max_new;
   a.row_limit = plan.row_limit;
   a.slots = static_cast<float*>(d_workspace);
   return launch_attn(a, cache->type, params->q_type, plan, as_stream(stream));

@@ -55,3 +55,20 @@ def test_many_short_segments(pool, io):
     out, lse, mag, slack = attention(s, few, pool_values(s, p, sc), q[rows].double().numpy(), s.D ** -0.5, True, 0)
     assert (np.abs(want[0][rows].double().cpu().numpy() - out) <= tolerance(s, io, out, mag, slack)).all()
     assert aibx.status_fetch() == (0, 0)
+
+
+# (tokens, bound, query heads per KV head): the row kernel alone, with rows to spare or not; both
+# kernels; the tile kernel alone for one request
+@pytest.mark.parametrize("new,bound,G", [([1, 3, 2, 1], 1, 2), ([1, 9, 1], 1, 8), ([200, 1, 30, 101], 100, 4),
+                                         ([1, 2, 20], 1, 17), ([41], 40, 2), ([6, 5, 3], 4, 4), ([2], 1, 4)])
+@pytest.mark.parametrize("pool,io", [("bf16", "bf16"), ("e4m3", "fp16")])
+def test_every_request_past_the_bound_is_reported(new, bound, G, pool, io):
+    s = Shape(H=1, D=64, T=16, pool=pool, blocks=60)
+    rng = np.random.default_rng(22)
+    b = Batch(rng, s, new, [n + 30 for n in new])
+    p, sc = make_pool(rng, s)
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, G, 64))).to(DTYPE[io]).cuda()
+    run(make_cache(s, p, sc), make_batch(b, max_new=bound), q)
+    assert aibx.status_fetch() == (aibx.ERR_RANGE, sum(n > bound for n in new))
+    run(make_cache(s, p, sc), make_batch(b, max_new=max(new)), q)
+    assert aibx.status_fetch() == (0, 0)
