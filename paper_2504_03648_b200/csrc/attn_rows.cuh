@@ -546,7 +546,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             kf = kb == 255 ? NAN : power_of_byte(kb);
             const int ve = max(vb - 127, -100);
             vexp = vb == 255 ? NAN : (float)ve;
-            unshift[r] = __uint_as_float((unsigned int)(127 - min(ve, 126)) << 23);
+            unshift[r] = power_of_byte(127 - ve);
           }
 #pragma unroll
           for (int x = 0; x < NQ; ++x)

@@ -668,7 +668,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         float total, other;
         split2(sum2, total, other);
         total += other;
-        l += F8 ? total * exp2_fast(-shift) : total;
+        l += F8 ? total * power_of_byte(127 - (int)shift) : total;   // (2^-127 too: no flushing here)
         tmem_wait_st();
         tmem_before();
         __syncwarp();

@@ -72,3 +72,28 @@ def test_every_request_past_the_bound_is_reported(new, bound, G, pool, io):
     assert aibx.status_fetch() == (aibx.ERR_RANGE, sum(n > bound for n in new))
     run(make_cache(s, p, sc), make_batch(b, max_new=max(new)), q)
     assert aibx.status_fetch() == (0, 0)
+
+
+def of_v(s, x, per_row):
+    """The V rows of a pool of layout 0 (a view: [blocks, layers, rows, per_row])."""
+    return x.reshape(s.blocks, s.layers, 2, s.H * s.T, per_row)[:, :, 1]
+
+
+@pytest.mark.parametrize("byte", [200, 253, 254])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("D", [64, 128])
+def test_largest_v_scales(byte, new, D):
+    """V rows of up to 2^(byte - 127), alone and beside the power below: weights, sums and lse."""
+    s = Shape(H=2, D=D, T=16, pool="e4m3", blocks=60)
+    b = Batch(np.random.default_rng(23), s, [new, new], [new + 5, new + 300])
+
+    for lower in (0, 1):
+        def change(pool, scales):
+            v = of_v(s, pool, D)
+            v[:] = (v.float() / 512).to(torch.float8_e4m3fn)        # magnitudes below 1: the values are finite
+            of_v(s, scales, 1)[:] = byte
+            of_v(s, scales, 1)[:, :, ::3] = byte - lower
+            return pool, scales
+
+        st, out, _ = check_attention(s, b, "bf16", G=4, change=change)
+        assert st == (0, 0) and (out != 0).any(-1).all()
