@@ -283,6 +283,34 @@ struct Bits16<__half> {
   }
 };
 
+// Weights are held 2^kWeightHead up where they become fp16, whose normal numbers end at 2^-14: the
+// running maximum m stands that much below the largest score, and follows once a score has grown by
+// 2^8, so that weights reach up to 2^15 and keep all their bits down to 2^-21 of the largest.
+template <typename T>
+constexpr float kWeightHead = std::is_same<T, __half>::value ? 7.0f : 0.0f;
+
+// Over e4m3 the weight that multiplies V carries V's exponent b_j beside the score, and m covers
+// t_j + b_j.  b_j says little about the row's size where the scale byte is larger than its elements
+// need: a row of zeros written by append has b = 0, beside b = -7 for rows of magnitude 3.  If such a
+// row leads, all others' weights lie b_j (and its lead) below m, and fp16 would lose them.  So keys whose
+// bytes lie more than kScaleSpread below the largest so far, or outside [kScaleLow, kScaleHigh], are
+// multiplied "wide": weights as the sum of two bf16 numbers (16 bits, range 2^-126), V as bf16
+// (exact: four bits).  What exceeds the range of bytes goes into V itself, so that 2^b_j and the sum
+// of 2^t_j stay within fp32 whatever the bytes are: a weight is lost below 2^-126 only, and then the
+// key's score is 37 below another's (a factor of 2^37) at the least.
+constexpr int kScaleLow = 79, kScaleHigh = 175, kScaleSpread = 4;
+
+__device__ __forceinline__ int weight_byte(int byte) { return min(max(byte, kScaleLow), kScaleHigh); }
+
+// A group of keys' V bytes, of those that a row may see: 16 + the least one (0 if one lies outside the
+// range), and the largest.  255 (NaN) is outside, and not the largest.
+__device__ __forceinline__ uint32_t scale_facts(uint32_t least16, uint32_t most) { return least16 | (most << 16); }
+// Whether the group is multiplied wide; `most` = the largest byte so far, moved on.
+__device__ __forceinline__ bool scales_wide(uint32_t facts, int& most) {
+  most = max(most, (int)(facts >> 16));
+  return most + 16 - (int)(facts & 0xffffu) > kScaleSpread;
+}
+
 // 2^-k and 2^k for the power k that brings a magnitude into [1, 2); k = 0 for 0, kept in range.
 __device__ __forceinline__ void power_scale(float amax, float& down, float& up) {
   int k = (int)(__float_as_uint(amax) >> 23) - 127;

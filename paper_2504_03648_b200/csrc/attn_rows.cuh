@@ -7,7 +7,7 @@
 // Over an e4m3 pool k_j = K_j 2^a_j and v_j = V_j 2^b_j with e4m3 rows K_j, V_j.  Those are exact
 // in fp16, so they go to the tensor core as they are: the scores take 2^a_j afterwards, and the
 // weight that multiplies V_j is w = 2^(t + b_j - m) with m the maximum of t + b_j; then
-// l = sum w 2^-b_j.  Queries are scaled to [1, 2) per row to fit fp16 (fp16 keeps 3 more bits than
+// l = sum w 2^-b_j (stages whose b_j are far apart: see kScaleSpread).  Queries are scaled to [1, 2) per row to fit fp16 (fp16 keeps 3 more bits than
 // bf16; what falls below 2^-24 of the row's maximum is lost).
 //
 // Bound: HBM.  Every K and V byte is read once and meets at most 16 rows, so the legacy tensor
@@ -75,6 +75,12 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 __device__ __forceinline__ uint32_t e4m3_bits(uint32_t pair) {
   const __half2 h = halves_of_e4m3(pair);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Two e4m3 numbers times powers of two, as bf16: exact.
+__device__ __forceinline__ uint32_t bf16_of_e4m3(uint32_t pair, float f0, float f1) {
+  const float2 y = __half22float2(halves_of_e4m3(pair));
+  return Bits16<__nv_bfloat16>::pack(y.x * f0, y.y * f1);
 }
 
 // The tiles of request r: first tile and how many (at least one, so that empty rows are written).
@@ -212,6 +218,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   extern __shared__ unsigned char s_raw[];
   __shared__ __align__(8) unsigned long long s_full[kRowStages], s_empty[kRowStages];
   __shared__ unsigned int s_mask[kRowStages];
+  __shared__ uint32_t s_facts[kRowStages];                  // of the stage's V bytes
   __shared__ float s_m[2][kRowWarps][ROWS], s_l[2][kRowWarps][ROWS];
   __shared__ long long s_scan[33];
   __shared__ WorkStart s_start;
@@ -312,10 +319,12 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (it % kScaleWarps != (unsigned int)k) continue;
         uint32_t kb = 0x7f7f7f7fu, vb = 0x7f7f7f7fu, kb2 = kb, vb2 = vb;
         const int tok = (walk.span.tile0 + t) * TOK + lane * kPer;     // kPer slots of one block
+        bool there = false;
         if (tok < walk.span.hi) {
           const int at = tok / a.pool.T;
           const uint32_t id = __ldg(row + at);
-          if (id < a.pool.num_blocks) {
+          there = id < a.pool.num_blocks;
+          if (there) {
             const unsigned char* p = a.pool.scales + (long long)id * a.pool.s_block +
                                      (long long)walk.head * a.pool.s_head +
                                      (long long)(tok - at * a.pool.T) * a.pool.s_slot;
@@ -334,8 +343,25 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             }
           }
         }
+        // least and largest V byte of the positions that a row may see
+        uint32_t least = 0xffffffffu, most = 0u;
+#pragma unroll
+        for (int w = 0; w < kPer / 4; ++w) {
+          const int t0w = tok + 4 * w;
+          const int n0 = min(max(walk.span.lo - t0w, 0), 4), n1 = there ? min(max(walk.span.hi - t0w, 0), 4) : 0;
+          const uint32_t in = (uint32_t)((1ull << (8 * n1)) - 1) & ~(uint32_t)((1ull << (8 * n0)) - 1);
+          const uint32_t b4 = w ? vb2 : vb;
+          least = __vminu4(least, (b4 & ~__vcmpgtu4(b4, kScaleHigh * 0x01010101u)) | ~in);
+          most = __vmaxu4(most, b4 & in & ~__vcmpeq4(b4, 0xffffffffu));
+        }
+        least = __vminu4(least, least >> 16 | 0xffff0000u);
+        most = __vmaxu4(most, most >> 16);
+        least = min(least & 255u, (least >> 8) & 255u);
+        least = __reduce_min_sync(0xffffffffu, least < kScaleLow ? 0u : least + 16u);
+        most = __reduce_max_sync(0xffffffffu, max(most & 255u, (most >> 8) & 255u));
         const int s = (int)(it % kRowStages);
         if (it >= kRowStages) ring_wait(smem_u32(&s_empty[s]), (it / kRowStages - 1) & 1u, abort_flag);
+        if (lane == 0) s_facts[s] = scale_facts(least, most);
         uint32_t* dst = reinterpret_cast<uint32_t*>(s_scale + s * 2 * TOK);
         if (kPer == 8) {
           dst[2 * lane] = kb;
@@ -427,6 +453,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         prow[x][h] = first + a.by_g.div(min(x * 8 + 2 * t4 + h, n_rows - 1));
       }
     }
+    int most = 0;                                          // largest V byte of the segment so far
     float m[NQ][2], l[NQ][2], o[NQ][kMT][4];
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
@@ -452,6 +479,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       }
       __syncwarp();
       const unsigned int boxmask = s_mask[s];
+      const bool wide = F8 && scales_wide(s_facts[s], most);
       const int tile_key0 = (walk.span.tile0 + t) * TOK;
       // the 16-token tasks of all stages go round the warps in turn
       for (int task = turn; task < S::kTasks; task += kRowWarps) {
@@ -542,11 +570,10 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         for (int r = 0; r < 2; ++r) {
           float kf = 1.0f, vexp = 0.0f;
           if constexpr (F8) {
-            const int kb = kbyte[r], vb = vbyte[r];
+            const int kb = kbyte[r], vb = weight_byte(vbyte[r]);
             kf = kb == 255 ? NAN : power_of_byte(kb);
-            const int ve = max(vb - 127, -100);
-            vexp = vb == 255 ? NAN : (float)ve;
-            unshift[r] = power_of_byte(127 - ve);
+            vexp = (float)(vb - 127);
+            unshift[r] = power_of_byte(254 - vb);
           }
 #pragma unroll
           for (int x = 0; x < NQ; ++x)
@@ -583,6 +610,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           }
         }
         // ---- running maximum, moved only when it grows by more than 2^8
+        constexpr float kHead = kWeightHead<MT>;
         float mt[NQ][2];
         bool grow = false;
 #pragma unroll
@@ -594,14 +622,14 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
             y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
             mt[x][h] = y;
-            grow |= y > m[x][h] + 8.0f;                     // also from -infinity
+            grow |= y > m[x][h] + (kHead + 8.0f);           // also from -infinity
           }
         if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
           for (int x = 0; x < NQ; ++x)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const float mn = fmaxf(m[x][h], mt[x][h]);
+              const float mn = fmaxf(m[x][h], mt[x][h] - kHead);
               const float al = mn == -INFINITY ? 1.0f : exp2_fast(m[x][h] - mn);
               m[x][h] = mn;
               l[x][h] *= al;
@@ -613,17 +641,64 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             }
         }
         uint32_t pb[NQ][2];
-#pragma unroll
-        for (int x = 0; x < NQ; ++x) {
+        auto weights = [&](int x, int r, float& p0, float& p1) {
           const float m0 = m[x][0] == -INFINITY ? 0.0f : m[x][0], m1 = m[x][1] == -INFINITY ? 0.0f : m[x][1];
+          p0 = exp2_fast(c[x][2 * r] - m0);
+          p1 = exp2_fast(c[x][2 * r + 1] - m1);
+          l[x][0] += F8 ? p0 * unshift[r] : p0;
+          l[x][1] += F8 ? p1 * unshift[r] : p1;
+        };
+        if constexpr (F8) {
+          if (wide) {
+            // ---- O^T += V^T P^T, V and the weights as bf16
+            uint32_t pb2[NQ][2];
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const float p0 = exp2_fast(c[x][2 * r] - m0), p1 = exp2_fast(c[x][2 * r + 1] - m1);
-            l[x][0] += F8 ? p0 * unshift[r] : p0;
-            l[x][1] += F8 ? p1 * unshift[r] : p1;
-            pb[x][r] = transpose8(Bits16<MT>::pack(p0, p1));
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+              for (int r = 0; r < 2; ++r) {
+                float p0, p1;
+                weights(x, r, p0, p1);
+                if (vbyte[r] == 255) {                       // a NaN row, for those that see it
+                  if (c[x][2 * r] != -INFINITY) p0 = NAN;
+                  if (c[x][2 * r + 1] != -INFINITY) p1 = NAN;
+                }
+                const uint32_t hi = Bits16<__nv_bfloat16>::pack(p0, p1);
+                const float2 y = Bits16<__nv_bfloat16>::unpack(hi);
+                pb[x][r] = transpose8(hi);
+                pb2[x][r] = transpose8(Bits16<__nv_bfloat16>::pack(p0 - y.x, p1 - y.y));
+              }
+            float vf[4];                                     // of this lane's tokens: what the weights do not carry
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int byte = s_scale[s * 2 * TOK + TOK + task * 16 + (e >> 1) * 8 + 2 * t4 + (e & 1)];
+              vf[e] = byte == 255 ? 1.0f : power_of_byte(127 + byte - weight_byte(byte));
+            }
+#pragma unroll
+            for (int w4 = 0; w4 < kW; ++w4) {
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                const uint32_t y0 = __byte_perm(v[0][0][w4], v[0][1][w4], half ? 0x7362 : 0x5140);
+                const uint32_t y1 = __byte_perm(v[0][2][w4], v[0][3][w4], half ? 0x7362 : 0x5140);
+                const uint32_t af[4] = {bf16_of_e4m3(y0 & 0xffffu, vf[0], vf[1]), bf16_of_e4m3(y0 >> 16, vf[0], vf[1]),
+                                        bf16_of_e4m3(y1 & 0xffffu, vf[2], vf[3]), bf16_of_e4m3(y1 >> 16, vf[2], vf[3])};
+#pragma unroll
+                for (int x = 0; x < NQ; ++x) {
+                  mma_16816(o[x][2 * w4 + half], af, pb[x][0], pb[x][1], __nv_bfloat16());
+                  mma_16816(o[x][2 * w4 + half], af, pb2[x][0], pb2[x][1], __nv_bfloat16());
+                }
+              }
+            }
+            continue;
           }
         }
+#pragma unroll
+        for (int x = 0; x < NQ; ++x)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            float p0, p1;
+            weights(x, r, p0, p1);
+            pb[x][r] = transpose8(Bits16<MT>::pack(p0, p1));
+          }
         // ---- O^T += V^T P^T
 #pragma unroll
         for (int cc = 0; cc < kVC; ++cc)

@@ -97,3 +97,147 @@ def test_largest_v_scales(byte, new, D):
 
         st, out, _ = check_attention(s, b, "bf16", G=4, change=change)
         assert st == (0, 0) and (out != 0).any(-1).all()
+
+
+# ------------------------------------------------------------------------------------------
+# e4m3 rows whose scales are far apart
+
+def definition(values, rows_k, rows_v, q, scale, first):
+    """Causal attention of one (request, KV head) in 64 bits, and what the roundings may add to the
+    output: q [n][G][D] at positions first .., rows of K and of V for positions 0 .."""
+    k, v = values[rows_k], values[rows_v]
+    z = scale * np.einsum("ngd,kd->ngk", q, k)
+    z[:, :, :][np.broadcast_to(np.arange(len(k))[None, None] > first + np.arange(len(q))[:, None, None], z.shape)] = -np.inf
+    m = z.max(-1, keepdims=True)
+    w = np.exp(z - m)
+    t = w.sum(-1, keepdims=True)
+    w /= t
+    out, lse = w @ v, (m + np.log(t))[..., 0]
+    mag = w @ np.abs(v)
+    # A score: fp32 products and sums of D terms; queries are fp16, within 2^-25 of their row's largest.
+    slack = scale * (q.shape[-1] + 4) * 2.0 ** -24 * np.abs(q).sum(-1) * np.abs(k).max() + 2.0 ** -22 * np.abs(m[..., 0])
+    # A weight: fp16 (2^-11), or below 2^-14 on a grid of 2^-24, in units 2^7 below the largest 2^(t + b)
+    # and of keys whose b is at most 4 below the largest: 2^-25 * 2^-7 * 2^4 of the largest weight each.
+    grid = 2.0 ** -28 * w.max(-1, keepdims=True) * np.abs(v).sum(0)
+    return out, lse, (2.0 ** -11 + 2 * slack[..., None] + 2.0 ** -20) * mag + grid, slack
+
+
+def check_scales(s, b, pool, scales, q, io, G):
+    """Every request of b against the definition; q: [n_tokens][H * G][D] on the host."""
+    cache, batch = make_cache(s, pool, scales), make_batch(b)
+    out, lse = run(cache, batch, q.cuda())
+    values = pool_values(s, pool, scales)
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for r, n in enumerate(b.new):
+        L, o = b.length[r], int(b.tok_off[r])
+        for h in range(s.H):
+            rows = [np.array([s.row(b.entry(s, r, p), kv, h, p % s.T) for p in range(L)]) for kv in range(2)]
+            heads = slice(h * G, h * G + G)
+            want, wl, tol, slack = definition(values, *rows, q[o:o + n, heads].double().numpy(), s.D ** -0.5, L - n)
+            # the result is rounded once; 2^-25 below fp16's normal numbers, 2^-134 below bf16's
+            tol = tol + HALF_STEP[io] * np.abs(want) + (2.0 ** -25 if io == "fp16" else 2.0 ** -133)
+            err = np.abs(out[o:o + n, heads] - want)
+            assert (err <= tol).all(), (r, h, float((err / tol).max()), float(err.max() / np.abs(want).max()))
+            assert (np.abs(lse[o:o + n, heads] - wl) <= slack + 2.0 ** -14 + 2.0 ** -22 * np.abs(wl)).all()
+    assert aibx.status_fetch() == (0, 0)
+
+
+def null_key_pool(rng, s, b, q, lead, size, where, G):
+    """A pool written by append: V of magnitude `size`, and at position where(length) a key that leads the
+    others' scores by about `lead`, with a V of zeros."""
+    cache = make_cache(s, torch.zeros(s.rows, s.D).to(torch.float8_e4m3fn), np.full(s.rows, 127, dtype=np.uint8))
+    total = sum(b.length)
+    whole = Batch.__new__(Batch)
+    whole.__dict__.update(b.__dict__)
+    whole.new = b.length
+    whole.tok_off = np.concatenate([[0], np.cumsum(b.length)]).astype(np.int64)
+    whole.n_tokens = total
+    k = rng.normal(size=(total, s.H, s.D)) * 0.3
+    v = rng.normal(size=(total, s.H, s.D)) * size
+    u = np.ones(s.D)
+    for r, L in enumerate(b.length):
+        i = int(whole.tok_off[r]) + where(L)
+        k[i] = u * (lead / (s.D ** -0.5 * s.D))
+        v[i] = 0.0
+    k, v = (torch.from_numpy(x).float().cuda() for x in (k, v))
+    aibx.kv_append(cache, make_batch(whole), k, v)
+    return cache._keep[0].cpu().view(torch.float8_e4m3fn).view(s.rows, s.D), cache._keep[1].cpu().numpy()
+
+
+def near_ones(rng, n, heads, D, io):
+    """Queries whose product with a row of ones is about D."""
+    return torch.from_numpy(1.0 + 0.1 * rng.normal(size=(n, heads, D))).to(DTYPE[io])
+
+
+WHERE = {"first": lambda L: 0, "middle": lambda L: L // 2, "late": lambda L: max(0, L - 45)}
+
+
+@pytest.mark.parametrize("size", [3.0, 1.0, 0.1, 0.01, 0.001, 1e-5])
+@pytest.mark.parametrize("lead", [3.0, 6.0, 8.0, 14.0])
+@pytest.mark.parametrize("where", list(WHERE))
+def test_a_leading_row_of_zeros_few_rows(size, lead, where):
+    for D, io, new, G in ((128, "bf16", 1, 8), (64, "fp16", 1, 4), (128, "fp16", 3, 5)):
+        s = Shape(H=2, D=D, T=16, pool="e4m3", blocks=340, layers=1, layer=0)
+        rng = np.random.default_rng(24)
+        b = Batch(rng, s, [new, new], [1000, 4003])
+        q = near_ones(rng, b.n_tokens, 2 * G, D, io)
+        pool, scales = null_key_pool(rng, s, b, q, lead, size, WHERE[where], G)
+        assert (scales == 127).any()
+        check_scales(s, b, pool, scales, q, io, G)
+
+
+def spread_pool(rng, s, kind):
+    """Pools as others may write them: bytes far apart, one byte for all, bytes larger than the rows need."""
+    pool = torch.from_numpy(rng.normal(size=(s.rows, s.D)) * 100).clamp(-448, 448).to(torch.float8_e4m3fn)
+    scales = rng.integers(118, 123, s.rows).astype(np.uint8)
+    v = of_v(s, scales, 1)
+    if kind == "spread of 40":
+        v[:] = rng.integers(90, 131, v.shape)
+    elif kind == "whole range":
+        v[:] = rng.integers(0, 240, v.shape)
+    elif kind == "lowest":
+        v[:] = rng.integers(0, 30, v.shape)
+    elif kind == "one byte":                                # elements around e4m3's least
+        v[:] = 127
+        x = of_v(s, pool, s.D)
+        x[:] = (x.float() / 8192).to(torch.float8_e4m3fn)
+    elif kind == "loose":                                    # one row in 50: 2^17 larger a scale than it needs
+        x = of_v(s, pool, s.D)
+        loose = torch.from_numpy(rng.random(tuple(x.shape[:3])) < 0.02)
+        x[loose] = (x[loose].float().sign() * 2.0 ** -9).to(torch.float8_e4m3fn)
+        v[:] = np.where(loose.numpy()[..., None], 127, 104)
+    return pool, scales
+
+
+KINDS = ["spread of 40", "whole range", "lowest", "one byte", "loose"]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D,io,new,G", [(128, "bf16", 1, 8), (64, "fp16", 1, 4), (128, "fp16", 3, 5), (64, "bf16", 2, 8)])
+def test_scales_far_apart_few_rows(kind, D, io, new, G):
+    s = Shape(H=2, D=D, T=16, pool="e4m3", blocks=120, layers=1, layer=0)
+    rng = np.random.default_rng(25)
+    b = Batch(rng, s, [new] * 3, [200, 37, 1500])
+    pool, scales = spread_pool(rng, s, kind)
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2 * G, D)) * 2).to(DTYPE[io])
+    if kind == "whole range" and io == "fp16":
+        q = q.to(torch.float16)
+        of_v(s, scales, 1)[:] = rng.integers(0, 130, of_v(s, scales, 1).shape)     # results that fp16 can hold
+    check_scales(s, b, pool, scales, q, io, G)
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+@pytest.mark.parametrize("kv", [0, 1])
+def test_nan_scale_of_a_visible_row(new, kv):
+    """Scale byte 255: NaN for the heads that see the row; of V it leaves lse alone."""
+    s = Shape(H=2, D=64, T=16, pool="e4m3", blocks=40)
+    rng = np.random.default_rng(26)
+    b = Batch(rng, s, [new], [new + 200])
+    pool, scales = make_pool(rng, s)
+    scales[s.row(b.entry(s, 0, 77), kv, 0, 77 % 16)] = 255
+    q = torch.from_numpy(rng.normal(size=(new, 4, 64))).bfloat16().cuda()
+    out, lse = run(make_cache(s, pool, scales), make_batch(b), q)
+    assert torch.isnan(out[:, :2]).all() and torch.isfinite(out[:, 2:]).all()
+    assert torch.isnan(lse[:, :2]).all() == (kv == 0) and torch.isfinite(lse[:, 2:]).all()
+    if kv == 1:
+        assert torch.isfinite(lse).all()
