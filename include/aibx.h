@@ -575,15 +575,17 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  *   q, out: [n_tokens][num_q_heads][head_dim] of type q_type (BF16 or FP16, the pool's type unless
  *   the pool is E4M3) with element strides per token and head, 16-byte aligned rows; out must not
  *   overlap q.  d_lse (nullable): float [n_tokens][num_q_heads].
- *   Products are accumulated in fp32; the weights are rounded to q_type (to fp16 over an E4M3
- *   pool, whose queries are held as fp16 times a power of two per row) before they multiply V; sums
- *   and maxima of the softmax stay in fp32; the result is rounded once.  Two calls on the same
+ *   Products are accumulated in fp32; the weights are rounded to q_type (over an E4M3 pool, whose
+ *   queries are held as fp16 times a power of two per row, to fp16, or to 16 bits where scale bytes
+ *   of V lie more than 4 apart or outside 79..175) before they multiply V; sums and maxima of the
+ *   softmax stay in fp32; the result is rounded once.  Two calls on the same
  *   inputs give the same bits.
  *   What lies in slots that no visible position names (stale bytes, NaN) does not matter.  NaN or
  *   infinite K of a position hidden from a row does not reach it; a NaN or infinite V of a
  *   position that only some of a request's rows see may reach the others.  Over an E4M3 pool
- *   a cached element may be off by 2^-34 of the largest magnitude among its 128 positions, and V
- *   scales below 2^-100 may count as 2^-100 (an error below 2^-91).
+ *   an element of K may be off by 2^-16 of the largest scale 2^(s - 127) among its 128 positions; an
+ *   element of V below 2^-115 of it, and a key whose weight is below 2^-37 of the largest, may count
+ *   as 0.
  * Shapes: head_dim 64 or 128, block_tokens a multiple of 8, at most 128 query heads per KV head,
  *   num_blocks below 2^31, n_tokens below 2^24: UNSUPPORTED otherwise.  INVALID for
  *   unaligned q or out, out in the place of q, strides that are no multiple of 8 elements, a scale

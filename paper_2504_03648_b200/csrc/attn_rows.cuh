@@ -565,7 +565,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
           for (int e = 0; e < 4; ++e) c[x][e] += c2[x][e];
         // ---- scores in powers of two; over e4m3 with the V exponent of each key added
-        float unshift[2];                                   // 2^-b_j
+        float unshift[2] = {1.0f, 1.0f};                    // 2^-b_j
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float kf = 1.0f, vexp = 0.0f;

@@ -21,7 +21,7 @@
 // 2^(e - E), e its row's exponent and E the tile's largest, which is exact down to 2^-24 of the
 // tile's range; 2^E then joins the scale of the scores (K) or the exponent of the weights (V: m
 // covers S c + E, and l takes the sum of the weights times 2^-E).  Queries become fp16 scaled to
-// [1, 2) per row.
+// [1, 2) per row.  Tiles whose V scales are far apart become bf16 (see kScaleSpread).
 //
 // Bound: the tensor pipe (1024 cycles per KV tile and 128 rows at D = 128, both products) and the
 // special function unit (128 * 128 exponentials at 16 a cycle: 1024 cycles too), neither of them
@@ -410,9 +410,10 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   __shared__ __align__(8) unsigned long long s_kv_full[S::kBufs], s_kv_empty[S::kBufs];
   __shared__ __align__(8) unsigned long long s_raw_full[S::kBufs];
   __shared__ __align__(8) unsigned long long s_fac_full[S::kFactorRing], s_fac_empty[S::kFactorRing];
-  __shared__ __align__(8) unsigned long long s_q_full[2], s_s_full[2], s_h_full[2], s_p_full[2], s_o_full[2], s_turn[2];
+  __shared__ __align__(8) unsigned long long s_q_full[2], s_s_full[2], s_h_full[2], s_p_full[2], s_o_full[2], s_turn[2], s_w_full[2];
   __shared__ unsigned int s_mask[kInfoRing];
   __shared__ float s_kscale[kInfoRing], s_vexp[kInfoRing];
+  __shared__ int s_wide[kInfoRing];                        // whether the step's V is multiplied wide
   __shared__ long long s_scan[33];
   __shared__ WorkStart s_start;
   __shared__ TileWalk s_walk[S::kThreads / 32];
@@ -446,6 +447,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       mbar_init(smem_u32(&s_p_full[t]), 4u);
       mbar_init(smem_u32(&s_o_full[t]), 1u);
       mbar_init(smem_u32(&s_turn[t]), 1u);
+      mbar_init(smem_u32(&s_w_full[t]), 1u);
     }
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -495,7 +497,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     const unsigned int lanes = (unsigned int)(warp & 3) << 21;
     const unsigned int tm_s = tmem + lanes + t * 128;
     const unsigned int tm_o = tmem + lanes + 256 + t * D;
-    unsigned int s_phase = 0, o_phase = 0, step = 0;
+    unsigned int s_phase = 0, o_phase = 0, w_phase = 0, step = 0;
     while (walk.next_warp(a, per)) {
       const int rows_here = walk.rows(a) - t * kTileRows;   // rows of this tile (<= 0: none)
       const int steps = walk.t1 - walk.t0;
@@ -504,6 +506,15 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         continue;
       }
       const int row0 = walk.block * 2 * kTileRows + t * kTileRows;   // in the request's rows
+      if constexpr (F8) {                                  // O = 0: every product of a step adds to it
+        uint32_t zero[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) zero[e] = 0;
+#pragma unroll
+        for (int k = 0; k < D; k += 32) tmem_st32(tm_o + k, zero);
+        tmem_wait_st();
+        tmem_before();
+      }
       // ---- queries into shared memory
       {
         constexpr int kChunks = D / 8;                     // 16-byte pieces of a row
@@ -567,7 +578,9 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         const int key0 = key_first + j * kTileKeys;
         const unsigned int mask = s_mask[step % kInfoRing];
         float c = c0, shift = 0.0f;
+        bool spread = false;
         if constexpr (F8) {
+          spread = s_wide[step % kInfoRing];
           c = fmaxf(c * s_kscale[step % kInfoRing], 1.2e-38f);   // (0 would make NaN of a hidden key's -infinity)
           shift = s_vexp[step % kInfoRing];
         }
@@ -633,13 +646,14 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         raise_max(s + 64);
         const float mt = max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[3]) * c + shift;
         if (!(mt < INFINITY)) l = NAN;                     // a NaN or infinite score: so is the row's result
-        if (__any_sync(0xffffffffu, mt > m + 8.0f)) {
-          const float mn = fmaxf(m, mt);
+        constexpr float kHead = kWeightHead<MT>;
+        if (__any_sync(0xffffffffu, mt > m + (kHead + 8.0f))) {
+          const float mn = fmaxf(m, mt - kHead);
           const float al = mn == -INFINITY ? 1.0f : exp2_fast(m - mn);
           m = mn;
           l *= al;
           if (j > 0) {
-#pragma unroll
+#pragma unroll 1
             for (int k = 0; k < D; k += 32) {
               uint32_t o[32];
               tmem_ld32(tm_o + k, o);
@@ -658,13 +672,75 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           sum2 = 0;
           weights(s, pk);
         }
-        tmem_st32(tm_s, pk);
-        tmem_wait_st();
-        tmem_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_h_full[t]));   // the first half may be multiplied already
-        weights(s + 64, pk);
-        tmem_st32(tm_s + 32, pk);
+        if (F8 && spread) {
+          // Scales far apart: weights as two bf16 numbers, 16 columns of the first and 16 of the second in
+          // the place of 32 scores; V is bf16 already.  The product is issued here, and the MMA warp's
+          // own of this step adds zeros: it knows of nothing (with these 16 MMAs in its loop as well,
+          // taken or not, a 1,023-token chunk over 130k positions took 2,820 us; so 2,340, without any of
+          // this 2,305; with all steps wide 4,250).
+          sum2 = 0;
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            uint32_t two[32];
+            tmem_ld32(tm_s + 32 * q, s);
+            tmem_wait_ld();
+            if (hide) {
+              const uint32_t seen = q < 2 ? (q ? vis[1] : vis[0]) : (q > 2 ? vis[3] : vis[2]);
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (!(seen & (1u << k))) s[k] = 0xff800000u;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              float p0, p1;
+              split2(fma2(pair2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, off2), p0, p1);
+              p0 = exp2_fast(p0);
+              p1 = exp2_fast(p1);
+              sum2 = add2(sum2, pair2(p0, p1));
+              two[e >> 1] = Bits16<__nv_bfloat16>::pack(p0, p1);
+              const float2 y = Bits16<__nv_bfloat16>::unpack(two[e >> 1]);
+              two[16 + (e >> 1)] = Bits16<__nv_bfloat16>::pack(p0 - y.x, p1 - y.y);
+            }
+            tmem_st32(tm_s + 32 * q, two);
+          }
+          tmem_wait_st();
+          tmem_before();
+          asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
+          if ((warp & 3) == 0) {
+            constexpr unsigned int kPVWide = mma_desc(false, D, true);
+            const unsigned int vbuf = (2 * step + 1) % S::kBufs;
+            ring_wait(smem_u32(&s_kv_full[vbuf]), ((2 * step + 1) / S::kBufs) & 1u, abort_flag);
+            __syncwarp();
+            tmem_after();
+            const unsigned int low = operand_low(kv0 + vbuf * S::kBuf, S::kColBytes);
+#pragma unroll 1
+            for (int k = 0; k < 16; ++k)                   // per 32 keys: 2 x 16 of the first part, then of the second
+              mma_tmem(tmem + 256 + t * D, tmem + t * 128 + k * 8,
+                       operand_desc(low + ((k >> 2) * 2 + (k & 1)) * (2048 >> 4)), kPVWide, 1u, lane == 0);
+            mma_commit(smem_u32(&s_w_full[t]), lane == 0);
+          }
+          ring_wait(smem_u32(&s_w_full[t]), w_phase, abort_flag);
+          w_phase ^= 1u;
+          __syncwarp();
+          tmem_after();
+          // the MMA warp's own product of the step: zeros (V's bf16 bits are finite numbers as fp16, too)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) pk[e] = 0;
+          tmem_st32(tm_s, pk);
+          tmem_st32(tm_s + 32, pk);
+          tmem_wait_st();
+          tmem_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&s_h_full[t]));
+        } else {
+          tmem_st32(tm_s, pk);
+          tmem_wait_st();
+          tmem_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&s_h_full[t]));   // the first half may be multiplied already
+          weights(s + 64, pk);
+          tmem_st32(tm_s + 32, pk);
+        }
         float total, other;
         split2(sum2, total, other);
         total += other;
@@ -805,7 +881,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
             advance();
           }
-          const unsigned int low = v_low + vbuf * (S::kBuf >> 4), old = j > 0;
+          const unsigned int low = v_low + vbuf * (S::kBuf >> 4), old = F8 || j > 0;
           if (active) {
             ring_wait(smem_u32(&s_h_full[t]), p_phase, abort_flag);
             if (turns) {
@@ -898,6 +974,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       // chain table -> scale byte is long: it runs ahead.
       unsigned int step = 0;
       while (walk.next_warp(a, per)) {
+        int most = 0;                                      // largest V byte of the segment so far
         const uint32_t* row;
         long long entries;
         table_row(a.b, walk.r, row, entries);
@@ -933,21 +1010,35 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
             int top = 27;                                  // exponents from -100: 2^-E stays finite
+            uint32_t least = 271;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (((there >> i) & 1u) && byte[kv][i] != 255) top = max(top, byte[kv][i]);
+              if ((there >> i) & 1u) {
+                const int b = byte[kv][i];
+                if (b != 255) top = max(top, b);
+                least = min(least, b < kScaleLow || b > kScaleHigh ? 0u : (uint32_t)b + 16u);
+              }
             top = __reduce_max_sync(0xffffffffu, top);
+            bool wide = false;
+            if (kv == 1) {
+              wide = scales_wide(scale_facts(__reduce_min_sync(0xffffffffu, least), (uint32_t)top), most);
+              top = weight_byte(top);
+            }
             __half out[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               float x = byte[kv][i] == 255 ? NAN : exp2f((float)(byte[kv][i] - top));
               if (!((there >> i) & 1u)) x = 0.0f;
-              out[i] = __float2half(x);
+              out[i] = wide ? __ushort_as_half(__bfloat16_as_ushort(__float2bfloat16(x))) : __float2half(x);
             }
             *reinterpret_cast<uint2*>(factors + (f * 2 + kv) * kTileKeys + lane * 4) = *reinterpret_cast<uint2*>(out);
             if (lane == 0) {
-              if (kv == 0) s_kscale[step % kInfoRing] = power_of_byte(top);
-              else s_vexp[step % kInfoRing] = (float)(top - 127);
+              if (kv == 0) {
+                s_kscale[step % kInfoRing] = power_of_byte(top);
+              } else {
+                s_vexp[step % kInfoRing] = (float)(top - 127);
+                s_wide[step % kInfoRing] = wide;
+              }
             }
           }
           __syncwarp();
@@ -977,6 +1068,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(fac);
           else
             *reinterpret_cast<uint2*>(x) = *reinterpret_cast<const uint2*>(fac);
+          const bool wide = kv == 1 && s_wide[step % kInfoRing];
           bool gone = false;                               // rows that are not there, or too small to show
 #pragma unroll
           for (int u = 0; u < kRows; ++u) gone |= __half_as_ushort(x[u]) == 0;
@@ -985,38 +1077,50 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           unsigned char* out = base + 2 * S::kQ + buf * S::kBuf + (c >> 2) * S::kColBytes;
           const unsigned char* src = base + 2 * S::kQ + buf * S::kBuf + S::kColBytes;
           constexpr int kTurn = kRows / 2;
+          auto convert = [&](auto to_bf16) {
 #pragma unroll
-          for (int u0 = 0; u0 < kRows; u0 += kTurn) {
-            uint4 v[kTurn];
+            for (int u0 = 0; u0 < kRows; u0 += kTurn) {
+              uint4 v[kTurn];
 #pragma unroll
-            for (int u = 0; u < kTurn; ++u) {
-              const int i = i0 + u0 + u;
-              v[u] = *reinterpret_cast<const uint4*>(src + i * D + ((D == 128 ? c ^ (i & 7) : c) << 4));
-            }
-            if (gone) {
-#pragma unroll
-              for (int u = 0; u < kTurn; ++u)
-                if (__half_as_ushort(x[u0 + u]) == 0) v[u] = make_uint4(0, 0, 0, 0);
-            }
-            __syncwarp();
-#pragma unroll
-            for (int u = 0; u < kTurn; ++u) {
-              const int i = i0 + u0 + u;
-              const __half2 x2 = __half2half2(x[u0 + u]);
-              const uint32_t wv[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-              uint32_t o[8];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const __half2 lo = __hmul2(halves_of_e4m3(wv[e] & 0xffffu), x2);
-                const __half2 hi = __hmul2(halves_of_e4m3(wv[e] >> 16), x2);
-                o[2 * e] = *reinterpret_cast<const uint32_t*>(&lo);
-                o[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&hi);
+              for (int u = 0; u < kTurn; ++u) {
+                const int i = i0 + u0 + u;
+                v[u] = *reinterpret_cast<const uint4*>(src + i * D + ((D == 128 ? c ^ (i & 7) : c) << 4));
               }
-              const int p0 = (2 * c) & 7;
-              *reinterpret_cast<uint4*>(out + i * 128 + ((p0 ^ (i & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-              *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + 1) ^ (i & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+              if (gone) {
+#pragma unroll
+                for (int u = 0; u < kTurn; ++u)
+                  if (__half_as_ushort(x[u0 + u]) == 0) v[u] = make_uint4(0, 0, 0, 0);
+              }
+              __syncwarp();
+#pragma unroll
+              for (int u = 0; u < kTurn; ++u) {
+                const int i = i0 + u0 + u;
+                const uint32_t wv[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+                uint32_t o[8];
+                if constexpr (decltype(to_bf16)::value) {    // the factor is one already
+                  const float xf = __uint_as_float((uint32_t)__half_as_ushort(x[u0 + u]) << 16);
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) o[e] = bf16_of_e4m3((wv[e >> 1] >> (16 * (e & 1))) & 0xffffu, xf, xf);
+                } else {
+                  const __half2 x2 = __half2half2(x[u0 + u]);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    const __half2 lo = __hmul2(halves_of_e4m3(wv[e] & 0xffffu), x2);
+                    const __half2 hi = __hmul2(halves_of_e4m3(wv[e] >> 16), x2);
+                    o[2 * e] = *reinterpret_cast<const uint32_t*>(&lo);
+                    o[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&hi);
+                  }
+                }
+                const int p0 = (2 * c) & 7;
+                *reinterpret_cast<uint4*>(out + i * 128 + ((p0 ^ (i & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + 1) ^ (i & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+              }
             }
-          }
+          };
+          if (wide)
+            convert(std::true_type());
+          else
+            convert(std::false_type());
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           mbar_arrive(smem_u32(&s_kv_full[buf]));
           if (++buf == S::kBufs) {

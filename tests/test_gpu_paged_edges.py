@@ -221,7 +221,6 @@ def test_scales_far_apart_few_rows(kind, D, io, new, G):
     pool, scales = spread_pool(rng, s, kind)
     q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2 * G, D)) * 2).to(DTYPE[io])
     if kind == "whole range" and io == "fp16":
-        q = q.to(torch.float16)
         of_v(s, scales, 1)[:] = rng.integers(0, 130, of_v(s, scales, 1).shape)     # results that fp16 can hold
     check_scales(s, b, pool, scales, q, io, G)
 
@@ -241,3 +240,41 @@ def test_nan_scale_of_a_visible_row(new, kv):
     assert torch.isnan(lse[:, :2]).all() == (kv == 0) and torch.isfinite(lse[:, 2:]).all()
     if kv == 1:
         assert torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("size", [3.0, 1.0, 0.1, 0.01, 0.001, 1e-5])
+@pytest.mark.parametrize("lead", [3.0, 6.0, 8.0, 14.0])
+@pytest.mark.parametrize("where", list(WHERE))
+def test_a_leading_row_of_zeros_chunks(size, lead, where):
+    for D, io, new, G in ((128, "bf16", 40, 3), (64, "fp16", 150, 1), (128, "fp16", 9, 40)):
+        s = Shape(H=2, D=D, T=16, pool="e4m3", blocks=340, layers=1, layer=0)
+        rng = np.random.default_rng(27)
+        b = Batch(rng, s, [new, new], [1000, 4003])
+        q = near_ones(rng, b.n_tokens, 2 * G, D, io)
+        pool, scales = null_key_pool(rng, s, b, q, lead, size, WHERE[where], G)
+        check_scales(s, b, pool, scales, q, io, G)
+
+
+@pytest.mark.parametrize("size", [1.0, 0.1, 0.001])
+@pytest.mark.parametrize("new", [1, 30])
+def test_a_leading_row_of_zeros_in_a_long_context(size, new):
+    """One key of V = 0 that leads 130,000 others by a factor of 10^5, in the first tile of the line."""
+    s = Shape(H=1, D=64, T=64, pool="e4m3", blocks=2050, layers=1, layer=0)
+    rng = np.random.default_rng(28)
+    b = Batch(rng, s, [new], [130001])
+    q = near_ones(rng, new, 2, 64, "fp16")
+    pool, scales = null_key_pool(rng, s, b, q, 11.5, size, WHERE["first"], 2)
+    check_scales(s, b, pool, scales, q, "fp16", 2)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D,io,new,G", [(128, "bf16", 40, 3), (64, "fp16", 150, 1), (128, "fp16", 5, 100), (64, "bf16", 300, 1)])
+def test_scales_far_apart_chunks(kind, D, io, new, G):
+    s = Shape(H=2, D=D, T=16, pool="e4m3", blocks=160, layers=1, layer=0)
+    rng = np.random.default_rng(29)
+    b = Batch(rng, s, [new] * 3, [new + 160, new, 1500])
+    pool, scales = spread_pool(rng, s, kind)
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2 * G, D)) * 2).to(DTYPE[io])
+    if kind == "whole range" and io == "fp16":
+        of_v(s, scales, 1)[:] = rng.integers(0, 130, of_v(s, scales, 1).shape)     # results that fp16 can hold
+    check_scales(s, b, pool, scales, q, io, G)
