@@ -583,9 +583,8 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  *   What lies in slots that no visible position names (stale bytes, NaN) does not matter.  NaN or
  *   infinite K of a position hidden from a row does not reach it; a NaN or infinite V of a
  *   position that only some of a request's rows see may reach the others.  Over an E4M3 pool
- *   an element of K may be off by 2^-16 of the largest scale 2^(s - 127) among its 128 positions; an
- *   element of V below 2^-115 of it, and a key whose weight is below 2^-37 of the largest, may count
- *   as 0.
+ *   an element of V below 2^-115 of the largest scale 2^(s - 127) among its 128 positions, and a key
+ *   whose weight is below 2^-37 of the largest, may count as 0.
  * Shapes: head_dim 64 or 128, block_tokens a multiple of 8, at most 128 query heads per KV head,
  *   num_blocks below 2^31, n_tokens below 2^24: UNSUPPORTED otherwise.  INVALID for
  *   unaligned q or out, out in the place of q, strides that are no multiple of 8 elements, a scale

@@ -18,10 +18,11 @@
 // S(j + 1) is therefore also seeing O(j), and no further barrier guards O.
 //
 // Over an e4m3 pool a warpgroup more turns each raw tile into fp16 as it arrives: element times
-// 2^(e - E), e its row's exponent and E the tile's largest, which is exact down to 2^-24 of the
-// tile's range; 2^E then joins the scale of the scores (K) or the exponent of the weights (V: m
-// covers S c + E, and l takes the sum of the weights times 2^-E).  Queries become fp16 scaled to
-// [1, 2) per row.  Tiles whose V scales are far apart become bf16 (see kScaleSpread).
+// 2^(e - E), e its row's exponent and E the tile's largest; 2^E then joins the scale of the scores (K) or
+// the exponent of the weights (V: m covers S c + E, and l takes the sum of the weights times 2^-E).
+// That is exact while the tile's exponents are close together.  Steps where they are far apart (see
+// kKeySpread, kScaleSpread) leave K without its scales, which the softmax applies score by score, and
+// turn V into bf16.  Queries become fp16 scaled to [1, 2) per row.
 //
 // Bound: the tensor pipe (1024 cycles per KV tile and 128 rows at D = 128, both products) and the
 // special function unit (128 * 128 exponentials at 16 a cycle: 1024 cycles too), neither of them
@@ -37,6 +38,7 @@ namespace aibx {
 
 constexpr int kTileRows = 128;
 constexpr int kTileKeys = 128;
+constexpr int kKeySpread = 14;       // of K's bytes in a tile: times 2^-14, fp16's least normal number, e4m3 is exact
 constexpr int kInfoRing = 16;        // per-step facts the softmax reads: far deeper than the rings
 
 template <int D, bool F8>
@@ -413,7 +415,9 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   __shared__ __align__(8) unsigned long long s_q_full[2], s_s_full[2], s_h_full[2], s_p_full[2], s_o_full[2], s_turn[2], s_w_full[2];
   __shared__ unsigned int s_mask[kInfoRing];
   __shared__ float s_kscale[kInfoRing], s_vexp[kInfoRing];
-  __shared__ int s_wide[kInfoRing];                        // whether the step's V is multiplied wide
+  __shared__ int s_wide[kInfoRing];                        // whether the step's scales are far apart, and if so
+  __shared__ float s_wide_vexp[kInfoRing];                 // V's exponent and K's bytes
+  __shared__ __align__(4) unsigned char s_kbytes[F8 ? kInfoRing : 1][kTileKeys];
   __shared__ long long s_scan[33];
   __shared__ WorkStart s_start;
   __shared__ TileWalk s_walk[S::kThreads / 32];
@@ -673,36 +677,65 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           weights(s, pk);
         }
         if (F8 && spread) {
-          // Scales far apart: weights as two bf16 numbers, 16 columns of the first and 16 of the second in
-          // the place of 32 scores; V is bf16 already.  The product is issued here, and the MMA warp's
-          // own of this step adds zeros: it knows of nothing (with these 16 MMAs in its loop as well,
-          // taken or not, a 1,023-token chunk over 130k positions took 2,820 us; so 2,340, without any of
-          // this 2,305; with all steps wide 4,250).
-          sum2 = 0;
+          // Scales far apart.  Up to here the step had V exponent -infinity: no weights, no new maximum.
+          // K is there without its scales, so every score takes its own; V is bf16, and weights are two
+          // bf16 numbers, 16 columns of the first and 16 of the second in the place of 32 scores.  The
+          // product is issued here, and the MMA warp's own of this step adds zeros: it knows of nothing
+          // (with these 16 MMAs in its loop as well, taken or not, a 1,023-token chunk over 130k
+          // positions took 2,820 us instead of 2,315; with every step like this 5,710).
+          const float vexp = s_wide_vexp[step % kInfoRing];
+          const unsigned char* bytes = s_kbytes[step % kInfoRing];
+          float most = -INFINITY;
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            tmem_ld32(tm_s + 32 * q, s);
+            tmem_wait_ld();
+            const uint32_t seen = !hide ? 0xffffffffu : q < 2 ? (q ? vis[1] : vis[0]) : (q > 2 ? vis[3] : vis[2]);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              const float z = __uint_as_float(s[k]) * power_of_byte(bytes[32 * q + k]);
+              s[k] = seen & (1u << k) ? __float_as_uint(z) : 0xff800000u;
+            }
+#pragma unroll
+            for (int k = 0; k < 32; k += 2) most = max3(most, __uint_as_float(s[k]), __uint_as_float(s[k + 1]));
+            tmem_st32(tm_s + 32 * q, s);
+          }
+          tmem_wait_st();
+          const float cw = fmaxf(c0, 1.2e-38f), mw = most * cw + vexp;
+          if (!(mw < INFINITY)) l = NAN;
+          if (__any_sync(0xffffffffu, mw > m + (kHead + 8.0f))) {
+            const float mn = fmaxf(m, mw - kHead);
+            const float al = mn == -INFINITY ? 1.0f : exp2_fast(m - mn);
+            m = mn;
+            l *= al;
+#pragma unroll 1
+            for (int k = 0; k < D; k += 32) {
+              tmem_ld32(tm_o + k, s);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) * al);
+              tmem_st32(tm_o + k, s);
+            }
+          }
+          const float below = vexp - (m == -INFINITY ? 0.0f : m);
+          float total = 0.0f;
 #pragma unroll 1
           for (int q = 0; q < 4; ++q) {
             uint32_t two[32];
             tmem_ld32(tm_s + 32 * q, s);
             tmem_wait_ld();
-            if (hide) {
-              const uint32_t seen = q < 2 ? (q ? vis[1] : vis[0]) : (q > 2 ? vis[3] : vis[2]);
-#pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (!(seen & (1u << k))) s[k] = 0xff800000u;
-            }
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-              float p0, p1;
-              split2(fma2(pair2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, off2), p0, p1);
-              p0 = exp2_fast(p0);
-              p1 = exp2_fast(p1);
-              sum2 = add2(sum2, pair2(p0, p1));
+              const float p0 = exp2_fast(fmaf(__uint_as_float(s[e]), cw, below));
+              const float p1 = exp2_fast(fmaf(__uint_as_float(s[e + 1]), cw, below));
+              total += p0 + p1;
               two[e >> 1] = Bits16<__nv_bfloat16>::pack(p0, p1);
               const float2 y = Bits16<__nv_bfloat16>::unpack(two[e >> 1]);
               two[16 + (e >> 1)] = Bits16<__nv_bfloat16>::pack(p0 - y.x, p1 - y.y);
             }
             tmem_st32(tm_s + 32 * q, two);
           }
+          l += total * power_of_byte(127 - (int)vexp);
           tmem_wait_st();
           tmem_before();
           asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
@@ -740,11 +773,11 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           if (lane == 0) mbar_arrive(smem_u32(&s_h_full[t]));   // the first half may be multiplied already
           weights(s + 64, pk);
           tmem_st32(tm_s + 32, pk);
+          float total, other;
+          split2(sum2, total, other);
+          total += other;
+          l += F8 ? total * power_of_byte(127 - (int)shift) : total;   // (2^-127 too: no flushing here)
         }
-        float total, other;
-        split2(sum2, total, other);
-        total += other;
-        l += F8 ? total * power_of_byte(127 - (int)shift) : total;   // (2^-127 too: no flushing here)
         tmem_wait_st();
         tmem_before();
         __syncwarp();
@@ -1007,39 +1040,54 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           const unsigned int f = step % S::kFactorRing;
           ring_wait(smem_u32(&s_fac_empty[f]), ((step / S::kFactorRing) & 1u) ^ 1u, abort_flag);
           __syncwarp();
+          // Bytes at most 14 (K, in the tile) or 4 (V, in the segment so far) below the largest: every
+          // factor is a power of two that bits make.
+          int top[2];
+          bool far = false;
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
-            int top = 27;                                  // exponents from -100: 2^-E stays finite
-            uint32_t least = 271;
+            top[kv] = 27;                                  // exponents from -100: 2^-E stays finite
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if ((there >> i) & 1u) {
-                const int b = byte[kv][i];
-                if (b != 255) top = max(top, b);
-                least = min(least, b < kScaleLow || b > kScaleHigh ? 0u : (uint32_t)b + 16u);
+              if (((there >> i) & 1u) && byte[kv][i] != 255) top[kv] = max(top[kv], byte[kv][i]);
+            top[kv] = __reduce_max_sync(0xffffffffu, top[kv]);
+          }
+          most = max(most, top[1]);
+          const int low[2] = {top[0] - kKeySpread, max(most - kScaleSpread, kScaleLow)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            far |= ((there >> i) & 1u) && (byte[0][i] < low[0] || byte[1][i] < low[1] || byte[1][i] > kScaleHigh);
+          const bool wide = __any_sync(0xffffffffu, far) || most > kScaleHigh;
+          uint32_t out[2][4];                              // 16 bits each
+          if (!wide) {
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                out[kv][i] = byte[kv][i] == 255 ? 0x7e00u : 0x3c00u - 1024u * (uint32_t)(top[kv] - byte[kv][i]);
+                if (!((there >> i) & 1u)) out[kv][i] = 0;
               }
-            top = __reduce_max_sync(0xffffffffu, top);
-            bool wide = false;
-            if (kv == 1) {
-              wide = scales_wide(scale_facts(__reduce_min_sync(0xffffffffu, least), (uint32_t)top), most);
-              top = weight_byte(top);
-            }
-            __half out[4];
+          } else {                                         // K's rows as they are, V as bf16
+            uint32_t packed = 0x7f7f7f7fu;
+            top[1] = weight_byte(top[1]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              float x = byte[kv][i] == 255 ? NAN : exp2f((float)(byte[kv][i] - top));
-              if (!((there >> i) & 1u)) x = 0.0f;
-              out[i] = wide ? __ushort_as_half(__bfloat16_as_ushort(__float2bfloat16(x))) : __float2half(x);
+              const bool on = (there >> i) & 1u;
+              out[0][i] = !on ? 0 : byte[0][i] == 255 ? 0x7e00u : 0x3c00u;
+              out[1][i] = !on ? 0 : byte[1][i] == 255 ? 0x7fc0u : (uint32_t)max(127 + byte[1][i] - top[1], 0) << 7;
+              if (out[0][i] == 0x3c00u) packed ^= (uint32_t)(byte[0][i] ^ 0x7f) << (8 * i);
             }
-            *reinterpret_cast<uint2*>(factors + (f * 2 + kv) * kTileKeys + lane * 4) = *reinterpret_cast<uint2*>(out);
-            if (lane == 0) {
-              if (kv == 0) {
-                s_kscale[step % kInfoRing] = power_of_byte(top);
-              } else {
-                s_vexp[step % kInfoRing] = (float)(top - 127);
-                s_wide[step % kInfoRing] = wide;
-              }
-            }
+            *reinterpret_cast<uint32_t*>(&s_kbytes[step % kInfoRing][lane * 4]) = packed;
+            if (lane == 0) s_wide_vexp[step % kInfoRing] = (float)(top[1] - 127);
+          }
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv)
+            *reinterpret_cast<uint2*>(factors + (f * 2 + kv) * kTileKeys + lane * 4) =
+                make_uint2(out[kv][0] | out[kv][1] << 16, out[kv][2] | out[kv][3] << 16);
+          if (lane == 0) {
+            s_kscale[step % kInfoRing] = power_of_byte(top[0]);
+            s_vexp[step % kInfoRing] = wide ? -INFINITY : (float)(top[1] - 127);
+            s_wide[step % kInfoRing] = wide;
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&s_fac_full[f]));

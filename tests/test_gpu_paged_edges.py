@@ -278,3 +278,66 @@ def test_scales_far_apart_chunks(kind, D, io, new, G):
     if kind == "whole range" and io == "fp16":
         of_v(s, scales, 1)[:] = rng.integers(0, 130, of_v(s, scales, 1).shape)     # results that fp16 can hold
     check_scales(s, b, pool, scales, q, io, G)
+
+
+def of_k(s, x, per_row):
+    return x.reshape(s.blocks, s.layers, 2, s.H * s.T, per_row)[:, :, 0]
+
+
+def key_tolerance(values, rows_k, rows_v, q, scale, first):
+    """As definition(), with the error of every score on its own: products and sums of that key's D
+    terms, and queries within 2^-25 of their row's largest element."""
+    k, v = values[rows_k], values[rows_v]
+    z = scale * np.einsum("ngd,kd->ngk", q, k)
+    z[np.broadcast_to(np.arange(len(k))[None, None] > first + np.arange(len(q))[:, None, None], z.shape)] = -np.inf
+    m = z.max(-1, keepdims=True)
+    w = np.exp(z - m)
+    w /= w.sum(-1, keepdims=True)
+    err = scale * ((q.shape[-1] + 4) * 2.0 ** -24 * np.einsum("ngd,kd->ngk", np.abs(q), np.abs(k))
+                   + 2.0 ** -25 * np.abs(q).max(-1, keepdims=True) * np.where(q == 0, 0, 1).max(-1, keepdims=True)
+                   * np.einsum("ngd,kd->ngk", np.where(q == 0, 0.0, 1.0), np.abs(k))) + 2.0 ** -22 * np.abs(m)
+    mag = w @ np.abs(v)
+    out = w @ v
+    # e^err - 1 <= 2 err for what moves a weight, once in it and once, on average, in the sum
+    moved = (w * err) @ np.abs(v) + (w * err).sum(-1, keepdims=True) * np.abs(out)
+    return 2 * moved + (2.0 ** -11 + 2.0 ** -20) * mag + 2.0 ** -28 * w.max(-1, keepdims=True) * np.abs(v).sum(0)
+
+
+@pytest.mark.parametrize("kind", ["a zero row with a large byte", "large rows beside the query", "rows 2^30 below"])
+@pytest.mark.parametrize("D,io,new,G", [(128, "bf16", 40, 3), (64, "fp16", 150, 1), (128, "fp16", 1, 8), (64, "bf16", 300, 1)])
+def test_key_scales_far_apart(kind, D, io, new, G):
+    """K rows whose scales say nothing about their scores must not take bits from the others."""
+    s = Shape(H=2, D=D, T=16, pool="e4m3", blocks=160, layers=1, layer=0)
+    rng = np.random.default_rng(31)
+    b = Batch(rng, s, [new] * 2, [new + 160, 1500])
+    pool, scales = make_pool(rng, s)
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2 * G, D)) * 2).to(DTYPE[io])
+    q[..., D // 2:] = 0
+    k, kb = of_k(s, pool, D), of_k(s, scales, 1)
+    odd = rng.random(kb.shape[:3]) < 0.05
+    if kind == "a zero row with a large byte":
+        k.view(torch.uint8)[torch.from_numpy(odd)] = 0
+        kb[odd] = 200
+    elif kind == "large rows beside the query":
+        x = k[torch.from_numpy(odd)].float()
+        x[:, :D // 2] = 0                                       # scores of 0
+        k[torch.from_numpy(odd)] = x.to(torch.float8_e4m3fn)
+        kb[odd] = 150
+    else:                                                       # scores of about 0, in the place of 0
+        kb[odd] = 90
+    cache, batch = make_cache(s, pool, scales), make_batch(b)
+    out, lse = run(cache, batch, q.cuda())
+    values = pool_values(s, pool, scales)
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for r, n in enumerate(b.new):
+        L, o = b.length[r], int(b.tok_off[r])
+        for h in range(2):
+            rows = [np.array([s.row(b.entry(s, r, p), kv, h, p % s.T) for p in range(L)]) for kv in range(2)]
+            heads = slice(h * G, h * G + G)
+            qq = q[o:o + n, heads].double().numpy()
+            want, wl, _, _ = definition(values, *rows, qq, s.D ** -0.5, L - n)
+            tol = key_tolerance(values, *rows, qq, s.D ** -0.5, L - n) + HALF_STEP[io] * np.abs(want)
+            err = np.abs(out[o:o + n, heads] - want)
+            assert (err <= tol).all(), (r, h, float((err / tol).max()), float(err.max() / np.abs(want).max()))
+            assert (np.abs(lse[o:o + n, heads] - wl) <= 2.0 ** -12).all()
+    assert aibx.status_fetch() == (0, 0)
