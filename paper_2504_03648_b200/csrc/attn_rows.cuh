@@ -95,7 +95,7 @@ __device__ __forceinline__ RowSpan row_span(const AttnArgs& a, const AttnRequest
   const long long lo = a.window > 0 ? (long long)q.len - q.n - a.window + 1 : 0;
   s.lo = lo < 0 ? 0 : lo > s.hi ? s.hi : (int)lo;
   s.tile0 = s.lo / TOK;
-  s.tiles = max(1, (s.hi + TOK - 1) / TOK - s.tile0);
+  s.tiles = max(1, (int)(((unsigned int)s.hi + TOK - 1) / TOK) - s.tile0);   // (hi may be 2^31 - 1)
   return s;
 }
 
@@ -486,7 +486,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         const int key0 = tile_key0 + task * 16;
         const int b0 = (task * 16) >> a.box_log;
         // all 16 keys there, and seen by all rows
-        const bool open = boxmask == all_boxes && key0 >= open_lo && key0 + 16 <= open_hi;
+        const bool open = boxmask == all_boxes && key0 >= open_lo && key0 <= open_hi - 16;
         if (!open) {
           const int b1 = (task * 16 + 15) >> a.box_log;
           const unsigned int want = ((2u << (b1 - b0)) - 1u) << b0;

@@ -184,7 +184,7 @@ __device__ __forceinline__ TileSpan tile_span(const AttnArgs& a, const AttnReque
   s.hi = (int)hi;
   s.lo = (int)lo;
   s.tile0 = s.lo / kTileKeys;
-  s.tiles = max(1, (s.hi + kTileKeys - 1) / kTileKeys - s.tile0);
+  s.tiles = max(1, (int)(((unsigned int)s.hi + kTileKeys - 1) / kTileKeys) - s.tile0);
   return s;
 }
 
@@ -969,8 +969,8 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           ids.step_slot();
           // a box that is not there, or that holds no visible key, comes as zeros from beyond the pool
           const int block = valid ? (int)id : (int)a.pool.num_blocks;
-          const int tok = (tile0 + j) * kTileKeys + lane * a.box;
-          const bool missing = lane < boxes && tok < hi && tok + a.box > lo && !valid;
+          const int tok = (tile0 + j) * kTileKeys + (lane & (boxes - 1)) * a.box;
+          const bool missing = lane < boxes && tok < hi && tok > lo - a.box && !valid;
           const unsigned int gone = __ballot_sync(0xffffffffu, missing);
           if (lane == 0) s_mask[step % kInfoRing] = ~gone;
           for (int kv = 0; kv < 2; ++kv) {

@@ -341,3 +341,80 @@ def test_key_scales_far_apart(kind, D, io, new, G):
             assert (err <= tol).all(), (r, h, float((err / tol).max()), float(err.max() / np.abs(want).max()))
             assert (np.abs(lse[o:o + n, heads] - wl) <= 2.0 ** -12).all()
     assert aibx.status_fetch() == (0, 0)
+
+
+# ------------------------------------------------------------------------------------------
+# positions at the end of their range
+
+@pytest.mark.parametrize("pool,io", POOLS)
+@pytest.mark.parametrize("new", [1, 70])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("back", [0, 1, 40])
+def test_positions_up_to_the_last_of_31_bits(pool, io, new, D, back):
+    """A sequence of 2^31 - 1 tokens (or a few less) seen through a window: written, read back, attended
+    to, with a missing block among the last ones."""
+    T, L, n, window, G = 8, 2 ** 31 - 1 - back, 1000, 600, 4
+    s = Shape(H=1, D=D, T=T, pool=pool, blocks=140, layers=1, layer=0)
+    rng = np.random.default_rng(32)
+    p, sc = make_pool(rng, s)
+    cache = make_cache(s, p, sc)
+    entries = -(-L // T)
+    used = 130                                                  # blocks of the last positions
+    table = torch.full((1, entries), -1, dtype=torch.int32, device="cuda")
+    ids = rng.permutation(s.blocks)[:used].astype(np.int32)
+    table[0, entries - used:] = dev(ids)
+    k, v = (torch.from_numpy(rng.normal(size=(n, 1, D))).to(DTYPE[io]).cuda() for _ in range(2))
+
+    def batch(m):
+        return aibx.KVBatch(table.view(torch.uint32), dev(np.array([0, m], dtype=np.int64)),
+                            dev(np.array([L], dtype=np.int32)), m, max_new=m)
+
+    aibx.kv_append(cache, batch(n), k, v)
+    back_k, back_v = torch.empty_like(k, dtype=torch.float32), torch.empty_like(v, dtype=torch.float32)
+    aibx.kv_read(cache, batch(n), back_k, back_v)
+    if pool != "e4m3":
+        assert torch.equal(back_k, k.float()) and torch.equal(back_v, v.float())
+    hole = entries - 1 if back == 40 else entries - 2           # not the only block of the last row
+    table[0, hole] = -1
+    q = torch.from_numpy(rng.normal(size=(new, G, D)) * 2).to(DTYPE[io])
+    out, lse = run(cache, batch(new), q.cuda(), window=window)
+    assert aibx.status_fetch() == (0, 0)
+    pos = np.arange(L - n, L)
+    kk, vv = (x.double().cpu().numpy()[:, 0] for x in (back_k, back_v))
+    row = np.arange(L - new, L)[:, None, None]
+    seen = (pos <= row) & (pos > row - window) & (pos // T != hole)
+    z = np.where(seen, D ** -0.5 * np.einsum("ngd,kd->ngk", q.double().numpy(), kk), -np.inf)
+    m = z.max(-1, keepdims=True)
+    w = np.exp(z - m)
+    t = w.sum(-1, keepdims=True)
+    w /= t
+    want, wl, mag = w @ vv, (m + np.log(t))[..., 0], w @ np.abs(vv)
+    slack = D ** -0.5 * (D + 4) * 2.0 ** -24 * np.abs(kk).max() * np.abs(q.double().numpy()).sum(-1) + 2.0 ** -22 * np.abs(m[..., 0])
+    # weights rounded to the operands' type (fp16 below 2^-14 of the largest: 2^-25 of it), scores, the result
+    tol = (HALF_STEP["fp16" if pool == "e4m3" else io] + 2 * slack[..., None] + 2.0 ** -20) * mag \
+        + 2.0 ** -25 * w.max(-1, keepdims=True) * np.abs(vv).sum(0) + HALF_STEP[io] * np.abs(want)
+    assert (np.abs(out.double().cpu().numpy() - want) <= tol).all()
+    assert (np.abs(lse.double().cpu().numpy() - wl) <= slack + 2.0 ** -14 + 2.0 ** -22 * np.abs(wl)).all()
+
+
+def test_every_position_of_31_bits_is_counted():
+    """No window: 2^31 - 1 positions that all hold one of two rows."""
+    T, L = 65536, 2 ** 31 - 1
+    s = Shape(H=1, D=64, T=T, pool="bf16", blocks=2, layers=1, layer=0)
+    pool = torch.zeros(s.rows, 64, dtype=torch.bfloat16)
+    for kv in range(2):
+        for blk in range(2):
+            at = s.row(blk, kv, 0, 0)
+            pool[at:at + T] = float(blk) if kv else 0.0         # equal scores, V = 0 or 1
+    cache = make_cache(s, pool, None)
+    table = torch.zeros(1, L // T + 1, dtype=torch.int32, device="cuda")
+    table[0, 3::4] = 1                                          # a quarter of the positions
+    for new in (1, 20):
+        batch = aibx.KVBatch(table.view(torch.uint32), dev(np.array([0, new], dtype=np.int64)),
+                             dev(np.array([L], dtype=np.int32)), new, max_new=new)
+        q = torch.ones(new, 2, 64, dtype=torch.bfloat16, device="cuda")
+        out, lse = run(cache, batch, q)
+        # a sum of 2^31 ones: fp32 sums of 2^7 per step and thread, a few thousand steps, 148 pieces
+        assert ((out.float() - 0.25).abs() <= 2.0 ** -8).all()
+        assert ((lse - 31 * np.log(2.0)).abs() <= 2.0 ** -8).all()
+    assert aibx.status_fetch() == (0, 0)
