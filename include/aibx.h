@@ -588,7 +588,7 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  * Shapes: head_dim 64 or 128, block_tokens a multiple of 8, at most 128 query heads per KV head,
  *   num_blocks below 2^31, n_tokens below 2^24: UNSUPPORTED otherwise.  INVALID for
  *   unaligned q or out, out in the place of q, strides that are no multiple of 8 elements, a scale
- *   that is not positive and finite, num_q_heads no multiple of num_kv_heads, a window < 0, a
+ *   that is not positive, normal and at most 2^127, num_q_heads no multiple of num_kv_heads, a window < 0, a
  *   workspace that is too small.
  * Workspace: aibx_attn_workspace_bytes(cache, batch, params) bytes, 16-byte aligned, content
  *   irrelevant before and after; calls that may overlap on the GPU need separate ones.

@@ -21,6 +21,8 @@ struct SmallDivisor {
 };
 inline SmallDivisor small_divisor(int d) { return SmallDivisor{((1ull << 40) + d - 1) / d}; }
 
+constexpr float kLog2E = 1.4426950408889634f;
+
 struct AttnArgs {
   PagedPool pool;
   PagedBatch b;

@@ -1,6 +1,7 @@
 // Host side of attn_paged: checks, the choice of kernels and the workspace.
 #pragma once
 
+#include <float.h>
 #include <math.h>
 
 #include "attn_tiles.cuh"
@@ -33,8 +34,10 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
   if (!p) return AIBX_ERR_INVALID;
   const aibx_kv_layout_t& L = c->layout;
   if (p->q_type != AIBX_TYPE_BF16 && p->q_type != AIBX_TYPE_FP16) return AIBX_ERR_INVALID;
+  // the scale times log2 e is a normal fp32 number: infinite it would make NaN of a score of 0, below
+  // 2^-126 the kernels take it for 2^-126
   if (p->num_q_heads <= 0 || p->num_q_heads % L.num_kv_heads != 0 || p->window < 0 ||
-      !(p->scale > 0.0f) || !isfinite(p->scale))
+      !(p->scale >= FLT_MIN) || !isfinite(p->scale * kLog2E))
     return AIBX_ERR_INVALID;
   const long long strides[4] = {p->q_token_stride, p->q_head_stride, p->out_token_stride,
                                 p->out_head_stride};

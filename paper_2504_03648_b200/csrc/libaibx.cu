@@ -927,7 +927,7 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
   a.q_head = params->q_head_stride;
   a.o_tok = params->out_token_stride;
   a.o_head = params->out_head_stride;
-  a.scale_log2 = fmaxf(params->scale * 1.4426950408889634f, 1.2e-38f);   // never 0: hidden keys are -infinity
+  a.scale_log2 = params->scale * kLog2E;   // never 0: hidden keys are -infinity
   a.G = plan.G;
   a.by_g = small_divisor(plan.G);
   a.causal = params->causal != 0;
