@@ -1057,7 +1057,8 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             far |= ((there >> i) & 1u) && (byte[0][i] < low[0] || byte[1][i] < low[1] || byte[1][i] > kScaleHigh);
-          const bool wide = __any_sync(0xffffffffu, far) || most > kScaleHigh;
+          // (K's largest too: the scale of the scores has to stay finite)
+          const bool wide = __any_sync(0xffffffffu, far) || most > kScaleHigh || top[0] > kScaleHigh;
           uint32_t out[2][4];                              // 16 bits each
           if (!wide) {
 #pragma unroll
@@ -1085,7 +1086,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             *reinterpret_cast<uint2*>(factors + (f * 2 + kv) * kTileKeys + lane * 4) =
                 make_uint2(out[kv][0] | out[kv][1] << 16, out[kv][2] | out[kv][3] << 16);
           if (lane == 0) {
-            s_kscale[step % kInfoRing] = power_of_byte(top[0]);
+            s_kscale[step % kInfoRing] = wide ? 1.0f : power_of_byte(top[0]);
             s_vexp[step % kInfoRing] = wide ? -INFINITY : (float)(top[1] - 127);
             s_wide[step % kInfoRing] = wide;
           }

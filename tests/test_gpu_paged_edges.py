@@ -418,3 +418,29 @@ def test_every_position_of_31_bits_is_counted():
         assert ((out.float() - 0.25).abs() <= 2.0 ** -8).all()
         assert ((lse - 31 * np.log(2.0)).abs() <= 2.0 ** -8).all()
     assert aibx.status_fetch() == (0, 0)
+
+
+@pytest.mark.parametrize("every", [1, 20])
+@pytest.mark.parametrize("D,io,new,G", [(128, "bf16", 40, 3), (64, "fp16", 150, 1), (128, "fp16", 1, 8)])
+def test_zero_keys_at_the_largest_scale(every, D, io, new, G):
+    """K rows of zeros with byte 254 have scores of 0, whatever the queries are."""
+    s = Shape(H=2, D=D, T=16, pool="e4m3", blocks=40, layers=1, layer=0)
+    rng = np.random.default_rng(33)
+    b = Batch(rng, s, [new], [new + 300])
+    pool, scales = make_pool(rng, s)
+    k, kb = of_k(s, pool, D).view(torch.uint8), of_k(s, scales, 1)
+    k[:, :, ::every] = 0
+    kb[:, :, ::every] = 254
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2 * G, D)) * (50 if every == 1 else 2)).to(DTYPE[io])
+    cache, batch = make_cache(s, pool, scales), make_batch(b)
+    out, lse = run(cache, batch, q.cuda())
+    values = pool_values(s, pool, scales)
+    for h in range(2):
+        rows = [np.array([s.row(b.entry(s, 0, p), kv, h, p % s.T) for p in range(new + 300)]) for kv in range(2)]
+        heads = slice(h * G, h * G + G)
+        qq = q[:, heads].double().numpy()
+        want, wl, _, _ = definition(values, *rows, qq, D ** -0.5, 300)
+        tol = key_tolerance(values, *rows, qq, D ** -0.5, 300) + HALF_STEP[io] * np.abs(want)
+        assert (np.abs(out[:, heads].double().cpu().numpy() - want) <= tol).all()
+        assert (np.abs(lse[:, heads].double().cpu().numpy() - wl) <= 2.0 ** -12).all()
+    assert aibx.status_fetch() == (0, 0)
