@@ -387,8 +387,8 @@ inline int32_t launch_join(const AttnArgs& a, const JoinSet& rows, const JoinSet
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attn_join_kernel<D, QT>, a, rows, tiles, y_rows) == cudaSuccess ? AIBX_OK
-                                                                                                : AIBX_ERR_CUDA;
+  cudaLaunchKernelEx(&cfg, attn_join_kernel<D, QT>, a, rows, tiles, y_rows);
+  return launch_status();
 }
 
 }  // namespace aibx
