@@ -7,7 +7,7 @@ import torch
 
 from paged_ref import DTYPE, HALF_STEP, Batch, Shape, attention, pool_values, tolerance
 from paper_2504_03648_b200 import binding as aibx
-from test_gpu_paged import POOLS, check_attention, dev, make_batch, make_cache, make_pool
+from test_gpu_paged import POOLS, check_attention, dev, expected_append, make_batch, make_cache, make_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -443,4 +443,40 @@ def test_zero_keys_at_the_largest_scale(every, D, io, new, G):
         tol = key_tolerance(values, *rows, qq, D ** -0.5, 300) + HALF_STEP[io] * np.abs(want)
         assert (np.abs(out[:, heads].double().cpu().numpy() - want) <= tol).all()
         assert (np.abs(lse[:, heads].double().cpu().numpy() - wl) <= 2.0 ** -12).all()
+    assert aibx.status_fetch() == (0, 0)
+
+
+# ------------------------------------------------------------------------------------------
+# batches of many requests, few of them with tokens
+
+@pytest.mark.parametrize("pool,io", [("bf16", "bf16"), ("e4m3", "fp16")])
+@pytest.mark.parametrize("every,pad", [(64, 0), (64, 40), (33, 3), (31, 1), (1000, 0)])
+def test_few_of_many_requests_have_tokens(pool, io, every, pad):
+    s = Shape(H=1, D=64, T=8, pool=pool, blocks=140, layers=1, layer=0)
+    rng = np.random.default_rng(34)
+    new = [0] * 4097
+    for i, r in enumerate(range(every // 2, 4097, every)):
+        new[r] = 1 + (i % 3 == 0)
+    b = Batch(rng, s, new, [n + 5 if n else 0 for n in new], pad=pad)
+    p, sc = make_pool(rng, s)
+    cache, batch = make_cache(s, p, sc), make_batch(b)
+    k, v = (torch.from_numpy(rng.normal(size=(b.n_tokens, 1, 64))).to(DTYPE[io]) for _ in range(2))
+    aibx.kv_append(cache, batch, k.cuda(), v.cuda())
+    want, want_s = expected_append(s, b, p, sc, k, v)
+    assert torch.equal(cache._keep[0].cpu().view(torch.uint8).view(-1), want.view(torch.uint8).view(-1))
+    if sc is not None:
+        assert np.array_equal(cache._keep[1].cpu().numpy(), want_s)
+    back = [torch.full((b.n_tokens, 1, 64), 7.0, device="cuda") for _ in range(2)]
+    aibx.kv_read(cache, batch, *back)
+    values = pool_values(s, want, want_s)
+    ref = np.full((2, b.n_tokens, 1, 64), 7.0)
+    for i, r, pos in b.tokens():
+        for kv in range(2):
+            ref[kv, i, 0] = values[s.row(b.entry(s, r, pos), kv, 0, pos % 8)]
+    assert all(torch.equal(x.cpu(), torch.from_numpy(y).float()) for x, y in zip(back, ref))
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2, 64))).to(DTYPE[io])
+    out, _ = run(cache, batch, q.cuda())
+    n = int(b.tok_off[-1])
+    full, _, mag, slack = attention(s, b, values, q.double().numpy(), 64 ** -0.5, True, 0)
+    assert (np.abs(out.double().cpu().numpy() - full)[:n] <= tolerance(s, io, full[:n], mag[:n], slack[:n])).all()
     assert aibx.status_fetch() == (0, 0)
