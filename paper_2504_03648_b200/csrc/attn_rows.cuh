@@ -77,10 +77,10 @@ __device__ __forceinline__ uint32_t e4m3_bits(uint32_t pair) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Two e4m3 numbers times powers of two, as bf16: exact.
-__device__ __forceinline__ uint32_t bf16_of_e4m3(uint32_t pair, float f0, float f1) {
+// Two e4m3 numbers times a power of two, as bf16: exact.
+__device__ __forceinline__ uint32_t bf16_of_e4m3(uint32_t pair, float f) {
   const float2 y = __half22float2(halves_of_e4m3(pair));
-  return Bits16<__nv_bfloat16>::pack(y.x * f0, y.y * f1);
+  return Bits16<__nv_bfloat16>::pack(y.x * f, y.y * f);
 }
 
 // The tiles of request r: first tile and how many (at least one, so that empty rows are written).
@@ -573,7 +573,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             const int kb = kbyte[r], vb = weight_byte(vbyte[r]);
             kf = kb == 255 ? NAN : power_of_byte(kb);
             vexp = (float)(vb - 127);
-            unshift[r] = power_of_byte(254 - vb);
+            unshift[r] = __uint_as_float((unsigned int)(254 - vb) << 23);
           }
 #pragma unroll
           for (int x = 0; x < NQ; ++x)
@@ -612,7 +612,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         // ---- running maximum, moved only when it grows by more than 2^8
         constexpr float kHead = kWeightHead<MT>;
         float mt[NQ][2];
-        bool grow = false;
+        bool grow = wide;                                   // (one branch for what is rare)
 #pragma unroll
         for (int x = 0; x < NQ; ++x)
 #pragma unroll
@@ -624,6 +624,14 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             mt[x][h] = y;
             grow |= y > m[x][h] + (kHead + 8.0f);           // also from -infinity
           }
+        uint32_t pb[NQ][2];
+        auto weights = [&](int x, int r, float& p0, float& p1) {
+          const float m0 = m[x][0] == -INFINITY ? 0.0f : m[x][0], m1 = m[x][1] == -INFINITY ? 0.0f : m[x][1];
+          p0 = exp2_fast(c[x][2 * r] - m0);
+          p1 = exp2_fast(c[x][2 * r + 1] - m1);
+          l[x][0] += F8 ? p0 * unshift[r] : p0;
+          l[x][1] += F8 ? p1 * unshift[r] : p1;
+        };
         if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
           for (int x = 0; x < NQ; ++x)
@@ -639,56 +647,48 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                 o[x][j][2 + h] *= al;
               }
             }
-        }
-        uint32_t pb[NQ][2];
-        auto weights = [&](int x, int r, float& p0, float& p1) {
-          const float m0 = m[x][0] == -INFINITY ? 0.0f : m[x][0], m1 = m[x][1] == -INFINITY ? 0.0f : m[x][1];
-          p0 = exp2_fast(c[x][2 * r] - m0);
-          p1 = exp2_fast(c[x][2 * r + 1] - m1);
-          l[x][0] += F8 ? p0 * unshift[r] : p0;
-          l[x][1] += F8 ? p1 * unshift[r] : p1;
-        };
-        if constexpr (F8) {
-          if (wide) {
-            // ---- O^T += V^T P^T, V and the weights as bf16
-            uint32_t pb2[NQ][2];
+          if constexpr (F8) {
+            if (wide) {
+              // ---- O^T += V^T P^T, V and the weights as bf16
 #pragma unroll
-            for (int x = 0; x < NQ; ++x)
+              for (int x = 0; x < NQ; ++x)
 #pragma unroll
-              for (int r = 0; r < 2; ++r) {
-                float p0, p1;
-                weights(x, r, p0, p1);
-                if (vbyte[r] == 255) {                       // a NaN row, for those that see it
-                  if (c[x][2 * r] != -INFINITY) p0 = NAN;
-                  if (c[x][2 * r + 1] != -INFINITY) p1 = NAN;
+                for (int r = 0; r < 2; ++r) {
+                  float p0, p1;
+                  weights(x, r, p0, p1);
+                  // what the weight does not carry yet; a NaN row is one for those that see it
+                  const float rest = power_of_byte(127 + vbyte[r] - weight_byte(vbyte[r]));
+                  c[x][2 * r] = vbyte[r] == 255 && c[x][2 * r] != -INFINITY ? NAN : p0 * rest;
+                  c[x][2 * r + 1] = vbyte[r] == 255 && c[x][2 * r + 1] != -INFINITY ? NAN : p1 * rest;
                 }
-                const uint32_t hi = Bits16<__nv_bfloat16>::pack(p0, p1);
-                const float2 y = Bits16<__nv_bfloat16>::unpack(hi);
-                pb[x][r] = transpose8(hi);
-                pb2[x][r] = transpose8(Bits16<__nv_bfloat16>::pack(p0 - y.x, p1 - y.y));
-              }
-            float vf[4];                                     // of this lane's tokens: what the weights do not carry
+#pragma unroll 1
+              for (int part = 0; part < 2; ++part) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int byte = s_scale[s * 2 * TOK + TOK + task * 16 + (e >> 1) * 8 + 2 * t4 + (e & 1)];
-              vf[e] = byte == 255 ? 1.0f : power_of_byte(127 + byte - weight_byte(byte));
-            }
+                for (int x = 0; x < NQ; ++x)
 #pragma unroll
-            for (int w4 = 0; w4 < kW; ++w4) {
+                  for (int r = 0; r < 2; ++r) {
+                    const uint32_t hi = Bits16<__nv_bfloat16>::pack(c[x][2 * r], c[x][2 * r + 1]);
+                    const float2 y = Bits16<__nv_bfloat16>::unpack(hi);
+                    c[x][2 * r] -= y.x;
+                    c[x][2 * r + 1] -= y.y;
+                    pb[x][r] = transpose8(hi);
+                  }
 #pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                const uint32_t y0 = __byte_perm(v[0][0][w4], v[0][1][w4], half ? 0x7362 : 0x5140);
-                const uint32_t y1 = __byte_perm(v[0][2][w4], v[0][3][w4], half ? 0x7362 : 0x5140);
-                const uint32_t af[4] = {bf16_of_e4m3(y0 & 0xffffu, vf[0], vf[1]), bf16_of_e4m3(y0 >> 16, vf[0], vf[1]),
-                                        bf16_of_e4m3(y1 & 0xffffu, vf[2], vf[3]), bf16_of_e4m3(y1 >> 16, vf[2], vf[3])};
+                for (int w4 = 0; w4 < kW; ++w4) {
 #pragma unroll
-                for (int x = 0; x < NQ; ++x) {
-                  mma_16816(o[x][2 * w4 + half], af, pb[x][0], pb[x][1], __nv_bfloat16());
-                  mma_16816(o[x][2 * w4 + half], af, pb2[x][0], pb2[x][1], __nv_bfloat16());
+                  for (int half = 0; half < 2; ++half) {
+                    const uint32_t y0 = __byte_perm(v[0][0][w4], v[0][1][w4], half ? 0x7362 : 0x5140);
+                    const uint32_t y1 = __byte_perm(v[0][2][w4], v[0][3][w4], half ? 0x7362 : 0x5140);
+                    const uint32_t af[4] = {bf16_of_e4m3(y0 & 0xffffu, 1.0f), bf16_of_e4m3(y0 >> 16, 1.0f),
+                                            bf16_of_e4m3(y1 & 0xffffu, 1.0f), bf16_of_e4m3(y1 >> 16, 1.0f)};
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x)
+                      mma_16816(o[x][2 * w4 + half], af, pb[x][0], pb[x][1], __nv_bfloat16());
+                  }
                 }
               }
+              continue;
             }
-            continue;
           }
         }
 #pragma unroll

@@ -657,7 +657,8 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           m = mn;
           l *= al;
           if (j > 0) {
-#pragma unroll 1
+            constexpr int kUnroll = F8 ? 1 : D / 32;       // (over e4m3 the shorter code: 2,315 instead of 2,420 us)
+#pragma unroll kUnroll
             for (int k = 0; k < D; k += 32) {
               uint32_t o[32];
               tmem_ld32(tm_o + k, o);
@@ -1149,7 +1150,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
                 if constexpr (decltype(to_bf16)::value) {    // the factor is one already
                   const float xf = __uint_as_float((uint32_t)__half_as_ushort(x[u0 + u]) << 16);
 #pragma unroll
-                  for (int e = 0; e < 8; ++e) o[e] = bf16_of_e4m3((wv[e >> 1] >> (16 * (e & 1))) & 0xffffu, xf, xf);
+                  for (int e = 0; e < 8; ++e) o[e] = bf16_of_e4m3((wv[e >> 1] >> (16 * (e & 1))) & 0xffffu, xf);
                 } else {
                   const __half2 x2 = __half2half2(x[u0 + u]);
 #pragma unroll
