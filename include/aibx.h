@@ -592,8 +592,8 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
  *   workspace that is too small.
  * Workspace: aibx_attn_workspace_bytes(cache, batch, params) bytes, 16-byte aligned, content
  *   irrelevant before and after; calls that may overlap on the GPU need separate ones.
- *   The answer depends on head_dim, num_q_heads / num_kv_heads, max_new and on whether R is 1, on
- *   nothing else (0 = arguments that attn_paged would refuse).
+ *   The answer depends on head_dim, num_q_heads / num_kv_heads, max_new, on whether R is 1 and on the
+ *   current device's number of SMs, on nothing else (0 = arguments that attn_paged would refuse).
  * RANGE is raised at least once for every request with a bad entry among the blocks that it reads,
  *   and for a request with more than max_new > 0 tokens (whose rows may be left unwritten).
  */

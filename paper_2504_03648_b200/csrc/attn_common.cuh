@@ -297,9 +297,10 @@ constexpr float kWeightHead = std::is_same<T, __half>::value ? 7.0f : 0.0f;
 // row leads, all others' weights lie b_j (and its lead) below m, and fp16 would lose them.  So keys whose
 // bytes lie more than kScaleSpread below the largest so far, or outside [kScaleLow, kScaleHigh], are
 // multiplied "wide": weights as the sum of two bf16 numbers (16 bits, range 2^-126), V as bf16
-// (exact: four bits).  What exceeds the range of bytes goes into V itself, so that 2^b_j and the sum
-// of 2^t_j stay within fp32 whatever the bytes are: a weight is lost below 2^-126 only, and then the
-// key's score is 37 below another's (a factor of 2^37) at the least.
+// (exact: four bits).  b_j is taken within the range; the rest of it joins those bf16 numbers (the
+// weights' in the row kernel, V's in the tile kernel), so that m, 2^b_j and the sum of 2^t_j stay within
+// fp32 whatever the bytes are: a weight is lost below 2^-126 only, and then the key's score is 37 below
+// another's (a factor of 2^37) at the least.
 constexpr int kScaleLow = 79, kScaleHigh = 175, kScaleSpread = 4;
 
 __device__ __forceinline__ int weight_byte(int byte) { return min(max(byte, kScaleLow), kScaleHigh); }
@@ -321,10 +322,6 @@ __device__ __forceinline__ void power_scale(float amax, float& down, float& up) 
   down = __uint_as_float((unsigned int)(127 - k) << 23);
   up = __uint_as_float((unsigned int)(127 + k) << 23);
 }
-
-}  // namespace aibx
-
-namespace aibx {
 
 // Joins rows that were cut: block c those that end in CTA c.  blockIdx.y takes 16 rows: the first
 // y_rows of them of the row kernel's set, the others of the tile kernel's.

@@ -7,8 +7,9 @@
 // Over an e4m3 pool k_j = K_j 2^a_j and v_j = V_j 2^b_j with e4m3 rows K_j, V_j.  Those are exact
 // in fp16, so they go to the tensor core as they are: the scores take 2^a_j afterwards, and the
 // weight that multiplies V_j is w = 2^(t + b_j - m) with m the maximum of t + b_j; then
-// l = sum w 2^-b_j (stages whose b_j are far apart: see kScaleSpread).  Queries are scaled to [1, 2) per row to fit fp16 (fp16 keeps 3 more bits than
-// bf16; what falls below 2^-24 of the row's maximum is lost).
+// l = sum w 2^-b_j (stages whose b_j are far apart: see kScaleSpread).  Queries are scaled to [1, 2)
+// per row to fit fp16 (fp16 keeps 3 more bits than bf16; what falls below 2^-24 of the row's maximum
+// is lost).
 //
 // Bound: HBM.  Every K and V byte is read once and meets at most 16 rows, so the legacy tensor
 // path (mma.sync m16n8k16) has an order of magnitude to spare: 16 tokens of D = 128 cost 32 MMAs
@@ -16,8 +17,9 @@
 // flight: one warp feeds a ring of five 32 KB stages with tensor-map boxes (one box = the slots
 // of one block and head), 160 KB per SM outstanding, and runs ahead over the seams between
 // requests, so that the memory never idles (64 single tokens over 292,000 cached ones of 8 heads,
-// bf16: 188 us, 6.36 TB/s; 32 over 131,072 each of 4 heads, e4m3: 755 us, 5.7 TB/s); eight warps consume, 16 tokens each at a time, with
-// their own m, l and O, joined once per (request, head).
+// bf16: 194 us, 6.2 TB/s; 32 over 131,072 each of 4 heads, e4m3: 816 us, 5.3 TB/s, with all stages'
+// scales far apart a third more); eight warps consume, 16 tokens each at a time, with their own m, l
+// and O, joined once per (request, head).
 // The keys are the MMA's M dimension and the query rows its N of 8: S^T = K Q^T and O^T = V^T P^T,
 // so that 8 rows (7 or 8 query heads of one token) waste nothing.  Fragments are read from shared
 // memory without transposition: the order of the contraction index is free as long as both

@@ -26,10 +26,12 @@
 //
 // Bound: the tensor pipe (1024 cycles per KV tile and 128 rows at D = 128, both products) and the
 // special function unit (128 * 128 exponentials at 16 a cycle: 1024 cycles too), neither of them
-// busy all the time: a step of both tiles takes about 3,500 cycles, 2,400 of a tile's softmax and
-// 1,050 from its last weights to its next scores.  Six chunks of 8,505 tokens over prefixes of 1k to
-// 8k (16-bit, 32 query heads on 8): 805 us, 950 TFLOP/s; a 1,023-token chunk over 130k e4m3 positions:
-// 2,200 us, 870 TFLOP/s.
+// busy all the time: a step of both tiles takes about 3,800 cycles where both pipes need 2,048, and
+// 5,300 over e4m3, where the converters share the schedulers and warps wait for instructions (the roles'
+// code together exceeds what the instruction cache holds: every addition to the softmax or MMA loop
+// shows).  Six chunks of 8,505 tokens over prefixes of 1k to 8k (16-bit, 32 query heads on 8): 890 us,
+// 865 TFLOP/s, at the 1.67 GHz that the power cap leaves; a 1,023-token chunk over 130k e4m3 positions:
+// 2,360 us, 810 TFLOP/s, at 1.9 GHz.
 #pragma once
 
 #include "attn_rows.cuh"
@@ -537,29 +539,29 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           }
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) {
-          const int i = i0 + u * (128 / kChunks);
-          uint4 v = i < rows_here ? batch[u] : make_uint4(0, 0, 0, 0);
-          if constexpr (F8) {
-            uint32_t x[4] = {v.x, v.y, v.z, v.w};
-            float amax = 0.0f;
+            const int i = i0 + u * (128 / kChunks);
+            uint4 v = i < rows_here ? batch[u] : make_uint4(0, 0, 0, 0);
+            if constexpr (F8) {
+              uint32_t x[4] = {v.x, v.y, v.z, v.w};
+              float amax = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 f = Bits16<QT>::unpack(x[e]);
-              amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+              for (int e = 0; e < 4; ++e) {
+                const float2 f = Bits16<QT>::unpack(x[e]);
+                amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+              }
+#pragma unroll
+              for (int m = 1; m < kChunks; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
+              float down, up;
+              power_scale(amax, down, up);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float2 f = Bits16<QT>::unpack(x[e]);
+                x[e] = Bits16<MT>::pack(f.x * down, f.y * down);
+              }
+              v = make_uint4(x[0], x[1], x[2], x[3]);
+              if (c == 0) s_qup[t * kTileRows + i] = up;
             }
-#pragma unroll
-            for (int m = 1; m < kChunks; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
-            float down, up;
-            power_scale(amax, down, up);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 f = Bits16<QT>::unpack(x[e]);
-              x[e] = Bits16<MT>::pack(f.x * down, f.y * down);
-            }
-            v = make_uint4(x[0], x[1], x[2], x[3]);
-            if (c == 0) s_qup[t * kTileRows + i] = up;
-          }
-          *reinterpret_cast<uint4*>(dst + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = v;
+            *reinterpret_cast<uint4*>(dst + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = v;
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -844,7 +846,6 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       unsigned int buf = 0, buf_phase = 0;                 // next buffer of the ring to be read
       unsigned int q_phase = 0, p_phase = 0;
       unsigned int turn_phase = t == 0;                    // (the first turn is tile 0's: a fresh barrier passes for phase 1)
-      constexpr bool kTurns = true;
       unsigned int last_buf = 0, last_phase = 1;           // (a fresh barrier passes for phase 1)
       auto advance = [&]() {
         if (++buf == S::kBufs) {
@@ -870,7 +871,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       };
       while (walk.next_warp(a, per)) {
         const int steps = (int)uniform(walk.t1 - walk.t0);
-        const bool turns = kTurns && uniform(walk.rows(a) > kTileRows);     // two tiles at work
+        const bool turns = uniform(walk.rows(a) > kTileRows);     // two tiles at work
         const bool active = uniform(walk.rows(a) > t * kTileRows);   // the tile has rows; else only hands buffers on
         const int key_first = (int)uniform((walk.span.tile0 + walk.t0) * kTileKeys);
         const int lo = (int)uniform(walk.span.lo), hi = (int)uniform(walk.span.hi);

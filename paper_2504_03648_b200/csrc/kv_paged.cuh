@@ -16,8 +16,8 @@
 // it once for all the warp's tokens together and hand the places on by shuffles, so that what is
 // left per row is an address and 16 pool bytes per lane.  (A warp per token, searching for itself,
 // spent 620 instructions on 1 KB: 444 us for 404,000 tokens of 4 e4m3 heads.)  With few tokens the
-// groups shrink, down to one step of rows per warp.  Now 200 us, 6.2 TB/s; 35,000 tokens quantised
-// in 26 us, 4.3 TB/s.  Every byte crosses the memory system once in
+// groups shrink, down to one step of rows per warp.  Now 212 us, 5.9 TB/s; 35,000 tokens quantised
+// in 29 us, 3.8 TB/s (ALU pipe 64 % busy, issue slots 60 %).  Every byte crosses the memory system once in
 // each direction: bound by HBM for long inputs, by the chain of loads for short ones.
 #pragma once
 
