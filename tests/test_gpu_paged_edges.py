@@ -480,3 +480,36 @@ def test_few_of_many_requests_have_tokens(pool, io, every, pad):
     full, _, mag, slack = attention(s, b, values, q.double().numpy(), 64 ** -0.5, True, 0)
     assert (np.abs(out.double().cpu().numpy() - full)[:n] <= tolerance(s, io, full[:n], mag[:n], slack[:n])).all()
     assert aibx.status_fetch() == (0, 0)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_scales_far_apart_captured_and_side_by_side(D):
+    """Pools of every kind at once, on several streams, eager and from graphs: the same bits."""
+    jobs = []
+    for i, (kind, new, lens) in enumerate([("spread of 40", 1, [900, 40, 300]), ("loose", 90, [700, 350]), ("one byte", 3, [500, 800]),
+                                           ("whole range", 260, [300, 1200]), (None, 120, [1000])]):
+        s = Shape(H=2, D=D, T=16, pool="e4m3", blocks=160, layers=1, layer=0)
+        rng = np.random.default_rng(40 + i)
+        pool, scales = spread_pool(rng, s, kind) if kind else make_pool(rng, s)
+        b = Batch(rng, s, [new] * len(lens), lens)
+        cache, batch = make_cache(s, pool, scales), make_batch(b)
+        q = torch.from_numpy(rng.normal(size=(b.n_tokens, 8, D))).bfloat16().cuda()
+        ws = torch.empty(aibx.attn_workspace_bytes(cache, batch, q), dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(q)
+        want = run(cache, batch, q)[0]
+        g, st = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(g):
+            aibx.attn_paged(cache, batch, q, out, workspace=ws)
+        jobs.append((cache, batch, q, want, st, g, out, ws))    # (a graph's workspace lives as long as it does)
+    torch.cuda.synchronize()
+    for turn in range(6):
+        got = []
+        for cache, batch, q, _, st, g, _, _ in jobs:
+            with torch.cuda.stream(st):
+                got.append(run(cache, batch, q)[0])
+                g.replay()
+        torch.cuda.synchronize()
+        for x, (_, _, _, want, _, _, out, _) in zip(got, jobs):
+            assert torch.equal(x.view(torch.int16), want.view(torch.int16)), turn
+            assert torch.equal(out.view(torch.int16), want.view(torch.int16)), turn
+    assert aibx.status_fetch() == (0, 0)
