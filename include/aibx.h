@@ -22,8 +22,8 @@
  *     with aibx_status_fetch.  Nothing aborts, throws or traps.
  *   - Keys, index, routing and block copies: all arithmetic is integer and results are defined
  *     bit-exactly.  So are the stored bytes of aibx_kv_append and the values of aibx_kv_read (one
- *     rounding, to the nearest, ties to even).  aibx_attn_paged is the one call with floating
- *     arithmetic of its own; it states what it rounds.
+ *     rounding, to the nearest, ties to even).  aibx_attn_paged, aibx_attn_tree, aibx_rope and
+ *     aibx_rope_append have floating arithmetic of their own; they state what they round.
  *   - Threads: calls on different indexes, pools and streams may come from different host
  *     threads at any time (the few one-time per-device settings - kernel attributes, the address
  *     of the status record - are made under a lock or as single atomic words).  Calls on one
@@ -612,6 +612,142 @@ uint64_t aibx_attn_workspace_bytes(const aibx_kv_cache_t* cache, const aibx_kv_b
 int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
                         const aibx_attn_params_t* params, const void* d_q, void* d_out,
                         float* d_lse, void* d_workspace, uint64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Trees of drafted tokens: the last n_r tokens of a request are nodes of a tree under its cached ones
+ * (several guesses of how it goes on, to be checked in one pass).  Node i stands in the slot of position
+ * base + i, base = kv_len - n_r, whatever its place in the tree; its position in the text is base + its
+ * depth.
+ *
+ * tree_masks: from each node's parent (index in its request; negative: it follows the cached tokens
+ *   directly) the nodes that it sees, itself and all above it:
+ *     d_mask  uint64 [n_tokens][mask_words], bit j of the row (bit j mod 64 of word j / 64) = node j
+ *     d_pos   int32 [n_tokens] (nullable; wants d_kv_len): base + depth
+ *   d_parent: int32 [n_tokens].  A parent that does not come before its node is taken for none and raises
+ *   RANGE.  A request with more than 64 * mask_words tokens raises RANGE, and its rows are left as they
+ *   are, as are rows behind the last request.  INVALID for null or unaligned pointers, negative counts,
+ *   mask_words < 1, outputs in the place of inputs; UNSUPPORTED for more than 8 words.
+ *
+ * attn_tree: aibx_attn_paged with these masks in the place of causality.  Node i sees the cached
+ *   positions j < base (window > 0: those with j > base + depth - window, depth = the number of nodes
+ *   that it sees less one, at least 0) and the nodes whose bits are set in its row of d_mask - any rows,
+ *   not only those of trees, and a node need not see itself.  Bits of nodes that the request has not are
+ *   ignored.  params->causal is not read.  Everything else as aibx_attn_paged: formats, shapes, errors,
+ *   roundings, workspace (aibx_attn_workspace_bytes of the same arguments); a NaN or infinite V of a
+ *   position from base - window + 1 on that is hidden from a row may reach it.  INVALID for a null or
+ *   unaligned d_mask or mask_words < 1, UNSUPPORTED for more than 8 words, RANGE for a request with more
+ *   than 64 * mask_words tokens (whose later nodes count as hidden).
+ */
+int32_t aibx_tree_masks(const int32_t* d_parent, const int64_t* d_tok_off, const int32_t* d_kv_len,
+                        int32_t R, int64_t n_tokens, int32_t mask_words, uint64_t* d_mask,
+                        int32_t* d_pos, void* stream);
+int32_t aibx_attn_tree(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
+                       const aibx_attn_params_t* params, const uint64_t* d_mask, int32_t mask_words,
+                       const void* d_q, void* d_out, float* d_lse, void* d_workspace,
+                       uint64_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Rotary positions.  The first rotary_dim elements of a row are rotary_dim / 2 pairs, (i, i +
+ * rotary_dim / 2) or, interleaved, (2 i, 2 i + 1); pair i of a row at position p becomes
+ *     y1 = factor * (x1 cos a - x2 sin a),  y2 = factor * (x2 cos a + x1 sin a),  a = p * d_inv_freq[i];
+ * the other elements stay.  Scaling for long contexts is a matter of the frequencies and the factor,
+ * which are the caller's.  Negative positions turn back: they give the gradient of a rotation (factor
+ * included), and p2 - p1 moves a row turned for p1 to p2.
+ * Arithmetic: p * d_inv_freq / 2 pi in 64 bits, less its nearest whole number; sine and cosine of that,
+ * products and sums in 32 bits; one rounding to the type that is stored.  V and unturned elements keep
+ * their bits where the types agree.
+ *   d_inv_freq  double [rotary_dim / 2], radians per position
+ *   d_pos       int32 [n_tokens]
+ *
+ * rope: x -> y, [n_tokens][num_heads][head_dim] of `type` (BF16, FP16, FP32), element strides per token
+ *   and per head, elements of a row adjacent.  y may be x with the same strides; they must not overlap in
+ *   any other way.
+ * rope_append: aibx_kv_append of turned K and plain V, and queries turned beside them, in one launch.
+ *   Positions of the rotation: d_pos, or where it is null those of the batch (kv_len - n_r + i); slots are
+ *   always the batch's.  Queries: num_q_heads may be 0; d_q_out may be d_q with the same strides.  Query
+ *   rows of every token of a request are written, rows behind the last request left as they are.  E4M3
+ *   rows take their scale from the turned K in 32 bits, before it is rounded.
+ * Errors: as aibx_kv_append; INVALID for a rotary_dim that is odd, not positive or above head_dim, an
+ *   unknown style, null or unaligned pointers, in place with other strides; UNSUPPORTED for a rotary_dim
+ *   that is no multiple of 16, head_dim above 512 or no multiple of 8, more than 65,536 heads.
+ */
+#define AIBX_ROPE_HALF        0
+#define AIBX_ROPE_INTERLEAVED 1
+
+typedef struct {
+  const double* d_inv_freq;
+  const int32_t* d_pos;
+  int32_t rotary_dim;
+  int32_t style;              /* AIBX_ROPE_* */
+  float factor;
+} aibx_rope_t;
+
+typedef struct {
+  const void* d_q;
+  void* d_q_out;
+  const void* d_k;
+  const void* d_v;
+  int64_t q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride;
+  int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+  int32_t num_q_heads;
+  int32_t type;               /* of all four */
+} aibx_rope_rows_t;
+
+int32_t aibx_rope(const aibx_rope_t* rope, int64_t n_tokens, int32_t num_heads, int32_t head_dim,
+                  const void* d_x, int64_t x_token_stride, int64_t x_head_stride, void* d_y,
+                  int64_t y_token_stride, int64_t y_head_stride, int32_t type, void* stream);
+int32_t aibx_rope_append(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
+                         const aibx_rope_t* rope, const aibx_rope_rows_t* rows, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Block tables and slots of a step (Section 3.2.5: matched blocks are used where they lie, the rest of a
+ * request gets blocks of its own).  Request r holds h = d_held[r] tokens and gets n = d_new[r] more; with
+ * T = block_tokens its row of the table has had = ceil(h / T) entries and grows to ceil((h + n) / T) by
+ * ids from the free list, requests in order, each taking its ids one after the other.
+ *   free list      a ring of free_capacity ids: ids number *d_free_head .. *d_free_tail - 1, number k at
+ *                  d_free_ids[k mod free_capacity].  *d_free_head_out = the first number not taken.
+ *                  (Handing ids back is writing them from the tail on and raising it.)
+ *   d_block_table  rows as in aibx_kv_batch_t: of table_stride entries, or with d_blk_off (int64 [R+1])
+ *                  ragged.  Entries below had are read (match: written), those that are new written, others
+ *                  left as they are.
+ *   d_match_ids    nullable; with d_match_off (int64 [R+1]): request r's first `had` entries are copied
+ *                  from d_match_ids[d_match_off[r]] on - what aibx_match_prefix leaves in d_block_ids.
+ *   d_tok_off      int64 [R+1], prefix sum of n;   d_kv_len  int32 [R], h + n
+ *   d_pos          int32 [n_tokens], nullable: h + i for token i of a request
+ *   d_slots        int64 [n_tokens], nullable: block id * T + position mod T; -1 where there is no block
+ * A request that wants more blocks than are left gets AIBX_NO_BLOCK for the rest: FULL, detail = such
+ * blocks of all requests.  RANGE at least once for a request with a negative length, or more than 2^31 - 1
+ * tokens (it counts as n = 0), for one with more blocks than its row has entries (they are left out, and
+ * take no ids) or fewer matched ids than `had` (AIBX_NO_BLOCK), for an id >= num_blocks under a new
+ * token, and where there are more than n_tokens tokens (whose d_pos and d_slots are left out).
+ * d_kv_len may be d_held and d_free_head_out may be d_free_head (a call captured once, replayed step
+ * after step); no other output may overlap an input, and calls on one free list are the caller's to
+ * order.  Arithmetic on whole numbers; calls on the same input give the same bits.  INVALID for null or
+ * unaligned pointers, negative counts; UNSUPPORTED for block_tokens > 65536.  R = 0 is a no-op.
+ */
+typedef struct {
+  const int32_t* d_held;
+  const int32_t* d_new;
+  const uint32_t* d_free_ids;
+  int64_t free_capacity;
+  const int64_t* d_free_head;
+  const int64_t* d_free_tail;
+  int64_t* d_free_head_out;
+  uint32_t* d_block_table;
+  const int64_t* d_blk_off;
+  int64_t table_stride;
+  const uint32_t* d_match_ids;
+  const int64_t* d_match_off;
+  int64_t* d_tok_off;
+  int32_t* d_kv_len;
+  int32_t* d_pos;
+  int64_t* d_slots;
+  int64_t n_tokens;
+  int32_t block_tokens;
+  uint32_t num_blocks;
+} aibx_kv_tables_t;
+
+int32_t aibx_kv_tables(const aibx_kv_tables_t* tables, int32_t R, void* stream);
 
 /* ---------------------------------------------------------------------------------------
  * Device status of the current device: the most severe (most negative) code recorded by any

@@ -23,6 +23,7 @@ ERR_INVALID, ERR_RANGE, ERR_FULL, ERR_CUDA, ERR_UNSUPPORTED, ERR_NOMEM, ERR_TIME
 NO_BLOCK = 0xFFFFFFFF
 NO_POD = -1
 TYPE_BF16, TYPE_FP16, TYPE_FP32, TYPE_E4M3 = range(4)
+ROPE_HALF, ROPE_INTERLEAVED = range(2)
 _TYPE_OF = {torch.bfloat16: TYPE_BF16, torch.float16: TYPE_FP16, torch.float32: TYPE_FP32}
 
 
@@ -79,6 +80,9 @@ class _AttnC(C.Structure):
 _CACHE_BYTES = struct.Struct("@PP6iI3i")
 _BATCH_BYTES = struct.Struct("@PPqPPqii")
 _ATTN_BYTES = struct.Struct("@iiqqqqfii")
+_ROPE_BYTES = struct.Struct("@PPiif")
+_ROPE_ROWS_BYTES = struct.Struct("@PPPP8qii")
+_TABLES_BYTES = struct.Struct("@PPPqPPPPPqPPPPPPqiI")
 
 
 class PodMetrics(C.Structure):
@@ -146,6 +150,11 @@ def lib():
             "aibx_kv_append": [vp, vp, vp, i64, i64, vp, i64, i64, i32, vp],
             "aibx_kv_read": [vp, vp, vp, i64, i64, vp, i64, i64, i32, vp],
             "aibx_attn_paged": [vp, vp, vp, vp, vp, vp, vp, u64, vp],
+            "aibx_attn_tree": [vp, vp, vp, vp, i32, vp, vp, vp, vp, u64, vp],
+            "aibx_tree_masks": [vp, vp, vp, i32, i64, i32, vp, vp, vp],
+            "aibx_rope": [vp, i64, i32, i32, vp, i64, i64, vp, i64, i64, i32, vp],
+            "aibx_rope_append": [vp, vp, vp, vp, vp],
+            "aibx_kv_tables": [vp, i32, vp],
             "aibx_kv_set_tuning": [i32, i32, i32, i32],
             "aibx_kv_set_store_lag": [i32],
             "aibx_kv_get_tuning": [vp, vp, vp, vp, vp],
@@ -598,11 +607,8 @@ def kv_read(cache: KVCache, batch: KVBatch, k, v) -> None:
     _kv_tokens("aibx_kv_read", cache, batch, k, v)
 
 
-def attn_paged(cache: KVCache, batch: KVBatch, q, out, lse=None, scale=None, causal: bool = True,
-               window: int = 0, workspace=None) -> None:
-    """Attention of the batch's tokens over their requests' cached keys.  q, out: [n_tokens,
-    q_heads, head_dim]; lse: float32 [n_tokens, q_heads] or None; scale: 1/sqrt(head_dim) if None.
-    workspace: uint8 tensor of attn_workspace_bytes(...) bytes, allocated here if None."""
+def _attention(name: str, cache: KVCache, batch: KVBatch, tree, q, out, lse, scale, causal, window,
+               workspace) -> None:
     if q.dtype != out.dtype or q.dtype not in _TYPE_OF or q.dim() != 3:
         raise ValueError("queries and output of one type and [n_tokens, q_heads, head_dim] expected")
     stream = _here(cache, batch)
@@ -623,8 +629,174 @@ def attn_paged(cache: KVCache, batch: KVBatch, q, out, lse=None, scale=None, cau
                                 dtype=torch.uint8)
     elif workspace.get_device() != cache.device or not workspace.is_contiguous():
         raise ValueError("a contiguous workspace on the pool's device expected")
-    _check("aibx_attn_paged", L.aibx_attn_paged(cache._ref, batch._ref, ref, qp, op, lp,
-                                                workspace.data_ptr(), workspace.nbytes, stream))
+    _check(name, getattr(L, name)(cache._ref, batch._ref, ref, *tree, qp, op, lp, workspace.data_ptr(),
+                                  workspace.nbytes, stream))
+
+
+def attn_paged(cache: KVCache, batch: KVBatch, q, out, lse=None, scale=None, causal: bool = True,
+               window: int = 0, workspace=None) -> None:
+    """Attention of the batch's tokens over their requests' cached keys.  q, out: [n_tokens,
+    q_heads, head_dim]; lse: float32 [n_tokens, q_heads] or None; scale: 1/sqrt(head_dim) if None.
+    workspace: uint8 tensor of attn_workspace_bytes(...) bytes, allocated here if None."""
+    _attention("aibx_attn_paged", cache, batch, (), q, out, lse, scale, causal, window, workspace)
+
+
+def _vector(t, what: str, dtype, n: int, device: int) -> int:
+    """Pointer of n contiguous numbers of a type, on the call's device."""
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError("%s: %d contiguous numbers of %s on device %d expected, got %s of %s on %s" % (
+            what, n, dtype, device, tuple(t.shape), t.dtype, t.device))
+    return t.data_ptr()
+
+
+def _current(t) -> int:
+    """The current device, which a call's tensors live on."""
+    device = torch._C._cuda_getDevice()
+    if t.get_device() != device:
+        raise ValueError("the call works on the current device (%d), not on %s" % (device, t.device))
+    return device
+
+
+def tree_masks(parent, tok_off, kv_len, mask, pos=None) -> None:
+    """What each node of the requests' drafted trees sees: parent int32 [n_tokens] (index in the
+    request, negative: none) -> mask uint64 [n_tokens, words], and pos int32 [n_tokens] (its position
+    in the text).  kv_len is read for pos alone, and may be None without it."""
+    device = _current(parent)
+    n, R = parent.numel(), tok_off.numel() - 1
+    if mask.dim() != 2 or mask.shape[0] != n or R < 0:
+        raise ValueError("a mask of %d rows and offsets of every request expected" % n)
+    words = mask.shape[1]
+    _check("aibx_tree_masks", lib().aibx_tree_masks(
+        _vector(parent, "parent", torch.int32, n, device), _vector(tok_off, "tok_off", torch.int64, R + 1, device),
+        None if kv_len is None else _vector(kv_len, "kv_len", torch.int32, R, device), R, n, words,
+        _vector(mask, "mask", torch.uint64, n * words, device),
+        None if pos is None else _vector(pos, "pos", torch.int32, n, device),
+        torch._C._cuda_getCurrentRawStream(device)))
+
+
+def attn_tree(cache: KVCache, batch: KVBatch, mask, q, out, lse=None, scale=None, window: int = 0,
+              workspace=None) -> None:
+    """attn_paged of drafted tokens that see their request's cached tokens and the drafted ones that
+    mask (uint64 [n_tokens, words], as tree_masks makes it) names."""
+    if mask.dim() != 2:
+        raise ValueError("a mask of [n_tokens, words] expected")
+    tree = _vector(mask, "mask", torch.uint64, batch.n_tokens * mask.shape[1], cache.device), mask.shape[1]
+    _attention("aibx_attn_tree", cache, batch, tree, q, out, lse, scale, False, window, workspace)
+
+
+class Rope:
+    """Rotary positions (aibx_rope_t): inv_freq float64 [rotary_dim / 2] on the device, radians per
+    position of each pair; factor on sine and cosine."""
+
+    def __init__(self, inv_freq, interleaved: bool = False, factor: float = 1.0):
+        self.device = inv_freq.get_device()
+        self._keep = inv_freq
+        self._fields = (_vector(inv_freq, "inv_freq", torch.float64, inv_freq.numel(), self.device),
+                        2 * inv_freq.numel(), ROPE_INTERLEAVED if interleaved else ROPE_HALF, factor)
+
+    def _pack(self, pos, n: int) -> bytes:
+        p, dim, style, factor = self._fields
+        return _ROPE_BYTES.pack(p, 0 if pos is None else _vector(pos, "pos", torch.int32, n, self.device), dim,
+                                style, factor)
+
+
+def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", scale: float = 1.0,
+                     trained: int = 0, fast: float = 32.0, slow: float = 1.0):
+    """(inv_freq, factor) for Rope, float64 on the host: base^(-2 i / rotary_dim) and 1, or scaled for
+    contexts `scale` times as long as the trained one:
+    "linear": every frequency over scale;
+    "base":   base * scale^(rotary_dim / (rotary_dim - 2)), which stretches the slowest pair alone by scale;
+    "parts":  pairs of at most `slow` turns over the `trained` positions over scale, pairs of `fast` turns
+              or more as they are, a straight line between; factor 0.1 ln(scale) + 1."""
+    if rotary_dim <= 0 or rotary_dim % 2 or base <= 0 or scale <= 0:
+        raise ValueError("an even positive rotary_dim, base and scale above 0 expected")
+    half = rotary_dim // 2
+    if scaling == "base":
+        if rotary_dim == 2:
+            raise ValueError("a single pair has no base to scale")
+        base = base * scale ** (rotary_dim / (rotary_dim - 2))
+    f = base ** (-torch.arange(half, dtype=torch.float64) / half)
+    if scaling in ("none", "base"):
+        return f, 1.0
+    if scaling == "linear":
+        return f / scale, 1.0
+    if scaling != "parts":
+        raise ValueError("scaling none, linear, base or parts expected, got %r" % scaling)
+    if trained <= 0 or fast <= slow:
+        raise ValueError("parts: trained positions and fast > slow expected")
+    turns = trained * f / 6.283185307179586
+    keep = ((turns - slow) / (fast - slow)).clamp(0, 1)
+    log = torch.log(torch.tensor(max(scale, 1.0), dtype=torch.float64)).item()
+    return f * (keep + (1 - keep) / scale), 0.1 * log + 1.0
+
+
+def rope(rope: Rope, pos, x, y) -> None:
+    """Rows of x ([n_tokens, heads, head_dim], elements adjacent, other strides free) turned by their
+    positions (int32 [n_tokens]) into y; y may be x."""
+    if x.dtype != y.dtype or x.dtype not in _TYPE_OF or x.dim() != 3 or x.shape != y.shape:
+        raise ValueError("x and y of one type and [n_tokens, heads, head_dim] expected")
+    device = _current(x)
+    xs, ys = x.stride(), y.stride()
+    if (x.shape[2] > 1 and (xs[2] != 1 or ys[2] != 1)) or y.get_device() != device or rope.device != device:
+        raise ValueError("rows of adjacent elements on one device expected")
+    n, heads, dim = x.shape
+    _check("aibx_rope", lib().aibx_rope(rope._pack(pos, n), n, heads, dim, x.data_ptr(), xs[0], xs[1], y.data_ptr(),
+                                        ys[0], ys[1], _TYPE_OF[x.dtype],
+                                        torch._C._cuda_getCurrentRawStream(device)))
+
+
+def rope_append(cache: KVCache, batch: KVBatch, rope: Rope, k, v, q=None, q_out=None, pos=None) -> None:
+    """kv_append of k turned by its positions and of v as it is; q ([n_tokens, q_heads, head_dim])
+    turned into q_out (which may be q) beside them.  pos: int32 [n_tokens], or the batch's positions."""
+    if k.dtype != v.dtype or k.dtype not in _TYPE_OF or (q is None) != (q_out is None):
+        raise ValueError("K, V and queries of one of bfloat16, float16, float32 expected")
+    stream = _here(cache, batch)
+    if rope.device != cache.device:
+        raise ValueError("all tensors of a call live on one CUDA device")
+    kp, kt, kh = _rows(k, cache, batch, cache.heads)
+    vp, vt, vh = _rows(v, cache, batch, cache.heads)
+    heads = qp = qt = qh = op = ot = oh = 0
+    if q is not None:
+        if q.dtype != k.dtype or q_out.dtype != k.dtype or q.dim() != 3:
+            raise ValueError("queries of K's type and [n_tokens, q_heads, head_dim] expected")
+        heads = q.shape[1]
+        qp, qt, qh = _rows(q, cache, batch, heads)
+        op, ot, oh = _rows(q_out, cache, batch, heads)
+    rows = _ROPE_ROWS_BYTES.pack(qp, op, kp, vp, qt, qh, ot, oh, kt, kh, vt, vh, heads, _TYPE_OF[k.dtype])
+    _check("aibx_rope_append", lib().aibx_rope_append(cache._ref, batch._ref, rope._pack(pos, batch.n_tokens), rows,
+                                                      stream))
+
+
+def kv_tables(held, new, block_tokens: int, num_blocks: int, free_ids, head, tail, block_table, tok_off,
+              kv_len, n_tokens: int, pos=None, slots=None, head_out=None, blk_off=None, match_ids=None,
+              match_off=None) -> None:
+    """Grows the requests' rows of block_table (uint32 [R, width], or flat with blk_off) from `held` to
+    held + new tokens (int32 [R]) by ids of the free list (free_ids uint32, a ring; head, tail int64 [1]:
+    numbers of the first id to take and of the first that is not there), and leaves tok_off (int64
+    [R+1]), kv_len (int32 [R], may be `held`), pos (int32 [n_tokens]), slots (int64 [n_tokens]) and the
+    new head (head_out, `head` itself if None).  match_ids (uint32) with match_off (int64 [R+1]): the
+    blocks that hold the held tokens, copied into the rows."""
+    device = _current(held)
+    R = held.numel()
+    if (match_ids is None) != (match_off is None):
+        raise ValueError("match_ids and match_off come together")
+    if blk_off is None and (block_table.dim() != 2 or block_table.shape[0] != R):
+        raise ValueError("a block table of %d rows expected" % R)
+
+    def vec(t, what, dtype, n):
+        return 0 if t is None else _vector(t, what, dtype, n, device)
+
+    ref = _TABLES_BYTES.pack(
+        vec(held, "held", torch.int32, R), vec(new, "new", torch.int32, R),
+        vec(free_ids, "free_ids", torch.uint32, free_ids.numel()), free_ids.numel(), vec(head, "head", torch.int64, 1),
+        vec(tail, "tail", torch.int64, 1), vec(head if head_out is None else head_out, "head_out", torch.int64, 1),
+        vec(block_table, "block_table", torch.uint32, block_table.numel()), vec(blk_off, "blk_off", torch.int64, R + 1),
+        0 if blk_off is not None else block_table.shape[1],
+        0 if match_ids is None else vec(match_ids, "match_ids", torch.uint32, match_ids.numel()),
+        vec(match_off, "match_off", torch.int64, R + 1), vec(tok_off, "tok_off", torch.int64, R + 1),
+        vec(kv_len, "kv_len", torch.int32, R), vec(pos, "pos", torch.int32, n_tokens),
+        vec(slots, "slots", torch.int64, n_tokens), n_tokens, block_tokens, num_blocks)
+    _check("aibx_kv_tables", lib().aibx_kv_tables(ref, R, torch._C._cuda_getCurrentRawStream(device)))
 
 
 def attn_workspace_bytes(cache: KVCache, batch: KVBatch, q) -> int:

@@ -19,6 +19,23 @@ struct SmallDivisor {
   unsigned long long m;
   __device__ __forceinline__ int div(int n) const { return (int)(((unsigned long long)n * m) >> 40); }
 };
+// Trees: a token's mask bits from d on (d may be negative), as far as they name one of its request's n
+// tokens.
+__device__ __forceinline__ uint32_t tree_bits(const uint32_t* row, int words, int n, int d) {
+  const int i = d >> 5;
+  const uint32_t lo = i >= 0 && i < words ? __ldg(row + i) : 0u;
+  const uint32_t hi = i >= -1 && i + 1 < words ? __ldg(row + i + 1) : 0u;
+  const int there = min(max(n - d, 0), 32);
+  return __funnelshift_r(lo, hi, d & 31) & (uint32_t)((1ull << there) - 1);
+}
+
+// How far a token stands above its request's cached ones: one less than the nodes that it sees of the tree.
+__device__ __forceinline__ int tree_depth(const uint32_t* row, int words, int n) {
+  int seen = 0;
+  for (int i = 0; i < words && 32 * i < n; ++i) seen += __popc(tree_bits(row, words, n, 32 * i));
+  return max(seen - 1, 0);
+}
+
 inline SmallDivisor small_divisor(int d) { return SmallDivisor{((1ull << 40) + d - 1) / d}; }
 
 constexpr float kLog2E = 1.4426950408889634f;
@@ -33,7 +50,10 @@ struct AttnArgs {
   float scale_log2;                         // scale * log2(e): scores in powers of two
   int G;                                    // query heads per KV head
   SmallDivisor by_g;
+  SmallDivisor by_pos;                      // by_g where a row's position follows its token; 0 for trees
   int causal, window;
+  const uint32_t* mask;                     // trees: 32-bit words of a token's mask, the lowest first
+  int mask_words;                           // how many
   int box, box_log;                         // tokens one tensor-map box covers: a power of two
   int row_limit;                            // requests of up to so many rows (tokens * G) are the
                                             // row kernel's, 0: none
@@ -333,6 +353,9 @@ attn_join_kernel(const __grid_constant__ AttnArgs a, JoinSet rows, JoinSet tiles
   if (a.max_new > 0 && blockIdx.x == 0 && blockIdx.y == 0)
     for (int r = threadIdx.x; r < a.b.R; r += 256)
       if (attn_request(a.b, a.pool.T, r).n > a.max_new) raise_status(AIBX_ERR_RANGE);
+  if (a.mask && blockIdx.x == 0 && blockIdx.y == 0)      // and those with more than their masks can name
+    for (int r = threadIdx.x; r < a.b.R; r += 256)
+      if (attn_request(a.b, a.pool.T, r).n > 32 * a.mask_words) raise_status(AIBX_ERR_RANGE);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const bool of_rows = (int)blockIdx.y < y_rows;
   const int y = of_rows ? (int)blockIdx.y : (int)blockIdx.y - y_rows;

@@ -5,6 +5,7 @@
 #include <math.h>
 
 #include "attn_tiles.cuh"
+#include "kv_tables.cuh"
 
 namespace aibx {
 
@@ -56,36 +57,81 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
   return AIBX_OK;
 }
 
-template <int D, bool F8, typename QT>
+template <int D, bool F8, typename QT, bool TREE>
 inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cudaStream_t st) {
   JoinSet rows = {nullptr, nullptr, 0}, tiles = rows;
   if (plan.rows) {
-    const int32_t rc = plan.row_limit == 8 ? launch_attn_rows<D, F8, QT, 8>(a, type, rows, st)
-                                           : launch_attn_rows<D, F8, QT, 16>(a, type, rows, st);
+    const int32_t rc = plan.row_limit == 8 ? launch_attn_rows<D, F8, QT, 8, TREE>(a, type, rows, st)
+                                           : launch_attn_rows<D, F8, QT, 16, TREE>(a, type, rows, st);
     if (rc != AIBX_OK) return rc;
     a.slots += plan.rows_bytes / sizeof(float);
   }
   if (plan.tiles) {
-    const int32_t rc = launch_attn_tiles<D, F8, QT>(a, type, tiles, st);
+    const int32_t rc = launch_attn_tiles<D, F8, QT, TREE>(a, type, tiles, st);
     if (rc != AIBX_OK) return rc;
   }
   return launch_join<D, QT>(a, rows, tiles, st);
 }
 
-template <int D>
+template <int D, bool TREE>
 inline int32_t launch_attn_dim(const AttnArgs& a, int type, int q_type, const AttnPlan& plan,
                                cudaStream_t st) {
   if (type == AIBX_TYPE_E4M3)
-    return q_type == AIBX_TYPE_BF16 ? launch_attn_kind<D, true, __nv_bfloat16>(a, type, plan, st)
-                                    : launch_attn_kind<D, true, __half>(a, type, plan, st);
-  return q_type == AIBX_TYPE_BF16 ? launch_attn_kind<D, false, __nv_bfloat16>(a, type, plan, st)
-                                  : launch_attn_kind<D, false, __half>(a, type, plan, st);
+    return q_type == AIBX_TYPE_BF16 ? launch_attn_kind<D, true, __nv_bfloat16, TREE>(a, type, plan, st)
+                                    : launch_attn_kind<D, true, __half, TREE>(a, type, plan, st);
+  return q_type == AIBX_TYPE_BF16 ? launch_attn_kind<D, false, __nv_bfloat16, TREE>(a, type, plan, st)
+                                  : launch_attn_kind<D, false, __half, TREE>(a, type, plan, st);
 }
 
+template <bool TREE>
 inline int32_t launch_attn(const AttnArgs& a, int type, int q_type, const AttnPlan& plan,
                            cudaStream_t st) {
-  return a.pool.D == 64 ? launch_attn_dim<64>(a, type, q_type, plan, st)
-                        : launch_attn_dim<128>(a, type, q_type, plan, st);
+  return a.pool.D == 64 ? launch_attn_dim<64, TREE>(a, type, q_type, plan, st)
+                        : launch_attn_dim<128, TREE>(a, type, q_type, plan, st);
+}
+
+// Both calls: `d_mask` for trees only.
+template <bool TREE>
+inline int32_t attention(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch, const aibx_attn_params_t* params,
+                         const uint64_t* d_mask, int32_t mask_words, const void* d_q, void* d_out, float* d_lse,
+                         void* d_workspace, uint64_t workspace_bytes, cudaStream_t st) {
+  AttnPlan plan;
+  int32_t rc = attn_plan(cache, batch, params, plan);
+  if (rc != AIBX_OK) return rc;
+  if (TREE && mask_words <= 0) return AIBX_ERR_INVALID;
+  if (TREE && mask_words > kTreeMaxWords) return AIBX_ERR_UNSUPPORTED;
+  AttnArgs a;
+  bool work;
+  rc = paged_views(cache, batch, a.pool, a.b, work);
+  if (rc != AIBX_OK || !work) return rc;
+  // a piece may still read queries of a row that another has written
+  if (!d_q || !d_out || !d_workspace || d_q == d_out) return AIBX_ERR_INVALID;
+  if ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_out) |
+       reinterpret_cast<uintptr_t>(d_workspace)) & 15)
+    return AIBX_ERR_INVALID;
+  if ((reinterpret_cast<uintptr_t>(d_lse) & 3) || workspace_bytes < plan.workspace)
+    return AIBX_ERR_INVALID;
+  if (TREE && (!d_mask || (reinterpret_cast<uintptr_t>(d_mask) & 7))) return AIBX_ERR_INVALID;
+  a.q = static_cast<const char*>(d_q);
+  a.out = static_cast<char*>(d_out);
+  a.lse = d_lse;
+  a.q_tok = params->q_token_stride;
+  a.q_head = params->q_head_stride;
+  a.o_tok = params->out_token_stride;
+  a.o_head = params->out_head_stride;
+  a.scale_log2 = params->scale * kLog2E;   // never 0: hidden keys are -infinity
+  a.G = plan.G;
+  a.by_g = small_divisor(plan.G);
+  a.by_pos = TREE ? SmallDivisor{0} : a.by_g;
+  a.causal = !TREE && params->causal != 0;
+  a.mask = TREE ? reinterpret_cast<const uint32_t*>(d_mask) : nullptr;
+  a.mask_words = 2 * mask_words;
+  a.window = params->window;
+  a.box = 0;
+  a.max_new = batch->max_new;
+  a.row_limit = plan.row_limit;
+  a.slots = static_cast<float*>(d_workspace);
+  return launch_attn<TREE>(a, cache->type, params->q_type, plan, st);
 }
 
 }  // namespace aibx

@@ -210,7 +210,7 @@ struct BoxIds {
   }
 };
 
-template <int D, bool F8, typename QT, int ROWS>
+template <int D, bool F8, typename QT, int ROWS, bool TREE>
 __global__ void __launch_bounds__(RowShape<D, F8, ROWS>::kThreads, 1)
 attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ AttnArgs a) {
@@ -403,6 +403,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     uint32_t qf[NQ][kPieces][kSteps][2];
     float qscale[NQ][2];
     int prow[NQ][2];
+    uint32_t tree[NQ][2];                                  // trees: the request's nodes that a row sees (at most 16)
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       const int i = x * 8 + g;
@@ -452,7 +453,12 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         qscale[x][h] = __shfl_sync(0xffffffffu, up, (2 * t4 + h) * 4) * a.scale_log2;
-        prow[x][h] = first + a.by_g.div(min(x * 8 + 2 * t4 + h, n_rows - 1));
+        const int ti = a.by_g.div(min(x * 8 + 2 * t4 + h, n_rows - 1));
+        prow[x][h] = first + ti;
+        if constexpr (TREE) {
+          tree[x][h] = tree_bits(a.mask + (walk.q.tok0 + ti) * a.mask_words, a.mask_words, walk.q.n, 0);
+          prow[x][h] = first + max(__popc(tree[x][h]) - 1, 0);
+        }
       }
     }
     int most = 0;                                          // largest V byte of the segment so far
@@ -468,7 +474,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
 
     // the rows' positions run from `first` to len - 1: keys from open_lo to open_hi - 1 all see
-    const int open_hi = a.causal ? min(walk.span.hi, first + 1) : walk.span.hi;
+    const int open_hi = TREE ? min(walk.span.hi, first) : a.causal ? min(walk.span.hi, first + 1) : walk.span.hi;
     const int open_lo = max(walk.span.lo, a.window > 0 ? walk.q.len - a.window : 0);
     for (int t = walk.t0; t < walk.t1; ++t) {
       // Every warp waits for every stage and hands every stage back, its own or not: a phase bit
@@ -594,8 +600,9 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             for (int x = 0; x < NQ; ++x)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                const bool ok = here && (!a.causal || key <= prow[x][h]) &&
-                                (a.window <= 0 || (long long)key > (long long)prow[x][h] - a.window);
+                bool ok = here && (TREE || !a.causal || key <= prow[x][h]) &&
+                          (a.window <= 0 || (long long)key > (long long)prow[x][h] - a.window);
+                if (TREE && key >= first) ok = here && ((tree[x][h] >> (key - first)) & 1u);
                 if (!ok) c[x][2 * r + h] = -INFINITY;
               }
           }
@@ -814,7 +821,7 @@ attn_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   }
 }
 
-template <int D, bool F8, typename QT, int ROWS>
+template <int D, bool F8, typename QT, int ROWS, bool TREE>
 inline int32_t launch_attn_rows(AttnArgs a, int type, JoinSet& join, cudaStream_t st) {
   using S = RowShape<D, F8, ROWS>;
   a.box = gcd_int(a.pool.T, S::kTok);
@@ -827,10 +834,10 @@ inline int32_t launch_attn_rows(AttnArgs a, int type, JoinSet& join, cudaStream_
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return AIBX_ERR_CUDA;
   static size_t configured[64] = {0};
   static std::mutex lock;
-  if (!ensure_dynamic_smem(attn_rows_kernel<D, F8, QT, ROWS>, S::kSmem, dev, configured, lock))
+  if (!ensure_dynamic_smem(attn_rows_kernel<D, F8, QT, ROWS, TREE>, S::kSmem, dev, configured, lock))
     return AIBX_ERR_CUDA;
   const unsigned int grid = (unsigned int)sm_count();
-  attn_rows_kernel<D, F8, QT, ROWS><<<grid, S::kThreads, S::kSmem, st>>>(map_k, map_v, a);
+  attn_rows_kernel<D, F8, QT, ROWS, TREE><<<grid, S::kThreads, S::kSmem, st>>>(map_k, map_v, a);
   join = JoinSet{a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot), ROWS};
   return launch_status();
 }

@@ -80,6 +80,60 @@ __device__ __forceinline__ int warp_find_request(const int64_t* tok_off, int R, 
   return behind ? -1 : lo;
 }
 
+// Where the `tokens` (a power of two up to 32) tokens from i0 on live; lane t holds token i0 + t mod
+// tokens: its position (kNoToken: none, a token of no request), and the byte offset of its slot in the
+// pool and (QUANT) among the scales, -1 where there is none.  False: all lie behind the last request.
+// `tell`: bad blocks raise RANGE here.
+constexpr long long kNoToken = -(1LL << 40);
+
+template <bool QUANT>
+__device__ __forceinline__ bool warp_token_places(const PagedPool& pool, const PagedBatch& b, long long i0,
+                                                  int tokens, bool tell, long long& pos, long long& place,
+                                                  long long& splace) {
+  const int lane = threadIdx.x & 31;
+  const int r0 = warp_find_request(b.tok_off, b.R, i0);
+  if (r0 < 0) return false;                               // padding behind the last request
+  const int t = lane & (tokens - 1);
+  const long long i = i0 + t;
+  const int behind = (int)min(__ldg(b.tok_off + min(r0 + 1 + lane, b.R)) - i0, (long long)(1 << 20));
+  int r = 0;                                              // requests that end at or before i
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1)
+    if (__shfl_sync(0xffffffffu, behind, r + d - 1) <= t) r += d;
+  const int last = __shfl_sync(0xffffffffu, behind, 31);
+  if (r == 31 && last <= t) r = 32;
+  r += r0;
+  // Past 32 requests (those without tokens count) the rest is halved: one by one, four tokens among 4,096
+  // requests took 82 us, now 6.
+  for (int end = r < r0 + 32 ? r : b.R; r < end;) {
+    const int mid = r + (end - r) / 2;
+    if (__ldg(b.tok_off + mid + 1) <= i)
+      r = mid + 1;
+    else
+      end = mid;
+  }
+  pos = kNoToken;
+  place = -1;
+  splace = 0;
+  if (r < b.R && i < b.n_tokens) {
+    pos = (long long)__ldg(b.kv_len + r) - (__ldg(b.tok_off + r + 1) - i);
+    if (pos >= 0) {
+      const uint32_t* row;
+      long long entries;
+      table_row(b, r, row, entries);
+      const int at = (int)pos / pool.T, slot = (int)pos - at * pool.T;
+      const uint32_t id = at < entries ? __ldg(row + at) : pool.num_blocks;
+      if (id < pool.num_blocks) {
+        place = (long long)id * pool.block + (long long)slot * pool.slot;
+        if (QUANT) splace = (long long)id * pool.s_block + (long long)slot * pool.s_slot;
+      } else if (id != AIBX_NO_BLOCK && tell && lane < tokens) {
+        raise_status(AIBX_ERR_RANGE);
+      }
+    }
+  }
+  return true;
+}
+
 // ------------------------------------------------------------------------------------------
 // elements of a row in registers
 
@@ -240,45 +294,8 @@ kv_token_kernel(PagedPool pool, PagedBatch b, PagedIO io) {
   if (i0 >= b.n_tokens) return;
   const int lane = threadIdx.x & 31;
 
-  // ---- lane t: where token i0 + t lives
-  const int r0 = warp_find_request(b.tok_off, b.R, i0);
-  if (r0 < 0) return;                                     // padding behind the last request
-  const int t = lane & (io.tokens - 1);
-  const long long i = i0 + t;
-  const int behind = (int)min(__ldg(b.tok_off + min(r0 + 1 + lane, b.R)) - i0, (long long)(1 << 20));
-  int r = 0;                                              // requests that end at or before i
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1)
-    if (__shfl_sync(0xffffffffu, behind, r + d - 1) <= t) r += d;
-  const int last = __shfl_sync(0xffffffffu, behind, 31);
-  if (r == 31 && last <= t) r = 32;
-  r += r0;
-  // Past 32 requests (those without tokens count) the rest is halved: one by one, four tokens among 4,096
-  // requests took 82 us, now 6.
-  for (int end = r < r0 + 32 ? r : b.R; r < end;) {
-    const int mid = r + (end - r) / 2;
-    if (__ldg(b.tok_off + mid + 1) <= i)
-      r = mid + 1;
-    else
-      end = mid;
-  }
-  long long place = -1, splace = 0;
-  if (r < b.R && i < b.n_tokens) {
-    const long long pos = (long long)__ldg(b.kv_len + r) - (__ldg(b.tok_off + r + 1) - i);
-    if (pos >= 0) {
-      const uint32_t* row;
-      long long entries;
-      table_row(b, r, row, entries);
-      const int at = (int)pos / pool.T, slot = (int)pos - at * pool.T;
-      const uint32_t id = at < entries ? __ldg(row + at) : pool.num_blocks;
-      if (id < pool.num_blocks) {
-        place = (long long)id * pool.block + (long long)slot * pool.slot;
-        if (kQuant) splace = (long long)id * pool.s_block + (long long)slot * pool.s_slot;
-      } else if (id != AIBX_NO_BLOCK && part == 0 && lane < io.tokens) {
-        raise_status(AIBX_ERR_RANGE);
-      }
-    }
-  }
+  long long pos, place, splace;                           // lane t: of token i0 + t
+  if (!warp_token_places<kQuant>(pool, b, i0, io.tokens, part == 0, pos, place, splace)) return;
 
   // ---- rows: `step` tokens at a time, a plane after the other
   const int lanes = 1 << io.lane_log, step = 32 >> io.lane_log;

@@ -1,0 +1,347 @@
+// What a step of an engine needs to know of its requests, from their lengths alone: block tables grown
+// from a free list, offsets, positions, slots (kv_tables), and the ancestor masks of drafted trees
+// (tree_masks).  Integers only.
+//
+// kv_tables, per request with h held and n new tokens, blocks of T slots:
+//   had = ceil(h / T), need = ceil((h + n) / T); F = sum of need - had over the requests before;
+//   table[had + k] = free[(head + F + k) mod capacity];  tok_off = sum of n before;  kv_len = h + n;
+//   token i: position p = h + i, slot table[p / T] * T + p mod T.
+// One launch: every CTA takes the prefix sums over all requests for itself, 512 at a time (they are a few
+// kilobytes out of L2, and a barrier or a second launch costs more than the sums), keeps them in shared
+// memory and then finds the request of each of its tokens by halving.  A new block's entry is written by
+// its first token: no search of its own.  Bound: launch and the chain lengths -> sums -> entry -> slot
+// for the calls that are usual; 12 bytes per token otherwise.
+//
+// tree_masks, per request: mask(i) = bit i, or that and mask(parent(i)).  In shared memory, twice as far
+// up each round: mask'(i) = mask(i) | mask(up(i)), up'(i) = up(up(i)), so that a chain of 512 takes nine
+// rounds; from one buffer to another, so that a round reads nothing that it writes.
+#pragma once
+
+#include <limits.h>
+
+#include "attn_common.cuh"
+
+namespace aibx {
+
+struct TablesArgs {
+  const int32_t *held, *fresh;     // tokens held, tokens new
+  int R, T;
+  uint32_t num_blocks;
+  const uint32_t* free_ids;
+  long long capacity;
+  const int64_t *head, *tail;
+  int64_t* head_out;
+  uint32_t* table;
+  const int64_t* blk_off;
+  long long stride;
+  const uint32_t* match;
+  const int64_t* match_off;
+  int64_t* tok_off;
+  int32_t* kv_len;
+  int32_t* pos;
+  int64_t* slots;
+  long long n_tokens;
+};
+
+constexpr int kTablesThreads = 512;
+
+// Last k in [0, n) with at[k] <= x (at[0] <= x): the request that holds x, past those without any.
+__device__ __forceinline__ int last_not_above(const long long* at, int n, long long x) {
+  int lo = 0;
+  while (n > 1) {
+    const int half = n >> 1;
+    if (at[lo + half] <= x) {
+      lo += half;
+      n -= half;
+    } else {
+      n = half;
+    }
+  }
+  return lo;
+}
+
+struct Lengths {
+  int h, n, had, need;
+  bool bad;
+};
+
+__device__ __forceinline__ Lengths request_lengths(const TablesArgs& a, int r) {
+  Lengths q = {0, 0, 0, 0, false};
+  if (r >= a.R) return q;
+  const int h = __ldg(a.held + r), n = __ldg(a.fresh + r);
+  q.bad = h < 0 || n < 0 || (long long)h + n > INT_MAX;
+  q.h = max(h, 0);
+  q.n = q.bad ? 0 : n;
+  q.had = (int)(((unsigned int)q.h + a.T - 1) / (unsigned int)a.T);
+  q.need = (int)(((unsigned int)q.h + q.n + a.T - 1) / (unsigned int)a.T);
+  return q;
+}
+
+// kTables: all but the two outputs that may stand in the place of inputs (kv_len, head), which need every
+// CTA to have read those; kCommit: these two.  A call with one CTA, or whose outputs stand apart, does both
+// at once; else a second launch of one CTA commits.
+template <bool TABLES, bool COMMIT>
+__global__ void __launch_bounds__(kTablesThreads)
+kv_tables_kernel(const __grid_constant__ TablesArgs a) {
+  constexpr int N = kTablesThreads;
+  __shared__ long long s_scan[33];
+  __shared__ long long s_tok[N], s_free[N], s_ent[N], s_row[N];
+  __shared__ int s_held[N], s_had[N], s_width[N];
+  const int tid = threadIdx.x;
+  const long long head = *a.head;
+  long long left = *a.tail - head;                         // ids to be had
+  left = left < 0 ? 0 : left > a.capacity ? a.capacity : left;
+  long long start = head % a.capacity;
+  if (start < 0) start += a.capacity;
+
+  auto matched = [&](int r, int e) -> uint32_t {           // entry e of request r among the matched ids
+    const long long at = __ldg(a.match_off + r);
+    if (e < __ldg(a.match_off + r + 1) - at) return __ldg(a.match + at + e);
+    raise_status(AIBX_ERR_RANGE);
+    return AIBX_NO_BLOCK;
+  };
+
+  long long tok_base = 0, free_base = 0;
+  for (int r0 = 0; r0 < a.R; r0 += N) {
+    const int r = r0 + tid, rows = min(N, a.R - r0);
+    const Lengths q = request_lengths(a, r);
+    long long row = 0, width = 0;
+    if (r < a.R) {
+      row = a.blk_off ? __ldg(a.blk_off + r) : (long long)r * a.stride;
+      width = a.blk_off ? __ldg(a.blk_off + r + 1) - row : a.stride;
+      width = width < 0 ? 0 : width > INT_MAX ? INT_MAX : width;
+    }
+    const int have = min(q.had, (int)width), new_blocks = max(min(q.need, (int)width) - q.had, 0);
+    long long toks, frees, ents = 0, before_ent = 0;
+    const long long before_tok = block_prefix<N>(q.n, s_scan, toks);
+    const long long before_free = block_prefix<N>(new_blocks, s_scan, frees);
+    if (TABLES) {
+      if (a.match) before_ent = block_prefix<N>(r < a.R ? have : 0, s_scan, ents);
+      s_tok[tid] = before_tok;
+      s_free[tid] = free_base + before_free;
+      s_ent[tid] = before_ent;
+      s_row[tid] = row;
+      s_held[tid] = q.h;
+      s_had[tid] = q.had;
+      s_width[tid] = (int)width;
+      if (blockIdx.x == (unsigned int)(r0 / N) % gridDim.x && r < a.R) {
+        if (q.bad || (q.n > 0 && q.need > width)) raise_status(AIBX_ERR_RANGE);
+        a.tok_off[r] = tok_base + before_tok;
+      }
+    }
+    if (COMMIT && blockIdx.x == (unsigned int)(r0 / N) % gridDim.x && r < a.R) a.kv_len[r] = q.h + q.n;
+    if (TABLES) {
+      __syncthreads();
+      for (long long i = (long long)blockIdx.x * N + tid; i < toks; i += (long long)gridDim.x * N) {
+        const int k = last_not_above(s_tok, rows, i);
+        const int p = s_held[k] + (int)(i - s_tok[k]);
+        const int blk = p / a.T, off = p - blk * a.T;
+        uint32_t id = AIBX_NO_BLOCK;
+        if (blk < s_width[k]) {
+          if (blk >= s_had[k]) {
+            const long long f = s_free[k] + (blk - s_had[k]);
+            if (f < left) id = __ldg(a.free_ids + (start + f < a.capacity ? start + f : start + f - a.capacity));
+            if (off == 0) a.table[s_row[k] + blk] = id;
+          } else {
+            id = a.match ? matched(r0 + k, blk) : a.table[s_row[k] + blk];
+          }
+        }
+        if (id >= a.num_blocks && id != AIBX_NO_BLOCK) raise_status(AIBX_ERR_RANGE);
+        const long long t = tok_base + i;
+        if (t < a.n_tokens) {
+          if (a.pos) a.pos[t] = p;
+          if (a.slots) a.slots[t] = id < a.num_blocks ? (int64_t)id * a.T + off : -1;
+        }
+      }
+      for (long long e = (long long)blockIdx.x * N + tid; e < ents; e += (long long)gridDim.x * N) {
+        const int k = last_not_above(s_ent, rows, e);
+        const int at = (int)(e - s_ent[k]);
+        a.table[s_row[k] + at] = matched(r0 + k, at);
+      }
+      __syncthreads();
+    }
+    tok_base += toks;
+    free_base += frees;
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    if (TABLES) {
+      a.tok_off[a.R] = tok_base;
+      if (free_base > left) raise_status_n(AIBX_ERR_FULL, (unsigned long long)(free_base - left));
+      if (tok_base > a.n_tokens) raise_status(AIBX_ERR_RANGE);
+    }
+    if (COMMIT) *a.head_out = head + (free_base < left ? free_base : left);
+  }
+}
+
+inline int32_t kv_tables(const aibx_kv_tables_t* t, int32_t R, cudaStream_t st) {
+  if (!t || R < 0 || t->block_tokens <= 0 || t->table_stride < 0 || t->free_capacity < 0 || t->n_tokens < 0)
+    return AIBX_ERR_INVALID;
+  if (t->block_tokens > 65536) return AIBX_ERR_UNSUPPORTED;
+  if (R == 0) return AIBX_OK;
+  if (!t->d_held || !t->d_new || !t->d_free_ids || !t->d_free_head || !t->d_free_tail || !t->d_free_head_out ||
+      !t->d_block_table || !t->d_tok_off || !t->d_kv_len || t->free_capacity == 0 ||
+      (t->d_match_ids == nullptr) != (t->d_match_off == nullptr))
+    return AIBX_ERR_INVALID;
+  const uintptr_t four = reinterpret_cast<uintptr_t>(t->d_held) | reinterpret_cast<uintptr_t>(t->d_new) |
+                         reinterpret_cast<uintptr_t>(t->d_free_ids) | reinterpret_cast<uintptr_t>(t->d_block_table) |
+                         reinterpret_cast<uintptr_t>(t->d_kv_len) | reinterpret_cast<uintptr_t>(t->d_match_ids) |
+                         reinterpret_cast<uintptr_t>(t->d_pos);
+  const uintptr_t eight = reinterpret_cast<uintptr_t>(t->d_free_head) | reinterpret_cast<uintptr_t>(t->d_free_tail) |
+                          reinterpret_cast<uintptr_t>(t->d_free_head_out) | reinterpret_cast<uintptr_t>(t->d_blk_off) |
+                          reinterpret_cast<uintptr_t>(t->d_match_off) | reinterpret_cast<uintptr_t>(t->d_tok_off) |
+                          reinterpret_cast<uintptr_t>(t->d_slots);
+  if ((four & 3) || (eight & 7)) return AIBX_ERR_INVALID;
+  // written by some threads while others read
+  if (t->d_kv_len == t->d_new || t->d_pos == t->d_held || t->d_pos == t->d_new || t->d_block_table == t->d_match_ids ||
+      t->d_block_table == t->d_free_ids || t->d_free_head_out == t->d_free_tail)
+    return AIBX_ERR_INVALID;
+  TablesArgs a;
+  a.held = t->d_held;
+  a.fresh = t->d_new;
+  a.R = R;
+  a.T = t->block_tokens;
+  a.num_blocks = t->num_blocks;
+  a.free_ids = t->d_free_ids;
+  a.capacity = t->free_capacity;
+  a.head = t->d_free_head;
+  a.tail = t->d_free_tail;
+  a.head_out = t->d_free_head_out;
+  a.table = t->d_block_table;
+  a.blk_off = t->d_blk_off;
+  a.stride = t->table_stride;
+  a.match = t->d_match_ids;
+  a.match_off = t->d_match_off;
+  a.tok_off = t->d_tok_off;
+  a.kv_len = t->d_kv_len;
+  a.pos = t->d_pos;
+  a.slots = t->d_slots;
+  a.n_tokens = t->n_tokens;
+  // four tokens or matched entries per thread, as far as the host can tell
+  const long long most = sm_count(), each = 4 * kTablesThreads;
+  const double copies = !a.match ? 0.0 : a.blk_off ? 1e18 : (double)a.stride * R;
+  const double want = ((double)a.n_tokens + copies) / each;
+  const unsigned int grid = want >= (double)most ? (unsigned int)most : want > 1.0 ? (unsigned int)want + 1 : 1u;
+  const bool apart = a.kv_len != a.held && a.head_out != a.head;
+  if (grid == 1 || apart) {
+    kv_tables_kernel<true, true><<<grid, kTablesThreads, 0, st>>>(a);
+  } else {
+    kv_tables_kernel<true, false><<<grid, kTablesThreads, 0, st>>>(a);
+    kv_tables_kernel<false, true><<<1, kTablesThreads, 0, st>>>(a);
+  }
+  return launch_status();
+}
+
+// ------------------------------------------------------------------------------------------
+// ancestors
+
+struct TreeArgs {
+  const int32_t* parent;
+  const int64_t* tok_off;
+  const int32_t* kv_len;
+  unsigned long long* mask;
+  int32_t* pos;
+  long long n_tokens;
+  int R;
+};
+
+constexpr int kTreeMaxWords = 8;
+template <int W>
+constexpr int kTreeThreads = W >= 4 ? 512 : W >= 2 ? 256 : 64;
+
+template <int W>
+__global__ void __launch_bounds__(kTreeThreads<W>)
+tree_masks_kernel(TreeArgs a) {
+  constexpr int N = kTreeThreads<W>, kNodes = 64 * W;
+  extern __shared__ unsigned long long s_mask[];           // [2][kNodes][W]
+  short* s_up = reinterpret_cast<short*>(s_mask + 2 * kNodes * W);   // [2][kNodes]
+  const int tid = threadIdx.x;
+  for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
+    const long long tok0 = __ldg(a.tok_off + r);
+    const long long end = min((long long)__ldg(a.tok_off + r + 1), a.n_tokens);
+    if (tok0 < 0 || end <= tok0) continue;
+    if (end - tok0 > kNodes) {
+      if (tid == 0) raise_status(AIBX_ERR_RANGE);
+      continue;
+    }
+    const int n = (int)(end - tok0);
+    bool more = false;
+    for (int i = tid; i < n; i += N) {
+      const int p = __ldg(a.parent + tok0 + i);
+      if (p >= i) raise_status(AIBX_ERR_RANGE);
+      s_up[i] = (short)(p < 0 || p >= i ? -1 : p);
+      more |= p >= 0 && p < i;
+    }
+    for (int x = tid; x < n * W; x += N) {
+      const int i = x / W;
+      s_mask[x] = x - i * W == i >> 6 ? 1ull << (i & 63) : 0ull;
+    }
+    int cur = 0;
+    while (__syncthreads_or(more)) {
+      const unsigned long long* m0 = s_mask + cur * kNodes * W;
+      unsigned long long* m1 = s_mask + (cur ^ 1) * kNodes * W;
+      const short* u0 = s_up + cur * kNodes;
+      short* u1 = s_up + (cur ^ 1) * kNodes;
+      more = false;
+      for (int x = tid; x < n * W; x += N) {
+        const int i = x / W, w = x - i * W, j = u0[i];
+        m1[x] = j >= 0 ? m0[x] | m0[j * W + w] : m0[x];
+        if (w == 0) {
+          const int up = j >= 0 ? u0[j] : -1;
+          u1[i] = (short)up;
+          more |= up >= 0;
+        }
+      }
+      cur ^= 1;
+    }
+    const unsigned long long* m = s_mask + cur * kNodes * W;
+    for (int x = tid; x < n * W; x += N) a.mask[tok0 * W + x] = m[x];
+    if (a.pos) {
+      const int base = __ldg(a.kv_len + r) - n;
+      for (int i = tid; i < n; i += N) {
+        int above = -1;
+#pragma unroll
+        for (int w = 0; w < W; ++w) above += __popcll(m[i * W + w]);
+        a.pos[tok0 + i] = base + above;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <int W>
+inline int32_t launch_tree_masks(const TreeArgs& a, cudaStream_t st) {
+  constexpr size_t smem = (size_t)2 * 64 * W * (8 * W + 2);
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return AIBX_ERR_CUDA;
+  static size_t configured[64] = {0};
+  static std::mutex lock;
+  if (smem > 48 * 1024 && !ensure_dynamic_smem(tree_masks_kernel<W>, smem, dev, configured, lock)) return AIBX_ERR_CUDA;
+  const long long most = (long long)sm_count() * 8;
+  tree_masks_kernel<W><<<(unsigned int)(a.R < most ? a.R : most), kTreeThreads<W>, smem, st>>>(a);
+  return launch_status();
+}
+
+inline int32_t tree_masks(const int32_t* parent, const int64_t* tok_off, const int32_t* kv_len, int32_t R,
+                          int64_t n_tokens, int32_t words, uint64_t* mask, int32_t* pos, cudaStream_t st) {
+  if (R < 0 || n_tokens < 0 || words <= 0) return AIBX_ERR_INVALID;
+  if (words > kTreeMaxWords) return AIBX_ERR_UNSUPPORTED;
+  if (R == 0 || n_tokens == 0) return AIBX_OK;
+  if (!parent || !tok_off || !mask || (pos && !kv_len)) return AIBX_ERR_INVALID;
+  if (((reinterpret_cast<uintptr_t>(parent) | reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(pos)) & 3) ||
+      ((reinterpret_cast<uintptr_t>(tok_off) | reinterpret_cast<uintptr_t>(mask)) & 7) || pos == parent ||
+      (pos && pos == kv_len))
+    return AIBX_ERR_INVALID;
+  const TreeArgs a = {parent, tok_off, kv_len, reinterpret_cast<unsigned long long*>(mask), pos, n_tokens, R};
+  switch (words) {
+    case 1: return launch_tree_masks<1>(a, st);
+    case 2: return launch_tree_masks<2>(a, st);
+    case 3: return launch_tree_masks<3>(a, st);
+    case 4: return launch_tree_masks<4>(a, st);
+    case 5: return launch_tree_masks<5>(a, st);
+    case 6: return launch_tree_masks<6>(a, st);
+    case 7: return launch_tree_masks<7>(a, st);
+    default: return launch_tree_masks<8>(a, st);
+  }
+}
+
+}  // namespace aibx

@@ -14,6 +14,8 @@
 #include "kv_copy.cuh"
 #include "kv_paged.cuh"
 #include "kv_permute.cuh"
+#include "kv_tables.cuh"
+#include "rope.cuh"
 #include "selftest.cuh"
 #include "route_head.cuh"
 #include "route_score.cuh"
@@ -906,37 +908,42 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
                         const aibx_attn_params_t* params, const void* d_q, void* d_out,
                         float* d_lse, void* d_workspace, uint64_t workspace_bytes, void* stream) {
   AIBX_CALL_RANGE();
-  AttnPlan plan;
-  int32_t rc = attn_plan(cache, batch, params, plan);
-  if (rc != AIBX_OK) return rc;
-  AttnArgs a;
-  bool work;
-  rc = paged_views(cache, batch, a.pool, a.b, work);
-  if (rc != AIBX_OK || !work) return rc;
-  // a piece may still read queries of a row that another has written
-  if (!d_q || !d_out || !d_workspace || d_q == d_out) return AIBX_ERR_INVALID;
-  if ((reinterpret_cast<uintptr_t>(d_q) | reinterpret_cast<uintptr_t>(d_out) |
-       reinterpret_cast<uintptr_t>(d_workspace)) & 15)
-    return AIBX_ERR_INVALID;
-  if ((reinterpret_cast<uintptr_t>(d_lse) & 3) || workspace_bytes < plan.workspace)
-    return AIBX_ERR_INVALID;
-  a.q = static_cast<const char*>(d_q);
-  a.out = static_cast<char*>(d_out);
-  a.lse = d_lse;
-  a.q_tok = params->q_token_stride;
-  a.q_head = params->q_head_stride;
-  a.o_tok = params->out_token_stride;
-  a.o_head = params->out_head_stride;
-  a.scale_log2 = params->scale * kLog2E;   // never 0: hidden keys are -infinity
-  a.G = plan.G;
-  a.by_g = small_divisor(plan.G);
-  a.causal = params->causal != 0;
-  a.window = params->window;
-  a.box = 0;
-  a.max_new = batch->max_new;
-  a.row_limit = plan.row_limit;
-  a.slots = static_cast<float*>(d_workspace);
-  return launch_attn(a, cache->type, params->q_type, plan, as_stream(stream));
+  return attention<false>(cache, batch, params, nullptr, 0, d_q, d_out, d_lse, d_workspace, workspace_bytes,
+                          as_stream(stream));
+}
+
+int32_t aibx_attn_tree(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
+                       const aibx_attn_params_t* params, const uint64_t* d_mask, int32_t mask_words,
+                       const void* d_q, void* d_out, float* d_lse, void* d_workspace,
+                       uint64_t workspace_bytes, void* stream) {
+  AIBX_CALL_RANGE();
+  return attention<true>(cache, batch, params, d_mask, mask_words, d_q, d_out, d_lse, d_workspace,
+                         workspace_bytes, as_stream(stream));
+}
+
+int32_t aibx_tree_masks(const int32_t* d_parent, const int64_t* d_tok_off, const int32_t* d_kv_len, int32_t R,
+                        int64_t n_tokens, int32_t mask_words, uint64_t* d_mask, int32_t* d_pos, void* stream) {
+  AIBX_CALL_RANGE();
+  return tree_masks(d_parent, d_tok_off, d_kv_len, R, n_tokens, mask_words, d_mask, d_pos, as_stream(stream));
+}
+
+int32_t aibx_kv_tables(const aibx_kv_tables_t* tables, int32_t R, void* stream) {
+  AIBX_CALL_RANGE();
+  return kv_tables(tables, R, as_stream(stream));
+}
+
+int32_t aibx_rope(const aibx_rope_t* rope, int64_t n_tokens, int32_t num_heads, int32_t head_dim, const void* d_x,
+                  int64_t x_token_stride, int64_t x_head_stride, void* d_y, int64_t y_token_stride,
+                  int64_t y_head_stride, int32_t type, void* stream) {
+  AIBX_CALL_RANGE();
+  return rope_rows(rope, n_tokens, num_heads, head_dim, d_x, x_token_stride, x_head_stride, d_y, y_token_stride,
+                   y_head_stride, type, as_stream(stream));
+}
+
+int32_t aibx_rope_append(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch, const aibx_rope_t* rope,
+                         const aibx_rope_rows_t* rows, void* stream) {
+  AIBX_CALL_RANGE();
+  return rope_append(cache, batch, rope, rows, as_stream(stream));
 }
 
 int32_t aibx_kv_set_tuning(int32_t mode, int32_t chunk_bytes, int32_t stages,
