@@ -632,15 +632,19 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
  *   positions j < base (window > 0: those with j > base + depth - window, depth = the number of nodes
  *   that it sees less one, at least 0) and the nodes whose bits are set in its row of d_mask - any rows,
  *   not only those of trees, and a node need not see itself.  Bits of nodes that the request has not are
- *   ignored.  params->causal is not read.  Everything else as aibx_attn_paged: formats, shapes, errors,
- *   roundings, workspace (aibx_attn_workspace_bytes of the same arguments); a NaN or infinite V of a
- *   position from base - window + 1 on that is hidden from a row may reach it.  INVALID for a null or
+ *   ignored.  params->causal is not read.  Everything else as aibx_attn_paged (formats, shapes, errors, the
+ *   same bits every time), but: weights over an E4M3 pool may be held as bf16, or with FP16 queries as the
+ *   sum of two bf16 numbers; a NaN or infinite V of a position from base - window + 1 on that is hidden
+ *   from a row may reach it; the workspace is of aibx_attn_tree_workspace_bytes bytes, which depend on
+ *   head_dim, num_q_heads / num_kv_heads, max_new, the types and the device alone.  INVALID for a null or
  *   unaligned d_mask or mask_words < 1, UNSUPPORTED for more than 8 words, RANGE for a request with more
  *   than 64 * mask_words tokens (whose later nodes count as hidden).
  */
 int32_t aibx_tree_masks(const int32_t* d_parent, const int64_t* d_tok_off, const int32_t* d_kv_len,
                         int32_t R, int64_t n_tokens, int32_t mask_words, uint64_t* d_mask,
                         int32_t* d_pos, void* stream);
+uint64_t aibx_attn_tree_workspace_bytes(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
+                                        const aibx_attn_params_t* params);
 int32_t aibx_attn_tree(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
                        const aibx_attn_params_t* params, const uint64_t* d_mask, int32_t mask_words,
                        const void* d_q, void* d_out, float* d_lse, void* d_workspace,

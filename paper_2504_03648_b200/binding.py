@@ -168,6 +168,8 @@ def lib():
             fn.restype = i32
         L.aibx_attn_workspace_bytes.argtypes = [vp, vp, vp]
         L.aibx_attn_workspace_bytes.restype = u64
+        L.aibx_attn_tree_workspace_bytes.argtypes = [vp, vp, vp]
+        L.aibx_attn_tree_workspace_bytes.restype = u64
         L.aibx_collect_scratch_bytes.argtypes = [u32]
         L.aibx_collect_scratch_bytes.restype = u64
         L.aibx_route_collect_scratch_bytes.argtypes = [u32]
@@ -625,8 +627,8 @@ def _attention(name: str, cache: KVCache, batch: KVBatch, tree, q, out, lse, sca
                            cache.head_dim ** -0.5 if scale is None else scale, 1 if causal else 0, window)
     L = lib()
     if workspace is None:
-        workspace = q.new_empty(max(L.aibx_attn_workspace_bytes(cache._ref, batch._ref, ref), 16),
-                                dtype=torch.uint8)
+        size = L.aibx_attn_tree_workspace_bytes if tree else L.aibx_attn_workspace_bytes
+        workspace = q.new_empty(max(size(cache._ref, batch._ref, ref), 16), dtype=torch.uint8)
     elif workspace.get_device() != cache.device or not workspace.is_contiguous():
         raise ValueError("a contiguous workspace on the pool's device expected")
     _check(name, getattr(L, name)(cache._ref, batch._ref, ref, *tree, qp, op, lp, workspace.data_ptr(),
@@ -799,10 +801,19 @@ def kv_tables(held, new, block_tokens: int, num_blocks: int, free_ids, head, tai
     _check("aibx_kv_tables", lib().aibx_kv_tables(ref, R, torch._C._cuda_getCurrentRawStream(device)))
 
 
+def _workspace_bytes(name: str, cache: KVCache, batch: KVBatch, q) -> int:
+    return int(getattr(lib(), name)(cache._ref, batch._ref, _ATTN_BYTES.pack(
+        _TYPE_OF.get(q.dtype, -1), q.shape[1], 8, 8, 8, 8, 1.0, 1, 0)))
+
+
 def attn_workspace_bytes(cache: KVCache, batch: KVBatch, q) -> int:
     """Workspace of attn_paged for queries shaped like q; 0 where attn_paged would refuse."""
-    return int(lib().aibx_attn_workspace_bytes(cache._ref, batch._ref, _ATTN_BYTES.pack(
-        _TYPE_OF.get(q.dtype, -1), q.shape[1], 8, 8, 8, 8, 1.0, 1, 0)))
+    return _workspace_bytes("aibx_attn_workspace_bytes", cache, batch, q)
+
+
+def attn_tree_workspace_bytes(cache: KVCache, batch: KVBatch, q) -> int:
+    """The same of attn_tree."""
+    return _workspace_bytes("aibx_attn_tree_workspace_bytes", cache, batch, q)
 
 
 def kv_set_tuning(mode: int = -1, chunk_bytes: int = 0, stages: int = 0,

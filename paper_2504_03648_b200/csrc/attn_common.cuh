@@ -50,7 +50,6 @@ struct AttnArgs {
   float scale_log2;                         // scale * log2(e): scores in powers of two
   int G;                                    // query heads per KV head
   SmallDivisor by_g;
-  SmallDivisor by_pos;                      // by_g where a row's position follows its token; 0 for trees
   int causal, window;
   const uint32_t* mask;                     // trees: 32-bit words of a token's mask, the lowest first
   int mask_words;                           // how many

@@ -1,10 +1,10 @@
-// Host side of attn_paged: checks, the choice of kernels and the workspace.
+// Host side of attn_paged and attn_tree: checks, the choice of kernels and the workspace.
 #pragma once
 
 #include <float.h>
 #include <math.h>
 
-#include "attn_tiles.cuh"
+#include "attn_cols.cuh"
 #include "kv_tables.cuh"
 
 namespace aibx {
@@ -13,6 +13,7 @@ struct AttnPlan {
   int G = 0;
   int row_limit = 0;                     // rows up to which a request is the row kernel's
   bool rows = false, tiles = false;      // which kernels run
+  int cols = 0;                          // trees: rows of a block of the third, 0: not that one
   uint64_t rows_bytes = 0, workspace = 0;
 };
 
@@ -25,8 +26,13 @@ inline uint64_t slot_bytes(int rows, int dim) {
 // single request; both for a batch, each taking the requests of its kind.  The row kernel comes
 // for 8 rows and for 16; beside the tile kernel it is the one for 8 where that holds a request's
 // single token.
+//
+// Trees: the row kernel alone where no request can have more than 8 rows (at 16 it takes 206 us where
+// the other takes 127: twice the products, and registers spill); else the kernel with the keys as M for all,
+// in blocks of 64 rows where none has more (half the registers and shared memory of 128).  fp16 queries over
+// e4m3 keep weights twice, for which blocks of 128 leave no room.
 inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
-                         const aibx_attn_params_t* p, AttnPlan& plan) {
+                         const aibx_attn_params_t* p, bool tree, AttnPlan& plan) {
   PagedPool pool;
   PagedBatch batch;
   bool work;
@@ -49,6 +55,13 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
   plan.G = p->num_q_heads / L.num_kv_heads;
   if (plan.G > 128 || L.num_blocks > 0x7fffffffu || b->n_tokens >= (1 << 24)) return AIBX_ERR_UNSUPPORTED;
   const long long bound = b->max_new > 0 ? b->max_new : (1LL << 31);
+  if (tree) {
+    plan.rows = bound * plan.G <= 8;
+    if (plan.rows) plan.row_limit = 8;
+    else plan.cols = bound * plan.G <= 64 || (c->type == AIBX_TYPE_E4M3 && p->q_type == AIBX_TYPE_FP16) ? 64 : 128;
+    plan.workspace = slot_bytes(plan.rows ? 8 : plan.cols, L.head_dim);
+    return AIBX_OK;
+  }
   plan.tiles = bound * plan.G > 16;
   plan.rows = !plan.tiles || (b->R > 1 && plan.G <= 16);
   if (plan.rows) plan.row_limit = (plan.tiles ? plan.G : bound * plan.G) <= 8 ? 8 : 16;
@@ -60,14 +73,21 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
 template <int D, bool F8, typename QT, bool TREE>
 inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cudaStream_t st) {
   JoinSet rows = {nullptr, nullptr, 0}, tiles = rows;
+  if constexpr (TREE) {
+    constexpr int kMost = F8 && std::is_same<QT, __half>::value ? 64 : 128;
+    const int32_t rc = plan.rows         ? launch_attn_rows<D, F8, QT, 8, true>(a, type, rows, st)
+                       : plan.cols == 64 ? launch_attn_cols<D, F8, QT, 64>(a, type, tiles, st)
+                                         : launch_attn_cols<D, F8, QT, kMost>(a, type, tiles, st);
+    return rc != AIBX_OK ? rc : launch_join<D, QT>(a, rows, tiles, st);
+  }
   if (plan.rows) {
-    const int32_t rc = plan.row_limit == 8 ? launch_attn_rows<D, F8, QT, 8, TREE>(a, type, rows, st)
-                                           : launch_attn_rows<D, F8, QT, 16, TREE>(a, type, rows, st);
+    const int32_t rc = plan.row_limit == 8 ? launch_attn_rows<D, F8, QT, 8, false>(a, type, rows, st)
+                                           : launch_attn_rows<D, F8, QT, 16, false>(a, type, rows, st);
     if (rc != AIBX_OK) return rc;
     a.slots += plan.rows_bytes / sizeof(float);
   }
   if (plan.tiles) {
-    const int32_t rc = launch_attn_tiles<D, F8, QT, TREE>(a, type, tiles, st);
+    const int32_t rc = launch_attn_tiles<D, F8, QT>(a, type, tiles, st);
     if (rc != AIBX_OK) return rc;
   }
   return launch_join<D, QT>(a, rows, tiles, st);
@@ -96,7 +116,7 @@ inline int32_t attention(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* ba
                          const uint64_t* d_mask, int32_t mask_words, const void* d_q, void* d_out, float* d_lse,
                          void* d_workspace, uint64_t workspace_bytes, cudaStream_t st) {
   AttnPlan plan;
-  int32_t rc = attn_plan(cache, batch, params, plan);
+  int32_t rc = attn_plan(cache, batch, params, TREE, plan);
   if (rc != AIBX_OK) return rc;
   if (TREE && mask_words <= 0) return AIBX_ERR_INVALID;
   if (TREE && mask_words > kTreeMaxWords) return AIBX_ERR_UNSUPPORTED;
@@ -122,7 +142,6 @@ inline int32_t attention(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* ba
   a.scale_log2 = params->scale * kLog2E;   // never 0: hidden keys are -infinity
   a.G = plan.G;
   a.by_g = small_divisor(plan.G);
-  a.by_pos = TREE ? SmallDivisor{0} : a.by_g;
   a.causal = !TREE && params->causal != 0;
   a.mask = TREE ? reinterpret_cast<const uint32_t*>(d_mask) : nullptr;
   a.mask_words = 2 * mask_words;

@@ -43,15 +43,14 @@ constexpr int kTileKeys = 128;
 constexpr int kKeySpread = 14;       // of K's bytes in a tile: times 2^-14, fp16's least normal number, e4m3 is exact
 constexpr int kInfoRing = 16;        // per-step facts the softmax reads: far deeper than the rings
 
-template <int D, bool F8, bool TREE>
+template <int D, bool F8>
 struct TileShape {
   static constexpr int kThreads = F8 ? 512 : 384;
   static constexpr int kRaw = kTileKeys * D;               // a tile's e4m3 rows, as they arrive
   // One K or V tile as MMA operand.  Raw rows arrive 16 KB into the buffer: at D = 128 that is the
   // second column, and every 128-byte raw row lies where the second half of its own fp16 row goes.
   static constexpr int kBuf = kTileKeys * D * 2 + (F8 && D == 64 ? kRaw : 0);
-  // Trees: a multiple of four, so that in a split segment a buffer is always the same tile's (see there).
-  static constexpr int kBufs = TREE ? (D == 64 && !F8 ? 8 : 4) : D == 64 ? (F8 ? 6 : 8) : (F8 ? 4 : 5);
+  static constexpr int kBufs = D == 64 ? (F8 ? 6 : 8) : (F8 ? 4 : 5);
   static constexpr int kFactorRing = 4;
   static constexpr int kCols = D / 64;                     // 128-byte columns of an operand row
   static constexpr int kColBytes = 128 * 128;
@@ -123,12 +122,6 @@ __device__ __forceinline__ void tmem_ld32(unsigned int addr, uint32_t* r) {
         "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
 }
-__device__ __forceinline__ void tmem_ld2(unsigned int addr, uint32_t* r) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr));
-}
-__device__ __forceinline__ void tmem_st2(unsigned int addr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%2], {%0,%1};" ::"r"(r[0]), "r"(r[1]), "r"(addr) : "memory");
-}
 __device__ __forceinline__ void tmem_st32(unsigned int addr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
@@ -181,29 +174,36 @@ struct TileSpan {
   int lo, hi, tile0, tiles;
 };
 
-__device__ __forceinline__ TileSpan tile_span(const AttnArgs& a, const AttnRequest& q, int block) {
-  const int rows = q.n * a.G;
-  const int r0 = block * 2 * kTileRows, r1 = min(r0 + 2 * kTileRows, rows) - 1;
-  const long long first = (long long)q.len - q.n;
-  TileSpan s;
-  long long hi = a.causal ? first + a.by_g.div(r1) + 1 : q.keys;
-  hi = hi < 0 ? 0 : hi > q.keys ? q.keys : hi;
-  long long lo = a.window > 0 ? first + a.by_pos.div(r0) - a.window + 1 : 0;
-  lo = lo < 0 ? 0 : lo > hi ? hi : lo;
-  s.hi = (int)hi;
-  s.lo = (int)lo;
-  s.tile0 = s.lo / kTileKeys;
-  s.tiles = max(1, (int)(((unsigned int)s.hi + kTileKeys - 1) / kTileKeys) - s.tile0);
-  return s;
-}
+// How a request's rows are cut into blocks, and which tiles a block has: of 256 rows, two tiles of a CTA.
+struct PairBlocks {
+  static __device__ __forceinline__ int size(int) { return 2 * kTileRows; }
+  static __device__ __forceinline__ TileSpan span(const AttnArgs& a, const AttnRequest& q, int block) {
+    const int rows = q.n * a.G;
+    const int r0 = block * 2 * kTileRows, r1 = min(r0 + 2 * kTileRows, rows) - 1;
+    const long long first = (long long)q.len - q.n;
+    TileSpan s;
+    long long hi = a.causal ? first + a.by_g.div(r1) + 1 : q.keys;
+    hi = hi < 0 ? 0 : hi > q.keys ? q.keys : hi;
+    long long lo = a.window > 0 ? first + a.by_g.div(r0) - a.window + 1 : 0;
+    lo = lo < 0 ? 0 : lo > hi ? hi : lo;
+    s.hi = (int)hi;
+    s.lo = (int)lo;
+    s.tile0 = s.lo / kTileKeys;
+    s.tiles = max(1, (int)(((unsigned int)s.hi + kTileKeys - 1) / kTileKeys) - s.tile0);
+    return s;
+  }
+};
 
 // Tiles of a request for one head.  Requests of many blocks of rows are summed by the whole warp,
 // 32 blocks at a time (one thread over 128 blocks took tens of microseconds before the first load).
+template <typename B>
 struct TileCost {
   const AttnArgs& a;
   __device__ __forceinline__ int blocks(const AttnRequest& q) const {
     const long long rows = (long long)q.n * a.G;
-    return rows <= a.row_limit ? 0 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
+    if (rows <= a.row_limit) return 0;
+    const int size = B::size((int)rows);
+    return (int)((rows + size - 1) / size);
   }
   __device__ __forceinline__ long long operator()(int r, bool on) const {
     AttnRequest q = {};
@@ -211,7 +211,7 @@ struct TileCost {
     const int n = on ? blocks(q) : 0;
     long long sum = 0;
     if (n <= 4)
-      for (int b = 0; b < n; ++b) sum += tile_span(a, q, b).tiles;
+      for (int b = 0; b < n; ++b) sum += B::span(a, q, b).tiles;
     for (unsigned int many = __ballot_sync(0xffffffffu, n > 4); many; many &= many - 1) {
       const int src = __ffs(many) - 1, lane = threadIdx.x & 31;
       AttnRequest w;
@@ -220,7 +220,7 @@ struct TileCost {
       w.keys = __shfl_sync(0xffffffffu, q.keys, src);
       const int wn = blocks(w);
       long long part = 0;
-      for (int b = lane; b < wn; b += 32) part += tile_span(a, w, b).tiles;
+      for (int b = lane; b < wn; b += 32) part += B::span(a, w, b).tiles;
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) part += (long long)shfl_xor64(0xffffffffu, (uint64_t)part, d);
       if (lane == src) sum = part;
@@ -239,11 +239,12 @@ struct RequestLine {
   int blocks, g;
 };
 
+template <typename B>
 __device__ __forceinline__ RequestLine request_line(const AttnArgs& a, const AttnRequest& q, long long per) {
   RequestLine line;
-  line.blocks = TileCost{a}.blocks(q);
+  line.blocks = TileCost<B>{a}.blocks(q);
   long long tiles = 0;
-  for (int b = threadIdx.x & 31; b < line.blocks; b += 32) tiles += tile_span(a, q, b).tiles;
+  for (int b = threadIdx.x & 31; b < line.blocks; b += 32) tiles += B::span(a, q, b).tiles;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) tiles += (long long)shfl_xor64(0xffffffffu, (uint64_t)tiles, d);
   const long long g = (tiles * a.pool.H + per / 2) / per, most = (long long)line.blocks * a.pool.H;
@@ -252,12 +253,13 @@ __device__ __forceinline__ RequestLine request_line(const AttnArgs& a, const Att
 }
 
 // By one warp: where in its request a piece begins.
+template <typename B>
 __device__ __forceinline__ void locate_block(const AttnArgs& a, unsigned int index, unsigned int pieces, WorkStart* w) {
   if (w->r < 0) return;
   const int lane = threadIdx.x & 31;
   const AttnRequest q = attn_request(a.b, a.pool.T, w->r);
   const long long per = (w->total + pieces - 1) / pieces;
-  const RequestLine line = request_line(a, q, per);
+  const RequestLine line = request_line<B>(a, q, per);
   long long off = per * index - w->base;
   const int dh = line.g / line.blocks, db = line.g - dh * line.blocks;      // g segments on
   for (int c0 = 0; c0 < line.g; c0 += 32) {
@@ -266,7 +268,7 @@ __device__ __forceinline__ void locate_block(const AttnArgs& a, unsigned int ind
     if (c < line.g) {
       int h = c / line.blocks, b = c - h * line.blocks;
       while (h < a.pool.H) {
-        tiles += tile_span(a, q, b).tiles;
+        tiles += B::span(a, q, b).tiles;
         h += dh;
         b += db;
         if (b >= line.blocks) {
@@ -287,7 +289,7 @@ __device__ __forceinline__ void locate_block(const AttnArgs& a, unsigned int ind
         long long left = off - (upto - tiles);
         int h = c / line.blocks, b = c - h * line.blocks;
         for (;;) {
-          const int here = tile_span(a, q, b).tiles;
+          const int here = B::span(a, q, b).tiles;
           if (left < here) break;
           left -= here;
           h += dh;
@@ -312,6 +314,7 @@ __device__ __forceinline__ void locate_block(const AttnArgs& a, unsigned int ind
 // Walks a CTA's piece of the line, one (request, head, block of rows) at a time.  Each warp keeps
 // its own in shared memory, moved on by its first lane: as registers of 16 warps it cost the
 // softmax warps spills.
+template <typename B>
 struct TileWalk {
   long long pos, start, end;
   AttnRequest q;
@@ -327,12 +330,12 @@ struct TileWalk {
     if (r < 0) pos = end = 0;
     if (pos >= end) return;
     q = attn_request(a.b, a.pool.T, r);
-    blocks = TileCost{a}.blocks(q);
+    blocks = TileCost<B>{a}.blocks(q);
     head = w.head;
     block = w.block;
     cls = w.cls;
     g = w.g;
-    span = tile_span(a, q, block);
+    span = B::span(a, q, block);
     t1 = w.off;                      // where next() goes on
     fresh = 0;
   }
@@ -354,7 +357,7 @@ struct TileWalk {
       }
     }
     if (fresh) {
-      span = tile_span(a, q, block);
+      span = B::span(a, q, block);
       t1 = 0;
     }
     t0 = t1;
@@ -372,8 +375,8 @@ struct TileWalk {
     do {
       ++x;
       next_q = attn_request(a.b, a.pool.T, x);
-    } while (TileCost{a}.blocks(next_q) == 0);
-    line = request_line(a, next_q, per);
+    } while (TileCost<B>{a}.blocks(next_q) == 0);
+    line = request_line<B>(a, next_q, per);
     __syncwarp();
     if ((threadIdx.x & 31) == 0) {
       r = x;
@@ -399,7 +402,8 @@ struct TileWalk {
   }
   __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == span.tiles; }
   __device__ __forceinline__ int rows(const AttnArgs& a) const {
-    return min(q.n * a.G - block * 2 * kTileRows, 2 * kTileRows);
+    const int size = B::size(q.n * a.G);
+    return min(q.n * a.G - block * size, size);
   }
 };
 
@@ -412,10 +416,10 @@ __device__ __forceinline__ void regs_down() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS));
 }
 
-template <int D, bool F8, typename QT, bool TREE>
-__global__ void __launch_bounds__(TileShape<D, F8, TREE>::kThreads, 1)
+template <int D, bool F8, typename QT>
+__global__ void __launch_bounds__(TileShape<D, F8>::kThreads, 1)
 attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a) {
-  using S = TileShape<D, F8, TREE>;
+  using S = TileShape<D, F8>;
   using MT = typename std::conditional<F8, __half, QT>::type;
   extern __shared__ unsigned char s_raw[];
   __shared__ __align__(8) unsigned long long s_kv_full[S::kBufs], s_kv_empty[S::kBufs];
@@ -429,7 +433,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   __shared__ __align__(4) unsigned char s_kbytes[F8 ? kInfoRing : 1][kTileKeys];
   __shared__ long long s_scan[33];
   __shared__ WorkStart s_start;
-  __shared__ TileWalk s_walk[S::kThreads / 32];
+  __shared__ TileWalk<PairBlocks> s_walk[S::kThreads / 32];
   __shared__ unsigned int s_tmem;
   __shared__ int s_abort;
 
@@ -471,13 +475,13 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     tmem_before();
   }
-  const TileCost cost{a};
+  const TileCost<PairBlocks> cost{a};
   locate_piece<S::kThreads>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
   if (warp == 0) {
-    locate_block(a, blockIdx.x, gridDim.x, &s_start);
+    locate_block<PairBlocks>(a, blockIdx.x, gridDim.x, &s_start);
     __syncwarp();
     if (lane == 0) {
-      TileWalk look;
+      TileWalk<PairBlocks> look;
       look.init(a, s_start, blockIdx.x, gridDim.x);
       JoinRecord rec = {};
       if (look.next(a) == 1 && look.t0 > 0 && look.t1 == look.span.tiles) {
@@ -498,7 +502,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   const unsigned int tmem = s_tmem;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const long long per = (s_start.total + gridDim.x - 1) / gridDim.x;
-  TileWalk& walk = s_walk[warp];
+  TileWalk<PairBlocks>& walk = s_walk[warp];
   if (lane == 0) walk.init(a, s_start, blockIdx.x, gridDim.x);
   __syncwarp();
 
@@ -512,17 +516,13 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     const unsigned int tm_o = tmem + lanes + 256 + t * D;
     unsigned int s_phase = 0, o_phase = 0, w_phase = 0, step = 0;
     while (walk.next_warp(a, per)) {
-      // A tree of up to 128 rows is split: both tiles hold the same rows and take every other step.
-      const bool split = TREE && walk.rows(a) <= kTileRows;
-      const int row_t = split ? 0 : t * kTileRows;
-      const int rows_here = walk.rows(a) - row_t;          // rows of this tile (<= 0: none)
-      const int steps = walk.t1 - walk.t0, j0 = split ? t : 0, dj = split ? 2 : 1;
-      const unsigned int step0 = step;
-      if (!TREE && rows_here <= 0) {
+      const int rows_here = walk.rows(a) - t * kTileRows;   // rows of this tile (<= 0: none)
+      const int steps = walk.t1 - walk.t0;
+      if (rows_here <= 0) {
         step += steps;
         continue;
       }
-      const int row0 = walk.block * 2 * kTileRows + row_t;   // in the request's rows
+      const int row0 = walk.block * 2 * kTileRows + t * kTileRows;   // in the request's rows
       if constexpr (F8) {                                  // O = 0: every product of a step adds to it
         uint32_t zero[32];
 #pragma unroll
@@ -533,7 +533,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         tmem_before();
       }
       // ---- queries into shared memory
-      if (!TREE || steps > j0) {
+      {
         constexpr int kChunks = D / 8;                     // 16-byte pieces of a row
         const int c = row % kChunks;
         unsigned char* dst = base + t * S::kQ + (c >> 3) * S::kColBytes;
@@ -581,18 +581,13 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       }
       const float c0 = F8 ? a.scale_log2 * s_qup[t * kTileRows + row] : a.scale_log2;
       const int tok = a.by_g.div(row0 + min(row, rows_here - 1));
-      const int first = walk.q.len - walk.q.n;
-      const uint32_t* tree = TREE ? a.mask + (walk.q.tok0 + tok) * a.mask_words : nullptr;
-      // this row's position
-      const long long p = (long long)first + (!TREE ? tok : a.window > 0 ? tree_depth(tree, a.mask_words, walk.q.n) : 0);
-      // positions [vis0, vis1) this row sees (of those that are there; trees: and of the cached ones)
-      const int vis1 = (int)max(0LL, TREE ? min((long long)first, (long long)walk.span.hi)
-                                     : a.causal ? min(p + 1, (long long)walk.span.hi) : (long long)walk.span.hi);
+      const long long p = (long long)walk.q.len - walk.q.n + tok;      // this row's position
+      // positions [vis0, vis1) this row sees (of those that are there)
+      const int vis1 = (int)max(0LL, a.causal ? min(p + 1, (long long)walk.span.hi) : (long long)walk.span.hi);
       const int vis0 = a.window > 0 ? (int)max((long long)walk.span.lo, p - a.window + 1) : walk.span.lo;
       const int key_first = (walk.span.tile0 + walk.t0) * kTileKeys;
       float m = -INFINITY, l = 0.0f;
-      for (int j = j0; j < steps; j += dj) {
-        step = step0 + j;
+      for (int j = 0; j < steps; ++j, ++step) {
         ring_wait(smem_u32(&s_s_full[t]), s_phase, abort_flag);
         s_phase ^= 1u;
         __syncwarp();
@@ -615,7 +610,6 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           for (int x = 0; x < 4; ++x) {
             const int lo = min(max(b0 - 32 * x, 0), 32), hi = min(max(b1 - 32 * x, 0), 32);
             vis[x] = (uint32_t)((1ull << hi) - 1) & ~(uint32_t)((1ull << lo) - 1);
-            if (TREE) vis[x] |= tree_bits(tree, a.mask_words, walk.span.hi - first, key0 + 32 * x - first);
           }
           if (mask != 0xffffffffu) {                       // blocks that are not there
             for (int k = 0; k < kTileKeys >> a.box_log; ++k)
@@ -675,7 +669,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           const float al = mn == -INFINITY ? 1.0f : exp2_fast(m - mn);
           m = mn;
           l *= al;
-          if (j > j0) {
+          if (j > 0) {
             constexpr int kUnroll = F8 ? 1 : D / 32;       // (over e4m3 the shorter code: 2,315 instead of 2,420 us)
 #pragma unroll kUnroll
             for (int k = 0; k < D; k += 32) {
@@ -803,84 +797,21 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_p_full[t]));
       }
-      step = step0 + steps;
       // ---- O out of tensor memory
-      if (!TREE || steps > j0) {
-        ring_wait(smem_u32(&s_o_full[t]), o_phase, abort_flag);
-        o_phase ^= 1u;
-      }
+      ring_wait(smem_u32(&s_o_full[t]), o_phase, abort_flag);
+      o_phase ^= 1u;
       __syncwarp();
       tmem_after();
       const bool whole = walk.whole();
       const bool at_start = walk.pos - steps == walk.start;
       float* slot = a.slots + ((long long)blockIdx.x * 2 + (at_start ? 0 : 1)) * S::kSlot;
-      const int srow = row_t + row;
+      const int srow = t * kTileRows + row;
       const bool on = row < rows_here;
       const long long otok = walk.q.tok0 + tok;
       const int qh = walk.head * a.G + (row0 + row - tok * a.G);
       if (m == -INFINITY) l = l == l ? 0.0f : l;           // a row that has seen no key
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       QT* dst = reinterpret_cast<QT*>(a.out) + otok * a.o_tok + (long long)qh * a.o_head;
-      if constexpr (TREE) {
-        if (split) {
-          // Both tiles' rows lie in the same lanes of tensor memory: each warpgroup adds up half of the columns
-          // of the two O, and what they need of each other, m and l, stands where the scores were.
-          constexpr int kHalf = D / 2;
-          const bool worked = steps > j0, other = steps > 1 - j0;
-          const uint32_t mine[2] = {__float_as_uint(m), __float_as_uint(l)};
-          uint32_t part[2];
-          tmem_st2(tm_s, mine);
-          tmem_wait_st();
-          tmem_before();
-          asm volatile("bar.sync 3, 256;" ::: "memory");
-          tmem_after();
-          tmem_ld2(tmem + lanes + (1 - t) * 128, part);
-          tmem_wait_ld();
-          const float m2 = __uint_as_float(part[0]), l2 = __uint_as_float(part[1]);
-          const float top = fmaxf(m, m2), safe = top == -INFINITY ? 0.0f : top;
-          const float f = exp2_fast(m - safe), f2 = exp2_fast(m2 - safe);
-          const float sum = l * f + l2 * f2;
-          const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-          for (int k = t * kHalf; k < t * kHalf + kHalf; k += 32) {
-            uint32_t o[32], o2[32];
-            __syncwarp();
-            tmem_ld32(tm_o + k, o);
-            tmem_ld32(tmem + lanes + 256 + (1 - t) * D + k, o2);
-            tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 32; ++e)                     // (a tile without a step has left its O as it was)
-              o[e] = __float_as_uint((worked ? __uint_as_float(o[e]) * f : 0.0f) +
-                                     (other ? __uint_as_float(o2[e]) * f2 : 0.0f));
-            if (on && whole) {
-#pragma unroll
-              for (int e = 0; e < 32; e += 8) {
-                uint32_t w[4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-                  w[y] = Bits16<QT>::pack(__uint_as_float(o[e + 2 * y]) * over, __uint_as_float(o[e + 2 * y + 1]) * over);
-                *reinterpret_cast<uint4*>(dst + k + e) = make_uint4(w[0], w[1], w[2], w[3]);
-              }
-            } else if (on) {
-              float* to = slot + 4 * kTileRows + (long long)srow * D + k;
-#pragma unroll
-              for (int e = 0; e < 32; e += 4)
-                *reinterpret_cast<uint4*>(to + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-            }
-          }
-          if (on && t == 0) {
-            if (!whole) {
-              slot[srow] = top;
-              slot[2 * kTileRows + srow] = sum;
-            } else if (a.lse) {
-              a.lse[otok * (a.pool.H * a.G) + qh] = sum == 0.0f ? -INFINITY : 0.69314718056f * (top + log2f(sum));
-            }
-          }
-          tmem_before();
-          asm volatile("bar.sync 3, 256;" ::: "memory");   // before the next segment's products go there
-          continue;
-        }
-      }
 #pragma unroll
       for (int k = 0; k < D; k += 32) {
         uint32_t o[32];
@@ -951,37 +882,21 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       };
       while (walk.next_warp(a, per)) {
         const int steps = (int)uniform(walk.t1 - walk.t0);
-        const bool split = TREE && uniform(walk.rows(a) <= kTileRows);
         const bool turns = uniform(walk.rows(a) > kTileRows);     // two tiles at work
-        const bool active = uniform(split ? steps > t : walk.rows(a) > t * kTileRows);   // the tile has rows; else only hands buffers on
-        const int j0 = split ? t : 0, dj = split ? 2 : 1;
-        // A buffer goes back when both warps have said so; of a split segment, when the one that uses it has twice.
-        auto hand_back = [&](unsigned int x) {
-          mma_commit(smem_u32(&s_kv_empty[x]), leader);
-          if (split) mma_commit(smem_u32(&s_kv_empty[x]), leader);
-        };
-        auto pass = [&]() {                                // a step that is the other warp's
-          advance();
-          advance();
-        };
-        if (split && t == 1) pass();
-        if (split && !active) continue;
+        const bool active = uniform(walk.rows(a) > t * kTileRows);   // the tile has rows; else only hands buffers on
         const int key_first = (int)uniform((walk.span.tile0 + walk.t0) * kTileKeys);
         const int lo = (int)uniform(walk.span.lo), hi = (int)uniform(walk.span.hi);
-        // Trees: queries first.  They come when both tiles are through with every split segment before this one,
-        // so that no buffer is still on its way for the other warp when this one looks at its barrier's phase.
-        if (TREE) ring_wait(smem_u32(&s_q_full[t]), q_phase, abort_flag);
         ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
         if (active) {
-          if (!TREE) ring_wait(smem_u32(&s_q_full[t]), q_phase, abort_flag);
+          ring_wait(smem_u32(&s_q_full[t]), q_phase, abort_flag);
           __syncwarp();
           q_phase ^= 1u;
           tmem_after();
           qk(buf);
         }
-        hand_back(buf);
+        mma_commit(smem_u32(&s_kv_empty[buf]), leader);
         advance();
-        for (int j = j0; j < steps; j += dj) {
+        for (int j = 0; j < steps; ++j) {
           const unsigned int vbuf = buf;
           last_buf = buf;
           last_phase = buf_phase;
@@ -1006,14 +921,13 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
               __syncwarp();
             }
           }
-          if (split && j + 1 < steps) pass();
-          const bool more = j + dj < steps;
+          const bool more = j + 1 < steps;
           const unsigned int kbuf = buf;
           if (more) {
             ring_wait(smem_u32(&s_kv_full[buf]), buf_phase, abort_flag);
             advance();
           }
-          const unsigned int low = v_low + vbuf * (S::kBuf >> 4), old = F8 || j > j0;
+          const unsigned int low = v_low + vbuf * (S::kBuf >> 4), old = F8 || j > 0;
           if (active) {
             ring_wait(smem_u32(&s_h_full[t]), p_phase, abort_flag);
             if (turns) {
@@ -1038,12 +952,12 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
             if (turns && lane == 0) mbar_arrive(smem_u32(&s_turn[1 - t]));
             __syncwarp();
           }
-          hand_back(vbuf);
-          if (more) hand_back(kbuf);
+          mma_commit(smem_u32(&s_kv_empty[vbuf]), leader);
+          if (more) mma_commit(smem_u32(&s_kv_empty[kbuf]), leader);
         }
       }
-      // the last commit has to arrive while its barrier is still this CTA's (trees: the loader sees to it)
-      if (!TREE) ring_wait(smem_u32(&s_kv_empty[last_buf]), last_phase, abort_flag);
+      // the last commit has to arrive while its barrier is still this CTA's
+      ring_wait(smem_u32(&s_kv_empty[last_buf]), last_phase, abort_flag);
     } else if (warp == 9) {
       // ============================================================== loader warp
       constexpr unsigned int kBytes = F8 ? S::kRaw : S::kBuf;
@@ -1100,9 +1014,6 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       // nothing may still be on its way into this CTA's shared memory when it ends
       for (unsigned int i = issued > S::kBufs ? issued - S::kBufs : 0; i < issued; ++i)
         ring_drain(smem_u32(&full[i % S::kBufs]), (i / S::kBufs) & 1u);
-      if (TREE)                                            // nor a commit, whose warp need not be the last one's
-        for (unsigned int i = issued > S::kBufs ? issued - S::kBufs : 0; i < issued; ++i)
-          ring_wait(smem_u32(&s_kv_empty[i % S::kBufs]), (i / S::kBufs) & 1u, abort_flag);
     } else if (F8 && warp == 11) {
       // ============================================================== scale warp (11)
       // Per step: the factor 2^(e - E) of every position of the K and of the V tile, and E.  The
@@ -1292,9 +1203,9 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   }
 }
 
-template <int D, bool F8, typename QT, bool TREE>
+template <int D, bool F8, typename QT>
 inline int32_t launch_attn_tiles(AttnArgs a, int type, JoinSet& join, cudaStream_t st) {
-  using S = TileShape<D, F8, TREE>;
+  using S = TileShape<D, F8>;
   a.box = gcd_int(a.pool.T, kTileKeys);
   a.box_log = log2_int(a.box);
   CUtensorMap map;
@@ -1304,10 +1215,10 @@ inline int32_t launch_attn_tiles(AttnArgs a, int type, JoinSet& join, cudaStream
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return AIBX_ERR_CUDA;
   static size_t configured[64] = {0};
   static std::mutex lock;
-  if (!ensure_dynamic_smem(attn_tiles_kernel<D, F8, QT, TREE>, S::kSmem, dev, configured, lock))
+  if (!ensure_dynamic_smem(attn_tiles_kernel<D, F8, QT>, S::kSmem, dev, configured, lock))
     return AIBX_ERR_CUDA;
   const unsigned int grid = (unsigned int)sm_count();
-  attn_tiles_kernel<D, F8, QT, TREE><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
+  attn_tiles_kernel<D, F8, QT><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
   join = JoinSet{a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot), 2 * kTileRows};
   return launch_status();
 }

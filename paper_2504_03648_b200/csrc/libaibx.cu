@@ -900,7 +900,14 @@ int32_t aibx_kv_read(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
 uint64_t aibx_attn_workspace_bytes(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
                                    const aibx_attn_params_t* params) {
   AttnPlan plan;
-  if (attn_plan(cache, batch, params, plan) != AIBX_OK) return 0;
+  if (attn_plan(cache, batch, params, false, plan) != AIBX_OK) return 0;
+  return plan.workspace;
+}
+
+uint64_t aibx_attn_tree_workspace_bytes(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batch,
+                                        const aibx_attn_params_t* params) {
+  AttnPlan plan;
+  if (attn_plan(cache, batch, params, true, plan) != AIBX_OK) return 0;
   return plan.workspace;
 }
 

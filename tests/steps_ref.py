@@ -2,7 +2,7 @@
 attention of drafted trees - and bounds on what their roundings can do."""
 import numpy as np
 
-from paged_ref import HALF_STEP, NO_BLOCK
+from paged_ref import HALF_STEP, NO_BLOCK, tolerance
 
 
 def ancestors(parents):
@@ -58,6 +58,14 @@ def tree_attention(s, b, values, q, scale, sets, window):
             slack[i, h] = scale * (D + 4) * 2.0 ** -24 * np.abs(values[kr]).max() * np.abs(q[i, h]).sum() \
                 + 4 * 2.0 ** -24 * abs(m)
     return out, lse, mag, slack
+
+
+def tree_tolerance(s, io, out, mag, slack):
+    """paged_ref.tolerance, but over e4m3 the weights of bf16 queries may be bf16: each is off by at most
+    half a step of that, relative to itself, so out by at most as much of the sum of w |v|.  (Those of fp16
+    queries are the sum of two bf16 numbers, within 2^-16: nearer than the fp16 that is allowed for.)"""
+    more = HALF_STEP["bf16"] - HALF_STEP["fp16"] if s.pool == "e4m3" and io == "bf16" else 0.0
+    return tolerance(s, io, out, mag, slack) + more * mag
 
 
 def rotate(x, pos, freq, interleaved, factor):

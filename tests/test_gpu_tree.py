@@ -3,9 +3,9 @@ import numpy as np
 import pytest
 import torch
 
-from paged_ref import DTYPE, NO_BLOCK, Batch, Shape, pool_values, tolerance
+from paged_ref import DTYPE, NO_BLOCK, Batch, Shape, pool_values
 from paper_2504_03648_b200 import binding as aibx
-from steps_ref import ancestors, pack, random_tree, tree_attention
+from steps_ref import ancestors, pack, random_tree, tree_attention, tree_tolerance
 from test_gpu_paged import POOLS, dev, make_batch, make_cache, make_pool
 
 pytestmark = pytest.mark.gpu
@@ -45,7 +45,7 @@ def check_tree(s, b, io="bf16", G=4, window=0, seed=0, spread=1.0, max_new=None,
     want, wl, mag, slack = tree_attention(s, b, pool_values(s, pool, scales), q.double().numpy(), scale, sets, window)
     n = int(b.tok_off[-1])
     assert (got[n:] == 7.0).all()
-    tol = tolerance(s, io, want[:n], mag[:n], slack[:n])
+    tol = tree_tolerance(s, io, want[:n], mag[:n], slack[:n])
     err = np.abs(got[:n] - want[:n])
     assert np.isfinite(got[:n]).all()
     assert (err <= tol).all(), (float((err / tol).max()), np.argwhere(err > tol)[:5])
@@ -68,7 +68,7 @@ def shape_for(lens, **kw):
 @pytest.mark.parametrize("layout,inner,T", [(0, 0, 16), (1, 1, 8), (2, 0, 24), (2, 1, 256)])
 @pytest.mark.parametrize("new", [[1, 3, 4, 0, 2], [26, 0, 17, 5, 32], [64, 33, 40, 1, 0]])
 def test_tree(new, layout, inner, T, D, pool, io):
-    """Up to 16 rows, up to 128 (split), more."""
+    """Few rows, up to a block, more."""
     lens = [n + c for n, c in zip(new, (0, 40, 300, 1, 95))]
     s = shape_for(lens, H=2, D=D, T=T, layout=layout, inner=inner, pool=pool)
     b = Batch(np.random.default_rng(T), s, new, lens, pad=3, ragged=T == 24)
@@ -143,7 +143,7 @@ def test_a_chain_is_causal_attention(G):
     aibx.attn_tree(cache, batch, mask, q, c)
     _, _, mag, slack = tree_attention(s, b, pool_values(s, pool, None), q.double().cpu().numpy(), 128 ** -0.5,
                                       [[set(range(i + 1)) for i in range(n)] for n in new], 0)
-    tol = 2 * tolerance(s, "bf16", a.double().cpu().numpy(), mag, slack)
+    tol = 2 * tree_tolerance(s, "bf16", a.double().cpu().numpy(), mag, slack)
     assert (np.abs(a.double().cpu().numpy() - c.double().cpu().numpy()) <= tol).all()
 
 
@@ -248,7 +248,7 @@ def test_far_positions():
         small.table = np.array([[2, 1]], dtype=np.uint32)
         assert (ctx + n) % T == T - 2
         want, _, mag, slack = tree_attention(s, small, pool_values(s, pool, None), q.double().numpy(), 64 ** -0.5, [sets], 200)
-        assert (np.abs(out.double().cpu().numpy() - want) <= tolerance(s, "bf16", want, mag, slack)).all()
+        assert (np.abs(out.double().cpu().numpy() - want) <= tree_tolerance(s, "bf16", want, mag, slack)).all()
     assert aibx.status_fetch() == (0, 0)
 
 
@@ -264,7 +264,7 @@ def test_same_bits_every_time_captured_and_beside_itself(pool, io):
     cache, batch = make_cache(s, p, sc), make_batch(b)
     q = torch.from_numpy(rng.normal(size=(b.n_tokens, 16, 128))).to(DTYPE[io]).cuda()
     mask = dev(np.concatenate([pack(t, 1) for t in trees(rng, b)]))
-    size = aibx.attn_workspace_bytes(cache, batch, q)
+    size = aibx.attn_tree_workspace_bytes(cache, batch, q)
     streams = [torch.cuda.Stream() for _ in range(3)]
     outs = [torch.empty_like(q) for _ in range(5)]
     ws = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(5)]

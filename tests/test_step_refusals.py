@@ -65,6 +65,18 @@ def test_masks_of_nothing(lib):  # noqa: F811
     assert masks(lib, R=0, parent=None) == aibx.OK and masks(lib, n=0, mask=None) == aibx.OK
 
 
+def test_tree_workspace(lib):  # noqa: F811
+    def size(c, b, p):
+        return lib.aibx_attn_tree_workspace_bytes(at(c), at(b), at(p))
+
+    few = size(cache(), batch(max_new=1), params())
+    assert 0 < few == size(cache(num_blocks=500, layout=2), batch(max_new=1, n_tokens=900, R=900), params())
+    assert few < size(cache(), batch(max_new=20), params()) < size(cache(), batch(max_new=100), params())
+    assert size(cache(), batch(max_new=0, R=7), params()) == size(cache(), batch(max_new=100), params())
+    assert size(cache(), batch(), params(scale=0.0)) == 0
+    assert tree(lib, cache(), batch(max_new=20), params(), size=size(cache(), batch(max_new=20), params()) - 1) == aibx.ERR_INVALID
+
+
 def tree(lib, c, b, p, mask=FAKE + 8192, words=1, q=FAKE, out=FAKE + 4096, lse=None, ws=FAKE, size=1 << 40):  # noqa: F811
     return lib.aibx_attn_tree(at(c), at(b), at(p), mask, words, q, out, lse, ws, size, None)
 
