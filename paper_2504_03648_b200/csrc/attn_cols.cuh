@@ -5,7 +5,7 @@
 // shrinks with the rows (a tile of 128 rows, filled or not, costs its softmax 128 exponentials a key; here
 // a row costs one).  A block of up to N rows meets KV tiles of 128 positions:
 //   S^T = K Q^T        [128 keys][rows], K and Q from shared memory, S^T in tensor memory (fp32)
-//   P^T = 2^(S^T c - m)   one thread per key and half of the rows; P^T to shared memory, 16-bit
+//   P^T = 2^(S^T c - m)   one thread per key and quarter of the rows; P^T to shared memory, 16-bit
 //   O^T += V^T P^T     [dims][rows], V as it lies in the pool ([position][dim]: V^T's M-major form)
 // A row's maximum runs across the threads, which is what makes this form dear; but m needs to move only
 // when a score passes it by 2^8 (weights up to 2^8 are as good as weights up to 1).  So a tile costs one
@@ -21,8 +21,8 @@
 // outside [kScaleLow, kScaleHigh] leave the rest with V).  fp16 queries get weights as the sum of two
 // bf16 numbers, so that they lose nothing to the type.
 //
-// Roles: two softmax warpgroups, one for each half of the rows, which never wait for each other; a warp
-// for S^T and one for O^T; a loader; over e4m3 a warp for the scale bytes and four that convert.  Rings of K
+// Roles: four softmax warpgroups, one for each quarter of the rows, which never wait for each other; a warp
+// for S^T and one for O^T; a loader of K and one of V (and of the scale bytes); over e4m3 eight that convert.  Rings of K
 // and of V tiles of their own, S^T twice, so that S^T(j + 1) runs beside the softmax of tile j.
 // Bound: HBM, 2,800 cycles a tile of 128 16-bit keys of D = 128 (this SM's share), 1,400 of e4m3 ones; the
 // products take (4 + 4) * N cycles of the tensor pipe.
@@ -51,9 +51,52 @@ struct EvenBlocks {
   }
 };
 
+// Tiles of a request over all heads.
+template <typename B>
+struct EvenCost {
+  const AttnArgs& a;
+  __device__ __forceinline__ long long operator()(int r, bool on) const {
+    if (!on) return 0;
+    const AttnRequest q = attn_request(a.b, a.pool.T, r);
+    return (long long)TileCost<B>{a}.blocks(q) * B::span(a, q, 0).tiles * a.pool.H;
+  }
+};
+
+// By one thread: where in its request a piece begins.  As locate_block, whose order of segments it keeps, but
+// with as many tiles in every segment there is nothing to search.
+template <typename B>
+__device__ __forceinline__ void locate_even(const AttnArgs& a, unsigned int index, unsigned int pieces, WorkStart* w) {
+  if (w->r < 0) return;
+  const AttnRequest q = attn_request(a.b, a.pool.T, w->r);
+  const long long per = (w->total + pieces - 1) / pieces;
+  const int blocks = TileCost<B>{a}.blocks(q), tiles = B::span(a, q, 0).tiles;
+  const long long segments = (long long)blocks * a.pool.H;
+  long long g = (segments * tiles + per / 2) / per;        // as in request_line
+  g = g < 1 ? 1 : g > segments ? segments : g;
+  const long long off = per * index - w->base;
+  long long k = off / tiles, cls;                          // k-th segment in the order
+  const long long some = segments / g, more = segments - some * g;   // classes of some + 1 segments: `more` of them
+  if (k < more * (some + 1)) {
+    cls = k / (some + 1);
+    k -= cls * (some + 1);
+  } else {
+    k -= more * (some + 1);
+    cls = more + k / some;
+    k -= (cls - more) * some;
+  }
+  const long long segment = cls + k * g;
+  w->off = (int)(off - off / tiles * tiles);
+  w->head = (int)(segment / blocks);
+  w->block = (int)(segment - (long long)w->head * blocks);
+  w->cls = (int)cls;
+  w->g = (int)g;
+}
+
 template <int D, bool F8, int N>
 struct ColShape {
-  static constexpr int kThreads = F8 ? 512 : 384;
+  static constexpr int kGroups = 4;                        // softmax warpgroups
+  static constexpr int kConverters = F8 ? 2 : 0;           // warpgroups that convert
+  static constexpr int kThreads = 128 * (kGroups + 1 + kConverters);
   static constexpr int kCols = D / 64;                     // 128-byte columns of an operand row
   static constexpr int kColBytes = 128 * 128;
   static constexpr int kRaw = kTileKeys * D;               // a tile's e4m3 rows, as they arrive
@@ -66,28 +109,33 @@ struct ColShape {
 template <int D, bool F8, int N, int PARTS>
 struct ColRings : ColShape<D, F8, N> {
   using B = ColShape<D, F8, N>;
-  static constexpr int kBufs = (B::kRoom - B::kQ - PARTS * B::kP - 1024) / B::kBuf;
+  static constexpr int kPs = N == 64 ? 2 : 1;              // P^T of that many tiles
+  static constexpr int kBufs = (B::kRoom - B::kQ - kPs * PARTS * B::kP - 1024) / B::kBuf;
   static constexpr int kK = kBufs / 2 < 4 ? kBufs / 2 : 4, kV = kBufs - kBufs / 2 < 4 ? kBufs - kBufs / 2 : 4;
   static constexpr int kQAt = (kK + kV) * B::kBuf, kPAt = kQAt + B::kQ;
-  static constexpr int kSmem = kPAt + PARTS * B::kP + 1024;
+  static constexpr int kSmem = kPAt + kPs * PARTS * B::kP + 1024;
   static constexpr int kSlot = N * (D + 2);                // floats per workspace slot
-  static constexpr int kRegsSoftmax = F8 ? 176 : 200;      // sums as in TileShape
-  static constexpr int kRegsOther = F8 ? 80 : 104;
+  static constexpr int kRegsSoftmax = F8 ? 80 : 104;       // launch: 72 (896 threads), 96 (640)
+  static constexpr int kRegsOther = F8 ? 56 : 64;          // 4 * 80 + 56 + 2 * 64 = 7 * 72; 4 * 104 + 64 = 5 * 96
+  static constexpr int kRegsConvert = 64;
   static_assert(kK >= 2 && kV >= 2, "two tiles of each at least");
 };
 
-// fp32 accumulator, M = 128, B's N at run time; operands N- or M-major where said
-__device__ __forceinline__ unsigned int col_mma_desc(bool half, int n, bool major) {
+// fp32 accumulator, M = 128; operands as they lie (K-major), or both M- and N-major
+__host__ __device__ constexpr unsigned int col_mma_desc(bool half, int n, bool major) {
   return (1u << 4) | ((half ? 0u : 1u) << 7) | ((half ? 0u : 1u) << 10) | (major ? 3u << 15 : 0u) |
          ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-__device__ __forceinline__ void tmem_ld16(unsigned int addr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(addr));
+__device__ __forceinline__ void tmem_ld8(unsigned int addr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st8(unsigned int addr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr)
+               : "memory");
 }
 
 // Whether any thread of a warpgroup says so (named barrier `id`, 128 threads).
@@ -119,14 +167,17 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   using Blocks = EvenBlocks<N>;
   using KT = typename std::conditional<F8, __half, QT>::type;            // operands of S^T
   using VT = typename std::conditional<F8, __nv_bfloat16, QT>::type;     // and of O^T
-  constexpr int kMine = N / 2, kChunks = kMine / 16;       // rows of a softmax warpgroup, 16 at a time
+  constexpr int kMine = N / S::kGroups, kChunks = kMine / 8;   // rows of a softmax warpgroup, 8 at a time
+  constexpr int kQK = 4 * S::kGroups, kPV = kQK + 2, kLoadV = kQK + 3;   // warps (kQK + 1 loads K)
   extern __shared__ unsigned char s_raw[];
   __shared__ __align__(8) unsigned long long s_k_full[S::kK], s_k_empty[S::kK], s_k_raw[S::kK];
   __shared__ __align__(8) unsigned long long s_v_full[S::kV], s_v_empty[S::kV], s_v_raw[S::kV];
-  __shared__ __align__(8) unsigned long long s_s_full[2], s_s_free[2], s_q_full, s_p_full, s_pv_done;
+  __shared__ __align__(8) unsigned long long s_s_full[2], s_s_free[2], s_q_full, s_p_full[2], s_pv_done[2];
+  __shared__ __align__(8) unsigned long long s_vote[S::kGroups];
+  __shared__ int s_grow[S::kGroups][2];                    // a vote's outcome
   __shared__ __align__(8) unsigned long long s_info_full[kColInfo], s_info_empty[kColInfo];
   __shared__ unsigned int s_mask[kInfoRing];
-  __shared__ __align__(16) float s_ref[N], s_scale[N];     // m (0 where no key was seen yet) and scale of each row
+  __shared__ __align__(16) float s_ref[N], s_scale[N], s_al[N];     // m (0 where no key was seen yet) and scale of each row
   __shared__ float s_top[N], s_inv[N];
   __shared__ int s_new[N], s_low[N], s_tok[N];
   __shared__ long long s_out[N];
@@ -148,66 +199,61 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kK; ++i) {
-      mbar_init(smem_u32(&s_k_full[i]), F8 ? 128u : 1u);
+      mbar_init(smem_u32(&s_k_full[i]), F8 ? 256u : 1u);
       mbar_init(smem_u32(&s_k_empty[i]), 1u);
       mbar_init(smem_u32(&s_k_raw[i]), 1u);
     }
     for (int i = 0; i < S::kV; ++i) {
-      mbar_init(smem_u32(&s_v_full[i]), F8 ? 128u : 1u);
+      mbar_init(smem_u32(&s_v_full[i]), F8 ? 256u : 1u);
       mbar_init(smem_u32(&s_v_empty[i]), 1u);
       mbar_init(smem_u32(&s_v_raw[i]), 1u);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&s_s_full[i]), 1u);
-      mbar_init(smem_u32(&s_s_free[i]), 8u);
+      mbar_init(smem_u32(&s_s_free[i]), 4u * S::kGroups);
+      mbar_init(smem_u32(&s_p_full[i]), 4u * S::kGroups);
+      mbar_init(smem_u32(&s_pv_done[i]), 1u);
     }
     for (int i = 0; i < kColInfo; ++i) {
       mbar_init(smem_u32(&s_info_full[i]), 1u);
-      mbar_init(smem_u32(&s_info_empty[i]), 12u);
+      mbar_init(smem_u32(&s_info_empty[i]), 4u * (S::kGroups + S::kConverters));
     }
-    mbar_init(smem_u32(&s_q_full), 256u);
-    mbar_init(smem_u32(&s_p_full), 8u);
-    mbar_init(smem_u32(&s_pv_done), 1u);
+    mbar_init(smem_u32(&s_q_full), 128u * S::kGroups);
+    for (int i = 0; i < S::kGroups; ++i) {
+      mbar_init(smem_u32(&s_vote[i]), 4u);
+      s_grow[i][0] = s_grow[i][1] = 0;
+    }
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 8) {
+  if (warp == kQK) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     tmem_before();
   }
-  const TileCost<Blocks> cost{a};
+  const EvenCost<Blocks> cost{a};
   locate_piece<S::kThreads>(a.b.R, blockIdx.x, gridDim.x, s_scan, &s_start, cost);
   const long long per = (s_start.total + gridDim.x - 1) / gridDim.x;
   if (warp == 0) {
-    locate_block<Blocks>(a, blockIdx.x, gridDim.x, &s_start);
-    __syncwarp();
+    // one thread finds the place, all warps start from copies of it
     if (lane == 0) {
-      TileWalk<Blocks> look;
-      look.init(a, s_start, blockIdx.x, gridDim.x);
-      JoinRecord rec = {};
-      if (look.next(a) == 1 && look.t0 > 0 && look.t1 == look.span.tiles) {
-        const long long p0 = look.pos - look.t1;           // position of the rows' first tile
-        rec.tok0 = look.q.tok0;
-        rec.rows = look.rows(a);
-        rec.row0 = look.block * Blocks::size(look.q.n * a.G);
-        rec.head = look.head;
-        rec.first_cta = (int)(p0 / per);
-        rec.first_slot = p0 != rec.first_cta * per;
-      }
-      reinterpret_cast<JoinRecord*>(a.slots + 2ull * gridDim.x * S::kSlot)[blockIdx.x] = rec;
+      locate_even<Blocks>(a, blockIdx.x, gridDim.x, &s_start);
+      s_walk[0].init(a, s_start, blockIdx.x, gridDim.x);
     }
+    __syncwarp();
+    constexpr int kWords = (int)(sizeof(TileWalk<Blocks>) / 4);
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(&s_walk[0]);
+    for (int x = lane; x < (S::kThreads / 32 - 1) * kWords; x += 32)
+      reinterpret_cast<uint32_t*>(&s_walk[1])[x] = from[x % kWords];
   }
   __syncthreads();
   tmem_after();
   const unsigned int tmem = s_tmem;                        // columns: S^T 0 and 128, O^T 256
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   TileWalk<Blocks>& walk = s_walk[warp];
-  if (lane == 0) walk.init(a, s_start, blockIdx.x, gridDim.x);
-  __syncwarp();
 
-  if (warp < 8) {
+  if (warp < kQK) {
     // ================================================================ softmax: thread = key
     regs_up<S::kRegsSoftmax>();
     const int w = warp >> 2, id = 1 + w;                   // warpgroup and its barrier
@@ -215,22 +261,27 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     const unsigned int lanes = (unsigned int)(warp & 3) << 21;
     const unsigned int tm_s = tmem + lanes, tm_o = tmem + lanes + 256;
     unsigned char* s_q = base + S::kQAt;
-    unsigned int step = 0, pv_phase = 0;
+    const int c0 = w * kMine;                              // first of this warpgroup's rows in a block
+    unsigned int step = 0, votes = 0;
+    auto pv_wait = [&](unsigned int x) {                   // the product of step x is done, and so are all before
+      ring_wait(smem_u32(&s_pv_done[x % S::kPs]), (x / S::kPs) & 1u, abort_flag);
+      __syncwarp();
+      tmem_after();
+    };
     while (walk.next_warp(a, per)) {
-      const int rows = walk.rows(a), steps = walk.t1 - walk.t0;
-      const int chunks = (rows + 31) >> 5, mine = chunks * 16;           // of this warpgroup's rows
-      const int c0 = w * mine;                             // its first row of the block
-      const int row0 = walk.block * Blocks::size(walk.q.n * a.G);
-      const int first = walk.q.len - walk.q.n;
+      const int steps = walk.t1 - walk.t0;
+      // (What only the rare paths need is read from the walk again where it is: a register saved.)
+      auto block_row0 = [&]() { return walk.block * Blocks::size(walk.q.n * a.G); };
       // ---- what is known of each row
-      if (tid < mine) {
+      const int rows = walk.rows(a), row0 = block_row0();
+      if (tid < kMine) {
         const int ri = row0 + min(c0 + tid, rows - 1), ti = a.by_g.div(ri);
         s_tok[c0 + tid] = ti;
         s_out[c0 + tid] = (walk.q.tok0 + ti) * a.o_tok + (long long)(walk.head * a.G + (ri - ti * a.G)) * a.o_head;
         int low = walk.span.lo;
         if (a.window > 0) {
           const int depth = tree_depth(a.mask + (walk.q.tok0 + ti) * a.mask_words, a.mask_words, walk.q.n);
-          low = (int)max((long long)low, (long long)first + depth - a.window + 1);
+          low = (int)max((long long)low, (long long)walk.q.len - walk.q.n + depth - a.window + 1);
         }
         s_low[c0 + tid] = low;
         s_ref[c0 + tid] = 0.0f;
@@ -243,7 +294,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         const int c = tid % kPieces;
         unsigned char* dst = s_q + (c >> 3) * (S::kQ / S::kCols);
         constexpr int kBatch = 4;
-        for (int i0 = tid / kPieces; i0 < mine; i0 += kBatch * (128 / kPieces)) {
+        for (int i0 = tid / kPieces; i0 < kMine; i0 += kBatch * (128 / kPieces)) {
           uint4 batch[kBatch];
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) {
@@ -256,7 +307,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 #pragma unroll
           for (int u = 0; u < kBatch; ++u) {
             const int i = c0 + i0 + u * (128 / kPieces);
-            const bool on = i0 + u * (128 / kPieces) < mine;
+            const bool on = i0 + u * (128 / kPieces) < kMine;
             uint4 v = i < rows ? batch[u] : make_uint4(0, 0, 0, 0);
             if constexpr (F8) {
               uint32_t x[4] = {v.x, v.y, v.z, v.w};
@@ -285,14 +336,19 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         mbar_arrive(smem_u32(&s_q_full));
         group_sync(id);
       }
-      float l[kMine];
+      uint64_t l[kMine / 2];                               // sums of this thread's keys, two rows in each
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) l[i] = 0.0f;
+      for (int i = 0; i < kMine / 2; ++i) l[i] = 0;
       bool blank = true;                                   // a row of this warpgroup has seen no key yet
-      const int key_first = (walk.span.tile0 + walk.t0) * kTileKeys;
-      const int lo = walk.span.lo, hi = walk.span.hi;
-      const int open_hi = min(first, hi);
-      const int open_lo = a.window > 0 ? max(lo, walk.q.len - a.window) : lo;
+      // steps [open0, open1): all of their keys are there and seen by all rows (if no block is missing)
+      int open0 = 0, open1;
+      {
+        const int key_first = (walk.span.tile0 + walk.t0) * kTileKeys, lo = walk.span.lo;
+        const int open_hi = min(walk.q.len - walk.q.n, walk.span.hi);
+        const int open_lo = a.window > 0 ? max(lo, walk.q.len - a.window) : lo;
+        if (open_lo > key_first) open0 = (int)(((unsigned int)(open_lo - key_first) + kTileKeys - 1) / kTileKeys);
+        open1 = open_hi > key_first ? (open_hi - key_first) / kTileKeys : 0;
+      }
       constexpr float kHead = kWeightHead<VT>;
       for (int j = 0; j < steps; ++j, ++step) {
         const unsigned int sb = step & 1u;
@@ -309,29 +365,38 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         ring_wait(smem_u32(&s_s_full[sb]), (step >> 1) & 1u, abort_flag);
         __syncwarp();
         tmem_after();
-        uint32_t z[kMine];
-#pragma unroll
-        for (int ch = 0; ch < kChunks; ++ch)
-          if (ch < chunks) tmem_ld16(tm_s + sb * 128 + c0 + ch * 16, z + ch * 16);
-        tmem_wait_ld();
-        tmem_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_s_free[sb]));
-        // ---- scores in powers of two, less the row's m
-        const int key0 = key_first + j * kTileKeys;
         const unsigned int mask = s_mask[step % kInfoRing];
-        const bool hide = mask != 0xffffffffu || key0 < open_lo || key0 > open_hi - kTileKeys;   // (key0 + 128 may be 2^31)
-        float most = -INFINITY;
+        const bool hide = mask != 0xffffffffu || j < open0 || j >= open1;
+        uint32_t vis = 0xffffffffu;                        // which of its rows see this thread's key
+        if (hide) {
+          const int key = (walk.span.tile0 + walk.t0 + j) * kTileKeys + tid, d = key - (walk.q.len - walk.q.n);
+          vis = key >= walk.span.lo && key < walk.span.hi && ((mask >> (tid >> a.box_log)) & 1u) ? 0xffffffffu : 0u;
+          if (vis && d >= 0) {                             // a node: its bit, token by token
+            const int t0 = s_tok[c0], t1 = s_tok[c0 + kMine - 1], left = walk.rows(a) - c0;
+            const uint32_t* bits = a.mask + (walk.q.tok0 + t0) * a.mask_words + (d >> 5);
+            const bool named = (d >> 5) < a.mask_words;
+            vis = left < kMine ? 0xffffffffu << max(left, 0) : 0u;       // (rows that are not there see all)
+            int from = t0 * a.G - block_row0() - c0;
+#pragma unroll 4
+            for (int t = t0; t <= t1; ++t, bits += a.mask_words, from += a.G) {
+              const uint32_t bit = named ? __ldg(bits) >> (d & 31) & 1u : 0u;
+              const uint32_t upto = from + a.G >= 32 ? 0xffffffffu : (1u << (from + a.G)) - 1u;
+              vis |= (0u - bit) & upto & (0xffffffffu << max(from, 0));
+            }
+          } else if (vis && a.window > 0) {
+            vis = 0;
+            for (int i = 0; i < kMine; ++i) vis |= (uint32_t)(key >= s_low[c0 + i]) << i;
+          }
+        }
+        // Scores of 8 rows in powers of two, less the rows' m.
+        auto scores = [&](int c, uint32_t* x, uint32_t seen) {
 #pragma unroll
-        for (int ch = 0; ch < kChunks; ++ch) {
-          if (ch >= chunks) continue;
-#pragma unroll
-          for (int i = ch * 16; i < ch * 16 + 16; i += 4) {
-            const float4 r = *reinterpret_cast<const float4*>(s_ref + c0 + i);
-            uint64_t x0 = pair2(__uint_as_float(z[i]), __uint_as_float(z[i + 1]));
-            uint64_t x1 = pair2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3]));
+          for (int i = 0; i < 8; i += 4) {
+            const float4 r = *reinterpret_cast<const float4*>(s_ref + c + i);
+            uint64_t x0 = pair2(__uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+            uint64_t x1 = pair2(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
             if constexpr (F8) {
-              const float4 sc = *reinterpret_cast<const float4*>(s_scale + c0 + i);
+              const float4 sc = *reinterpret_cast<const float4*>(s_scale + c + i);
               x0 = fma2(fma2(x0, pair2(kf, kf), pair2(0.0f, 0.0f)), pair2(sc.x, sc.y), pair2(-r.x, -r.y));
               x1 = fma2(fma2(x1, pair2(kf, kf), pair2(0.0f, 0.0f)), pair2(sc.z, sc.w), pair2(-r.z, -r.w));
             } else {
@@ -342,96 +407,107 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             split2(x0, y[0], y[1]);
             split2(x1, y[2], y[3]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[i + e] = __float_as_uint(y[e]);
+            for (int e = 0; e < 4; ++e) x[i + e] = __float_as_uint(y[e]);
           }
-        }
-        if (hide) {
-          const int key = key0 + tid, d = key - first;
-          const bool here = key >= lo && key < hi && ((mask >> (tid >> a.box_log)) & 1u);
-          const uint32_t* bits = a.mask + walk.q.tok0 * a.mask_words + (d >> 5);
-          const bool node = here && d >= 0 && (d >> 5) < a.mask_words;
+          if (hide) {
 #pragma unroll
-          for (int ch = 0; ch < kChunks; ++ch) {
-            if (ch >= chunks) continue;
-#pragma unroll
-            for (int i = ch * 16; i < ch * 16 + 16; ++i) {
-              bool ok = here && d < 0 && key >= s_low[c0 + i];
-              if (node) ok = (__ldg(bits + (long long)s_tok[c0 + i] * a.mask_words) >> (d & 31)) & 1u;
-              if (!ok) z[i] = 0xff800000u;
-            }
+            for (int i = 0; i < 8; ++i)
+              if (!(seen & (1u << i))) x[i] = 0xff800000u;
           }
-        }
-#pragma unroll
-        for (int ch = 0; ch < kChunks; ++ch) {
-          if (ch >= chunks) continue;
-#pragma unroll
-          for (int i = ch * 16; i < ch * 16 + 16; i += 2) most = max3(most, __uint_as_float(z[i]), __uint_as_float(z[i + 1]));
-        }
-        // ---- m, moved only when a score passes it by 2^8
-        if (group_any(id, blank || most > kHead + 8.0f)) {
-          if (j > 0) {
-            ring_wait(smem_u32(&s_pv_done), pv_phase, abort_flag);     // (looked at once more below)
-            __syncwarp();
-            tmem_after();
-          }
-          int best[(kMine + 31) / 32];                     // lane: of row 32 k + lane, the warp's largest score
-#pragma unroll
-          for (int k = 0; k < (kMine + 31) / 32; ++k) best[k] = float_order(-INFINITY);
-#pragma unroll
-          for (int i = 0; i < kMine; ++i) {
-            if (i / 16 >= chunks) continue;
-            const int top = __reduce_max_sync(0xffffffffu, float_order(__uint_as_float(z[i])));
-            if (lane == (i & 31)) best[i / 32] = top;
-          }
-#pragma unroll
-          for (int k = 0; k < (kMine + 31) / 32; ++k)
-            if (32 * k + lane < mine) atomicMax(&s_new[c0 + 32 * k + lane], best[k]);
-          group_sync(id);
-          blank = false;
-#pragma unroll
-          for (int ch = 0; ch < kChunks; ++ch) {
-            if (ch >= chunks) continue;
-            uint32_t o[16];
-            const bool scale_o = j > 0 && (D == 128 || (warp & 2) == 0);
-            if (scale_o) {
-              tmem_ld16(tm_o + c0 + ch * 16, o);
+        };
+        // ---- weights.  They are taken with the m there is, while the warpgroup votes on whether that will do;
+        // where it will not (and where a row has none yet) m moves first, and they are taken again.
+        uint32_t z[kMine];
+        bool move = blank;
+        for (;;) {
+          if (move) {
+            // largest scores of the rows over all keys; m, l and O follow
+            int best = float_order(-INFINITY);             // lane: of row `lane`, the warp's
+#pragma unroll 1
+            for (int ch = 0; ch < kChunks; ++ch) {
+              uint32_t x[8];
+              tmem_ld8(tm_s + sb * 128 + c0 + ch * 8, x);
               tmem_wait_ld();
-            }
+              scores(c0 + ch * 8, x, vis >> (ch * 8));
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int c = c0 + ch * 16 + i;
+              for (int i = 0; i < 8; ++i) {
+                const int top = __reduce_max_sync(0xffffffffu, float_order(__uint_as_float(x[i])));
+                if (lane == ch * 8 + i) best = top;
+              }
+            }
+            if (lane < kMine) atomicMax(&s_new[c0 + lane], best);
+            if (j > 0) pv_wait(step - 1);
+            group_sync(id);
+            if (tid < kMine) {
+              const int c = c0 + tid;
               const float old = s_top[c], ref = s_ref[c];
               const float mn = fmaxf(old, order_float(s_new[c]) + ref - kHead);
-              const float al = old == -INFINITY ? 1.0f : exp2_fast(old - mn);
-              l[ch * 16 + i] *= al;
-              blank |= mn == -INFINITY;
-              z[ch * 16 + i] = __float_as_uint(__uint_as_float(z[ch * 16 + i]) + (ref - (mn == -INFINITY ? 0.0f : mn)));
-              o[i] = __float_as_uint(__uint_as_float(o[i]) * al);
+              s_al[c] = old == -INFINITY ? 1.0f : exp2_fast(old - mn);
+              s_top[c] = mn;
+              s_ref[c] = mn == -INFINITY ? 0.0f : mn;
+              s_new[c] = float_order(-INFINITY);
             }
-            if (scale_o) tmem_st16(tm_o + c0 + ch * 16, o);
+            if (tid == 0) s_grow[w][0] = s_grow[w][1] = 0;
+            blank = group_any(id, false);                  // (a barrier)
+            for (int i = 0; i < kMine; ++i) blank |= s_top[c0 + i] == -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kMine; i += 4) {
+              const float4 al = *reinterpret_cast<const float4*>(s_al + c0 + i);
+              l[i / 2] = fma2(l[i / 2], pair2(al.x, al.y), 0);
+              l[i / 2 + 1] = fma2(l[i / 2 + 1], pair2(al.z, al.w), 0);
+            }
+            if (j > 0 && (D == 128 || (warp & 2) == 0)) {
+#pragma unroll 1
+              for (int ch = 0; ch < kChunks; ++ch) {
+                uint32_t o[8];
+                tmem_ld8(tm_o + c0 + ch * 8, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * s_al[c0 + ch * 8 + i]);
+                tmem_st8(tm_o + c0 + ch * 8, o);
+              }
+              tmem_wait_st();
+            }
           }
-          tmem_wait_st();
-          tmem_before();
-          group_sync(id);                                  // all have read what changes now
-          if (tid < mine) {
-            const int c = c0 + tid;
-            const float mn = fmaxf(s_top[c], order_float(s_new[c]) + s_ref[c] - kHead);
-            s_top[c] = mn;
-            s_ref[c] = mn == -INFINITY ? 0.0f : mn;
-            s_new[c] = float_order(-INFINITY);
+#pragma unroll
+          for (int ch = 0; ch < kChunks; ++ch)
+            tmem_ld8(tm_s + sb * 128 + c0 + ch * 8, z + ch * 8);
+          tmem_wait_ld();
+          float most = -INFINITY;
+#pragma unroll
+          for (int ch = 0; ch < kChunks; ++ch) {
+            scores(c0 + ch * 8, z + ch * 8, vis >> (ch * 8));
+#pragma unroll
+            for (int i = ch * 8; i < ch * 8 + 8; i += 2) most = max3(most, __uint_as_float(z[i]), __uint_as_float(z[i + 1]));
           }
-          group_sync(id);
+          if (!move) {
+            const bool grow = __any_sync(0xffffffffu, most > kHead + 8.0f);
+            if (lane == 0) {
+              if (grow) s_grow[w][votes & 1u] = 1;
+              mbar_arrive(smem_u32(&s_vote[w]));
+            }
+          }
+#pragma unroll
+          for (int ch = 0; ch < kChunks; ++ch) {
+#pragma unroll
+            for (int i = ch * 8; i < ch * 8 + 8; ++i) z[i] = __float_as_uint(exp2_fast(__uint_as_float(z[i])));
+          }
+          if (move) break;
+          ring_wait(smem_u32(&s_vote[w]), votes & 1u, abort_flag);
+          move = *reinterpret_cast<volatile int*>(&s_grow[w][votes & 1u]) != 0;
+          ++votes;
+          if (!move) break;
         }
-        // ---- weights
+        tmem_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_s_free[sb]));
         uint32_t pk[kParts][kMine / 2];
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
-          if (ch >= chunks) continue;
 #pragma unroll
-          for (int i = ch * 16; i < ch * 16 + 16; i += 2) {
-            float p0 = exp2_fast(__uint_as_float(z[i])), p1 = exp2_fast(__uint_as_float(z[i + 1]));
-            l[i] += p0;
-            l[i + 1] += p1;
+          for (int i = ch * 8; i < ch * 8 + 8; i += 2) {
+            float p0 = __uint_as_float(z[i]), p1 = __uint_as_float(z[i + 1]);
+            l[i >> 1] = add2(l[i >> 1], pair2(p0, p1));
             if constexpr (F8) {
               p0 *= vf;
               p1 *= vf;
@@ -443,52 +519,58 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             }
           }
         }
-        if (j > 0) {                                       // the product before has read its weights
-          ring_wait(smem_u32(&s_pv_done), pv_phase, abort_flag);
-          pv_phase ^= 1u;
-          __syncwarp();
-        }
+        if (j >= S::kPs) pv_wait(step - S::kPs);           // the product that had this place has read its weights
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-          unsigned char* s_p = base + S::kPAt + part * S::kP + tid * 128;
+          unsigned char* s_p = base + S::kPAt + ((step % S::kPs) * kParts + part) * S::kP + tid * 128;
 #pragma unroll
           for (int ch = 0; ch < kChunks; ++ch) {
-            if (ch >= chunks) continue;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int c = c0 + ch * 16 + h * 8;
-              *reinterpret_cast<uint4*>(s_p + (c >> 6) * S::kColBytes + ((((c >> 3) & 7) ^ (tid & 7)) << 4)) =
-                  make_uint4(pk[part][ch * 8 + h * 4], pk[part][ch * 8 + h * 4 + 1], pk[part][ch * 8 + h * 4 + 2],
-                             pk[part][ch * 8 + h * 4 + 3]);
-            }
+            const int c = c0 + ch * 8;
+            *reinterpret_cast<uint4*>(s_p + (c >> 6) * S::kColBytes + ((((c >> 3) & 7) ^ (tid & 7)) << 4)) =
+                make_uint4(pk[part][ch * 4], pk[part][ch * 4 + 1], pk[part][ch * 4 + 2], pk[part][ch * 4 + 3]);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        tmem_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_p_full));
+        if (lane == 0) mbar_arrive(smem_u32(&s_p_full[step % S::kPs]));
       }
-      // ---- sums over the keys: each lane ends with the warp's sum of row 32 k + lane
+      // ---- sums over the keys, 8 rows at a time, by way of tensor memory: taken from registers in a rolled
+      // loop (unrolled over all rows, this part took registers from the loop above: 237 instead of 1XX us)
 #pragma unroll
-      for (int k = 0; k < kMine; k += 32) {
-        if (k >= mine) continue;
-        float x[32];
+      for (int ch = 0; ch < kChunks; ++ch) {
+        float x[8];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) x[i] = k + i < kMine ? l[k + i < kMine ? k + i : 0] : 0.0f;
+        for (int i = 0; i < 8; i += 2) split2(l[ch * 4 + i / 2], x[i], x[i + 1]);
+        tmem_st8(tm_o + 128 + c0 + ch * 8, reinterpret_cast<const uint32_t*>(x));
+      }
+      tmem_wait_st();
+#pragma unroll 1
+      for (int ch = 0; ch < kChunks; ++ch) {
+        uint32_t x[8];
+        tmem_ld8(tm_o + 128 + c0 + ch * 8, x);
+        tmem_wait_ld();
+        float y[8];
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1)
+        for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(x[i]);
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1)                    // lane: of row lane mod 8
 #pragma unroll
           for (int i = 0; i < d; ++i) {
             const bool up = lane & d;
-            const float send = up ? x[i] : x[i + d];
-            x[i] = (up ? x[i + d] : x[i]) + __shfl_xor_sync(0xffffffffu, send, d);
+            const float send = up ? y[i] : y[i + d];
+            y[i] = (up ? y[i + d] : y[i]) + __shfl_xor_sync(0xffffffffu, send, d);
           }
-        if (k + lane < mine) s_part[warp & 3][c0 + k + lane] = x[0];
+        y[0] += __shfl_xor_sync(0xffffffffu, y[0], 8);
+        y[0] += __shfl_xor_sync(0xffffffffu, y[0], 16);
+        if (lane < 8) s_part[warp & 3][c0 + ch * 8 + lane] = y[0];
       }
       group_sync(id);
       const bool whole = walk.whole();
       const bool at_start = walk.pos - steps == walk.start;
       float* slot = a.slots + ((long long)blockIdx.x * 2 + (at_start ? 0 : 1)) * S::kSlot;
-      if (tid < mine && c0 + tid < rows) {
+      const int rows_end = walk.rows(a);
+      if (tid < kMine && c0 + tid < rows_end) {
         const int c = c0 + tid;
         float sum = (s_part[0][c] + s_part[1][c]) + (s_part[2][c] + s_part[3][c]);
         const float m = s_top[c];
@@ -498,51 +580,48 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           slot[c] = m;
           slot[N + c] = sum;
         } else if (a.lse) {
-          const int ti = s_tok[c], gi = row0 + c - ti * a.G;
+          const int ti = s_tok[c], gi = block_row0() + c - ti * a.G;
           a.lse[(walk.q.tok0 + ti) * (a.pool.H * a.G) + walk.head * a.G + gi] =
               sum == 0.0f ? -INFINITY : 0.69314718056f * (m + log2f(sum));
         }
       }
       group_sync(id);
       // ---- O out of tensor memory
-      ring_wait(smem_u32(&s_pv_done), pv_phase, abort_flag);
-      pv_phase ^= 1u;
-      __syncwarp();
-      tmem_after();
+      pv_wait(step - 1);
       if (D == 128 || (warp & 2) == 0) {
-#pragma unroll
+#pragma unroll 1
         for (int ch = 0; ch < kChunks; ++ch) {
-          if (ch >= chunks) continue;
-          uint32_t o[16];
-          tmem_ld16(tm_o + c0 + ch * 16, o);
+          uint32_t o[8];
+          tmem_ld8(tm_o + c0 + ch * 8, o);
           tmem_wait_ld();
+          const int c = c0 + ch * 8, left = rows_end - c;
+          if (whole) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int c = c0 + ch * 16 + i;
-            if (c < rows) {
-              if (whole)
-                reinterpret_cast<QT*>(a.out)[s_out[c] + tid] = QT(__uint_as_float(o[i]) * s_inv[c]);
-              else
-                slot[2 * N + (long long)c * D + tid] = __uint_as_float(o[i]);
-            }
+            for (int i = 0; i < 8; ++i)
+              if (i < left) reinterpret_cast<QT*>(a.out)[s_out[c + i] + tid] = QT(__uint_as_float(o[i]) * s_inv[c + i]);
+          } else {
+            float* to = slot + 2 * N + c * D + tid;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (i < left) to[i * D] = __uint_as_float(o[i]);
           }
         }
       }
       tmem_before();
       group_sync(id);                                      // before the rows' facts change
     }
-  } else if (warp < 12) {
+  } else if (warp < kQK + 4) {
     regs_down<S::kRegsOther>();
     const unsigned int leader = lane == 0;
     auto uniform = [](unsigned int x) { return __shfl_sync(0xffffffffu, x, 0); };
     const unsigned int tmu = uniform(tmem);
-    if (warp == 8) {
+    if (warp == kQK) {
       // ============================================================== S^T = K Q^T
       unsigned int buf = 0, phase = 0, q_phase = 0, step = 0;
       const unsigned int q_low = uniform(operand_low(smem0 + S::kQAt, 16)), k_low = uniform(operand_low(k0, 16));
       while (walk.next_warp(a, per)) {
         const int steps = (int)uniform(walk.t1 - walk.t0);
-        const unsigned int desc = uniform(col_mma_desc(std::is_same<KT, __half>::value, (walk.rows(a) + 31) / 32 * 32, false));
+        constexpr unsigned int desc = col_mma_desc(std::is_same<KT, __half>::value, N, false);
         ring_wait(smem_u32(&s_q_full), q_phase, abort_flag);
         q_phase ^= 1u;
         for (int j = 0; j < steps; ++j, ++step) {
@@ -564,17 +643,33 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           }
         }
       }
-    } else if (warp == 10) {
+    } else if (warp == kPV) {
       // ============================================================== O^T += V^T P^T
-      unsigned int buf = 0, phase = 0, p_phase = 0;
+      unsigned int buf = 0, phase = 0, step = 0;
+      if (lane == 0) {
+        TileWalk<Blocks> look = walk;
+        JoinRecord rec = {};
+        if (look.next(a) == 1 && look.t0 > 0 && look.t1 == look.span.tiles) {
+          const long long p0 = look.pos - look.t1;         // position of the rows' first tile
+          rec.tok0 = look.q.tok0;
+          rec.rows = look.rows(a);
+          rec.row0 = look.block * Blocks::size(look.q.n * a.G);
+          rec.head = look.head;
+          rec.first_cta = (int)(p0 / per);
+          rec.first_slot = p0 != rec.first_cta * per;
+        }
+        reinterpret_cast<JoinRecord*>(a.slots + 2ull * gridDim.x * S::kSlot)[blockIdx.x] = rec;
+      }
+      __syncwarp();
       // (at D = 64 the M of 128 reaches past V, into what lies there: lanes that nobody reads)
       const unsigned int v_low = uniform(operand_low(v0, S::kColBytes)), p_low = uniform(operand_low(smem0 + S::kPAt, S::kColBytes));
       while (walk.next_warp(a, per)) {
         const int steps = (int)uniform(walk.t1 - walk.t0);
-        const unsigned int desc = uniform(col_mma_desc(std::is_same<VT, __half>::value, (walk.rows(a) + 31) / 32 * 32, true));
+        constexpr unsigned int desc = col_mma_desc(std::is_same<VT, __half>::value, N, true);
         const int key_first = (int)uniform((walk.span.tile0 + walk.t0) * kTileKeys);
         const int lo = (int)uniform(walk.span.lo), hi = (int)uniform(walk.span.hi);
-        for (int j = 0; j < steps; ++j) {
+        for (int j = 0; j < steps; ++j, ++step) {
+          const unsigned int pb = step % S::kPs;
           ring_wait(smem_u32(&s_v_full[buf]), phase, abort_flag);
           if (!F8) {
             // V rows of positions that no row sees, whatever the pool holds there, become zero (0 * NaN is NaN)
@@ -594,8 +689,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
               __syncwarp();
             }
           }
-          ring_wait(smem_u32(&s_p_full), p_phase, abort_flag);
-          p_phase ^= 1u;
+          ring_wait(smem_u32(&s_p_full[pb]), (step / S::kPs) & 1u, abort_flag);
           __syncwarp();
           tmem_after();
           const unsigned int low = v_low + buf * (S::kBuf >> 4);
@@ -603,9 +697,9 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           for (int part = 0; part < kParts; ++part)
 #pragma unroll
             for (int k = 0; k < kTileKeys / 16; ++k)
-              mma_smem(tmu + 256, operand_desc(low + k * (2048 >> 4)), operand_desc(p_low + ((part * S::kP + k * 2048) >> 4)),
+              mma_smem(tmu + 256, operand_desc(low + k * (2048 >> 4)), operand_desc(p_low + (((pb * kParts + part) * S::kP + k * 2048) >> 4)),
                        desc, part > 0 || k > 0 || j > 0, leader);
-          mma_commit(smem_u32(&s_pv_done), leader);
+          mma_commit(smem_u32(&s_pv_done[pb]), leader);
           mma_commit(smem_u32(&s_v_empty[buf]), leader);
           if (++buf == S::kV) {
             buf = 0;
@@ -613,25 +707,52 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           }
         }
       }
-    } else if (warp == 9) {
-      // ============================================================== loader warp
+    } else {
+      // ============================================================== loader warps, of K and of V
+      // (A box takes its warp 75 cycles to issue: 16 of either K or V in one warp's loop took longer than
+      // the bytes need.)
+      const bool is_v = uniform(warp == kLoadV);
       constexpr unsigned int kBytes = F8 ? S::kRaw : S::kBuf;
       constexpr int kRow = F8 ? D : 128;
+      unsigned long long* full = is_v ? (F8 ? s_v_raw : s_v_full) : (F8 ? s_k_raw : s_k_full);
+      unsigned long long* empty = is_v ? s_v_empty : s_k_empty;
+      const unsigned int ring0 = (is_v ? v0 : k0) + (F8 ? S::kColBytes : 0), bufs = is_v ? S::kV : S::kK;
       const int boxes = kTileKeys >> a.box_log;
-      unsigned int kbuf = 0, kphase = 1, vbuf = 0, vphase = 1, issued = 0;   // (a fresh barrier passes for phase 1)
+      unsigned int buf = 0, phase = 1, issued = 0;         // (a fresh barrier passes for phase 1)
       while (walk.next_warp(a, per)) {
         const uint32_t* row;
         long long entries;
         table_row(a.b, walk.r, row, entries);
-        const bool tell = walk.head == 0 && walk.block == 0;
-        if (walk.q.keys < walk.q.len && tell && walk.t0 == 0 && lane == 0)
+        if (!is_v && walk.q.keys < walk.q.len && walk.head == 0 && walk.block == 0 && walk.t0 == 0 && lane == 0)
           raise_status(AIBX_ERR_RANGE);                    // tokens the table has no entry for
         BoxIds<kTileKeys> ids(a, row, walk.span.tile0 + walk.t0, walk.span.tile0 + walk.t1, walk.span.lo,
                               walk.span.hi);
         const int head = walk.head, tile0 = walk.span.tile0, lo = walk.span.lo, hi = walk.span.hi, t1 = walk.t1;
+        // Scale bytes, four keys a lane, by V's loader: block ids two tiles ahead, bytes one tile ahead.
+        uint32_t id_next = AIBX_NO_BLOCK, kb_next[4], vb_next[4];   // (combined when used: nothing waits for a load before)
+        auto fetch_id = [&](int t) {
+          const int tok = (tile0 + t) * kTileKeys + lane * 4;
+          return t < t1 && tok < hi && tok + 4 > lo ? __ldg(row + tok / a.pool.T) : AIBX_NO_BLOCK;
+        };
+        auto fetch_bytes = [&](int t) {
+          const bool there = id_next < a.pool.num_blocks;  // four slots of one block
+          const int tok = (tile0 + t) * kTileKeys + lane * 4;
+          const unsigned char* src = a.pool.scales + (long long)id_next * a.pool.s_block + (long long)head * a.pool.s_head +
+                                     (long long)(tok % a.pool.T) * a.pool.s_slot;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            kb_next[i] = there ? __ldg(src + i * a.pool.s_slot) : 127u;
+            vb_next[i] = there ? __ldg(src + a.pool.s_kv + i * a.pool.s_slot) : 127u;
+          }
+        };
+        if (F8 && is_v) {
+          id_next = fetch_id(walk.t0);
+          fetch_bytes(walk.t0);
+          id_next = fetch_id(walk.t0 + 1);
+        }
         for (int j = walk.t0; j < t1; ++j, ++issued) {
           uint32_t block_id;
-          const bool valid = ids.give(block_id, head == 0);
+          const bool valid = ids.give(block_id, !is_v && head == 0);
           const int slot = ids.slot;
           ids.step_slot();
           // a box that is not there, or that holds no visible key, comes as zeros from beyond the pool
@@ -639,100 +760,62 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           const int tok = (tile0 + j) * kTileKeys + (lane & (boxes - 1)) * a.box;
           const bool missing = lane < boxes && tok < hi && tok > lo - a.box && !valid;
           const unsigned int gone = __ballot_sync(0xffffffffu, missing);
-          if (lane == 0) s_mask[issued % kInfoRing] = ~gone;
-          for (int kv = 0; kv < 2; ++kv) {
-            const unsigned int buf = kv ? vbuf : kbuf;
-            ring_wait(smem_u32(kv ? &s_v_empty[vbuf] : &s_k_empty[kbuf]), kv ? vphase : kphase, abort_flag);
-            __syncwarp();
-            const unsigned int bar = smem_u32(kv ? (F8 ? &s_v_raw[vbuf] : &s_v_full[vbuf]) : (F8 ? &s_k_raw[kbuf] : &s_k_full[kbuf]));
-            if (__any_sync(0xffffffffu, *abort_flag)) {
-              if (lane == 0) mbar_arrive(bar);
-            } else {
-              if (lane == 0) mbar_arrive_expect_tx(bar, kBytes);
-              __syncwarp();
-              if (lane < boxes) {
-                const unsigned int dst = (kv ? v0 : k0) + (F8 ? S::kColBytes : 0) + buf * S::kBuf + lane * a.box * kRow;
+          if (!is_v && lane == 0) s_mask[issued % kInfoRing] = ~gone;
+          if (F8 && is_v) {
+            const int first = (tile0 + j) * kTileKeys + lane * 4;
+            bool odd = first < lo || first > hi - 4;       // (rows outside: zeros)
+            const uint32_t kb = kb_next[0] | kb_next[1] << 8 | kb_next[2] << 16 | kb_next[3] << 24;
+            const uint32_t vb = vb_next[0] | vb_next[1] << 8 | vb_next[2] << 16 | vb_next[3] << 24;
 #pragma unroll
-                for (int cc = 0; cc < (F8 ? 1 : S::kCols); ++cc)
-                  tensor_load_5d(dst + cc * S::kColBytes, &map, bar, cc * 64, slot, head, block, kv);
-              }
-            }
+            for (int i = 0; i < 4; ++i) odd |= (int)((vb >> (8 * i)) & 255u) != weight_byte((vb >> (8 * i)) & 255u);
+            odd = __any_sync(0xffffffffu, odd);
+            const unsigned int f = issued % kColInfo;
+            ring_wait(smem_u32(&s_info_empty[f]), ((issued / kColInfo) & 1u) ^ 1u, abort_flag);
             __syncwarp();
+            *reinterpret_cast<uint32_t*>(&s_bytes[f][0][lane * 4]) = kb;
+            *reinterpret_cast<uint32_t*>(&s_bytes[f][1][lane * 4]) = vb;
+            if (lane == 0) s_odd[f] = odd;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_info_full[f]));
+            fetch_bytes(j + 1);
+            id_next = fetch_id(j + 2);
           }
-          if (++kbuf == S::kK) {
-            kbuf = 0;
-            kphase ^= 1u;
+          ring_wait(smem_u32(&empty[buf]), phase, abort_flag);
+          __syncwarp();
+          const unsigned int bar = smem_u32(&full[buf]);
+          if (__any_sync(0xffffffffu, *abort_flag)) {
+            if (lane == 0) mbar_arrive(bar);
+          } else {
+            if (lane == 0) mbar_arrive_expect_tx(bar, kBytes);
+            __syncwarp();
+            if (lane < boxes) {
+              const unsigned int dst = ring0 + buf * S::kBuf + lane * a.box * kRow;
+#pragma unroll
+              for (int cc = 0; cc < (F8 ? 1 : S::kCols); ++cc)
+                tensor_load_5d(dst + cc * S::kColBytes, &map, bar, cc * 64, slot, head, block, is_v ? 1 : 0);
+            }
           }
-          if (++vbuf == S::kV) {
-            vbuf = 0;
-            vphase ^= 1u;
+          __syncwarp();
+          if (++buf == bufs) {
+            buf = 0;
+            phase ^= 1u;
           }
         }
       }
       // nothing may still be on its way here when the CTA ends: no copy, no word of a product
-      for (unsigned int i = issued > S::kK ? issued - S::kK : 0; i < issued; ++i) {
-        ring_drain(smem_u32(F8 ? &s_k_raw[i % S::kK] : &s_k_full[i % S::kK]), (i / S::kK) & 1u);
-        ring_wait(smem_u32(&s_k_empty[i % S::kK]), (i / S::kK) & 1u, abort_flag);
-      }
-      for (unsigned int i = issued > S::kV ? issued - S::kV : 0; i < issued; ++i) {
-        ring_drain(smem_u32(F8 ? &s_v_raw[i % S::kV] : &s_v_full[i % S::kV]), (i / S::kV) & 1u);
-        ring_wait(smem_u32(&s_v_empty[i % S::kV]), (i / S::kV) & 1u, abort_flag);
-      }
-    } else if (F8 && warp == 11) {
-      // ============================================================== scale bytes, four keys a lane
-      unsigned int step = 0;
-      while (walk.next_warp(a, per)) {
-        const uint32_t* row;
-        long long entries;
-        table_row(a.b, walk.r, row, entries);
-        const int head = walk.head, tile0 = walk.span.tile0, lo = walk.span.lo, hi = walk.span.hi, t1 = walk.t1;
-        for (int j = walk.t0; j < t1; ++j, ++step) {
-          const int tok = (tile0 + j) * kTileKeys + lane * 4;   // four slots of one block
-          uint32_t kb = 0x7f7f7f7fu, vb = 0x7f7f7f7fu;
-          unsigned int there = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (tok + i >= lo && tok + i < hi) there |= 1u << i;
-          if (there) {
-            const int at = tok / a.pool.T;
-            const uint32_t block = __ldg(row + at);
-            if (block < a.pool.num_blocks) {
-              const unsigned char* src = a.pool.scales + (long long)block * a.pool.s_block +
-                                         (long long)head * a.pool.s_head +
-                                         (long long)(tok - at * a.pool.T) * a.pool.s_slot;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t x = __ldg(src + i * a.pool.s_slot), y = __ldg(src + a.pool.s_kv + i * a.pool.s_slot);
-                if ((there >> i) & 1u) {
-                  kb = (kb & ~(255u << (8 * i))) | x << (8 * i);
-                  vb = (vb & ~(255u << (8 * i))) | y << (8 * i);
-                }
-              }
-            }
-          }
-          bool odd = there != 15u;                         // (rows outside: zeros)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) odd |= (int)((vb >> (8 * i)) & 255u) != weight_byte((vb >> (8 * i)) & 255u);
-          odd = __any_sync(0xffffffffu, odd);
-          const unsigned int f = step % kColInfo;
-          ring_wait(smem_u32(&s_info_empty[f]), ((step / kColInfo) & 1u) ^ 1u, abort_flag);
-          __syncwarp();
-          *reinterpret_cast<uint32_t*>(&s_bytes[f][0][lane * 4]) = kb;
-          *reinterpret_cast<uint32_t*>(&s_bytes[f][1][lane * 4]) = vb;
-          if (lane == 0) s_odd[f] = odd;
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&s_info_full[f]));
-        }
+      for (unsigned int i = issued > bufs ? issued - bufs : 0; i < issued; ++i) {
+        ring_drain(smem_u32(&full[i % bufs]), (i / bufs) & 1u);
+        ring_wait(smem_u32(&empty[i % bufs]), (i / bufs) & 1u, abort_flag);
       }
     }
   } else if constexpr (F8) {
-    // ================================================================ converter warps (12 .. 15)
-    regs_down<S::kRegsOther>();
-    // A thread takes one 16-byte piece of kRows neighbouring rows, half of them at a time; a row's
-    // pieces are one warp's, which has read them all before it writes over them.
-    const int tid = threadIdx.x - 384;
+    // ================================================================ converter warps
+    regs_down<S::kRegsConvert>();
+    // A thread takes one 16-byte piece of kRows neighbouring rows; a row's pieces are one warp's, which has
+    // read them all before it writes over them.
+    const int tid = threadIdx.x - 32 * (kQK + 4);
     constexpr int kPieces = D / 16;                        // 16-byte pieces of a raw row
-    constexpr int kRows = kTileKeys * kPieces / 128;
+    constexpr int kRows = kTileKeys * kPieces / (128 * S::kConverters);
     const int c = tid % kPieces, i0 = tid / kPieces * kRows;
     unsigned int kbuf = 0, kphase = 0, vbuf = 0, vphase = 0, step = 0;
     while (walk.next_warp(a, per)) {
@@ -743,7 +826,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         auto convert = [&](unsigned int at, auto is_v, auto odd) {
           unsigned char* out = base + at + (c >> 2) * S::kColBytes;
           const unsigned char* src = base + at + S::kColBytes;
-          constexpr int kTurn = kRows / 2;
+          constexpr int kTurn = kRows;
 #pragma unroll
           for (int u0 = 0; u0 < kRows; u0 += kTurn) {
             uint4 v[kTurn];
@@ -773,7 +856,10 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
                 else if constexpr (decltype(odd)::value)
                   o[e] = gone ? 0u : bf16_of_e4m3(two, rest);
                 else
-                  o[e] = bf16_of_e4m3(two, 1.0f);
+{
+                  const float2 y = __half22float2(halves_of_e4m3(two));
+                  o[e] = Bits16<__nv_bfloat16>::pack(y.x, y.y);
+                }
               }
               const int p0 = (2 * c) & 7;
               *reinterpret_cast<uint4*>(out + i * 128 + ((p0 ^ (i & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
@@ -809,7 +895,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   }
   tmem_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == kQK) {
     tmem_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
