@@ -5,7 +5,7 @@
 // shrinks with the rows (a tile of 128 rows, filled or not, costs its softmax 128 exponentials a key; here
 // a row costs one).  A block of up to N rows meets KV tiles of 128 positions:
 //   S^T = K Q^T        [128 keys][rows], K and Q from shared memory, S^T in tensor memory (fp32)
-//   P^T = 2^(S^T c - m)   one thread per key and quarter of the rows; P^T to shared memory, 16-bit
+//   P^T = 2^(S^T c - m)   one thread per key and a quarter or half of the rows; P^T to shared memory, 16-bit
 //   O^T += V^T P^T     [dims][rows], V as it lies in the pool ([position][dim]: V^T's M-major form)
 // A row's maximum runs across the threads, which is what makes this form dear; but m needs to move only
 // when a score passes it by 2^8 (weights up to 2^8 are as good as weights up to 1).  So a tile costs one
@@ -21,8 +21,9 @@
 // outside [kScaleLow, kScaleHigh] leave the rest with V).  fp16 queries get weights as the sum of two
 // bf16 numbers, so that they lose nothing to the type.
 //
-// Roles: four softmax warpgroups, one for each quarter of the rows, which never wait for each other; a warp
-// for S^T and one for O^T; a loader of K and one of V (and of the scale bytes); over e4m3 eight that convert.  Rings of K
+// Roles: four softmax warpgroups (e4m3: two), each with its part of the rows, which never wait for each other; a warp
+// for S^T and one for O^T; a loader of K and one of V; over e4m3 eight that convert and
+// fetch the scale bytes.  Rings of K
 // and of V tiles of their own, S^T twice, so that S^T(j + 1) runs beside the softmax of tile j.
 // Bound: HBM, 2,800 cycles a tile of 128 16-bit keys of D = 128 (this SM's share), 1,400 of e4m3 ones; the
 // products take (4 + 4) * N cycles of the tensor pipe.
@@ -38,6 +39,13 @@ struct EvenBlocks {
   static __device__ __forceinline__ int size(int rows) {
     const int blocks = (int)(((long long)rows + MOST - 1) / MOST);
     return (int)(((long long)rows + blocks - 1) / blocks);
+  }
+  // (requests of more rows than col_limit are the tile kernel's)
+  static __device__ __forceinline__ int blocks(const AttnArgs& a, const AttnRequest& q) {
+    const long long rows = (long long)q.n * a.G;
+    if (rows == 0 || rows > a.col_limit) return 0;
+    const int each = size((int)rows);
+    return (int)((rows + each - 1) / each);
   }
   static __device__ __forceinline__ TileSpan span(const AttnArgs& a, const AttnRequest& q, int) {
     const long long first = (long long)q.len - q.n;
@@ -58,7 +66,7 @@ struct EvenCost {
   __device__ __forceinline__ long long operator()(int r, bool on) const {
     if (!on) return 0;
     const AttnRequest q = attn_request(a.b, a.pool.T, r);
-    return (long long)TileCost<B>{a}.blocks(q) * B::span(a, q, 0).tiles * a.pool.H;
+    return (long long)B::blocks(a, q) * B::span(a, q, 0).tiles * a.pool.H;
   }
 };
 
@@ -69,7 +77,7 @@ __device__ __forceinline__ void locate_even(const AttnArgs& a, unsigned int inde
   if (w->r < 0) return;
   const AttnRequest q = attn_request(a.b, a.pool.T, w->r);
   const long long per = (w->total + pieces - 1) / pieces;
-  const int blocks = TileCost<B>{a}.blocks(q), tiles = B::span(a, q, 0).tiles;
+  const int blocks = B::blocks(a, q), tiles = B::span(a, q, 0).tiles;
   const long long segments = (long long)blocks * a.pool.H;
   long long g = (segments * tiles + per / 2) / per;        // as in request_line
   g = g < 1 ? 1 : g > segments ? segments : g;
@@ -94,7 +102,9 @@ __device__ __forceinline__ void locate_even(const AttnArgs& a, unsigned int inde
 
 template <int D, bool F8, int N>
 struct ColShape {
-  static constexpr int kGroups = 4;                        // softmax warpgroups
+  // Softmax warpgroups.  (Over e4m3 two, of 32 rows each: with four the waits and barriers of twice the warps
+  // stand in the converters' way, 371 instead of 356 us.)
+  static constexpr int kGroups = F8 ? 2 : 4;
   static constexpr int kConverters = F8 ? 2 : 0;           // warpgroups that convert
   static constexpr int kThreads = 128 * (kGroups + 1 + kConverters);
   static constexpr int kCols = D / 64;                     // 128-byte columns of an operand row
@@ -115,9 +125,8 @@ struct ColRings : ColShape<D, F8, N> {
   static constexpr int kQAt = (kK + kV) * B::kBuf, kPAt = kQAt + B::kQ;
   static constexpr int kSmem = kPAt + kPs * PARTS * B::kP + 1024;
   static constexpr int kSlot = N * (D + 2);                // floats per workspace slot
-  static constexpr int kRegsSoftmax = F8 ? 80 : 104;       // launch: 72 (896 threads), 96 (640)
-  static constexpr int kRegsOther = F8 ? 56 : 64;          // 4 * 80 + 56 + 2 * 64 = 7 * 72; 4 * 104 + 64 = 5 * 96
-  static constexpr int kRegsConvert = 64;
+  static constexpr int kRegsSoftmax = F8 ? 136 : 104;      // launch: 96 (640 threads both)
+  static constexpr int kRegsOther = 64, kRegsConvert = 72; // 2 * 136 + 64 + 2 * 72 = 4 * 104 + 64 = 5 * 96
   static_assert(kK >= 2 && kV >= 2, "two tiles of each at least");
 };
 
@@ -157,7 +166,7 @@ __device__ __forceinline__ int float_order(float x) {
 }
 __device__ __forceinline__ float order_float(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
 
-constexpr int kColInfo = 4;                                // per-tile facts of an e4m3 pool
+constexpr int kColBatch = 4, kColInfo = 4;                 // scale bytes: tiles at a time, and batches in the ring
 
 template <int D, bool F8, typename QT, int N>
 __global__ void __launch_bounds__(ColShape<D, F8, N>::kThreads, 1)
@@ -182,8 +191,8 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
   __shared__ int s_new[N], s_low[N], s_tok[N];
   __shared__ long long s_out[N];
   __shared__ float s_part[4][N];
-  __shared__ __align__(4) unsigned char s_bytes[F8 ? kColInfo : 1][2][kTileKeys];
-  __shared__ int s_odd[kColInfo];                          // whether V's bytes leave a rest with V
+  __shared__ __align__(4) unsigned char s_bytes[F8 ? kColInfo * kColBatch : 1][2][kTileKeys];
+  __shared__ int s_odd[kColInfo * kColBatch][4];                     // whether V's bytes leave a rest with V, by 32 keys
   __shared__ long long s_scan[33];
   __shared__ WorkStart s_start;
   __shared__ TileWalk<Blocks> s_walk[S::kThreads / 32];
@@ -215,7 +224,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       mbar_init(smem_u32(&s_pv_done[i]), 1u);
     }
     for (int i = 0; i < kColInfo; ++i) {
-      mbar_init(smem_u32(&s_info_full[i]), 1u);
+      mbar_init(smem_u32(&s_info_full[i]), 4u * (F8 ? S::kConverters : 1));
       mbar_init(smem_u32(&s_info_empty[i]), 4u * (S::kGroups + S::kConverters));
     }
     mbar_init(smem_u32(&s_q_full), 128u * S::kGroups);
@@ -262,7 +271,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     const unsigned int tm_s = tmem + lanes, tm_o = tmem + lanes + 256;
     unsigned char* s_q = base + S::kQAt;
     const int c0 = w * kMine;                              // first of this warpgroup's rows in a block
-    unsigned int step = 0, votes = 0;
+    unsigned int step = 0, votes = 0, batch = 0;
     auto pv_wait = [&](unsigned int x) {                   // the product of step x is done, and so are all before
       ring_wait(smem_u32(&s_pv_done[x % S::kPs]), (x / S::kPs) & 1u, abort_flag);
       __syncwarp();
@@ -354,13 +363,16 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         const unsigned int sb = step & 1u;
         float kf = 1.0f, vf = 1.0f;
         if constexpr (F8) {
-          const unsigned int f = step % kColInfo;
-          ring_wait(smem_u32(&s_info_full[f]), (step / kColInfo) & 1u, abort_flag);
-          const int kb = s_bytes[f][0][tid], vb = s_bytes[f][1][tid];
+          const unsigned int f = batch % kColInfo;
+          if (j % kColBatch == 0) ring_wait(smem_u32(&s_info_full[f]), (batch / kColInfo) & 1u, abort_flag);
+          const int kb = s_bytes[f * kColBatch + j % kColBatch][0][tid], vb = s_bytes[f * kColBatch + j % kColBatch][1][tid];
           kf = kb == 255 ? NAN : power_of_byte(kb);
           vf = power_of_byte(weight_byte(vb));
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&s_info_empty[f]));
+          if (j % kColBatch == kColBatch - 1 || j == steps - 1) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_info_empty[f]));
+            ++batch;
+          }
         }
         ring_wait(smem_u32(&s_s_full[sb]), (step >> 1) & 1u, abort_flag);
         __syncwarp();
@@ -536,7 +548,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         if (lane == 0) mbar_arrive(smem_u32(&s_p_full[step % S::kPs]));
       }
       // ---- sums over the keys, 8 rows at a time, by way of tensor memory: taken from registers in a rolled
-      // loop (unrolled over all rows, this part took registers from the loop above: 237 instead of 1XX us)
+      // loop (unrolled over all rows, this part took registers from the loop above: 230 instead of 163 us for 32 drafts of 128 rows)
 #pragma unroll
       for (int ch = 0; ch < kChunks; ++ch) {
         float x[8];
@@ -728,28 +740,6 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         BoxIds<kTileKeys> ids(a, row, walk.span.tile0 + walk.t0, walk.span.tile0 + walk.t1, walk.span.lo,
                               walk.span.hi);
         const int head = walk.head, tile0 = walk.span.tile0, lo = walk.span.lo, hi = walk.span.hi, t1 = walk.t1;
-        // Scale bytes, four keys a lane, by V's loader: block ids two tiles ahead, bytes one tile ahead.
-        uint32_t id_next = AIBX_NO_BLOCK, kb_next[4], vb_next[4];   // (combined when used: nothing waits for a load before)
-        auto fetch_id = [&](int t) {
-          const int tok = (tile0 + t) * kTileKeys + lane * 4;
-          return t < t1 && tok < hi && tok + 4 > lo ? __ldg(row + tok / a.pool.T) : AIBX_NO_BLOCK;
-        };
-        auto fetch_bytes = [&](int t) {
-          const bool there = id_next < a.pool.num_blocks;  // four slots of one block
-          const int tok = (tile0 + t) * kTileKeys + lane * 4;
-          const unsigned char* src = a.pool.scales + (long long)id_next * a.pool.s_block + (long long)head * a.pool.s_head +
-                                     (long long)(tok % a.pool.T) * a.pool.s_slot;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            kb_next[i] = there ? __ldg(src + i * a.pool.s_slot) : 127u;
-            vb_next[i] = there ? __ldg(src + a.pool.s_kv + i * a.pool.s_slot) : 127u;
-          }
-        };
-        if (F8 && is_v) {
-          id_next = fetch_id(walk.t0);
-          fetch_bytes(walk.t0);
-          id_next = fetch_id(walk.t0 + 1);
-        }
         for (int j = walk.t0; j < t1; ++j, ++issued) {
           uint32_t block_id;
           const bool valid = ids.give(block_id, !is_v && head == 0);
@@ -761,25 +751,6 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           const bool missing = lane < boxes && tok < hi && tok > lo - a.box && !valid;
           const unsigned int gone = __ballot_sync(0xffffffffu, missing);
           if (!is_v && lane == 0) s_mask[issued % kInfoRing] = ~gone;
-          if (F8 && is_v) {
-            const int first = (tile0 + j) * kTileKeys + lane * 4;
-            bool odd = first < lo || first > hi - 4;       // (rows outside: zeros)
-            const uint32_t kb = kb_next[0] | kb_next[1] << 8 | kb_next[2] << 16 | kb_next[3] << 24;
-            const uint32_t vb = vb_next[0] | vb_next[1] << 8 | vb_next[2] << 16 | vb_next[3] << 24;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) odd |= (int)((vb >> (8 * i)) & 255u) != weight_byte((vb >> (8 * i)) & 255u);
-            odd = __any_sync(0xffffffffu, odd);
-            const unsigned int f = issued % kColInfo;
-            ring_wait(smem_u32(&s_info_empty[f]), ((issued / kColInfo) & 1u) ^ 1u, abort_flag);
-            __syncwarp();
-            *reinterpret_cast<uint32_t*>(&s_bytes[f][0][lane * 4]) = kb;
-            *reinterpret_cast<uint32_t*>(&s_bytes[f][1][lane * 4]) = vb;
-            if (lane == 0) s_odd[f] = odd;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_info_full[f]));
-            fetch_bytes(j + 1);
-            id_next = fetch_id(j + 2);
-          }
           ring_wait(smem_u32(&empty[buf]), phase, abort_flag);
           __syncwarp();
           const unsigned int bar = smem_u32(&full[buf]);
@@ -817,12 +788,54 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
     constexpr int kPieces = D / 16;                        // 16-byte pieces of a raw row
     constexpr int kRows = kTileKeys * kPieces / (128 * S::kConverters);
     const int c = tid % kPieces, i0 = tid / kPieces * kRows;
-    unsigned int kbuf = 0, kphase = 0, vbuf = 0, vphase = 0, step = 0;
+    unsigned int kbuf = 0, kphase = 0, vbuf = 0, vphase = 0, batch = 0, made = 0;
     while (walk.next_warp(a, per)) {
       const int steps = walk.t1 - walk.t0;
       const int key_first = (walk.span.tile0 + walk.t0) * kTileKeys, lo = walk.span.lo, hi = walk.span.hi;
-      for (int j = 0; j < steps; ++j, ++step) {
-        const unsigned int f = step % kColInfo;
+      // Scale bytes are fetched four tiles at a time, the next four while these are converted: two dependent
+      // loads, which the warps wait for here once in four tiles.
+      const uint32_t* row;
+      long long entries;
+      table_row(a.b, walk.r, row, entries);
+      const unsigned char* scales = a.pool.scales + (long long)walk.head * a.pool.s_head;
+      auto fetch = [&](int j0) {
+        constexpr int kEach = kColBatch * kTileKeys / (128 * (F8 ? S::kConverters : 1));   // keys of a thread
+        const unsigned int f = made % kColInfo;
+        uint32_t block[kEach], kb[kEach], vb[kEach];
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+          const int key = key_first + j0 * kTileKeys + u * (128 * S::kConverters) + tid;
+          block[u] = key >= lo && key < hi ? __ldg(row + key / a.pool.T) : AIBX_NO_BLOCK;
+          kb[u] = vb[u] = 127;
+        }
+#pragma unroll
+        for (int u = 0; u < kEach; ++u)
+          if (block[u] < a.pool.num_blocks) {
+            const int key = key_first + j0 * kTileKeys + u * (128 * S::kConverters) + tid;
+            const unsigned char* src = scales + (long long)block[u] * a.pool.s_block + (long long)(key % a.pool.T) * a.pool.s_slot;
+            kb[u] = __ldg(src);
+            vb[u] = __ldg(src + a.pool.s_kv);
+          }
+        ring_wait(smem_u32(&s_info_empty[f]), ((made / kColInfo) & 1u) ^ 1u, abort_flag);
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < kEach; ++u) {
+          const int x = u * (128 * S::kConverters) + tid, t = x / kTileKeys, k = x % kTileKeys;
+          const int key = key_first + j0 * kTileKeys + x;
+          s_bytes[f * kColBatch + t][0][k] = (unsigned char)kb[u];
+          s_bytes[f * kColBatch + t][1][k] = (unsigned char)vb[u];
+          // (rows outside: zeros)
+          const bool odd = __any_sync(0xffffffffu, (int)vb[u] != weight_byte((int)vb[u]) || key < lo || key >= hi);
+          if (lane == 0) s_odd[f * kColBatch + t][k >> 5] = odd;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_info_full[f]));
+        ++made;
+      };
+      fetch(0);
+      for (int j = 0; j < steps; ++j) {
+        const unsigned int f = batch % kColInfo, ft = f * kColBatch + j % kColBatch;
+        if (j % kColBatch == 0 && j + kColBatch < steps) fetch(j + kColBatch);
         auto convert = [&](unsigned int at, auto is_v, auto odd) {
           unsigned char* out = base + at + (c >> 2) * S::kColBytes;
           const unsigned char* src = base + at + S::kColBytes;
@@ -844,7 +857,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
               float rest = 1.0f;
               bool gone = false;
               if constexpr (decltype(odd)::value) {
-                const int key = key_first + j * kTileKeys + i, vb = s_bytes[f][1][i];
+                const int key = key_first + j * kTileKeys + i, vb = s_bytes[ft][1][i];
                 gone = key < lo || key >= hi;              // whatever the pool holds there
                 rest = vb == 255 ? NAN : power_of_byte(127 + vb - weight_byte(vb));
               }
@@ -861,9 +874,13 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
                   o[e] = Bits16<__nv_bfloat16>::pack(y.x, y.y);
                 }
               }
-              const int p0 = (2 * c) & 7;
-              *reinterpret_cast<uint4*>(out + i * 128 + ((p0 ^ (i & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-              *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + 1) ^ (i & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+              // (pieces 2 c and 2 c + 1; the upper half of a row's lanes the other way round: with their
+              // column 16 KB on they would meet the lower half's banks)
+              const int p0 = (2 * c) & 7, flip = c >> 2 & 1;
+              *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + flip) ^ (i & 7)) << 4)) =
+                  flip ? make_uint4(o[4], o[5], o[6], o[7]) : make_uint4(o[0], o[1], o[2], o[3]);
+              *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + 1 - flip) ^ (i & 7)) << 4)) =
+                  flip ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(o[4], o[5], o[6], o[7]);
             }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -876,16 +893,19 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           kbuf = 0;
           kphase ^= 1u;
         }
-        ring_wait(smem_u32(&s_info_full[f]), (step / kColInfo) & 1u, abort_flag);
+        if (j % kColBatch == 0) ring_wait(smem_u32(&s_info_full[f]), (batch / kColInfo) & 1u, abort_flag);
         ring_wait(smem_u32(&s_v_raw[vbuf]), vphase, abort_flag);
         __syncwarp();
-        if (s_odd[f])
+        if (s_odd[ft][0] | s_odd[ft][1] | s_odd[ft][2] | s_odd[ft][3])
           convert((v0 - smem0) + vbuf * S::kBuf, std::true_type(), std::true_type());
         else
           convert((v0 - smem0) + vbuf * S::kBuf, std::true_type(), std::false_type());
         mbar_arrive(smem_u32(&s_v_full[vbuf]));
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_info_empty[f]));
+        if (j % kColBatch == kColBatch - 1 || j == steps - 1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&s_info_empty[f]));
+          ++batch;
+        }
         if (++vbuf == S::kV) {
           vbuf = 0;
           vphase ^= 1u;

@@ -51,11 +51,13 @@ struct AttnArgs {
   int G;                                    // query heads per KV head
   SmallDivisor by_g;
   int causal, window;
+  SmallDivisor by_pos;                      // by_g where a row's position follows its token; 0 for trees
   const uint32_t* mask;                     // trees: 32-bit words of a token's mask, the lowest first
   int mask_words;                           // how many
   int box, box_log;                         // tokens one tensor-map box covers: a power of two
   int row_limit;                            // requests of up to so many rows (tokens * G) are the
                                             // row kernel's, 0: none
+  int col_limit;                            // trees: the most rows of the requests that are the column kernel's
   int max_new;                              // bound on a request's tokens, 0: none given
   float* slots;                             // two per CTA, then a JoinRecord per CTA
 };
@@ -352,9 +354,6 @@ attn_join_kernel(const __grid_constant__ AttnArgs a, JoinSet rows, JoinSet tiles
   if (a.max_new > 0 && blockIdx.x == 0 && blockIdx.y == 0)
     for (int r = threadIdx.x; r < a.b.R; r += 256)
       if (attn_request(a.b, a.pool.T, r).n > a.max_new) raise_status(AIBX_ERR_RANGE);
-  if (a.mask && blockIdx.x == 0 && blockIdx.y == 0)      // and those with more than their masks can name
-    for (int r = threadIdx.x; r < a.b.R; r += 256)
-      if (attn_request(a.b, a.pool.T, r).n > 32 * a.mask_words) raise_status(AIBX_ERR_RANGE);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const bool of_rows = (int)blockIdx.y < y_rows;
   const int y = of_rows ? (int)blockIdx.y : (int)blockIdx.y - y_rows;
@@ -394,19 +393,81 @@ attn_join_kernel(const __grid_constant__ AttnArgs a, JoinSet rows, JoinSet tiles
   }
 }
 
+// The same for trees, whose few rows over long contexts are cut into many pieces: a warp per row, the pieces'
+// maxima and sums a piece a lane, their outputs several at once.
 template <int D, typename QT>
+__global__ void __launch_bounds__(512)
+attn_join_tree_kernel(const __grid_constant__ AttnArgs a, JoinSet rows, JoinSet tiles, int y_rows) {
+  // Requests with more tokens than the caller's bound, or than their masks can name
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int r = threadIdx.x; r < a.b.R; r += 512) {
+      const int n = attn_request(a.b, a.pool.T, r).n;
+      if ((a.max_new > 0 && n > a.max_new) || n > 32 * a.mask_words) raise_status(AIBX_ERR_RANGE);
+    }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const bool of_rows = (int)blockIdx.y < y_rows;
+  const int lane = threadIdx.x & 31, i = ((int)blockIdx.y - (of_rows ? 0 : y_rows)) * 16 + (threadIdx.x >> 5);
+  const float* slots = of_rows ? rows.slots : tiles.slots;
+  const int cap = of_rows ? rows.cap : tiles.cap;
+  const JoinRecord rec = (of_rows ? rows.records : tiles.records)[blockIdx.x];
+  const size_t size = (size_t)cap * (D + 2);
+  const int pieces = (int)blockIdx.x - rec.first_cta + 1;
+  auto piece = [&](int k) { return slots + (size_t)(2 * (rec.first_cta + k) + (k == 0 ? rec.first_slot : 0)) * size; };
+  if (i >= rec.rows) return;
+  float top = -INFINITY;
+  for (int k = lane; k < pieces; k += 32) top = fmaxf(top, piece(k)[i]);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  const float safe = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f, v[D / 32] = {};
+  for (int k0 = 0; k0 < pieces; k0 += 32) {
+    float f = 0.0f;
+    if (k0 + lane < pieces) {
+      f = exp2_fast(piece(k0 + lane)[i] - safe);
+      sum += piece(k0 + lane)[cap + i] * f;
+    }
+    const int n = min(pieces - k0, 32);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+      const float w = __shfl_sync(0xffffffffu, f, k);
+      const float* o = piece(k0 + k) + 2 * cap + (size_t)i * D + lane * (D / 32);
+#pragma unroll
+      for (int e = 0; e < D / 32; e += 2) {
+        const float2 x = *reinterpret_cast<const float2*>(o + e);
+        v[e] += x.x * w;
+        v[e + 1] += x.y * w;
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  const int ri = rec.row0 + i, ti = a.by_g.div(ri);
+  const long long tok = rec.tok0 + ti;
+  const int qh = rec.head * a.G + (ri - ti * a.G);
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<QT*>(a.out) + tok * a.o_tok + (long long)qh * a.o_head) + lane * (D / 64);
+#pragma unroll
+  for (int e = 0; e < D / 32; e += 2) dst[e / 2] = Bits16<QT>::pack(v[e] * inv, v[e + 1] * inv);
+  if (a.lse && lane == 0)
+    a.lse[tok * (a.pool.H * a.G) + qh] = sum == 0.0f ? -INFINITY : 0.69314718056f * (top + log2f(sum));
+}
+
+template <int D, typename QT, bool TREE>
 inline int32_t launch_join(const AttnArgs& a, const JoinSet& rows, const JoinSet& tiles, cudaStream_t st) {
   const int y_rows = (rows.cap + 15) / 16, y_tiles = (tiles.cap + 15) / 16;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned int)sm_count(), (unsigned int)(y_rows + y_tiles));
-  cfg.blockDim = dim3(256);
+  cfg.blockDim = dim3(TREE ? 512 : 256);
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  cudaLaunchKernelEx(&cfg, attn_join_kernel<D, QT>, a, rows, tiles, y_rows);
+  if constexpr (TREE)
+    cudaLaunchKernelEx(&cfg, attn_join_tree_kernel<D, QT>, a, rows, tiles, y_rows);
+  else
+    cudaLaunchKernelEx(&cfg, attn_join_kernel<D, QT>, a, rows, tiles, y_rows);
   return launch_status();
 }
 

@@ -13,7 +13,7 @@ struct AttnPlan {
   int G = 0;
   int row_limit = 0;                     // rows up to which a request is the row kernel's
   bool rows = false, tiles = false;      // which kernels run
-  int cols = 0;                          // trees: rows of a block of the third, 0: not that one
+  int cols = 0, col_limit = 0;           // trees: rows of the column kernel's blocks (0: not that one) and requests
   uint64_t rows_bytes = 0, workspace = 0;
 };
 
@@ -28,9 +28,10 @@ inline uint64_t slot_bytes(int rows, int dim) {
 // single token.
 //
 // Trees: the row kernel alone where no request can have more than 8 rows (at 16 it takes 206 us where
-// the other takes 127: twice the products, and registers spill); else the kernel with the keys as M for all,
-// in blocks of 64 rows where none has more (half the registers and shared memory of 128).  fp16 queries over
-// e4m3 keep weights twice, for which blocks of 128 leave no room.
+// the column kernel takes 127: twice the products, and registers spill).  The column kernel for requests of up to
+// 128 rows, in blocks of 64 where none has more (half the registers and shared memory); over e4m3, where a
+// block of 128 leaves its warps too few registers, up to 64.  The tile kernel for more: there a step costs
+// less per row (bf16, 256 rows: 225 us against 290 of two blocks).
 inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
                          const aibx_attn_params_t* p, bool tree, AttnPlan& plan) {
   PagedPool pool;
@@ -58,8 +59,12 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
   if (tree) {
     plan.rows = bound * plan.G <= 8;
     if (plan.rows) plan.row_limit = 8;
-    else plan.cols = bound * plan.G <= 64 || (c->type == AIBX_TYPE_E4M3 && p->q_type == AIBX_TYPE_FP16) ? 64 : 128;
-    plan.workspace = slot_bytes(plan.rows ? 8 : plan.cols, L.head_dim);
+    const int most = c->type == AIBX_TYPE_E4M3 ? 64 : 128;
+    plan.tiles = bound * plan.G > most;
+    if (!plan.rows && (!plan.tiles || b->R > 1)) plan.cols = bound * plan.G <= 64 ? 64 : most;
+    plan.col_limit = plan.cols ? most : 0;
+    plan.rows_bytes = plan.rows ? slot_bytes(8, L.head_dim) : plan.cols ? slot_bytes(plan.cols, L.head_dim) : 0;
+    plan.workspace = plan.rows_bytes + (plan.tiles ? slot_bytes(2 * kTileRows, L.head_dim) : 0);
     return AIBX_OK;
   }
   plan.tiles = bound * plan.G > 16;
@@ -74,11 +79,19 @@ template <int D, bool F8, typename QT, bool TREE>
 inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cudaStream_t st) {
   JoinSet rows = {nullptr, nullptr, 0}, tiles = rows;
   if constexpr (TREE) {
-    constexpr int kMost = F8 && std::is_same<QT, __half>::value ? 64 : 128;
-    const int32_t rc = plan.rows         ? launch_attn_rows<D, F8, QT, 8, true>(a, type, rows, st)
-                       : plan.cols == 64 ? launch_attn_cols<D, F8, QT, 64>(a, type, tiles, st)
-                                         : launch_attn_cols<D, F8, QT, kMost>(a, type, tiles, st);
-    return rc != AIBX_OK ? rc : launch_join<D, QT>(a, rows, tiles, st);
+    constexpr int kMost = F8 ? 64 : 128;
+    int32_t rc = AIBX_OK;
+    if (plan.rows)
+      rc = launch_attn_rows<D, F8, QT, 8, true>(a, type, rows, st);
+    else if (plan.cols)
+      rc = plan.cols == 64 ? launch_attn_cols<D, F8, QT, 64>(a, type, rows, st)
+                           : launch_attn_cols<D, F8, QT, kMost>(a, type, rows, st);
+    if (rc == AIBX_OK && plan.tiles) {
+      a.slots += plan.rows_bytes / sizeof(float);
+      a.row_limit = plan.col_limit;
+      rc = launch_attn_tiles<D, F8, QT, true>(a, type, tiles, st);
+    }
+    return rc != AIBX_OK ? rc : launch_join<D, QT, true>(a, rows, tiles, st);
   }
   if (plan.rows) {
     const int32_t rc = plan.row_limit == 8 ? launch_attn_rows<D, F8, QT, 8, false>(a, type, rows, st)
@@ -87,10 +100,10 @@ inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cuda
     a.slots += plan.rows_bytes / sizeof(float);
   }
   if (plan.tiles) {
-    const int32_t rc = launch_attn_tiles<D, F8, QT>(a, type, tiles, st);
+    const int32_t rc = launch_attn_tiles<D, F8, QT, false>(a, type, tiles, st);
     if (rc != AIBX_OK) return rc;
   }
-  return launch_join<D, QT>(a, rows, tiles, st);
+  return launch_join<D, QT, false>(a, rows, tiles, st);
 }
 
 template <int D, bool TREE>
@@ -142,6 +155,7 @@ inline int32_t attention(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* ba
   a.scale_log2 = params->scale * kLog2E;   // never 0: hidden keys are -infinity
   a.G = plan.G;
   a.by_g = small_divisor(plan.G);
+  a.by_pos = TREE ? SmallDivisor{0} : a.by_g;
   a.causal = !TREE && params->causal != 0;
   a.mask = TREE ? reinterpret_cast<const uint32_t*>(d_mask) : nullptr;
   a.mask_words = 2 * mask_words;
@@ -149,6 +163,7 @@ inline int32_t attention(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* ba
   a.box = 0;
   a.max_new = batch->max_new;
   a.row_limit = plan.row_limit;
+  a.col_limit = plan.col_limit;
   a.slots = static_cast<float*>(d_workspace);
   return launch_attn<TREE>(a, cache->type, params->q_type, plan, st);
 }

@@ -177,6 +177,10 @@ struct TileSpan {
 // How a request's rows are cut into blocks, and which tiles a block has: of 256 rows, two tiles of a CTA.
 struct PairBlocks {
   static __device__ __forceinline__ int size(int) { return 2 * kTileRows; }
+  static __device__ __forceinline__ int blocks(const AttnArgs& a, const AttnRequest& q) {
+    const long long rows = (long long)q.n * a.G;
+    return rows <= a.row_limit ? 0 : (int)((rows + 2 * kTileRows - 1) / (2 * kTileRows));
+  }
   static __device__ __forceinline__ TileSpan span(const AttnArgs& a, const AttnRequest& q, int block) {
     const int rows = q.n * a.G;
     const int r0 = block * 2 * kTileRows, r1 = min(r0 + 2 * kTileRows, rows) - 1;
@@ -184,7 +188,7 @@ struct PairBlocks {
     TileSpan s;
     long long hi = a.causal ? first + a.by_g.div(r1) + 1 : q.keys;
     hi = hi < 0 ? 0 : hi > q.keys ? q.keys : hi;
-    long long lo = a.window > 0 ? first + a.by_g.div(r0) - a.window + 1 : 0;
+    long long lo = a.window > 0 ? first + a.by_pos.div(r0) - a.window + 1 : 0;
     lo = lo < 0 ? 0 : lo > hi ? hi : lo;
     s.hi = (int)hi;
     s.lo = (int)lo;
@@ -199,12 +203,7 @@ struct PairBlocks {
 template <typename B>
 struct TileCost {
   const AttnArgs& a;
-  __device__ __forceinline__ int blocks(const AttnRequest& q) const {
-    const long long rows = (long long)q.n * a.G;
-    if (rows <= a.row_limit) return 0;
-    const int size = B::size((int)rows);
-    return (int)((rows + size - 1) / size);
-  }
+  __device__ __forceinline__ int blocks(const AttnRequest& q) const { return B::blocks(a, q); }
   __device__ __forceinline__ long long operator()(int r, bool on) const {
     AttnRequest q = {};
     if (on) q = attn_request(a.b, a.pool.T, r);
@@ -416,7 +415,8 @@ __device__ __forceinline__ void regs_down() {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS));
 }
 
-template <int D, bool F8, typename QT>
+// TREE: rows are a drafted tree's, and see the nodes that their masks name.
+template <int D, bool F8, typename QT, bool TREE>
 __global__ void __launch_bounds__(TileShape<D, F8>::kThreads, 1)
 attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a) {
   using S = TileShape<D, F8>;
@@ -581,9 +581,13 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
       }
       const float c0 = F8 ? a.scale_log2 * s_qup[t * kTileRows + row] : a.scale_log2;
       const int tok = a.by_g.div(row0 + min(row, rows_here - 1));
-      const long long p = (long long)walk.q.len - walk.q.n + tok;      // this row's position
-      // positions [vis0, vis1) this row sees (of those that are there)
-      const int vis1 = (int)max(0LL, a.causal ? min(p + 1, (long long)walk.span.hi) : (long long)walk.span.hi);
+      const int first = walk.q.len - walk.q.n;
+      const uint32_t* tree = TREE ? a.mask + (walk.q.tok0 + tok) * a.mask_words : nullptr;
+      // this row's position
+      const long long p = (long long)first + (!TREE ? tok : a.window > 0 ? tree_depth(tree, a.mask_words, walk.q.n) : 0);
+      // positions [vis0, vis1) this row sees (of those that are there; trees: of the cached ones)
+      const int vis1 = (int)max(0LL, TREE ? min((long long)first, (long long)walk.span.hi)
+                                     : a.causal ? min(p + 1, (long long)walk.span.hi) : (long long)walk.span.hi);
       const int vis0 = a.window > 0 ? (int)max((long long)walk.span.lo, p - a.window + 1) : walk.span.lo;
       const int key_first = (walk.span.tile0 + walk.t0) * kTileKeys;
       float m = -INFINITY, l = 0.0f;
@@ -610,6 +614,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
           for (int x = 0; x < 4; ++x) {
             const int lo = min(max(b0 - 32 * x, 0), 32), hi = min(max(b1 - 32 * x, 0), 32);
             vis[x] = (uint32_t)((1ull << hi) - 1) & ~(uint32_t)((1ull << lo) - 1);
+            if (TREE) vis[x] |= tree_bits(tree, a.mask_words, walk.span.hi - first, key0 + 32 * x - first);
           }
           if (mask != 0xffffffffu) {                       // blocks that are not there
             for (int k = 0; k < kTileKeys >> a.box_log; ++k)
@@ -1203,7 +1208,7 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
   }
 }
 
-template <int D, bool F8, typename QT>
+template <int D, bool F8, typename QT, bool TREE>
 inline int32_t launch_attn_tiles(AttnArgs a, int type, JoinSet& join, cudaStream_t st) {
   using S = TileShape<D, F8>;
   a.box = gcd_int(a.pool.T, kTileKeys);
@@ -1215,10 +1220,10 @@ inline int32_t launch_attn_tiles(AttnArgs a, int type, JoinSet& join, cudaStream
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return AIBX_ERR_CUDA;
   static size_t configured[64] = {0};
   static std::mutex lock;
-  if (!ensure_dynamic_smem(attn_tiles_kernel<D, F8, QT>, S::kSmem, dev, configured, lock))
+  if (!ensure_dynamic_smem(attn_tiles_kernel<D, F8, QT, TREE>, S::kSmem, dev, configured, lock))
     return AIBX_ERR_CUDA;
   const unsigned int grid = (unsigned int)sm_count();
-  attn_tiles_kernel<D, F8, QT><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
+  attn_tiles_kernel<D, F8, QT, TREE><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
   join = JoinSet{a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot), 2 * kTileRows};
   return launch_status();
 }
