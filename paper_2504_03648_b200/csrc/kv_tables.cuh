@@ -14,7 +14,7 @@
 //
 // tree_masks, per request: mask(i) = bit i, or that and mask(parent(i)).  In shared memory, twice as far
 // up each round: mask'(i) = mask(i) | mask(up(i)), up'(i) = up(up(i)), so that a chain of 512 takes nine
-// rounds; from one buffer to another, so that a round reads nothing that it writes.
+// rounds; all of a round's reads come before its writes.
 #pragma once
 
 #include <limits.h>
@@ -23,9 +23,23 @@
 
 namespace aibx {
 
+// Division of 0 <= p < 2^31 by T: with 2^(s-1) < T <= 2^s and m = floor(2^(31+s) / T) + 1, m T exceeds 2^(31+s)
+// by at most T <= 2^s, so p m / 2^(31+s) exceeds p / T by less than 1 / T.
+struct PositionDivisor {
+  uint32_t m;
+  int shift;
+  __device__ __forceinline__ int div(int p) const { return (int)(((uint64_t)(uint32_t)p * m) >> shift); }
+};
+inline PositionDivisor position_divisor(int T) {
+  int s = 0;
+  while ((1 << s) < T) ++s;
+  return PositionDivisor{(uint32_t)((1ull << (31 + s)) / (uint64_t)T + 1), 31 + s};
+}
+
 struct TablesArgs {
   const int32_t *held, *fresh;     // tokens held, tokens new
   int R, T;
+  PositionDivisor by_T;
   uint32_t num_blocks;
   const uint32_t* free_ids;
   long long capacity;
@@ -45,12 +59,14 @@ struct TablesArgs {
 
 constexpr int kTablesThreads = 512;
 
-// Last k in [0, n) with at[k] <= x (at[0] <= x): the request that holds x, past those without any.
-__device__ __forceinline__ int last_not_above(const long long* at, int n, long long x) {
+// Last k in [0, n) with at[k] <= x (at[0] <= x): the request that holds x, past those without any.  In as many
+// bits as X has.
+template <typename X>
+__device__ __forceinline__ int last_not_above(const long long* at, int n, X x) {
   int lo = 0;
   while (n > 1) {
     const int half = n >> 1;
-    if (at[lo + half] <= x) {
+    if ((X)at[lo + half] <= x) {
       lo += half;
       n -= half;
     } else {
@@ -58,6 +74,38 @@ __device__ __forceinline__ int last_not_above(const long long* at, int n, long l
     }
   }
   return lo;
+}
+
+// Exclusive prefixes and sums of three numbers per thread over the block.
+template <int N>
+__device__ __forceinline__ void block_prefix3(long long (&v)[3], long long (&scratch)[3][N / 32], long long (&total)[3]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  long long inc[3];
+#pragma unroll
+  for (int x = 0; x < 3; ++x) {
+    inc[x] = v[x];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long up = (long long)shfl_up64((uint64_t)inc[x], d);
+      if (lane >= d) inc[x] += up;
+    }
+    if (lane == 31) scratch[x][warp] = inc[x];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < 3; ++x) {
+    long long w = lane < N / 32 ? scratch[x][lane] : 0;     // warps' sums, a lane each
+    const long long own = w;
+#pragma unroll
+    for (int d = 1; d < N / 32; d <<= 1) {
+      const long long up = (long long)shfl_up64((uint64_t)w, d);
+      if (lane >= d) w += up;
+    }
+    total[x] = (long long)shfl64(0xffffffffu, (uint64_t)w, N / 32 - 1);
+    const long long before = (long long)shfl64(0xffffffffu, (uint64_t)(w - own), warp);
+    v[x] = before + inc[x] - v[x];
+  }
+  __syncthreads();
 }
 
 struct Lengths {
@@ -81,12 +129,12 @@ __device__ __forceinline__ Lengths request_lengths(const TablesArgs& a, int r) {
 // CTA to have read those; kCommit: these two.  A call with one CTA, or whose outputs stand apart, does both
 // at once; else a second launch of one CTA commits.
 template <bool TABLES, bool COMMIT>
-__global__ void __launch_bounds__(kTablesThreads)
+__global__ void __launch_bounds__(kTablesThreads, 2)
 kv_tables_kernel(const __grid_constant__ TablesArgs a) {
   constexpr int N = kTablesThreads;
-  __shared__ long long s_scan[33];
-  __shared__ long long s_tok[N], s_free[N], s_ent[N], s_row[N];
-  __shared__ int s_held[N], s_had[N], s_width[N];
+  __shared__ long long s_scan[3][N / 32];
+  __shared__ long long s_tok[N], s_free[N], s_ent[N], s_row[N], s_match[N];
+  __shared__ int s_held[N], s_had[N], s_width[N], s_matches[N];
   const int tid = threadIdx.x;
   const long long head = *a.head;
   long long left = *a.tail - head;                         // ids to be had
@@ -94,11 +142,10 @@ kv_tables_kernel(const __grid_constant__ TablesArgs a) {
   long long start = head % a.capacity;
   if (start < 0) start += a.capacity;
 
-  auto matched = [&](int r, int e) -> uint32_t {           // entry e of request r among the matched ids
-    const long long at = __ldg(a.match_off + r);
-    if (e < __ldg(a.match_off + r + 1) - at) return __ldg(a.match + at + e);
+  auto matched = [&](int k, int e) -> const uint32_t* {   // entry e of the tile's request k among the matched ids
+    if (e < s_matches[k]) return a.match + s_match[k] + e;
     raise_status(AIBX_ERR_RANGE);
-    return AIBX_NO_BLOCK;
+    return nullptr;
   };
 
   long long tok_base = 0, free_base = 0;
@@ -112,14 +159,20 @@ kv_tables_kernel(const __grid_constant__ TablesArgs a) {
       width = width < 0 ? 0 : width > INT_MAX ? INT_MAX : width;
     }
     const int have = min(q.had, (int)width), new_blocks = max(min(q.need, (int)width) - q.had, 0);
-    long long toks, frees, ents = 0, before_ent = 0;
-    const long long before_tok = block_prefix<N>(q.n, s_scan, toks);
-    const long long before_free = block_prefix<N>(new_blocks, s_scan, frees);
+    long long match_at = 0, matches = 0;
+    if (TABLES && a.match && r < a.R) {
+      match_at = __ldg(a.match_off + r);
+      matches = __ldg(a.match_off + r + 1) - match_at;
+    }
+    long long sums[3] = {q.n, new_blocks, a.match && r < a.R ? have : 0}, totals[3];
+    block_prefix3<N>(sums, s_scan, totals);
+    const long long before_tok = sums[0], before_free = sums[1], toks = totals[0], frees = totals[1], ents = totals[2];
     if (TABLES) {
-      if (a.match) before_ent = block_prefix<N>(r < a.R ? have : 0, s_scan, ents);
       s_tok[tid] = before_tok;
       s_free[tid] = free_base + before_free;
-      s_ent[tid] = before_ent;
+      s_ent[tid] = sums[2];
+      s_match[tid] = match_at;
+      s_matches[tid] = (int)(matches < 0 ? 0 : matches > INT_MAX ? INT_MAX : matches);
       s_row[tid] = row;
       s_held[tid] = q.h;
       s_had[tid] = q.had;
@@ -132,31 +185,78 @@ kv_tables_kernel(const __grid_constant__ TablesArgs a) {
     if (COMMIT && blockIdx.x == (unsigned int)(r0 / N) % gridDim.x && r < a.R) a.kv_len[r] = q.h + q.n;
     if (TABLES) {
       __syncthreads();
-      for (long long i = (long long)blockIdx.x * N + tid; i < toks; i += (long long)gridDim.x * N) {
-        const int k = last_not_above(s_tok, rows, i);
-        const int p = s_held[k] + (int)(i - s_tok[k]);
-        const int blk = p / a.T, off = p - blk * a.T;
-        uint32_t id = AIBX_NO_BLOCK;
-        if (blk < s_width[k]) {
-          if (blk >= s_had[k]) {
-            const long long f = s_free[k] + (blk - s_had[k]);
-            if (f < left) id = __ldg(a.free_ids + (start + f < a.capacity ? start + f : start + f - a.capacity));
-            if (off == 0) a.table[s_row[k] + blk] = id;
-          } else {
-            id = a.match ? matched(r0 + k, blk) : a.table[s_row[k] + blk];
+      // Four tokens per thread at a time, so that their ids are on their way together: 32 apart where there are
+      // many (a warp then takes 128 neighbours), else far apart, so that every thread gets its first one.
+      const int all = (int)gridDim.x * N, slot = (int)blockIdx.x * N + tid;
+      auto give = [&](auto wide, int apart, int from) {
+        using X = decltype(wide);                          // of what counts tokens of this tile
+        for (X i0 = (X)from; i0 < (X)toks; i0 += 4 * (X)all) {
+          // the request of the warp's first token, which most of them share
+          int k, had, width;
+          X begin, next;                                   // its tokens
+          int held;
+          long long free_at;
+          uint32_t* entries;
+          auto enter = [&](int to) {
+            k = to;
+            begin = (X)s_tok[k];
+            next = k + 1 < rows ? (X)s_tok[k + 1] : (X)toks;
+            held = s_held[k];
+            had = s_had[k];
+            width = s_width[k];
+            free_at = s_free[k] - had;
+            entries = a.table + s_row[k];
+          };
+          enter(last_not_above<X>(s_tok, rows, apart == 32 ? i0 - (tid & 31) : i0));
+          int p[4], off[4];
+          uint32_t id[4];
+          const uint32_t* src[4];
+          uint32_t* dst[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const X i = i0 + (X)(u * apart);
+            src[u] = nullptr;
+            dst[u] = nullptr;
+            p[u] = off[u] = 0;
+            if (i >= (X)toks) continue;
+            if (i >= next) enter(last_not_above<X>(s_tok, rows, i));
+            p[u] = held + (int)(i - begin);
+            const int blk = a.by_T.div(p[u]);
+            off[u] = p[u] - blk * a.T;
+            if (blk >= width) continue;
+            if (blk >= had) {
+              const long long f = free_at + blk;
+              if (f < left) src[u] = a.free_ids + (start + f < a.capacity ? start + f : start + f - a.capacity);
+              if (off[u] == 0) dst[u] = entries + blk;
+            } else {
+              src[u] = a.match ? matched(k, blk) : entries + blk;
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) id[u] = src[u] ? *src[u] : AIBX_NO_BLOCK;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const X i = i0 + (X)(u * apart);
+            const long long t = tok_base + (long long)i;
+            if (i >= (X)toks) continue;
+            if (dst[u]) *dst[u] = id[u];
+            if (id[u] >= a.num_blocks && id[u] != AIBX_NO_BLOCK) raise_status(AIBX_ERR_RANGE);
+            if (t >= a.n_tokens) continue;
+            if (a.pos) a.pos[t] = p[u];
+            if (a.slots) a.slots[t] = id[u] < a.num_blocks ? (int64_t)id[u] * a.T + off[u] : -1;
           }
         }
-        if (id >= a.num_blocks && id != AIBX_NO_BLOCK) raise_status(AIBX_ERR_RANGE);
-        const long long t = tok_base + i;
-        if (t < a.n_tokens) {
-          if (a.pos) a.pos[t] = p;
-          if (a.slots) a.slots[t] = id < a.num_blocks ? (int64_t)id * a.T + off : -1;
-        }
-      }
-      for (long long e = (long long)blockIdx.x * N + tid; e < ents; e += (long long)gridDim.x * N) {
-        const int k = last_not_above(s_ent, rows, e);
+      };
+      const int apart = toks > all ? 32 : all, from = toks > all ? (slot >> 5) * 128 + (slot & 31) : slot;
+      if (toks < (1ll << 31) - 8ll * all)                  // (i0 goes at most 8 * all past it)
+        give(0u, apart, from);
+      else
+        give(0ull, apart, from);
+      for (long long e = slot; e < ents; e += all) {
+        const int k = last_not_above<long long>(s_ent, rows, e);
         const int at = (int)(e - s_ent[k]);
-        a.table[s_row[k] + at] = matched(r0 + k, at);
+        const uint32_t* from_match = matched(k, at);
+        a.table[s_row[k] + at] = from_match ? *from_match : AIBX_NO_BLOCK;
       }
       __syncthreads();
     }
@@ -200,6 +300,7 @@ inline int32_t kv_tables(const aibx_kv_tables_t* t, int32_t R, cudaStream_t st) 
   a.fresh = t->d_new;
   a.R = R;
   a.T = t->block_tokens;
+  a.by_T = position_divisor(a.T);
   a.num_blocks = t->num_blocks;
   a.free_ids = t->d_free_ids;
   a.capacity = t->free_capacity;
@@ -217,7 +318,7 @@ inline int32_t kv_tables(const aibx_kv_tables_t* t, int32_t R, cudaStream_t st) 
   a.slots = t->d_slots;
   a.n_tokens = t->n_tokens;
   // four tokens or matched entries per thread, as far as the host can tell
-  const long long most = sm_count(), each = 4 * kTablesThreads;
+  const long long most = 2 * sm_count(), each = 4 * kTablesThreads;
   const double copies = !a.match ? 0.0 : a.blk_off ? 1e18 : (double)a.stride * R;
   const double want = ((double)a.n_tokens + copies) / each;
   const unsigned int grid = want >= (double)most ? (unsigned int)most : want > 1.0 ? (unsigned int)want + 1 : 1u;
@@ -246,14 +347,18 @@ struct TreeArgs {
 
 constexpr int kTreeMaxWords = 8;
 template <int W>
-constexpr int kTreeThreads = W >= 4 ? 512 : W >= 2 ? 256 : 64;
+constexpr int kTreeThreads = W >= 6 ? 1024 : W >= 4 ? 512 : W >= 2 ? 256 : 64;
 
 template <int W>
 __global__ void __launch_bounds__(kTreeThreads<W>)
 tree_masks_kernel(TreeArgs a) {
-  constexpr int N = kTreeThreads<W>, kNodes = 64 * W;
-  extern __shared__ unsigned long long s_mask[];           // [2][kNodes][W]
-  short* s_up = reinterpret_cast<short*>(s_mask + 2 * kNodes * W);   // [2][kNodes]
+  constexpr int N = kTreeThreads<W>, kNodes = 64 * W, kV = W % 2 == 0 ? 2 : 1, kItems = W / kV;   // words at a time
+  constexpr int kEach = (kNodes * kItems + N - 1) / N;     // such pieces of masks per thread
+  struct alignas(8 * kV) Words {
+    unsigned long long w[kV];
+  };
+  extern __shared__ __align__(16) unsigned long long s_mask[];   // [kNodes][W]
+  short* s_up = reinterpret_cast<short*>(s_mask + kNodes * W);   // [kNodes]
   const int tid = threadIdx.x;
   for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
     const long long tok0 = __ldg(a.tok_off + r);
@@ -271,36 +376,57 @@ tree_masks_kernel(TreeArgs a) {
       s_up[i] = (short)(p < 0 || p >= i ? -1 : p);
       more |= p >= 0 && p < i;
     }
-    for (int x = tid; x < n * W; x += N) {
-      const int i = x / W;
-      s_mask[x] = x - i * W == i >> 6 ? 1ull << (i & 63) : 0ull;
+    Words v[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int x = tid + e * N, i = x / kItems, w = (x - i * kItems) * kV;
+#pragma unroll
+      for (int y = 0; y < kV; ++y) v[e].w[y] = w + y == i >> 6 ? 1ull << (i & 63) : 0ull;
+      if (x < n * kItems) *reinterpret_cast<Words*>(s_mask + x * kV) = v[e];
     }
-    int cur = 0;
+    // A round: every node reads the mask of the one its `up` names, and that one's own; then all write.
     while (__syncthreads_or(more)) {
-      const unsigned long long* m0 = s_mask + cur * kNodes * W;
-      unsigned long long* m1 = s_mask + (cur ^ 1) * kNodes * W;
-      const short* u0 = s_up + cur * kNodes;
-      short* u1 = s_up + (cur ^ 1) * kNodes;
-      more = false;
-      for (int x = tid; x < n * W; x += N) {
-        const int i = x / W, w = x - i * W, j = u0[i];
-        m1[x] = j >= 0 ? m0[x] | m0[j * W + w] : m0[x];
-        if (w == 0) {
-          const int up = j >= 0 ? u0[j] : -1;
-          u1[i] = (short)up;
-          more |= up >= 0;
+      int up[kEach];
+      bool grown[kEach];
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int x = tid + e * N, i = x / kItems, w = x - i * kItems;
+        const int j = x < n * kItems ? s_up[i] : -1;
+        grown[e] = j >= 0;
+        up[e] = -1;
+        if (j < 0) continue;
+        if (w * kV <= j >> 6) {                            // (beyond its own bit a mask is zero)
+          const Words above = *reinterpret_cast<const Words*>(s_mask + (j * kItems + w) * kV);
+#pragma unroll
+          for (int y = 0; y < kV; ++y) v[e].w[y] |= above.w[y];
         }
+        up[e] = s_up[j];
       }
-      cur ^= 1;
+      __syncthreads();
+      more = false;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        if (!grown[e]) continue;
+        const int x = tid + e * N, i = x / kItems;
+        *reinterpret_cast<Words*>(s_mask + x * kV) = v[e];
+        if (x == i * kItems) s_up[i] = (short)up[e];
+        more |= up[e] >= 0;
+      }
     }
-    const unsigned long long* m = s_mask + cur * kNodes * W;
-    for (int x = tid; x < n * W; x += N) a.mask[tok0 * W + x] = m[x];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int x = tid + e * N;
+      if (x < n * kItems) {
+#pragma unroll
+        for (int y = 0; y < kV; ++y) a.mask[tok0 * W + x * kV + y] = v[e].w[y];
+      }
+    }
     if (a.pos) {
       const int base = __ldg(a.kv_len + r) - n;
       for (int i = tid; i < n; i += N) {
         int above = -1;
 #pragma unroll
-        for (int w = 0; w < W; ++w) above += __popcll(m[i * W + w]);
+        for (int w = 0; w < W; ++w) above += __popcll(s_mask[i * W + w]);
         a.pos[tok0 + i] = base + above;
       }
     }
@@ -310,12 +436,7 @@ tree_masks_kernel(TreeArgs a) {
 
 template <int W>
 inline int32_t launch_tree_masks(const TreeArgs& a, cudaStream_t st) {
-  constexpr size_t smem = (size_t)2 * 64 * W * (8 * W + 2);
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return AIBX_ERR_CUDA;
-  static size_t configured[64] = {0};
-  static std::mutex lock;
-  if (smem > 48 * 1024 && !ensure_dynamic_smem(tree_masks_kernel<W>, smem, dev, configured, lock)) return AIBX_ERR_CUDA;
+  constexpr size_t smem = (size_t)64 * W * (8 * W + 2);    // at most 33 KB
   const long long most = (long long)sm_count() * 8;
   tree_masks_kernel<W><<<(unsigned int)(a.R < most ? a.R : most), kTreeThreads<W>, smem, st>>>(a);
   return launch_status();

@@ -108,124 +108,124 @@ rope_kernel(PagedPool pool, PagedBatch b, RopeIO io) {
       c[e + 1] = f.z;
       s[e + 1] = f.w;
     }
-    for (int y0 = part * per_part; y0 < y1; y0 += step * kUnroll) {
-      uint32_t a[kUnroll][kW], d[kUnroll][kW];            // the two pieces
+    // Queries and cached rows in loops of their own: what a pool of 8 bits needs would cost the queries, the
+    // most of the rows, a third of their time.
+    auto turn_rows = [&](auto of_q, int y0, int y_end) {
+      constexpr bool kQ = decltype(of_q)::value;
+      for (; y0 < y_end; y0 += step * kUnroll) {
+        uint32_t a[kUnroll][kW], d[kUnroll][kW];          // the two pieces
 #pragma unroll
-      for (int r = 0; r < kUnroll; ++r) {
-        const int y = y0 + r * step + sub;
-        const X* src = nullptr;
-        if (y < y1) {
-          if (!kPool || y < io.q_heads)
-            src = reinterpret_cast<const X*>(io.q) + i * io.q_tok + (long long)y * io.q_head;
-          else if (at >= 0)
-            src = y < io.q_heads + heads
-                      ? reinterpret_cast<const X*>(io.k) + i * io.k_tok + (long long)(y - io.q_heads) * io.k_head
-                      : reinterpret_cast<const X*>(io.v) + i * io.v_tok + (long long)(y - io.q_heads - heads) * io.v_head;
+        for (int r = 0; r < kUnroll; ++r) {
+          const int y = y0 + r * step + sub;
+          const X* src = reinterpret_cast<const X*>(io.q) + i * io.q_tok + (long long)y * io.q_head;
+          if constexpr (!kQ)
+            src = y < heads ? reinterpret_cast<const X*>(io.k) + i * io.k_tok + (long long)y * io.k_head
+                            : reinterpret_cast<const X*>(io.v) + i * io.v_tok + (long long)(y - heads) * io.v_head;
+#pragma unroll
+          for (int e = 0; e < kW; ++e) a[r][e] = d[r][e] = 0;
+          if (y < y_end && on_a) load_words_rw<X, kW>(src + oa, io.vec, a[r]);
+          if (y < y_end && on_b) load_words_rw<X, kW>(src + ob, io.vec, d[r]);
         }
 #pragma unroll
-        for (int e = 0; e < kW; ++e) a[r][e] = d[r][e] = 0;
-        if (src && on_a) load_words_rw<X, kW>(src + oa, io.vec, a[r]);
-        if (src && on_b) load_words_rw<X, kW>(src + ob, io.vec, d[r]);
-      }
-#pragma unroll
-      for (int r = 0; r < kUnroll; ++r) {
-        const int y = y0 + r * step + sub;
-        const bool is_q = !kPool || y < io.q_heads, is_v = kPool && y >= io.q_heads + heads;
-        const bool same = is_v || !turns;                 // as it came
-        float fa[8], fb[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          fa[e] = Elems<X>::get(a[r], e);
-          fb[e] = Elems<X>::get(d[r], e);
-        }
-        if (!same) {
-          if constexpr (INTER) {
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-              const float xa = fa[e], xb = fb[e];
-              fa[e] = xa * c[e / 2] - fa[e + 1] * s[e / 2];
-              fa[e + 1] = fa[e + 1] * c[e / 2] + xa * s[e / 2];
-              fb[e] = xb * c[4 + e / 2] - fb[e + 1] * s[4 + e / 2];
-              fb[e + 1] = fb[e + 1] * c[4 + e / 2] + xb * s[4 + e / 2];
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float x1 = fa[e], x2 = fb[e];
-              fa[e] = x1 * c[e] - x2 * s[e];
-              fb[e] = x2 * c[e] + x1 * s[e];
-            }
-          }
-        }
-        float f = 1.0f;
-        int byte = 127;
-        bool odd = false;
-        if constexpr (kQuant) {
-          uint32_t top = 0;
+        for (int r = 0; r < kUnroll; ++r) {
+          const int y = y0 + r * step + sub;
+          const bool is_v = !kQ && y >= heads;
+          const bool same = is_v || !turns;               // as it came
+          float fa[8], fb[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            top = max_bits<float>(top, __float_as_uint(fa[e]));
-            top = max_bits<float>(top, __float_as_uint(fb[e]));
+            fa[e] = Elems<X>::get(a[r], e);
+            fb[e] = Elems<X>::get(d[r], e);
           }
-          odd = __any_sync(0xffffffffu, top >= 0x7f800000u);
-          float m = __uint_as_float(top);
-          if (odd) {
-            m = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) m = fmaxf(m, fmaxf(finite_abs(fa[e]), finite_abs(fb[e])));
-          }
-          for (int x = lanes >> 1; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-          byte = scale_byte(m);
-          f = power_of_byte(254 - byte);
-        }
-        if (y >= y1 || !on_a) continue;
-        if (is_q) {
           if (!same) {
+            if constexpr (INTER) {
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-              Elems<X>::put(a[r], e, fa[e], fa[e + 1]);
-              Elems<X>::put(d[r], e, fb[e], fb[e + 1]);
-            }
-          }
-          X* dst = reinterpret_cast<X*>(io.q_out) + i * io.o_tok + (long long)y * io.o_head;
-          store_words<X, kW>(dst + oa, io.vec, a[r]);
-          if (on_b) store_words<X, kW>(dst + ob, io.vec, d[r]);
-        } else if constexpr (kPool) {
-          if (at < 0) continue;
-          const int h = y - io.q_heads - (is_v ? heads : 0);
-          char* row = pool.base + at + (is_v ? pool.kv : 0) + h * pool.head;
-          if constexpr (kQuant) {
-            uint32_t w[2][2];
+              for (int e = 0; e < 8; e += 2) {
+                const float xa = fa[e], xb = fb[e];
+                fa[e] = xa * c[e / 2] - fa[e + 1] * s[e / 2];
+                fa[e + 1] = fa[e + 1] * c[e / 2] + xa * s[e / 2];
+                fb[e] = xb * c[4 + e / 2] - fb[e + 1] * s[4 + e / 2];
+                fb[e + 1] = fb[e + 1] * c[4 + e / 2] + xb * s[4 + e / 2];
+              }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-              w[0][e / 4] = e4m3_pair(fa[e] * f, fa[e + 1] * f, odd) | (e4m3_pair(fa[e + 2] * f, fa[e + 3] * f, odd) << 16);
-              w[1][e / 4] = e4m3_pair(fb[e] * f, fb[e + 1] * f, odd) | (e4m3_pair(fb[e + 2] * f, fb[e + 3] * f, odd) << 16);
-            }
-            *reinterpret_cast<uint2*>(row + oa) = make_uint2(w[0][0], w[0][1]);
-            if (on_b) *reinterpret_cast<uint2*>(row + ob) = make_uint2(w[1][0], w[1][1]);
-            if (u == 0) pool.scales[sat + (is_v ? pool.s_kv : 0) + h * pool.s_head] = (unsigned char)byte;
-          } else {
-            uint32_t w[2][4];
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-              Elems<P>::put(w[0], e, fa[e], fa[e + 1]);
-              Elems<P>::put(w[1], e, fb[e], fb[e + 1]);
-            }
-            if constexpr (kCopy) {
-              if (same) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  w[0][e] = a[r][e];
-                  w[1][e] = d[r][e];
-                }
+              for (int e = 0; e < 8; ++e) {
+                const float x1 = fa[e], x2 = fb[e];
+                fa[e] = x1 * c[e] - x2 * s[e];
+                fb[e] = x2 * c[e] + x1 * s[e];
               }
             }
-            *reinterpret_cast<uint4*>(row + 2 * oa) = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
-            if (on_b) *reinterpret_cast<uint4*>(row + 2 * ob) = make_uint4(w[1][0], w[1][1], w[1][2], w[1][3]);
+          }
+          if constexpr (kQ) {
+            if (y >= y_end || !on_a) continue;
+            if (!same) {
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) {
+                Elems<X>::put(a[r], e, fa[e], fa[e + 1]);
+                Elems<X>::put(d[r], e, fb[e], fb[e + 1]);
+              }
+            }
+            X* dst = reinterpret_cast<X*>(io.q_out) + i * io.o_tok + (long long)y * io.o_head;
+            store_words<X, kW>(dst + oa, io.vec, a[r]);
+            if (on_b) store_words<X, kW>(dst + ob, io.vec, d[r]);
+          } else if constexpr (kPool) {
+            const int h = y - (is_v ? heads : 0);
+            char* row = pool.base + at + (is_v ? pool.kv : 0) + h * pool.head;
+            if constexpr (kQuant) {
+              uint32_t top = 0;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                top = max_bits<float>(top, __float_as_uint(fa[e]));
+                top = max_bits<float>(top, __float_as_uint(fb[e]));
+              }
+              const bool odd = __any_sync(0xffffffffu, top >= 0x7f800000u);
+              float m = __uint_as_float(top);
+              if (odd) {
+                m = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m = fmaxf(m, fmaxf(finite_abs(fa[e]), finite_abs(fb[e])));
+              }
+              for (int x = lanes >> 1; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+              const int byte = scale_byte(m);
+              const float f = power_of_byte(254 - byte);
+              if (y >= y_end || !on_a) continue;
+              uint32_t w[2][2];
+#pragma unroll
+              for (int e = 0; e < 8; e += 4) {
+                w[0][e / 4] = e4m3_pair(fa[e] * f, fa[e + 1] * f, odd) | (e4m3_pair(fa[e + 2] * f, fa[e + 3] * f, odd) << 16);
+                w[1][e / 4] = e4m3_pair(fb[e] * f, fb[e + 1] * f, odd) | (e4m3_pair(fb[e + 2] * f, fb[e + 3] * f, odd) << 16);
+              }
+              *reinterpret_cast<uint2*>(row + oa) = make_uint2(w[0][0], w[0][1]);
+              if (on_b) *reinterpret_cast<uint2*>(row + ob) = make_uint2(w[1][0], w[1][1]);
+              if (u == 0) pool.scales[sat + (is_v ? pool.s_kv : 0) + h * pool.s_head] = (unsigned char)byte;
+            } else {
+              if (y >= y_end || !on_a) continue;
+              uint32_t w[2][4];
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) {
+                Elems<P>::put(w[0], e, fa[e], fa[e + 1]);
+                Elems<P>::put(w[1], e, fb[e], fb[e + 1]);
+              }
+              if constexpr (kCopy) {
+                if (same) {
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    w[0][e] = a[r][e];
+                    w[1][e] = d[r][e];
+                  }
+                }
+              }
+              *reinterpret_cast<uint4*>(row + 2 * oa) = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
+              if (on_b) *reinterpret_cast<uint4*>(row + 2 * ob) = make_uint4(w[1][0], w[1][1], w[1][2], w[1][3]);
+            }
           }
         }
       }
-    }
+    };
+    const int y0 = part * per_part;
+    turn_rows(std::true_type(), y0, min(y1, io.q_heads));
+    if constexpr (kPool)
+      if (at >= 0) turn_rows(std::false_type(), max(y0 - io.q_heads, 0), y1 - io.q_heads);
   }
 }
 
@@ -241,8 +241,8 @@ inline int32_t launch_rope(const PagedPool& pool, const PagedBatch& b, RopeIO io
   const int rows = 2 * (32 >> io.lane_log);               // of a token that a warp has in flight
   const int most = (planes + rows - 1) / rows;
   const long long enough = (long long)sm_count() * 24;    // warps that the GPU holds at once
-  io.tokens = 8;
-  while (io.tokens > 1 && (io.n_tokens + io.tokens - 1) / io.tokens < enough) io.tokens /= 2;
+  io.tokens = 8;                                          // (at least two rounds of warps, or the last one shows:
+  while (io.tokens > 1 && (io.n_tokens + io.tokens - 1) / io.tokens < 2 * enough) io.tokens /= 2;   // 128 instead of 109 us)
   const long long groups = (io.n_tokens + io.tokens - 1) / io.tokens;
   io.parts = 1;
   while (io.parts < most && groups * io.parts < enough) ++io.parts;
