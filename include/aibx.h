@@ -634,9 +634,9 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
  *   not only those of trees, and a node need not see itself.  Bits of nodes that the request has not are
  *   ignored.  params->causal is not read.  Everything else as aibx_attn_paged (formats, shapes, errors, the
  *   same bits every time), but: weights over an E4M3 pool may be held as bf16, or with FP16 queries as the
- *   sum of two bf16 numbers; a NaN or infinite V of a position from base - window + 1 on that is hidden
- *   from a row may reach it; the workspace is of aibx_attn_tree_workspace_bytes bytes, which depend on
- *   head_dim, num_q_heads / num_kv_heads, max_new, the types and the device alone.  INVALID for a null or
+ *   sum of two bf16 numbers; a NaN or infinite V of a node, or of a cached position that only some rows'
+ *   windows reach, may reach a row that it is hidden from; the workspace is of aibx_attn_tree_workspace_bytes bytes, which depend on
+ *   head_dim, num_q_heads / num_kv_heads, max_new, the types, whether R is 1 and the device alone.  INVALID for a null or
  *   unaligned d_mask or mask_words < 1, UNSUPPORTED for more than 8 words, RANGE for a request with more
  *   than 64 * mask_words tokens (whose later nodes count as hidden).
  */
@@ -717,6 +717,7 @@ int32_t aibx_rope_append(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* ba
  *   d_match_ids    nullable; with d_match_off (int64 [R+1]): request r's first `had` entries are copied
  *                  from d_match_ids[d_match_off[r]] on - what aibx_match_prefix leaves in d_block_ids.
  *   d_tok_off      int64 [R+1], prefix sum of n;   d_kv_len  int32 [R], h + n
+ *   n_tokens       rows of d_pos and d_slots (without them a bound that helps to size the launch)
  *   d_pos          int32 [n_tokens], nullable: h + i for token i of a request
  *   d_slots        int64 [n_tokens], nullable: block id * T + position mod T; -1 where there is no block
  * A request that wants more blocks than are left gets AIBX_NO_BLOCK for the rest: FULL, detail = such
@@ -724,6 +725,8 @@ int32_t aibx_rope_append(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* ba
  * tokens (it counts as n = 0), for one with more blocks than its row has entries (they are left out, and
  * take no ids) or fewer matched ids than `had` (AIBX_NO_BLOCK), for an id >= num_blocks under a new
  * token, and where there are more than n_tokens tokens (whose d_pos and d_slots are left out).
+ * Where h is no multiple of T, the new tokens go on in the block of position h - 1: that no other request
+ * reads that block, too, is the caller's to see to.
  * d_kv_len may be d_held and d_free_head_out may be d_free_head (a call captured once, replayed step
  * after step); no other output may overlap an input, and calls on one free list are the caller's to
  * order.  Arithmetic on whole numbers; calls on the same input give the same bits.  INVALID for null or

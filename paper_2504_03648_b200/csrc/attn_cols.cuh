@@ -112,14 +112,14 @@ struct ColShape {
   static constexpr int kRaw = kTileKeys * D;               // a tile's e4m3 rows, as they arrive
   static constexpr int kBuf = kTileKeys * D * 2 + (F8 && D == 64 ? kRaw : 0);   // as in TileShape
   static constexpr int kQ = kCols * kColBytes * N / 128;
-  static constexpr int kP = kTileKeys * 128 * (N / 64);    // P^T: 64 rows in 128 bytes a key
+  static constexpr int kP = kTileKeys * 128 * ((N + 63) / 64);   // P^T: 64 rows in 128 bytes a key
   static constexpr int kRoom = 216 * 1024;
 };
 // P^T as one 16-bit number or the sum of two; what is left of shared memory goes to the rings.
 template <int D, bool F8, int N, int PARTS>
 struct ColRings : ColShape<D, F8, N> {
   using B = ColShape<D, F8, N>;
-  static constexpr int kPs = N == 64 ? 2 : 1;              // P^T of that many tiles
+  static constexpr int kPs = N <= 64 ? 2 : 1;              // P^T of that many tiles
   static constexpr int kBufs = (B::kRoom - B::kQ - kPs * PARTS * B::kP - 1024) / B::kBuf;
   static constexpr int kK = kBufs / 2 < 4 ? kBufs / 2 : 4, kV = kBufs - kBufs / 2 < 4 ? kBufs - kBufs / 2 : 4;
   static constexpr int kQAt = (kK + kV) * B::kBuf, kPAt = kQAt + B::kQ;
@@ -392,7 +392,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 #pragma unroll 4
             for (int t = t0; t <= t1; ++t, bits += a.mask_words, from += a.G) {
               const uint32_t bit = named ? __ldg(bits) >> (d & 31) & 1u : 0u;
-              const uint32_t upto = from + a.G >= 32 ? 0xffffffffu : (1u << (from + a.G)) - 1u;
+              const uint32_t upto = from + a.G >= 32 ? 0xffffffffu : from + a.G > 0 ? (1u << (from + a.G)) - 1u : 0u;
               vis |= (0u - bit) & upto & (0xffffffffu << max(from, 0));
             }
           } else if (vis && a.window > 0) {
@@ -804,15 +804,15 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         uint32_t block[kEach], kb[kEach], vb[kEach];
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
-          const int key = key_first + j0 * kTileKeys + u * (128 * S::kConverters) + tid;
-          block[u] = key >= lo && key < hi ? __ldg(row + key / a.pool.T) : AIBX_NO_BLOCK;
+          const uint32_t key = (uint32_t)(key_first + tid) + (uint32_t)(j0 * kTileKeys + u * (128 * S::kConverters));
+          block[u] = key >= (uint32_t)lo && key < (uint32_t)hi ? __ldg(row + key / (uint32_t)a.pool.T) : AIBX_NO_BLOCK;
           kb[u] = vb[u] = 127;
         }
 #pragma unroll
         for (int u = 0; u < kEach; ++u)
           if (block[u] < a.pool.num_blocks) {
-            const int key = key_first + j0 * kTileKeys + u * (128 * S::kConverters) + tid;
-            const unsigned char* src = scales + (long long)block[u] * a.pool.s_block + (long long)(key % a.pool.T) * a.pool.s_slot;
+            const uint32_t key = (uint32_t)(key_first + tid) + (uint32_t)(j0 * kTileKeys + u * (128 * S::kConverters));
+            const unsigned char* src = scales + (long long)block[u] * a.pool.s_block + (long long)(key % (uint32_t)a.pool.T) * a.pool.s_slot;
             kb[u] = __ldg(src);
             vb[u] = __ldg(src + a.pool.s_kv);
           }
@@ -821,11 +821,11 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 #pragma unroll
         for (int u = 0; u < kEach; ++u) {
           const int x = u * (128 * S::kConverters) + tid, t = x / kTileKeys, k = x % kTileKeys;
-          const int key = key_first + j0 * kTileKeys + x;
+          const uint32_t key = (uint32_t)key_first + (uint32_t)(j0 * kTileKeys + x);   // (past 2^31 behind the last tile)
           s_bytes[f * kColBatch + t][0][k] = (unsigned char)kb[u];
           s_bytes[f * kColBatch + t][1][k] = (unsigned char)vb[u];
           // (rows outside: zeros)
-          const bool odd = __any_sync(0xffffffffu, (int)vb[u] != weight_byte((int)vb[u]) || key < lo || key >= hi);
+          const bool odd = __any_sync(0xffffffffu, (int)vb[u] != weight_byte((int)vb[u]) || key < (uint32_t)lo || key >= (uint32_t)hi);
           if (lane == 0) s_odd[f * kColBatch + t][k >> 5] = odd;
         }
         __syncwarp();

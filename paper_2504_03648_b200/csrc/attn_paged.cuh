@@ -61,7 +61,7 @@ inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
     if (plan.rows) plan.row_limit = 8;
     const int most = c->type == AIBX_TYPE_E4M3 ? 64 : 128;
     plan.tiles = bound * plan.G > most;
-    if (!plan.rows && (!plan.tiles || b->R > 1)) plan.cols = bound * plan.G <= 64 ? 64 : most;
+    if (!plan.rows && (!plan.tiles || b->R > 1)) plan.cols = bound * plan.G <= 32 ? 32 : bound * plan.G <= 64 ? 64 : most;
     plan.col_limit = plan.cols ? most : 0;
     plan.rows_bytes = plan.rows ? slot_bytes(8, L.head_dim) : plan.cols ? slot_bytes(plan.cols, L.head_dim) : 0;
     plan.workspace = plan.rows_bytes + (plan.tiles ? slot_bytes(2 * kTileRows, L.head_dim) : 0);
@@ -84,8 +84,9 @@ inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cuda
     if (plan.rows)
       rc = launch_attn_rows<D, F8, QT, 8, true>(a, type, rows, st);
     else if (plan.cols)
-      rc = plan.cols == 64 ? launch_attn_cols<D, F8, QT, 64>(a, type, rows, st)
-                           : launch_attn_cols<D, F8, QT, kMost>(a, type, rows, st);
+      rc = plan.cols == 32   ? launch_attn_cols<D, F8, QT, 32>(a, type, rows, st)
+           : plan.cols == 64 ? launch_attn_cols<D, F8, QT, 64>(a, type, rows, st)
+                             : launch_attn_cols<D, F8, QT, kMost>(a, type, rows, st);
     if (rc == AIBX_OK && plan.tiles) {
       a.slots += plan.rows_bytes / sizeof(float);
       a.row_limit = plan.col_limit;

@@ -267,7 +267,7 @@ kv_tables_kernel(const __grid_constant__ TablesArgs a) {
     if (TABLES) {
       a.tok_off[a.R] = tok_base;
       if (free_base > left) raise_status_n(AIBX_ERR_FULL, (unsigned long long)(free_base - left));
-      if (tok_base > a.n_tokens) raise_status(AIBX_ERR_RANGE);
+      if ((a.pos || a.slots) && tok_base > a.n_tokens) raise_status(AIBX_ERR_RANGE);
     }
     if (COMMIT) *a.head_out = head + (free_base < left ? free_base : left);
   }
