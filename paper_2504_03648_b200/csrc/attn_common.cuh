@@ -393,10 +393,13 @@ attn_join_kernel(const __grid_constant__ AttnArgs a, JoinSet rows, JoinSet tiles
   }
 }
 
-// The same for trees, whose few rows over long contexts are cut into many pieces: a warp per row, the pieces'
-// maxima and sums a piece a lane, their outputs several at once.
-template <int D, typename QT>
-__global__ void __launch_bounds__(512)
+// The same for trees, whose rows over long contexts are cut into many pieces.  A warp takes a row or (EACH = 2)
+// two: the pieces' maxima and sums a piece a lane, their outputs several at once.  blockIdx.y: 16 EACH rows of
+// one set or the other.  Bound by the latency of three dependent loads and by blocks without rows: two rows a
+// warp where there are the tile kernel's many (33 -> 25 us), one where latency is all (a draft of 26 nodes
+// over 2,000 tokens 28.7 -> 26 us).
+template <int D, typename QT, int EACH>
+__global__ void __launch_bounds__(512, 2)
 attn_join_tree_kernel(const __grid_constant__ AttnArgs a, JoinSet rows, JoinSet tiles, int y_rows) {
   // Requests with more tokens than the caller's bound, or than their masks can name
   if (blockIdx.x == 0 && blockIdx.y == 0)
@@ -406,55 +409,81 @@ attn_join_tree_kernel(const __grid_constant__ AttnArgs a, JoinSet rows, JoinSet 
     }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const bool of_rows = (int)blockIdx.y < y_rows;
-  const int lane = threadIdx.x & 31, i = ((int)blockIdx.y - (of_rows ? 0 : y_rows)) * 16 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, i0 = ((int)blockIdx.y - (of_rows ? 0 : y_rows)) * 16 * EACH + (int)(threadIdx.x >> 5);
   const float* slots = of_rows ? rows.slots : tiles.slots;
   const int cap = of_rows ? rows.cap : tiles.cap;
   const JoinRecord rec = (of_rows ? rows.records : tiles.records)[blockIdx.x];
   const size_t size = (size_t)cap * (D + 2);
   const int pieces = (int)blockIdx.x - rec.first_cta + 1;
   auto piece = [&](int k) { return slots + (size_t)(2 * (rec.first_cta + k) + (k == 0 ? rec.first_slot : 0)) * size; };
-  if (i >= rec.rows) return;
-  float top = -INFINITY;
-  for (int k = lane; k < pieces; k += 32) top = fmaxf(top, piece(k)[i]);
+  if (i0 >= rec.rows) return;
+  constexpr int kStep = 16;
+  float top[EACH], sum[EACH], v[EACH][D / 32];
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-  const float safe = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f, v[D / 32] = {};
+  for (int x = 0; x < EACH; ++x) {
+    top[x] = -INFINITY;
+    sum[x] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) v[x][e] = 0.0f;
+  }
+  for (int k = lane; k < pieces; k += 32)
+#pragma unroll
+    for (int x = 0; x < EACH; ++x)
+      if (i0 + x * kStep < rec.rows) top[x] = fmaxf(top[x], piece(k)[i0 + x * kStep]);
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+    for (int x = 0; x < EACH; ++x) top[x] = fmaxf(top[x], __shfl_xor_sync(0xffffffffu, top[x], d));
   for (int k0 = 0; k0 < pieces; k0 += 32) {
-    float f = 0.0f;
-    if (k0 + lane < pieces) {
-      f = exp2_fast(piece(k0 + lane)[i] - safe);
-      sum += piece(k0 + lane)[cap + i] * f;
+    float f[EACH];
+#pragma unroll
+    for (int x = 0; x < EACH; ++x) {
+      const int i = i0 + x * kStep;
+      f[x] = 0.0f;
+      if (k0 + lane < pieces && i < rec.rows) {
+        f[x] = exp2_fast(piece(k0 + lane)[i] - (top[x] == -INFINITY ? 0.0f : top[x]));
+        sum[x] += piece(k0 + lane)[cap + i] * f[x];
+      }
     }
     const int n = min(pieces - k0, 32);
 #pragma unroll 4
     for (int k = 0; k < n; ++k) {
-      const float w = __shfl_sync(0xffffffffu, f, k);
-      const float* o = piece(k0 + k) + 2 * cap + (size_t)i * D + lane * (D / 32);
+      const float* from = piece(k0 + k) + 2 * cap + lane * (D / 32);
 #pragma unroll
-      for (int e = 0; e < D / 32; e += 2) {
-        const float2 x = *reinterpret_cast<const float2*>(o + e);
-        v[e] += x.x * w;
-        v[e + 1] += x.y * w;
+      for (int x = 0; x < EACH; ++x) {
+        const float w = __shfl_sync(0xffffffffu, f[x], k);
+        const float* o = from + (size_t)min(i0 + x * kStep, rec.rows - 1) * D;
+#pragma unroll
+        for (int e = 0; e < D / 32; e += 2) {
+          const float2 z = *reinterpret_cast<const float2*>(o + e);
+          v[x][e] += z.x * w;
+          v[x][e + 1] += z.y * w;
+        }
       }
     }
   }
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  const int ri = rec.row0 + i, ti = a.by_g.div(ri);
-  const long long tok = rec.tok0 + ti;
-  const int qh = rec.head * a.G + (ri - ti * a.G);
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<QT*>(a.out) + tok * a.o_tok + (long long)qh * a.o_head) + lane * (D / 64);
+  for (int x = 0; x < EACH; ++x) {
 #pragma unroll
-  for (int e = 0; e < D / 32; e += 2) dst[e / 2] = Bits16<QT>::pack(v[e] * inv, v[e + 1] * inv);
-  if (a.lse && lane == 0)
-    a.lse[tok * (a.pool.H * a.G) + qh] = sum == 0.0f ? -INFINITY : 0.69314718056f * (top + log2f(sum));
+    for (int d = 16; d > 0; d >>= 1) sum[x] += __shfl_xor_sync(0xffffffffu, sum[x], d);
+    const int i = i0 + x * kStep;
+    if (i >= rec.rows) continue;
+    const int ri = rec.row0 + i, ti = a.by_g.div(ri);
+    const long long tok = rec.tok0 + ti;
+    const int qh = rec.head * a.G + (ri - ti * a.G);
+    const float inv = sum[x] == 0.0f ? 0.0f : 1.0f / sum[x];
+    uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<QT*>(a.out) + tok * a.o_tok + (long long)qh * a.o_head) + lane * (D / 64);
+#pragma unroll
+    for (int e = 0; e < D / 32; e += 2) dst[e / 2] = Bits16<QT>::pack(v[x][e] * inv, v[x][e + 1] * inv);
+    if (a.lse && lane == 0)
+      a.lse[tok * (a.pool.H * a.G) + qh] = sum[x] == 0.0f ? -INFINITY : 0.69314718056f * (top[x] + log2f(sum[x]));
+  }
 }
 
 template <int D, typename QT, bool TREE>
 inline int32_t launch_join(const AttnArgs& a, const JoinSet& rows, const JoinSet& tiles, cudaStream_t st) {
-  const int y_rows = (rows.cap + 15) / 16, y_tiles = (tiles.cap + 15) / 16;
+  const int each = TREE && tiles.cap > 0 ? 32 : 16;        // rows of a block
+  const int y_rows = (rows.cap + each - 1) / each, y_tiles = (tiles.cap + each - 1) / each;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned int)sm_count(), (unsigned int)(y_rows + y_tiles));
   cfg.blockDim = dim3(TREE ? 512 : 256);
@@ -464,10 +493,14 @@ inline int32_t launch_join(const AttnArgs& a, const JoinSet& rows, const JoinSet
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  if constexpr (TREE)
-    cudaLaunchKernelEx(&cfg, attn_join_tree_kernel<D, QT>, a, rows, tiles, y_rows);
-  else
+  if constexpr (TREE) {
+    if (each == 32)
+      cudaLaunchKernelEx(&cfg, attn_join_tree_kernel<D, QT, 2>, a, rows, tiles, y_rows);
+    else
+      cudaLaunchKernelEx(&cfg, attn_join_tree_kernel<D, QT, 1>, a, rows, tiles, y_rows);
+  } else {
     cudaLaunchKernelEx(&cfg, attn_join_kernel<D, QT>, a, rows, tiles, y_rows);
+  }
   return launch_status();
 }
 
