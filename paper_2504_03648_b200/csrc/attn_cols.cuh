@@ -15,18 +15,24 @@
 // Visible: cached positions (window: those near enough to the row's node) and the nodes whose bit is set
 // in the row's mask; a thread looks at bits only in tiles that touch the nodes.
 //
-// Over an e4m3 pool a warpgroup turns raw tiles into operands as they arrive: K into fp16, exact and
+// Over an e4m3 pool two warpgroups turn raw tiles into operands as they arrive: K into fp16, exact and
 // without its scales, which the thread that has the key applies to its scores; V into bf16, exact too.
 // V's scales go with the weights, in bf16, whose range holds them however far apart they are (scale bytes
 // outside [kScaleLow, kScaleHigh] leave the rest with V).  fp16 queries get weights as the sum of two
 // bf16 numbers, so that they lose nothing to the type.
 //
-// Roles: four softmax warpgroups (e4m3: two), each with its part of the rows, which never wait for each other; a warp
-// for S^T and one for O^T; a loader of K and one of V; over e4m3 eight that convert and
-// fetch the scale bytes.  Rings of K
-// and of V tiles of their own, S^T twice, so that S^T(j + 1) runs beside the softmax of tile j.
-// Bound: HBM, 2,800 cycles a tile of 128 16-bit keys of D = 128 (this SM's share), 1,400 of e4m3 ones; the
-// products take (4 + 4) * N cycles of the tensor pipe.
+// Roles: four softmax warpgroups (e4m3: two), each with its part of the rows, which never wait for each
+// other; a warp for S^T and one for O^T; a loader of K and one of V; over e4m3 eight that convert and fetch the
+// scale bytes.  Rings of K and of V tiles of their own, S^T twice, so that S^T(j + 1) runs beside the softmax of
+// tile j.  What a warp of the softmax keeps for rare paths is read again there: with all of it in registers the
+// main loop spilled (32 requests of 32 nodes, 230 instead of 163 us).
+//
+// Bound, 16-bit: HBM, 2,800 cycles a tile of 128 keys of D = 128 (this SM's share); the products take 8 N
+// cycles of the tensor pipe, a step of 128 rows about 2,900 of the softmax.  32 requests over 2k to 8k cached
+// tokens of 8 heads: 122 us for 16 rows (5.5 TB/s), 137 for 64, 163 for 128 (4.2 TB/s); 48 requests of 4 nodes
+// 159 us (5.6 TB/s).  Of that some 15 us are start, a segment's first and last step, and the join.
+// e4m3: 1,400 cycles would be the share of HBM, a tile takes 3,600 (8 requests over 60k to 131k tokens, 28
+// rows: 317 us, 2.6 TB/s): the eight converters need 2,400, of instructions that the softmax warps wait for too.
 #pragma once
 
 #include "attn_tiles.cuh"
