@@ -424,7 +424,7 @@ tree_masks_kernel(TreeArgs a) {
       }
     }
     if (a.pos) {
-      const int base = __ldg(a.kv_len + r) - n;
+      const int base = (int)(__ldg(a.kv_len + r) - (__ldg(a.tok_off + r + 1) - tok0));
       for (int i = tid; i < n; i += N) {
         int above = -1;
 #pragma unroll
@@ -451,9 +451,11 @@ inline int32_t tree_masks(const int32_t* parent, const int64_t* tok_off, const i
   if (R == 0 || n_tokens == 0) return AIBX_OK;
   if (!parent || !tok_off || !mask || (pos && !kv_len)) return AIBX_ERR_INVALID;
   if (((reinterpret_cast<uintptr_t>(parent) | reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(pos)) & 3) ||
-      ((reinterpret_cast<uintptr_t>(tok_off) | reinterpret_cast<uintptr_t>(mask)) & 7) || pos == parent ||
-      (pos && pos == kv_len))
+      ((reinterpret_cast<uintptr_t>(tok_off) | reinterpret_cast<uintptr_t>(mask)) & 7))
     return AIBX_ERR_INVALID;
+  const void* in[] = {parent, tok_off, kv_len};
+  for (const void* x : in)
+    if (x && (x == mask || x == pos)) return AIBX_ERR_INVALID;
   const TreeArgs a = {parent, tok_off, kv_len, reinterpret_cast<unsigned long long*>(mask), pos, n_tokens, R};
   switch (words) {
     case 1: return launch_tree_masks<1>(a, st);

@@ -246,3 +246,13 @@ def test_masks_refuse_on_the_device():
     assert aibx.status_fetch() == (aibx.ERR_RANGE, 4)        # nodes 2 and 3 of the first, 3 of the last; the second request
     got = mask.cpu().numpy()[:, 0].tolist()
     assert got[:5] == [1, 3, 4, 8, 1 | 2 | 16] and got[5:75] == [7] * 70 and got[75:] == [1, 3, 7, 8]
+
+
+def test_masks_of_fewer_rows_than_nodes():
+    """A request that the per-token tensors cut off: positions still count from its first node."""
+    off, kv = dev([0, 4, 10], np.int64), dev([50, 90], np.int32)
+    mask = torch.zeros(7, 1, dtype=torch.int64, device="cuda").view(torch.uint64)
+    pos = torch.zeros(7, dtype=torch.int32, device="cuda")
+    aibx.tree_masks(dev([-1, 0, 0, 2, -1, 0, 1], np.int32), off, kv, mask, pos=pos)
+    assert mask.cpu().numpy()[:, 0].tolist() == [1, 3, 5, 13, 1, 3, 7]
+    assert pos.tolist() == [46, 47, 47, 48, 84, 85, 86]

@@ -60,6 +60,11 @@ def test_bad_masks(lib, kw):  # noqa: F811
     assert masks(lib, **kw) == aibx.ERR_INVALID
 
 
+@pytest.mark.parametrize("kw", [dict(mask=FAKE), dict(mask=FAKE + 64), dict(mask=FAKE + 128), dict(pos=FAKE + 64)])
+def test_masks_in_the_place_of_inputs(lib, kw):  # noqa: F811
+    assert masks(lib, **kw) == aibx.ERR_INVALID
+
+
 def test_masks_of_nothing(lib):  # noqa: F811
     assert masks(lib, words=9) == aibx.ERR_UNSUPPORTED
     assert masks(lib, R=0, parent=None) == aibx.OK and masks(lib, n=0, mask=None) == aibx.OK
