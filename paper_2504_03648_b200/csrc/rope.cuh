@@ -96,9 +96,11 @@ rope_kernel(PagedPool pool, PagedBatch b, RopeIO io) {
     for (int x = lane; x < io.half; x += 32) {
       double w = (double)p_t * (__ldg(io.inv_freq + x) * 0.15915494309189535);
       w -= rint(w);
+      // what the turns lose in 32 bits is put back to first order (up to 2^-26 turns: as much as all else)
+      const float near = (float)w, rest = (float)(w - near) * 6.283185307f;
       float sn, cs;
-      sincospif(2.0f * (float)w, &sn, &cs);
-      turn[x] = make_float2(cs * io.factor, sn * io.factor);
+      sincospif(2.0f * near, &sn, &cs);
+      turn[x] = make_float2((cs - sn * rest) * io.factor, (sn + cs * rest) * io.factor);
     }
     __syncwarp();
 #pragma unroll
