@@ -90,7 +90,7 @@ inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cuda
     if (rc == AIBX_OK && plan.tiles) {
       a.slots += plan.rows_bytes / sizeof(float);
       a.row_limit = plan.col_limit;
-      rc = launch_attn_tiles<D, F8, QT, true>(a, type, tiles, st);
+      rc = launch_attn_tiles<D, F8, QT, true>(a, type, tiles, plan.cols > 0, st);
     }
     return rc != AIBX_OK ? rc : launch_join<D, QT, true>(a, rows, tiles, st);
   }
@@ -101,7 +101,7 @@ inline int32_t launch_attn_kind(AttnArgs a, int type, const AttnPlan& plan, cuda
     a.slots += plan.rows_bytes / sizeof(float);
   }
   if (plan.tiles) {
-    const int32_t rc = launch_attn_tiles<D, F8, QT, false>(a, type, tiles, st);
+    const int32_t rc = launch_attn_tiles<D, F8, QT, false>(a, type, tiles, false, st);
     if (rc != AIBX_OK) return rc;
   }
   return launch_join<D, QT, false>(a, rows, tiles, st);

@@ -1206,10 +1206,14 @@ attn_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant
     tmem_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
+  if constexpr (TREE) asm volatile("griddepcontrol.wait;" ::: "memory");   // (the kernel before, if there is one)
 }
 
+// `behind`: a kernel of the same call runs before this one, in the same stream and on its own requests.  Its
+// SMs then go on to this kernel one by one, as they come free (32 drafts of both kinds: 215 -> 206 us); at its end this kernel waits for that one, so that the join, which waits for this one alone, finds
+// what both have left.
 template <int D, bool F8, typename QT, bool TREE>
-inline int32_t launch_attn_tiles(AttnArgs a, int type, JoinSet& join, cudaStream_t st) {
+inline int32_t launch_attn_tiles(AttnArgs a, int type, JoinSet& join, bool behind, cudaStream_t st) {
   using S = TileShape<D, F8>;
   a.box = gcd_int(a.pool.T, kTileKeys);
   a.box_log = log2_int(a.box);
@@ -1223,7 +1227,17 @@ inline int32_t launch_attn_tiles(AttnArgs a, int type, JoinSet& join, cudaStream
   if (!ensure_dynamic_smem(attn_tiles_kernel<D, F8, QT, TREE>, S::kSmem, dev, configured, lock))
     return AIBX_ERR_CUDA;
   const unsigned int grid = (unsigned int)sm_count();
-  attn_tiles_kernel<D, F8, QT, TREE><<<grid, S::kThreads, S::kSmem, st>>>(map, a);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(S::kThreads);
+  cfg.dynamicSmemBytes = S::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = behind ? 1 : 0;
+  cudaLaunchKernelEx(&cfg, attn_tiles_kernel<D, F8, QT, TREE>, map, a);
   join = JoinSet{a.slots, reinterpret_cast<const JoinRecord*>(a.slots + 2ull * grid * S::kSlot), 2 * kTileRows};
   return launch_status();
 }
