@@ -117,7 +117,9 @@ struct ColShape {
   static constexpr int kColBytes = 128 * 128;
   static constexpr int kRaw = kTileKeys * D;               // a tile's e4m3 rows, as they arrive
   static constexpr int kBuf = kTileKeys * D * 2 + (F8 && D == 64 ? kRaw : 0);   // as in TileShape
-  static constexpr int kQ = kCols * kColBytes * N / 128;
+  // K as it lies, if a row's 8-bit numbers fill the 128 bytes of an operand row
+  static constexpr bool kPlain = F8 && D == 128;
+  static constexpr int kKBuf = kPlain ? kRaw : kBuf;
   static constexpr int kP = kTileKeys * 128 * ((N + 63) / 64);   // P^T: 64 rows in 128 bytes a key
   static constexpr int kRoom = 216 * 1024;
 };
@@ -126,9 +128,13 @@ template <int D, bool F8, int N, int PARTS>
 struct ColRings : ColShape<D, F8, N> {
   using B = ColShape<D, F8, N>;
   static constexpr int kPs = N <= 64 ? 2 : 1;              // P^T of that many tiles
-  static constexpr int kBufs = (B::kRoom - B::kQ - kPs * PARTS * B::kP - 1024) / B::kBuf;
-  static constexpr int kK = kBufs / 2 < 4 ? kBufs / 2 : 4, kV = kBufs - kBufs / 2 < 4 ? kBufs - kBufs / 2 : 4;
-  static constexpr int kQAt = (kK + kV) * B::kBuf, kPAt = kQAt + B::kQ;
+  static constexpr int kQParts = B::kPlain ? PARTS + 1 : 1;   // 8-bit numbers that make up a query's
+  static constexpr int kQ = B::kPlain ? kQParts * N * 128 : B::kCols * B::kColBytes * N / 128;
+  static constexpr int kLeft = B::kRoom - kQ - kPs * PARTS * B::kP - 1024;
+  static constexpr int kHalf = kLeft / (B::kKBuf + B::kBuf);
+  static constexpr int kV = (kLeft - kHalf * B::kKBuf) / B::kBuf < 4 ? (kLeft - kHalf * B::kKBuf) / B::kBuf : 4;
+  static constexpr int kK = (kLeft - kV * B::kBuf) / B::kKBuf < 4 ? (kLeft - kV * B::kBuf) / B::kKBuf : 4;
+  static constexpr int kVAt = kK * B::kKBuf, kQAt = kVAt + kV * B::kBuf, kPAt = kQAt + kQ;
   static constexpr int kSmem = kPAt + kPs * PARTS * B::kP + 1024;
   static constexpr int kSlot = N * (D + 2);                // floats per workspace slot
   static constexpr int kRegsSoftmax = F8 ? 136 : 104;      // launch: 96 (640 threads both)
@@ -140,6 +146,19 @@ struct ColRings : ColShape<D, F8, N> {
 __host__ __device__ constexpr unsigned int col_mma_desc(bool half, int n, bool major) {
   return (1u << 4) | ((half ? 0u : 1u) << 7) | ((half ? 0u : 1u) << 10) | (major ? 3u << 15 : 0u) |
          ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+
+// The same of e4m3 numbers (K = 32), both K-major.
+__host__ __device__ constexpr unsigned int col_mma_desc8(int n) {
+  return (1u << 4) | ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void mma_smem8(unsigned int d, uint64_t a, uint64_t b, unsigned int idesc, unsigned int add,
+                                          unsigned int leader) {
+  asm volatile(
+      "{\n.reg .pred p, q;\nsetp.ne.u32 p, %4, 0;\nsetp.ne.u32 q, %5, 0;\n"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(add), "r"(leader)
+      : "memory");
 }
 
 __device__ __forceinline__ void tmem_ld8(unsigned int addr, uint32_t* r) {
@@ -207,14 +226,14 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 
   const unsigned int smem0 = (smem_u32(s_raw) + 1023u) & ~1023u;
   unsigned char* base = s_raw + (smem0 - smem_u32(s_raw));
-  const unsigned int k0 = smem0, v0 = smem0 + S::kK * S::kBuf;
+  const unsigned int k0 = smem0, v0 = smem0 + S::kVAt;
   const int lane = threadIdx.x & 31;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   volatile int* abort_flag = &s_abort;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kK; ++i) {
-      mbar_init(smem_u32(&s_k_full[i]), F8 ? 256u : 1u);
+      mbar_init(smem_u32(&s_k_full[i]), F8 && !S::kPlain ? 256u : 1u);
       mbar_init(smem_u32(&s_k_empty[i]), 1u);
       mbar_init(smem_u32(&s_k_raw[i]), 1u);
     }
@@ -336,15 +355,45 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
               for (int m = 1; m < kPieces; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
               float down, up;
               power_scale(amax, down, up);
+              if constexpr (S::kPlain) {
+                // The row's largest element into [128, 256), then all as the sum of e4m3 numbers: each takes
+                // four bits of what the ones before have left, two make a bf16 number, three an fp16 number.
+                // Elements below 2^-9 (2^-6) of the largest lose what is below 2^-17 of it.
+                down *= 128.0f;
+                up *= 1.0f / 128.0f;
+                if (!(amax < INFINITY)) up = NAN;          // (these bits know no infinity)
+                float2 f[4];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float2 f = Bits16<QT>::unpack(x[e]);
-                x[e] = Bits16<KT>::pack(f.x * down, f.y * down);
+                for (int e = 0; e < 4; ++e) {
+                  f[e] = Bits16<QT>::unpack(x[e]);
+                  f[e].x *= down;
+                  f[e].y *= down;
+                }
+#pragma unroll
+                for (int part = 0; part < S::kQParts; ++part) {
+                  uint32_t y[4];
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    y[e] = e4m3_pair(f[e].x, f[e].y, false);
+                    const float2 g = __half22float2(halves_of_e4m3(y[e]));
+                    f[e].x -= g.x;
+                    f[e].y -= g.y;
+                  }
+                  if (on)
+                    *reinterpret_cast<uint2*>(s_q + part * N * 128 + i * 128 + (((c >> 1) ^ (i & 7)) << 4) + (c & 1) * 8) =
+                        make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
+                }
+              } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float2 f = Bits16<QT>::unpack(x[e]);
+                  x[e] = Bits16<KT>::pack(f.x * down, f.y * down);
+                }
+                v = make_uint4(x[0], x[1], x[2], x[3]);
               }
-              v = make_uint4(x[0], x[1], x[2], x[3]);
               if (on && c == 0) s_scale[i] = a.scale_log2 * up;
             }
-            if (on) *reinterpret_cast<uint4*>(dst + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = v;
+            if (on && !S::kPlain) *reinterpret_cast<uint4*>(dst + i * 128 + (((c & 7) ^ (i & 7)) << 4)) = v;
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -639,7 +688,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       const unsigned int q_low = uniform(operand_low(smem0 + S::kQAt, 16)), k_low = uniform(operand_low(k0, 16));
       while (walk.next_warp(a, per)) {
         const int steps = (int)uniform(walk.t1 - walk.t0);
-        constexpr unsigned int desc = col_mma_desc(std::is_same<KT, __half>::value, N, false);
+        constexpr unsigned int desc = S::kPlain ? col_mma_desc8(N) : col_mma_desc(std::is_same<KT, __half>::value, N, false);
         ring_wait(smem_u32(&s_q_full), q_phase, abort_flag);
         q_phase ^= 1u;
         for (int j = 0; j < steps; ++j, ++step) {
@@ -648,9 +697,15 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           ring_wait(smem_u32(&s_s_free[sb]), ((step >> 1) & 1u) ^ 1u, abort_flag);
           __syncwarp();
           tmem_after();
-          const unsigned int low = k_low + buf * (S::kBuf >> 4);
+          const unsigned int low = k_low + buf * (S::kKBuf >> 4);
+          if constexpr (S::kPlain) {
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k)
+            for (int x = 0; x < S::kQParts * 4; ++x)       // (part x / 4, 32 dimensions from 32 (x % 4) on)
+              mma_smem8(tmu + sb * 128, operand_desc(low + ((x & 3) * 32 >> 4)),
+                        operand_desc(q_low + (((x >> 2) * N * 128 + (x & 3) * 32) >> 4)), desc, x > 0, leader);
+          }
+#pragma unroll
+          for (int k = 0; k < (S::kPlain ? 0 : D / 16); ++k)
             mma_smem(tmu + sb * 128, operand_desc(low + (((k >> 2) * S::kColBytes + (k & 3) * 32) >> 4)),
                      operand_desc(q_low + (((k >> 2) * (S::kQ / S::kCols) + (k & 3) * 32) >> 4)), desc, k > 0, leader);
           mma_commit(smem_u32(&s_s_full[sb]), leader);
@@ -730,11 +785,12 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       // (A box takes its warp 75 cycles to issue: 16 of either K or V in one warp's loop took longer than
       // the bytes need.)
       const bool is_v = uniform(warp == kLoadV);
-      constexpr unsigned int kBytes = F8 ? S::kRaw : S::kBuf;
+      constexpr unsigned int kBytes = F8 ? S::kRaw : S::kBuf;   // of a tile of K or V
       constexpr int kRow = F8 ? D : 128;
-      unsigned long long* full = is_v ? (F8 ? s_v_raw : s_v_full) : (F8 ? s_k_raw : s_k_full);
+      unsigned long long* full = is_v ? (F8 ? s_v_raw : s_v_full) : (F8 && !S::kPlain ? s_k_raw : s_k_full);
       unsigned long long* empty = is_v ? s_v_empty : s_k_empty;
-      const unsigned int ring0 = (is_v ? v0 : k0) + (F8 ? S::kColBytes : 0), bufs = is_v ? S::kV : S::kK;
+      const unsigned int ring0 = is_v ? v0 + (F8 ? S::kColBytes : 0) : k0 + (F8 && !S::kPlain ? S::kColBytes : 0);
+      const unsigned int bufs = is_v ? S::kV : S::kK, each = is_v ? S::kBuf : S::kKBuf;
       const int boxes = kTileKeys >> a.box_log;
       unsigned int buf = 0, phase = 1, issued = 0;         // (a fresh barrier passes for phase 1)
       while (walk.next_warp(a, per)) {
@@ -766,7 +822,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             if (lane == 0) mbar_arrive_expect_tx(bar, kBytes);
             __syncwarp();
             if (lane < boxes) {
-              const unsigned int dst = ring0 + buf * S::kBuf + lane * a.box * kRow;
+              const unsigned int dst = ring0 + buf * each + lane * a.box * kRow;
 #pragma unroll
               for (int cc = 0; cc < (F8 ? 1 : S::kCols); ++cc)
                 tensor_load_5d(dst + cc * S::kColBytes, &map, bar, cc * 64, slot, head, block, is_v ? 1 : 0);
@@ -845,59 +901,56 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         auto convert = [&](unsigned int at, auto is_v, auto odd) {
           unsigned char* out = base + at + (c >> 2) * S::kColBytes;
           const unsigned char* src = base + at + S::kColBytes;
-          constexpr int kTurn = kRows;
+          uint4 v[kRows];
 #pragma unroll
-          for (int u0 = 0; u0 < kRows; u0 += kTurn) {
-            uint4 v[kTurn];
+          for (int u = 0; u < kRows; ++u) {
+            const int i = i0 + u;
+            v[u] = *reinterpret_cast<const uint4*>(src + i * D + ((D == 128 ? c ^ (i & 7) : c) << 4));
+          }
+          __syncwarp();
 #pragma unroll
-            for (int u = 0; u < kTurn; ++u) {
-              const int i = i0 + u0 + u;
-              v[u] = *reinterpret_cast<const uint4*>(src + i * D + ((D == 128 ? c ^ (i & 7) : c) << 4));
+          for (int u = 0; u < kRows; ++u) {
+            const int i = i0 + u;
+            const uint32_t wv[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+            uint32_t o[8];
+            float rest = 1.0f;
+            bool gone = false;
+            if constexpr (decltype(odd)::value) {
+              const int key = key_first + j * kTileKeys + i, vb = s_bytes[ft][1][i];
+              gone = key < lo || key >= hi;              // whatever the pool holds there
+              rest = vb == 255 ? NAN : power_of_byte(127 + vb - weight_byte(vb));
             }
-            __syncwarp();
 #pragma unroll
-            for (int u = 0; u < kTurn; ++u) {
-              const int i = i0 + u0 + u;
-              const uint32_t wv[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-              uint32_t o[8];
-              float rest = 1.0f;
-              bool gone = false;
-              if constexpr (decltype(odd)::value) {
-                const int key = key_first + j * kTileKeys + i, vb = s_bytes[ft][1][i];
-                gone = key < lo || key >= hi;              // whatever the pool holds there
-                rest = vb == 255 ? NAN : power_of_byte(127 + vb - weight_byte(vb));
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t two = (wv[e >> 1] >> (16 * (e & 1))) & 0xffffu;
+              if constexpr (!decltype(is_v)::value)
+                o[e] = e4m3_bits(two);
+              else if constexpr (decltype(odd)::value)
+                o[e] = gone ? 0u : bf16_of_e4m3(two, rest);
+              else {
+                const float2 y = __half22float2(halves_of_e4m3(two));
+                o[e] = Bits16<__nv_bfloat16>::pack(y.x, y.y);
               }
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const uint32_t two = (wv[e >> 1] >> (16 * (e & 1))) & 0xffffu;
-                if constexpr (!decltype(is_v)::value)
-                  o[e] = e4m3_bits(two);
-                else if constexpr (decltype(odd)::value)
-                  o[e] = gone ? 0u : bf16_of_e4m3(two, rest);
-                else
-{
-                  const float2 y = __half22float2(halves_of_e4m3(two));
-                  o[e] = Bits16<__nv_bfloat16>::pack(y.x, y.y);
-                }
-              }
-              // (pieces 2 c and 2 c + 1; the upper half of a row's lanes the other way round: with their
-              // column 16 KB on they would meet the lower half's banks)
-              const int p0 = (2 * c) & 7, flip = c >> 2 & 1;
-              *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + flip) ^ (i & 7)) << 4)) =
-                  flip ? make_uint4(o[4], o[5], o[6], o[7]) : make_uint4(o[0], o[1], o[2], o[3]);
-              *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + 1 - flip) ^ (i & 7)) << 4)) =
-                  flip ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(o[4], o[5], o[6], o[7]);
             }
+            // (pieces 2 c and 2 c + 1; the upper half of a row's lanes the other way round: with their
+            // column 16 KB on they would meet the lower half's banks)
+            const int p0 = (2 * c) & 7, flip = c >> 2 & 1;
+            *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + flip) ^ (i & 7)) << 4)) =
+                flip ? make_uint4(o[4], o[5], o[6], o[7]) : make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(out + i * 128 + (((p0 + 1 - flip) ^ (i & 7)) << 4)) =
+                flip ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(o[4], o[5], o[6], o[7]);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         };
-        ring_wait(smem_u32(&s_k_raw[kbuf]), kphase, abort_flag);
-        __syncwarp();
-        convert((k0 - smem0) + kbuf * S::kBuf, std::false_type(), std::false_type());
-        mbar_arrive(smem_u32(&s_k_full[kbuf]));
-        if (++kbuf == S::kK) {
-          kbuf = 0;
-          kphase ^= 1u;
+        if constexpr (!S::kPlain) {
+          ring_wait(smem_u32(&s_k_raw[kbuf]), kphase, abort_flag);
+          __syncwarp();
+          convert((k0 - smem0) + kbuf * S::kKBuf, std::false_type(), std::false_type());
+          mbar_arrive(smem_u32(&s_k_full[kbuf]));
+          if (++kbuf == S::kK) {
+            kbuf = 0;
+            kphase ^= 1u;
+          }
         }
         if (j % kColBatch == 0) ring_wait(smem_u32(&s_info_full[f]), (batch / kColInfo) & 1u, abort_flag);
         ring_wait(smem_u32(&s_v_raw[vbuf]), vphase, abort_flag);
