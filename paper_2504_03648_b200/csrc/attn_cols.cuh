@@ -233,12 +233,12 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kK; ++i) {
-      mbar_init(smem_u32(&s_k_full[i]), F8 && !S::kPlain ? 256u : 1u);
+      mbar_init(smem_u32(&s_k_full[i]), F8 && !S::kPlain ? 128u * S::kConverters : 1u);
       mbar_init(smem_u32(&s_k_empty[i]), 1u);
       mbar_init(smem_u32(&s_k_raw[i]), 1u);
     }
     for (int i = 0; i < S::kV; ++i) {
-      mbar_init(smem_u32(&s_v_full[i]), F8 ? 256u : 1u);
+      mbar_init(smem_u32(&s_v_full[i]), F8 ? 128u * S::kConverters : 1u);
       mbar_init(smem_u32(&s_v_empty[i]), 1u);
       mbar_init(smem_u32(&s_v_raw[i]), 1u);
     }
