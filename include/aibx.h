@@ -634,11 +634,13 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
  *   not only those of trees, and a node need not see itself.  Bits of nodes that the request has not are
  *   ignored.  params->causal is not read.  Everything else as aibx_attn_paged (formats, shapes, errors, the
  *   same bits every time), but: weights over an E4M3 pool may be held as bf16, or with FP16 queries as the
- *   sum of two bf16 numbers; a NaN or infinite V of a node, or of a cached position that only some rows'
- *   windows reach, may reach a row that it is hidden from; the workspace is of aibx_attn_tree_workspace_bytes bytes, which depend on
- *   head_dim, num_q_heads / num_kv_heads, max_new, the types, whether R is 1 and the device alone.  INVALID for a null or
- *   unaligned d_mask or mask_words < 1, UNSUPPORTED for more than 8 words, RANGE for a request with more
- *   than 64 * mask_words tokens (whose later nodes count as hidden).
+ *   sum of two bf16 numbers, and elements of a query may lose what is below 2^-17 of its largest (a query that
+ *   is not finite then gives NaN); a NaN or infinite V of a node, or of a cached position that only some rows'
+ *   windows reach, may reach a row that it is hidden from; the workspace is of
+ *   aibx_attn_tree_workspace_bytes bytes, which depend on head_dim, num_q_heads / num_kv_heads, max_new, the
+ *   types, whether R is 1 and the device alone.  INVALID for a null or unaligned d_mask or mask_words < 1,
+ *   UNSUPPORTED for more than 8 words, RANGE for a request with more than 64 * mask_words tokens (whose later
+ *   nodes count as hidden).
  */
 int32_t aibx_tree_masks(const int32_t* d_parent, const int64_t* d_tok_off, const int32_t* d_kv_len,
                         int32_t R, int64_t n_tokens, int32_t mask_words, uint64_t* d_mask,

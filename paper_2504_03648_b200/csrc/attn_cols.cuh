@@ -15,24 +15,26 @@
 // Visible: cached positions (window: those near enough to the row's node) and the nodes whose bit is set
 // in the row's mask; a thread looks at bits only in tiles that touch the nodes.
 //
-// Over an e4m3 pool two warpgroups turn raw tiles into operands as they arrive: K into fp16, exact and
-// without its scales, which the thread that has the key applies to its scores; V into bf16, exact too.
-// V's scales go with the weights, in bf16, whose range holds them however far apart they are (scale bytes
-// outside [kScaleLow, kScaleHigh] leave the rest with V).  fp16 queries get weights as the sum of two
+// Over an e4m3 pool K of D = 128 is multiplied as it lies, 8 bits by 8 bits: a query becomes the sum of two
+// (fp16: three) e4m3 numbers, whose products with K add up in one accumulator (converting K instead, 28 rows:
+// 316 us, so 226).  K of D = 64, whose rows do not fill an operand's, two warpgroups turn into fp16 as it
+// arrives, exact.  K's scales the thread that has the key applies to its scores.  V the same two turn into bf16,
+// exact too; its scales go with the weights, in bf16, whose range holds them however far apart they are
+// (scale bytes outside [kScaleLow, kScaleHigh] leave the rest with V).  fp16 queries get weights as the sum of two
 // bf16 numbers, so that they lose nothing to the type.
 //
-// Roles: four softmax warpgroups (e4m3: two), each with its part of the rows, which never wait for each
-// other; a warp for S^T and one for O^T; a loader of K and one of V; over e4m3 eight that convert and fetch the
-// scale bytes.  Rings of K and of V tiles of their own, S^T twice, so that S^T(j + 1) runs beside the softmax of
-// tile j.  What a warp of the softmax keeps for rare paths is read again there: with all of it in registers the
-// main loop spilled (32 requests of 32 nodes, 230 instead of 163 us).
+// Roles: four softmax warpgroups (e4m3 and 32 rows: two), each with its part of the rows, which never wait
+// for each other; a warp for S^T and one for O^T; a loader of K and one of V; over e4m3 eight that convert and
+// fetch the scale bytes.  Rings of K and of V tiles of their own, S^T twice, so that S^T(j + 1) runs beside the
+// softmax of tile j.  What a warp of the softmax keeps for rare paths is read again there: with all of it in
+// registers the main loop spilled (32 requests of 32 nodes, 230 instead of 163 us).
 //
-// Bound, 16-bit: HBM, 2,800 cycles a tile of 128 keys of D = 128 (this SM's share); the products take 8 N
-// cycles of the tensor pipe, a step of 128 rows about 2,900 of the softmax.  32 requests over 2k to 8k cached
-// tokens of 8 heads: 122 us for 16 rows (5.5 TB/s), 137 for 64, 163 for 128 (4.2 TB/s); 48 requests of 4 nodes
-// 159 us (5.6 TB/s).  Of that some 15 us are start, a segment's first and last step, and the join.
-// e4m3: 1,400 cycles would be the share of HBM, a tile takes 3,600 (8 requests over 60k to 131k tokens, 28
-// rows: 317 us, 2.6 TB/s): the eight converters need 2,400, of instructions that the softmax warps wait for too.
+// Bound, 16-bit: HBM, 2,740 cycles a tile of 128 keys of D = 128 (this SM's share); the products take 8 N
+// cycles of the tensor pipe.  32 requests over 2k to 8k cached tokens of 8 heads: 123 us for 16 rows (5.4
+// TB/s), 136 for 64, 166 for 128 (4.1 TB/s, where the softmax takes as long as the bytes); 48 requests of 4
+// nodes 161 us (5.5 TB/s).  Without a segment's sums and outputs (a copy, for timing): 141 us for 128 rows.
+// e4m3: 1,370 cycles would be the share of HBM, a tile takes 2,600 (8 requests over 60k to 131k tokens, 28
+// rows: 226 us, 3.6 TB/s): the conversion of V (with half the warps for it 329 us).
 #pragma once
 
 #include "attn_tiles.cuh"
@@ -108,9 +110,9 @@ __device__ __forceinline__ void locate_even(const AttnArgs& a, unsigned int inde
 
 template <int D, bool F8, int N>
 struct ColShape {
-  // Softmax warpgroups.  (Over e4m3 two, of 32 rows each: with four the waits and barriers of twice the warps
-  // stand in the converters' way, 371 instead of 356 us.)
-  static constexpr int kGroups = F8 ? 2 : 4;
+  // Softmax warpgroups.  Over e4m3 two for 32 rows: with four the waits of twice the warps stand in the converters'
+  // way (28 rows: 237 instead of 226 us); for 64 rows four (63 rows: 286 us, with two 306; fp16 queries 340 and 411).
+  static constexpr int kGroups = F8 && N == 32 ? 2 : 4;
   static constexpr int kConverters = F8 ? 2 : 0;           // warpgroups that convert
   static constexpr int kThreads = 128 * (kGroups + 1 + kConverters);
   static constexpr int kCols = D / 64;                     // 128-byte columns of an operand row
@@ -137,8 +139,9 @@ struct ColRings : ColShape<D, F8, N> {
   static constexpr int kVAt = kK * B::kKBuf, kQAt = kVAt + kV * B::kBuf, kPAt = kQAt + kQ;
   static constexpr int kSmem = kPAt + kPs * PARTS * B::kP + 1024;
   static constexpr int kSlot = N * (D + 2);                // floats per workspace slot
-  static constexpr int kRegsSoftmax = F8 ? 136 : 104;      // launch: 96 (640 threads both)
-  static constexpr int kRegsOther = 64, kRegsConvert = 72; // 2 * 136 + 64 + 2 * 72 = 4 * 104 + 64 = 5 * 96
+  // 16 bits: 4 * 104 + 64 = 5 * 96 (launch); e4m3: 2 * 136 + 64 + 2 * 72 = 5 * 96, or 4 * 72 + 64 + 2 * 72 < 7 * 72
+  static constexpr int kRegsSoftmax = !F8 ? 104 : N == 32 ? 136 : 72;
+  static constexpr int kRegsOther = 64, kRegsConvert = 72;
   static_assert(kK >= 2 && kV >= 2, "two tiles of each at least");
 };
 

@@ -28,10 +28,10 @@ inline uint64_t slot_bytes(int rows, int dim) {
 // single token.
 //
 // Trees: the row kernel alone where no request can have more than 8 rows (at 16 it takes 206 us where
-// the column kernel takes 127: twice the products, and registers spill).  The column kernel for requests of up to
-// 128 rows, in blocks of 64 where none has more (half the registers and shared memory); over e4m3, where a
+// the column kernel takes 123: twice the products, and registers spill).  The column kernel for requests of up to
+// 128 rows, in blocks of 32 or 64 where none has more (fewer registers, less shared memory); over e4m3, where a
 // block of 128 leaves its warps too few registers, up to 64.  The tile kernel for more: there a step costs
-// less per row (bf16, 256 rows: 225 us against 290 of two blocks).
+// less per row (bf16, 256 rows: 236 us against 291 of two blocks; e4m3, 112 rows: 532 against 569 of two).
 inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
                          const aibx_attn_params_t* p, bool tree, AttnPlan& plan) {
   PagedPool pool;

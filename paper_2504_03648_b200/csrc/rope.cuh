@@ -8,11 +8,12 @@
 // and sums of 32 bits, one rounding to what is stored; e4m3 rows take their scale from the turned values
 // before any rounding.
 //
-// Bound: HBM for long inputs, each row being read once and written once (40,001 tokens of 32 fp16 heads: 108
-// us, 6.1 TB/s; 25,000 tokens of 28 heads of queries and 4 of K and V into an e4m3 pool: 95 us, 4.9 TB/s, where the
-// quantisation's instructions show), the chain of dependent loads for few tokens (64 tokens: 6 us).  A warp takes some tokens and some planes (a head of Q, K or V); per token its lanes
-// share out the sines and cosines, which then stay in registers for all planes.  A lane holds the two
-// 8-element pieces of a row that belong to each other, so that a pair never leaves its lane.
+// A warp takes some tokens and some planes (a head of Q, K or V); per token its lanes share out the sines and
+// cosines, which then stay in registers for all planes.  A lane holds the two 8-element pieces of a row that
+// belong to each other, so that a pair never leaves its lane.
+// Bound: HBM for long inputs, each row being read once and written once (40,001 tokens of 32 fp16 heads: 109
+// us, 6.0 TB/s; 26,600 tokens of 28 heads of queries and 4 of K and V into an e4m3 pool: 97 us, 4.8 TB/s, where
+// the quantisation's instructions show), the chain of dependent loads for few tokens (64 tokens: 6 us).
 #pragma once
 
 #include "kv_paged.cuh"
