@@ -284,3 +284,32 @@ def test_same_bits_every_time_captured_and_beside_itself(pool, io):
     for o in outs[1:]:
         assert torch.equal(o, outs[0])
     assert aibx.status_fetch() == (0, 0)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("io", ["bf16", "fp16"])
+@pytest.mark.parametrize("new", [[2, 5], [9, 16]])
+def test_queries_of_wide_range(new, io, D):
+    """Over e4m3 an element of a query may lose what is below 2^-17 of the query's largest: a score is off by at
+    most that times the sum of a key's magnitudes, beside what slack counts.  A query with an infinity gives
+    NaN, and leaves the others alone."""
+    rng = np.random.default_rng(D + len(io))
+    lens = [n + c for n, c in zip(new, (300, 77))]
+    s = shape_for(lens, H=2, D=D, T=16, pool="e4m3")
+    b = Batch(rng, s, new, lens)
+    pool, scales = make_pool(rng, s)
+    sets = trees(rng, b)
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 8, D)) * 2.0 ** -rng.uniform(0, 12, (b.n_tokens, 8, D))).to(DTYPE[io])
+    q[1, 3, 5] = float("inf")
+    out = torch.empty(q.shape, dtype=q.dtype, device="cuda")
+    aibx.attn_tree(make_cache(s, pool, scales), make_batch(b, max(new)), dev(pack([x for one in sets for x in one], 1)), q.cuda(), out)
+    got = out.double().cpu().numpy()
+    assert np.isnan(got[1, 3]).all()
+    q[1, 3, 5] = 0.0
+    values, qd, scale = pool_values(s, pool, scales), q.double().numpy(), D ** -0.5
+    want, _, mag, slack = tree_attention(s, b, values, qd, scale, sets, 0)
+    slack = slack + scale * 2.0 ** -17 * np.abs(qd).max(-1) * np.abs(values).sum(-1).max()
+    tol = tree_tolerance(s, io, want, mag, slack)
+    fine = np.ones(got.shape[:2], dtype=bool)
+    fine[1, 3] = False
+    assert (np.abs(got - want) <= tol)[fine].all()
