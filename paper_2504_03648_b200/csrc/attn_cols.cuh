@@ -357,13 +357,12 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 #pragma unroll
               for (int m = 1; m < kPieces; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
               float down, up;
-              power_scale(amax, down, up);
+              power_scale(S::kPlain ? amax * (1.0f / 128.0f) : amax, down, up);
               if constexpr (S::kPlain) {
                 // The row's largest element into [128, 256), then all as the sum of e4m3 numbers: each takes
                 // four bits of what the ones before have left, two make a bf16 number, three an fp16 number.
-                // Elements below 2^-9 (2^-6) of the largest lose what is below 2^-17 of it.
-                down *= 128.0f;
-                up *= 1.0f / 128.0f;
+                // Elements below 2^-9 (2^-6) of the largest lose what is below 2^-17 of it.  (The power is that of
+                // amax / 128, which power_scale need not cut short however large amax is: 448 ends these bits.)
                 if (!(amax < INFINITY)) up = NAN;          // (these bits know no infinity)
                 float2 f[4];
 #pragma unroll

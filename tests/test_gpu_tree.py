@@ -313,3 +313,15 @@ def test_queries_of_wide_range(new, io, D):
     fine = np.ones(got.shape[:2], dtype=bool)
     fine[1, 3] = False
     assert (np.abs(got - want) <= tol)[fine].all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new", [[1, 2], [2, 5], [9, 16], [40, 30]])
+def test_queries_near_the_ends_of_their_type(new, D):
+    """Queries of 2^124, and of 2^-112, whose scores are ordinary numbers."""
+    lens = [n + c for n, c in zip(new, (300, 77))]
+    s = shape_for(lens, H=2, D=D, T=16, pool="e4m3")
+    for e in (122, -114):
+        b = Batch(np.random.default_rng(6), s, new, lens)
+        st, _, _ = check_tree(s, b, "bf16", G=4, seed=D, spread=2.0 ** e, scale=2.0 ** (min(-e, 112) - 4))
+        assert st == (0, 0)
