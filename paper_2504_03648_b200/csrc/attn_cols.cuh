@@ -34,7 +34,7 @@
 // TB/s), 136 for 64, 166 for 128 (4.1 TB/s, where the softmax takes as long as the bytes); 48 requests of 4
 // nodes 161 us (5.5 TB/s).  Without a segment's sums and outputs (a copy, for timing): 141 us for 128 rows.
 // e4m3: 1,370 cycles would be the share of HBM, a tile takes 2,600 (8 requests over 60k to 131k tokens, 28
-// rows: 226 us, 3.6 TB/s): the conversion of V (with half the warps for it 329 us).
+// rows: 230 us, 3.5 TB/s): the conversion of V (with half the warps for it 329 us).
 #pragma once
 
 #include "attn_tiles.cuh"
