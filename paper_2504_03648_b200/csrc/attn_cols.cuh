@@ -187,6 +187,13 @@ __device__ __forceinline__ bool group_any(int id, bool mine) {
 }
 __device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
 
+// The largest of those that are not NaN (max3 would give NaN).
+__device__ __forceinline__ float max3_numbers(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
 // Whole numbers that order as the floats do (not for NaN).
 __device__ __forceinline__ int float_order(float x) {
   const int u = __float_as_int(x);
@@ -542,12 +549,15 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           for (int ch = 0; ch < kChunks; ++ch)
             tmem_ld8(tm_s + sb * 128 + c0 + ch * 8, z + ch * 8);
           tmem_wait_ld();
+          // (A row whose query is infinite has m = infinity after its first tile, and NaN where a score is infinite
+          // again.  That is its own affair: the other rows of this thread's key have their say all the same.)
           float most = -INFINITY;
 #pragma unroll
           for (int ch = 0; ch < kChunks; ++ch) {
             scores(c0 + ch * 8, z + ch * 8, vis >> (ch * 8));
 #pragma unroll
-            for (int i = ch * 8; i < ch * 8 + 8; i += 2) most = max3(most, __uint_as_float(z[i]), __uint_as_float(z[i + 1]));
+            for (int i = ch * 8; i < ch * 8 + 8; i += 2)
+              most = max3_numbers(most, __uint_as_float(z[i]), __uint_as_float(z[i + 1]));
           }
           if (!move) {
             const bool grow = __any_sync(0xffffffffu, most > kHead + 8.0f);

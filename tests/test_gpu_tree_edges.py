@@ -1,0 +1,88 @@
+"""GPU tests of attention of drafted trees where one row's numbers could reach another's, and where queries,
+weights and scores are at the edge of the types that hold them."""
+import numpy as np
+import pytest
+import torch
+
+from paged_ref import DTYPE, Batch, pool_values
+from paper_2504_03648_b200 import binding as aibx
+from steps_ref import ancestors, pack, random_tree, tree_tolerance
+from test_gpu_paged import dev, make_batch, make_cache, make_pool
+from test_gpu_tree import shape_for
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _clean_status():
+    aibx.status_fetch()
+    yield
+
+
+def dense(s, b, values, q, scale, sets):
+    """steps_ref.tree_attention without a window, a request and KV head at a time."""
+    n, Hq, D = q.shape
+    G = Hq // s.H
+    out, lse = np.full((n, Hq, D), np.nan), np.full((n, Hq), np.nan)
+    mag, slack = np.zeros_like(out), np.zeros_like(lse)
+    for r, k in enumerate(b.new):
+        at, base = slice(int(b.tok_off[r]), int(b.tok_off[r + 1])), b.length[r] - k
+        seen = np.zeros((k, b.length[r]), dtype=bool)
+        seen[:, :base] = True
+        for i, nodes in enumerate(sets[r]):
+            seen[i, [base + j for j in nodes]] = True
+        for h in range(s.H):
+            rows = [s.row(b.entry(s, r, j), 0, h, j % s.T) for j in range(b.length[r])]
+            K, V = values[rows], values[[s.row(b.entry(s, r, j), 1, h, j % s.T) for j in range(b.length[r])]]
+            for g in range(h * G, h * G + G):
+                z = np.where(seen, scale * (q[at, g] @ K.T), -np.inf)
+                m = z.max(-1, keepdims=True)
+                w = np.exp(z - m)
+                t = w.sum(-1, keepdims=True)
+                lse[at, g] = (m + np.log(t))[:, 0]
+                out[at, g], mag[at, g] = (w / t) @ V, (w / t) @ np.abs(V)
+                most = np.where(seen, np.abs(K).max(-1), 0).max(-1)
+                slack[at, g] = scale * (D + 4) * 2.0 ** -24 * most * np.abs(q[at, g]).sum(-1) + 4 * 2.0 ** -24 * np.abs(m[:, 0])
+    return out, lse, mag, slack
+
+
+def call(s, b, pool, scales, q, sets, scale, words=1):
+    out = torch.empty(q.shape, dtype=q.dtype, device="cuda")
+    lse = torch.empty(q.shape[:2], device="cuda")
+    mask = dev(np.concatenate([pack(x, words) for x in sets]))
+    aibx.attn_tree(make_cache(s, pool, scales), make_batch(b), mask, q.cuda(), out, lse=lse, scale=scale)
+    assert aibx.status_fetch() == (0, 0)
+    return out.double().cpu().numpy(), lse.double().cpu().numpy()
+
+
+# rows of one KV head: 24, 48, 120
+@pytest.mark.parametrize("n,G", [(3, 8), (12, 4), (30, 4)])
+@pytest.mark.parametrize("pool", ["fp16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_an_infinite_query_beside_scores_that_grow(D, pool, n, G):
+    """Every 128 keys hold one whose score is 8 above all before it, for every row, and is infinite for one: the
+    others' running maximum has to follow all the same, or their weights (e^8 from one to the next) leave fp16."""
+    rng = np.random.default_rng(n + D)
+    ctx = 40 * 128 + 5                            # (8 heads of 41 tiles: several to a CTA)
+    s = shape_for([n + ctx], H=8, D=D, T=16, pool=pool)
+    b = Batch(rng, s, [n], [n + ctx])
+    kv, _ = make_pool(rng, s)
+    scale = D ** -0.5
+    line = np.where(rng.random(D) < 0.5, -1.0, 1.0)
+    line[5] = 1.0
+    for h in range(s.H):
+        for t in range(41):
+            j = 128 * t + (64 + 7 * h) % 128 if t < 40 else 128 * t
+            kv[s.row(b.entry(s, 0, j), 0, h, j % s.T)] = torch.from_numpy(line * 8 * t / (scale * D)).to(DTYPE[pool])
+    sets = [ancestors(random_tree(rng, n))]
+    q = torch.from_numpy(line + 0.1 * rng.normal(size=(n, s.H * G, D))).to(DTYPE[pool])
+    fine = np.ones((n, s.H * G), dtype=bool)
+    fine[1, 1::G] = False                         # a row of every KV head
+    q[1, 1::G, 5] = float("inf")
+    got, gl = call(s, b, kv, None, q, sets, scale)
+    assert np.isnan(got[~fine]).all()
+    q[1, 1::G, 5] = 0.0
+    want, wl, mag, slack = dense(s, b, pool_values(s, kv, None), q.double().numpy(), scale, sets)
+    assert np.isfinite(got[fine]).all()
+    assert (np.abs(got - want) <= tree_tolerance(s, pool, want, mag, slack))[fine].all()
+    assert (np.abs(gl - wl) <= slack + 2.0 ** -14 + 2.0 ** -22 * np.abs(wl))[fine].all()
