@@ -15,8 +15,8 @@
 // Visible: cached positions (window: those near enough to the row's node) and the nodes whose bit is set
 // in the row's mask; a thread looks at bits only in tiles that touch the nodes.
 //
-// Over an e4m3 pool K of D = 128 is multiplied as it lies, 8 bits by 8 bits: a query becomes the sum of two
-// (fp16: three) e4m3 numbers, whose products with K add up in one accumulator (converting K instead, 28 rows:
+// Over an e4m3 pool K of D = 128 is multiplied as it lies, 8 bits by 8 bits: a query becomes the sum of three
+// e5m2 numbers, whose products with K add up in one accumulator (converting K instead, 28 rows:
 // 316 us, so 226).  K of D = 64, whose rows do not fill an operand's, two warpgroups turn into fp16 as it
 // arrives, exact.  K's scales the thread that has the key applies to its scores.  V the same two turn into bf16,
 // exact too; its scales go with the weights, in bf16, whose range holds them however far apart they are
@@ -130,7 +130,7 @@ template <int D, bool F8, int N, int PARTS>
 struct ColRings : ColShape<D, F8, N> {
   using B = ColShape<D, F8, N>;
   static constexpr int kPs = N <= 64 ? 2 : 1;              // P^T of that many tiles
-  static constexpr int kQParts = B::kPlain ? PARTS + 1 : 1;   // 8-bit numbers that make up a query's
+  static constexpr int kQParts = B::kPlain ? 3 : 1;        // 8-bit numbers that make up a query's
   static constexpr int kQ = B::kPlain ? kQParts * N * 128 : B::kCols * B::kColBytes * N / 128;
   static constexpr int kLeft = B::kRoom - kQ - kPs * PARTS * B::kP - 1024;
   static constexpr int kHalf = kLeft / (B::kKBuf + B::kBuf);
@@ -151,9 +151,9 @@ __host__ __device__ constexpr unsigned int col_mma_desc(bool half, int n, bool m
          ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 
-// The same of e4m3 numbers (K = 32), both K-major.
+// The same of e4m3 numbers by e5m2 numbers (K = 32), both K-major.
 __host__ __device__ constexpr unsigned int col_mma_desc8(int n) {
-  return (1u << 4) | ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
+  return (1u << 4) | (1u << 10) | ((unsigned int)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
 __device__ __forceinline__ void mma_smem8(unsigned int d, uint64_t a, uint64_t b, unsigned int idesc, unsigned int add,
                                           unsigned int leader) {
@@ -186,6 +186,15 @@ __device__ __forceinline__ bool group_any(int id, bool mine) {
   return any != 0;
 }
 __device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+
+// Two e5m2 numbers, and as halves again: those, without the lower byte.
+__device__ __forceinline__ uint32_t e5m2_pair(float a, float b) {
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E5M2);
+}
+__device__ __forceinline__ __half2 halves_of_e5m2(uint32_t pair) {
+  const uint32_t w = __byte_perm(pair, 0, 0x1404);
+  return *reinterpret_cast<const __half2*>(&w);
+}
 
 // The largest of those that are not NaN (max3 would give NaN).
 __device__ __forceinline__ float max3_numbers(float a, float b, float c) {
@@ -366,11 +375,14 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
               float down, up;
               power_scale(S::kPlain ? amax * (1.0f / 128.0f) : amax, down, up);
               if constexpr (S::kPlain) {
-                // The row's largest element into [128, 256), then all as the sum of e4m3 numbers: each takes
-                // four bits of what the ones before have left, two make a bf16 number, three an fp16 number.
-                // Elements below 2^-9 (2^-6) of the largest lose what is below 2^-17 of it.  (The power is that of
-                // amax / 128, which power_scale need not cut short however large amax is: 448 ends these bits.)
-                if (!(amax < INFINITY)) up = NAN;          // (these bits know no infinity)
+                // The row's largest element into [128, 256), then all as the sum of e5m2 numbers: each takes three
+                // bits of what the ones before have left, and its sign one more from the second on, so that three
+                // make an fp16 number (of its 11 bits the first leaves at most 128 units, the second 8, which the
+                // third has).  Their steps end at 2^-16: elements lose what is below 2^-24 of the largest, as where
+                // queries are fp16 (two e4m3 numbers, whose steps end at 2^-9, kept 2^-17).  The power is that of
+                // amax / 128, which power_scale need not cut short however large amax is; the smallest it does cut
+                // short, at 2^120, and bf16's steps of 2^-133 are multiples of 2^-16 then.
+                if (!(amax < INFINITY)) up = NAN;          // (saturated: these bits have no infinity)
                 float2 f[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -383,8 +395,8 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
                   uint32_t y[4];
 #pragma unroll
                   for (int e = 0; e < 4; ++e) {
-                    y[e] = e4m3_pair(f[e].x, f[e].y, false);
-                    const float2 g = __half22float2(halves_of_e4m3(y[e]));
+                    y[e] = e5m2_pair(f[e].x, f[e].y);
+                    const float2 g = __half22float2(halves_of_e5m2(y[e]));
                     f[e].x -= g.x;
                     f[e].y -= g.y;
                   }

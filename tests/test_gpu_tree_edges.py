@@ -86,3 +86,55 @@ def test_an_infinite_query_beside_scores_that_grow(D, pool, n, G):
     assert np.isfinite(got[fine]).all()
     assert (np.abs(got - want) <= tree_tolerance(s, pool, want, mag, slack))[fine].all()
     assert (np.abs(gl - wl) <= slack + 2.0 ** -14 + 2.0 ** -22 * np.abs(wl))[fine].all()
+
+
+# ------------------------------------------------------------------------------------------
+# over e4m3
+
+
+@pytest.mark.parametrize("new,G", [([3, 2], 2), ([12, 5], 2), ([20, 9], 3), ([40, 33], 4)])
+@pytest.mark.parametrize("io", ["bf16", "fp16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_queries_with_an_element_far_above_the_others(D, io, new, G):
+    """One element 2^15 times the others, where all keys are zero.  Elements of a query may lose what is below
+    2^-24 of its largest: a score is off by at most that times the sum of a key's magnitudes."""
+    rng = np.random.default_rng(D + len(new))
+    lens = [n + c for n, c in zip(new, (300, 77))]
+    s = shape_for(lens, H=2, D=D, T=16, pool="e4m3")
+    b = Batch(rng, s, new, lens)
+    pool, scales = make_pool(rng, s)
+    pool.view(torch.uint8).view(s.rows, D)[:, 5] = 0
+    sets = [ancestors(random_tree(rng, n)) for n in new]
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2 * G, D)))
+    q[..., 5] = 2.0 ** 15
+    q = q.to(DTYPE[io])
+    scale = 3 * D ** -0.5
+    got, gl = call(s, b, pool, scales, q, sets, scale)
+    values, qd = pool_values(s, pool, scales), q.double().numpy()
+    far = scale * 2.0 ** -24 * 2.0 ** 15 * np.abs(values).sum(-1).max()
+    qd[..., 5] = 0.0                              # (that product is zero: no part of any sum)
+    want, wl, mag, slack = dense(s, b, values, qd, scale, sets)
+    slack = slack + far
+    assert (np.abs(got - want) <= tree_tolerance(s, io, want, mag, slack)).all()
+    assert (np.abs(gl - wl) <= slack + 2.0 ** -14 + 2.0 ** -22 * np.abs(wl)).all()
+
+
+@pytest.mark.parametrize("new,G", [([3, 2], 2), ([12, 5], 2), ([20, 9], 3), ([40, 33], 4)])
+@pytest.mark.parametrize("e", [-118, -121, -124, -126])
+@pytest.mark.parametrize("D", [64, 128])
+def test_the_smallest_queries(D, e, new, G):
+    """bf16 queries about 2^e, subnormal ones among them, and a scale that makes ordinary scores of them: they lose
+    nothing that larger ones keep."""
+    rng = np.random.default_rng(D - e)
+    lens = [n + c for n, c in zip(new, (300, 77))]
+    s = shape_for(lens, H=2, D=D, T=16, pool="e4m3")
+    b = Batch(rng, s, new, lens)
+    pool, scales = make_pool(rng, s)
+    sets = [ancestors(random_tree(rng, n)) for n in new]
+    q = torch.from_numpy((rng.normal(size=(b.n_tokens, 2 * G, D)) * 2.0 ** e).astype(np.float32)).bfloat16()
+    assert int((q != 0).sum()) > 0.9 * q.numel()
+    scale = 2.0 ** (-e - 1)
+    got, gl = call(s, b, pool, scales, q, sets, scale)
+    want, wl, mag, slack = dense(s, b, pool_values(s, pool, scales), q.double().numpy(), scale, sets)
+    assert (np.abs(got - want) <= tree_tolerance(s, "bf16", want, mag, slack)).all()
+    assert (np.abs(gl - wl) <= slack + 2.0 ** -14 + 2.0 ** -22 * np.abs(wl)).all()
