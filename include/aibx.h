@@ -633,12 +633,12 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
  *   that it sees less one, at least 0) and the nodes whose bits are set in its row of d_mask - any rows,
  *   not only those of trees, and a node need not see itself.  Bits of nodes that the request has not are
  *   ignored.  params->causal is not read.  Everything else as aibx_attn_paged (formats, shapes, errors, the
- *   same bits every time), but: weights over an E4M3 pool may be held as bf16, or with FP16 queries as the
- *   sum of two bf16 numbers, and elements of a query may lose what is below 2^-24 of its largest (a query that
- *   is not finite then gives NaN); a NaN or infinite V of a node, or of a cached position that only some rows'
- *   windows reach, may reach a row that it is hidden from; the workspace is of
- *   aibx_attn_tree_workspace_bytes bytes, which depend on head_dim, num_q_heads / num_kv_heads, max_new, the
- *   types, whether R is 1 and the device alone.  INVALID for a null or unaligned d_mask or mask_words < 1,
+ *   same bits every time), but: weights over an E4M3 pool may be held as the sum of two bf16 numbers, and
+ *   elements of a query may lose what is below 2^-24 of its largest (a query that is not finite then gives
+ *   NaN); a NaN or infinite V of a node, or of a cached position that only some rows' windows reach, may reach
+ *   a row that it is hidden from; the workspace is of aibx_attn_tree_workspace_bytes bytes, which depend on
+ *   head_dim, num_q_heads / num_kv_heads, max_new, the types, whether R is 1 and the device alone.  INVALID
+ *   for a null or unaligned d_mask or mask_words < 1,
  *   UNSUPPORTED for more than 8 words, RANGE for a request with more than 64 * mask_words tokens (whose later
  *   nodes count as hidden).
  */

@@ -17,11 +17,12 @@
 //
 // Over an e4m3 pool K of D = 128 is multiplied as it lies, 8 bits by 8 bits: a query becomes the sum of three
 // e5m2 numbers, whose products with K add up in one accumulator (converting K instead, 28 rows:
-// 316 us, so 226).  K of D = 64, whose rows do not fill an operand's, two warpgroups turn into fp16 as it
+// 316 us where this took 226).  K of D = 64, whose rows do not fill an operand's, two warpgroups turn into fp16 as it
 // arrives, exact.  K's scales the thread that has the key applies to its scores.  V the same two turn into bf16,
 // exact too; its scales go with the weights, in bf16, whose range holds them however far apart they are
-// (scale bytes outside [kScaleLow, kScaleHigh] leave the rest with V).  fp16 queries get weights as the sum of two
-// bf16 numbers, so that they lose nothing to the type.
+// (scale bytes outside [kScaleLow, kScaleHigh] leave the rest with V).  Weights are the sum of two bf16 numbers: one
+// has 8 bits, where fp16, which the tile and row kernels have, has 11.  P^T holds the first and the second side by
+// side, as twice the rows; so does O^T, whose halves are added at the end.
 //
 // Roles: four softmax warpgroups (e4m3 and 32 rows: two), each with its part of the rows, which never wait
 // for each other; a warp for S^T and one for O^T; a loader of K and one of V; over e4m3 eight that convert and
@@ -33,8 +34,9 @@
 // cycles of the tensor pipe.  32 requests over 2k to 8k cached tokens of 8 heads: 123 us for 16 rows (5.4
 // TB/s), 136 for 64, 166 for 128 (4.1 TB/s, where the softmax takes as long as the bytes); 48 requests of 4
 // nodes 161 us (5.5 TB/s).  Without a segment's sums and outputs (a copy, for timing): 141 us for 128 rows.
-// e4m3: 1,370 cycles would be the share of HBM, a tile takes 2,600 (8 requests over 60k to 131k tokens, 28
-// rows: 230 us, 3.5 TB/s): the conversion of V (with half the warps for it 329 us).
+// e4m3: 1,370 cycles would be the share of HBM, a tile takes 2,900 (8 requests over 60k to 131k tokens, 28
+// rows: 260 us, 3.1 TB/s; 63 rows: 327): the conversion of V (with half the warps for it 329 us where this took
+// 230) and the weights' two numbers (with one, of 8 bits, 230 and 288 us).
 #pragma once
 
 #include "attn_tiles.cuh"
@@ -111,7 +113,8 @@ __device__ __forceinline__ void locate_even(const AttnArgs& a, unsigned int inde
 template <int D, bool F8, int N>
 struct ColShape {
   // Softmax warpgroups.  Over e4m3 two for 32 rows: with four the waits of twice the warps stand in the converters'
-  // way (28 rows: 237 instead of 226 us); for 64 rows four (63 rows: 286 us, with two 306; fp16 queries 340 and 411).
+  // way (28 rows: 281 instead of 273 us at D = 64, 256 instead of 259 at 128); for 64 rows four (with two, whose
+  // registers spill, 63 rows with weights of two numbers took 411 instead of 340 us; now 327).
   static constexpr int kGroups = F8 && N == 32 ? 2 : 4;
   static constexpr int kConverters = F8 ? 2 : 0;           // warpgroups that convert
   static constexpr int kThreads = 128 * (kGroups + 1 + kConverters);
@@ -122,22 +125,24 @@ struct ColShape {
   // K as it lies, if a row's 8-bit numbers fill the 128 bytes of an operand row
   static constexpr bool kPlain = F8 && D == 128;
   static constexpr int kKBuf = kPlain ? kRaw : kBuf;
-  static constexpr int kP = kTileKeys * 128 * ((N + 63) / 64);   // P^T: 64 rows in 128 bytes a key
+  static constexpr int kParts = F8 ? 2 : 1;                // 16-bit numbers that make up a weight
+  static constexpr int kPRows = kParts * N;                // rows of P^T and O^T
+  static constexpr int kP = kTileKeys * 128 * ((kPRows + 63) / 64);   // P^T: 64 rows in 128 bytes a key
   static constexpr int kRoom = 216 * 1024;
 };
-// P^T as one 16-bit number or the sum of two; what is left of shared memory goes to the rings.
-template <int D, bool F8, int N, int PARTS>
+// What is left of shared memory goes to the rings.
+template <int D, bool F8, int N>
 struct ColRings : ColShape<D, F8, N> {
   using B = ColShape<D, F8, N>;
   static constexpr int kPs = N <= 64 ? 2 : 1;              // P^T of that many tiles
   static constexpr int kQParts = B::kPlain ? 3 : 1;        // 8-bit numbers that make up a query's
   static constexpr int kQ = B::kPlain ? kQParts * N * 128 : B::kCols * B::kColBytes * N / 128;
-  static constexpr int kLeft = B::kRoom - kQ - kPs * PARTS * B::kP - 1024;
+  static constexpr int kLeft = B::kRoom - kQ - kPs * B::kP - 1024;
   static constexpr int kHalf = kLeft / (B::kKBuf + B::kBuf);
   static constexpr int kV = (kLeft - kHalf * B::kKBuf) / B::kBuf < 4 ? (kLeft - kHalf * B::kKBuf) / B::kBuf : 4;
   static constexpr int kK = (kLeft - kV * B::kBuf) / B::kKBuf < 4 ? (kLeft - kV * B::kBuf) / B::kKBuf : 4;
   static constexpr int kVAt = kK * B::kKBuf, kQAt = kVAt + kV * B::kBuf, kPAt = kQAt + kQ;
-  static constexpr int kSmem = kPAt + kPs * PARTS * B::kP + 1024;
+  static constexpr int kSmem = kPAt + kPs * B::kP + 1024;
   static constexpr int kSlot = N * (D + 2);                // floats per workspace slot
   // 16 bits: 4 * 104 + 64 = 5 * 96 (launch); e4m3: 2 * 136 + 64 + 2 * 72 = 5 * 96, or 4 * 72 + 64 + 2 * 72 < 7 * 72
   static constexpr int kRegsSoftmax = !F8 ? 104 : N == 32 ? 136 : 72;
@@ -215,12 +220,11 @@ constexpr int kColBatch = 4, kColInfo = 4;                 // scale bytes: tiles
 template <int D, bool F8, typename QT, int N>
 __global__ void __launch_bounds__(ColShape<D, F8, N>::kThreads, 1)
 attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a) {
-  constexpr int kParts = F8 && std::is_same<QT, __half>::value ? 2 : 1;
-  using S = ColRings<D, F8, N, kParts>;
+  using S = ColRings<D, F8, N>;
   using Blocks = EvenBlocks<N>;
   using KT = typename std::conditional<F8, __half, QT>::type;            // operands of S^T
   using VT = typename std::conditional<F8, __nv_bfloat16, QT>::type;     // and of O^T
-  constexpr int kMine = N / S::kGroups, kChunks = kMine / 8;   // rows of a softmax warpgroup, 8 at a time
+  constexpr int kParts = S::kParts, kMine = N / S::kGroups, kChunks = kMine / 8;   // rows of a softmax warpgroup, 8 at a time
   constexpr int kQK = 4 * S::kGroups, kPV = kQK + 2, kLoadV = kQK + 3;   // warps (kQK + 1 loads K)
   extern __shared__ unsigned char s_raw[];
   __shared__ __align__(8) unsigned long long s_k_full[S::kK], s_k_empty[S::kK], s_k_raw[S::kK];
@@ -546,13 +550,14 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
             }
             if (j > 0 && (D == 128 || (warp & 2) == 0)) {
 #pragma unroll 1
-              for (int ch = 0; ch < kChunks; ++ch) {
+              for (int x = 0; x < kParts * kChunks; ++x) {
+                const int c = c0 + x % kChunks * 8, at = x / kChunks * N + c;
                 uint32_t o[8];
-                tmem_ld8(tm_o + c0 + ch * 8, o);
+                tmem_ld8(tm_o + at, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * s_al[c0 + ch * 8 + i]);
-                tmem_st8(tm_o + c0 + ch * 8, o);
+                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * s_al[c + i]);
+                tmem_st8(tm_o + at, o);
               }
               tmem_wait_st();
             }
@@ -613,10 +618,10 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         if (j >= S::kPs) pv_wait(step - S::kPs);           // the product that had this place has read its weights
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-          unsigned char* s_p = base + S::kPAt + ((step % S::kPs) * kParts + part) * S::kP + tid * 128;
+          unsigned char* s_p = base + S::kPAt + (step % S::kPs) * S::kP + tid * 128;
 #pragma unroll
           for (int ch = 0; ch < kChunks; ++ch) {
-            const int c = c0 + ch * 8;
+            const int c = part * N + c0 + ch * 8;
             *reinterpret_cast<uint4*>(s_p + (c >> 6) * S::kColBytes + ((((c >> 3) & 7) ^ (tid & 7)) << 4)) =
                 make_uint4(pk[part][ch * 4], pk[part][ch * 4 + 1], pk[part][ch * 4 + 2], pk[part][ch * 4 + 3]);
           }
@@ -684,7 +689,15 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
         for (int ch = 0; ch < kChunks; ++ch) {
           uint32_t o[8];
           tmem_ld8(tm_o + c0 + ch * 8, o);
-          tmem_wait_ld();
+          if constexpr (kParts == 2) {
+            uint32_t more[8];
+            tmem_ld8(tm_o + N + c0 + ch * 8, more);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) + __uint_as_float(more[i]));
+          } else {
+            tmem_wait_ld();
+          }
           const int c = c0 + ch * 8, left = rows_end - c;
           if (whole) {
 #pragma unroll
@@ -762,7 +775,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
       const unsigned int v_low = uniform(operand_low(v0, S::kColBytes)), p_low = uniform(operand_low(smem0 + S::kPAt, S::kColBytes));
       while (walk.next_warp(a, per)) {
         const int steps = (int)uniform(walk.t1 - walk.t0);
-        constexpr unsigned int desc = col_mma_desc(std::is_same<VT, __half>::value, N, true);
+        constexpr unsigned int desc = col_mma_desc(std::is_same<VT, __half>::value, S::kPRows, true);
         const int key_first = (int)uniform((walk.span.tile0 + walk.t0) * kTileKeys);
         const int lo = (int)uniform(walk.span.lo), hi = (int)uniform(walk.span.hi);
         for (int j = 0; j < steps; ++j, ++step) {
@@ -791,11 +804,9 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
           tmem_after();
           const unsigned int low = v_low + buf * (S::kBuf >> 4);
 #pragma unroll
-          for (int part = 0; part < kParts; ++part)
-#pragma unroll
-            for (int k = 0; k < kTileKeys / 16; ++k)
-              mma_smem(tmu + 256, operand_desc(low + k * (2048 >> 4)), operand_desc(p_low + (((pb * kParts + part) * S::kP + k * 2048) >> 4)),
-                       desc, part > 0 || k > 0 || j > 0, leader);
+          for (int k = 0; k < kTileKeys / 16; ++k)
+            mma_smem(tmu + 256, operand_desc(low + k * (2048 >> 4)), operand_desc(p_low + ((pb * S::kP + k * 2048) >> 4)),
+                     desc, k > 0 || j > 0, leader);
           mma_commit(smem_u32(&s_pv_done[pb]), leader);
           mma_commit(smem_u32(&s_v_empty[buf]), leader);
           if (++buf == S::kV) {
@@ -1006,7 +1017,7 @@ attn_cols_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant_
 
 template <int D, bool F8, typename QT, int N>
 inline int32_t launch_attn_cols(AttnArgs a, int type, JoinSet& join, cudaStream_t st) {
-  using S = ColRings<D, F8, N, F8 && std::is_same<QT, __half>::value ? 2 : 1>;
+  using S = ColRings<D, F8, N>;
   a.box = gcd_int(a.pool.T, kTileKeys);
   a.box_log = log2_int(a.box);
   CUtensorMap map;

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from paged_ref import DTYPE, Batch, pool_values
+from paged_ref import DTYPE, Batch, pool_values, tolerance
 from paper_2504_03648_b200 import binding as aibx
 from steps_ref import ancestors, pack, random_tree, tree_tolerance
 from test_gpu_paged import dev, make_batch, make_cache, make_pool
@@ -138,3 +138,27 @@ def test_the_smallest_queries(D, e, new, G):
     want, wl, mag, slack = dense(s, b, pool_values(s, pool, scales), q.double().numpy(), scale, sets)
     assert (np.abs(got - want) <= tree_tolerance(s, "bf16", want, mag, slack)).all()
     assert (np.abs(gl - wl) <= slack + 2.0 ** -14 + 2.0 ** -22 * np.abs(wl)).all()
+
+
+@pytest.mark.parametrize("n,G", [(8, 1), (16, 1), (24, 2), (50, 1), (64, 2)])
+@pytest.mark.parametrize("io", ["bf16", "fp16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_weights_whose_values_cancel(D, io, n, G):
+    """Every node sees two, whose V are 1 and -1 and whose weights are nearly the same: what is left of their
+    difference shows how many bits the weights have.  11, as attn_paged's over the same pool."""
+    rng = np.random.default_rng(n + D)
+    new = [n] * 6
+    s = shape_for(new, H=2, D=D, T=16, pool="e4m3")
+    b = Batch(rng, s, new, new)
+    pool, scales = make_pool(rng, s)
+    at = np.array([[s.row(b.entry(s, r, j), 1, h, j % s.T) for j in range(n)] for r in range(6) for h in range(2)])
+    rows = pool.view(torch.uint8).view(s.rows, D)
+    rows[at[:, ::2].reshape(-1)] = 0x38           # 1
+    rows[at[:, 1::2].reshape(-1)] = 0xB8          # -1
+    scales[at] = 127
+    sets = [[{2 * int(rng.integers(0, n // 2)), 2 * int(rng.integers(0, n // 2)) + 1} for _ in range(n)] for _ in range(6)]
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2 * G, D))).to(DTYPE[io])
+    scale = 0.2 * D ** -0.5
+    got, _ = call(s, b, pool, scales, q, sets, scale)
+    want, _, mag, slack = dense(s, b, pool_values(s, pool, scales), q.double().numpy(), scale, sets)
+    assert (np.abs(got - want) <= tolerance(s, io, want, mag, slack)).all()
