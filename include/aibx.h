@@ -724,9 +724,10 @@ int32_t aibx_rope_append(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* ba
  *   d_slots        int64 [n_tokens], nullable: block id * T + position mod T; -1 where there is no block
  * A request that wants more blocks than are left gets AIBX_NO_BLOCK for the rest: FULL, detail = such
  * blocks of all requests.  RANGE at least once for a request with a negative length, or more than 2^31 - 1
- * tokens (it counts as n = 0), for one with more blocks than its row has entries (they are left out, and
- * take no ids) or fewer matched ids than `had` (AIBX_NO_BLOCK), for an id >= num_blocks under a new
- * token, and where there are more than n_tokens tokens (whose d_pos and d_slots are left out).
+ * tokens (it counts as n = 0), for one, with new tokens or without, with more blocks than its row has entries
+ * (they are left out, and take no ids) or fewer matched ids than `had` (AIBX_NO_BLOCK), for an id >=
+ * num_blocks other than AIBX_NO_BLOCK under a new token, and where there are more than n_tokens tokens (whose
+ * d_pos and d_slots are left out).
  * Where h is no multiple of T, the new tokens go on in the block of position h - 1: that no other request
  * reads that block, too, is the caller's to see to.
  * d_kv_len may be d_held and d_free_head_out may be d_free_head (a call captured once, replayed step

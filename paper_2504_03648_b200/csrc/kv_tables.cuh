@@ -180,7 +180,7 @@ kv_tables_kernel(const __grid_constant__ TablesArgs a) {
       s_had[tid] = q.had;
       s_width[tid] = (int)width;
       if (blockIdx.x == (unsigned int)(r0 / N) % gridDim.x && r < a.R) {
-        if (q.bad || (q.n > 0 && q.need > width)) raise_status(AIBX_ERR_RANGE);
+        if (q.bad || q.need > width) raise_status(AIBX_ERR_RANGE);   // (without new tokens, too)
         a.tok_off[r] = tok_base + before_tok;
       }
     }
