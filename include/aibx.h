@@ -667,15 +667,16 @@ int32_t aibx_attn_tree(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* batc
  *
  * rope: x -> y, [n_tokens][num_heads][head_dim] of `type` (BF16, FP16, FP32), element strides per token
  *   and per head, elements of a row adjacent.  y may be x with the same strides; they must not overlap in
- *   any other way.
+ *   any other way, nor may rows of y among themselves (rows of x may: a stride of 0).
  * rope_append: aibx_kv_append of turned K and plain V, and queries turned beside them, in one launch.
  *   Positions of the rotation: d_pos, or where it is null those of the batch (kv_len - n_r + i); slots are
  *   always the batch's.  Queries: num_q_heads may be 0; d_q_out may be d_q with the same strides.  Query
  *   rows of every token of a request are written, rows behind the last request left as they are.  E4M3
  *   rows take their scale from the turned K in 32 bits, before it is rounded.
  * Errors: as aibx_kv_append; INVALID for a rotary_dim that is odd, not positive or above head_dim, an
- *   unknown style, null or unaligned pointers, in place with other strides; UNSUPPORTED for a rotary_dim
- *   that is no multiple of 16, head_dim above 512 or no multiple of 8, more than 65,536 heads.
+ *   unknown style, null or unaligned pointers, in place with other strides, turned rows that would lie upon
+ *   one another; UNSUPPORTED for a rotary_dim that is no multiple of 16, head_dim above 512 or no multiple of
+ *   8, more than 65,536 heads.
  */
 #define AIBX_ROPE_HALF        0
 #define AIBX_ROPE_INTERLEAVED 1

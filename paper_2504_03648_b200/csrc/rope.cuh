@@ -293,6 +293,21 @@ inline void rope_io(const aibx_rope_t* rope, int head_dim, RopeIO& io) {
   io.D = head_dim;
 }
 
+// Whether rows of D elements at t * tok + h * head, t < n and h < heads, lie upon one another.  Rows that follow one
+// another and lists of them that do not touch are told at once; else, for a step in h, the nearest two in t.
+inline bool rows_overlap(long long n, long long tok, long long heads, long long head, long long D) {
+  if ((n > 1 && tok < D) || (heads > 1 && head < D)) return true;
+  if (n <= 1 || heads <= 1) return false;
+  if ((tok - D) / head >= heads - 1 || (head - D) / tok >= n - 1) return false;
+  for (long long h = 1; h < heads; ++h) {
+    const __int128 at = (__int128)h * head;
+    const __int128 t = at / tok;
+    if (t >= n) return false;                              // (all further ones are beyond, too)
+    if (at - t * tok < D || (t + 1 < n && (t + 1) * tok - at < D)) return true;
+  }
+  return false;
+}
+
 // Pointers and strides of the caller's rows: whether they are usable at all, and in 16-byte pieces.
 struct RopeRows {
   uintptr_t bits = 0;
@@ -317,7 +332,7 @@ inline int32_t rope_rows(const aibx_rope_t* rope, int64_t n, int32_t heads, int3
   RopeRows rows;
   rows.add(x, x_tok, x_head, type_bytes(type));
   rows.add(y, y_tok, y_head, type_bytes(type));
-  if (!rows.good) return AIBX_ERR_INVALID;
+  if (!rows.good || rows_overlap(n, y_tok, heads, y_head, head_dim)) return AIBX_ERR_INVALID;
   // in place means each row onto itself
   if (x == y && ((n > 1 && x_tok != y_tok) || (heads > 1 && x_head != y_head))) return AIBX_ERR_INVALID;
   RopeIO io = {};
@@ -352,6 +367,8 @@ inline int32_t rope_append(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b, c
   if (r->num_q_heads > 0) {
     rows.add(r->d_q, r->q_token_stride, r->q_head_stride, size);
     rows.add(r->d_q_out, r->q_out_token_stride, r->q_out_head_stride, size);
+    if (rows.good && rows_overlap(b->n_tokens, r->q_out_token_stride, r->num_q_heads, r->q_out_head_stride, pool.D))
+      return AIBX_ERR_INVALID;
     if (r->d_q == r->d_q_out && ((b->n_tokens > 1 && r->q_token_stride != r->q_out_token_stride) ||
                                  (r->num_q_heads > 1 && r->q_head_stride != r->q_out_head_stride)))
       return AIBX_ERR_INVALID;
