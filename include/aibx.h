@@ -631,8 +631,9 @@ int32_t aibx_attn_paged(const aibx_kv_cache_t* cache, const aibx_kv_batch_t* bat
  * attn_tree: aibx_attn_paged with these masks in the place of causality.  Node i sees the cached
  *   positions j < base (window > 0: those with j > base + depth - window, depth = the number of nodes
  *   that it sees less one, at least 0) and the nodes whose bits are set in its row of d_mask - any rows,
- *   not only those of trees, and a node need not see itself.  Bits of nodes that the request has not are
- *   ignored.  params->causal is not read.  Everything else as aibx_attn_paged (formats, shapes, errors, the
+ *   not only those of trees, and a node need not see itself.  The window hides cached positions alone: a chain
+ *   of more nodes than the window sees more than aibx_attn_paged would show it; with the bits of ancestors
+ *   `window` and more nodes up cleared it sees the same.  Bits of nodes that the request has not are ignored.  params->causal is not read.  Everything else as aibx_attn_paged (formats, shapes, errors, the
  *   same bits every time), but: weights over an E4M3 pool may be held as the sum of two bf16 numbers, and
  *   elements of a query may lose what is below 2^-24 of its largest (a query that is not finite then gives
  *   NaN); a NaN or infinite V of a node, or of a cached position that only some rows' windows reach, may reach

@@ -679,7 +679,8 @@ def tree_masks(parent, tok_off, kv_len, mask, pos=None) -> None:
 def attn_tree(cache: KVCache, batch: KVBatch, mask, q, out, lse=None, scale=None, window: int = 0,
               workspace=None) -> None:
     """attn_paged of drafted tokens that see their request's cached tokens and the drafted ones that
-    mask (uint64 [n_tokens, words], as tree_masks makes it) names."""
+    mask (uint64 [n_tokens, words], as tree_masks makes it) names.  The window hides cached tokens alone: with
+    the bits of ancestors `window` and more nodes up cleared, a chain sees what attn_paged would show it."""
     if mask.dim() != 2:
         raise ValueError("a mask of [n_tokens, words] expected")
     tree = _vector(mask, "mask", torch.uint64, batch.n_tokens * mask.shape[1], cache.device), mask.shape[1]
@@ -709,7 +710,9 @@ def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "non
     "linear": every frequency over scale;
     "base":   base * scale^(rotary_dim / (rotary_dim - 2)), which stretches the slowest pair alone by scale;
     "parts":  pairs of at most `slow` turns over the `trained` positions over scale, pairs of `fast` turns
-              or more as they are, a straight line between; factor 0.1 ln(scale) + 1."""
+              or more as they are, between them a straight line in the number of turns (a line in the
+              pair's index, which some programs draw, gives other frequencies there); factor
+              0.1 ln(scale) + 1."""
     if rotary_dim <= 0 or rotary_dim % 2 or base <= 0 or scale <= 0:
         raise ValueError("an even positive rotary_dim, base and scale above 0 expected")
     half = rotary_dim // 2
@@ -734,7 +737,7 @@ def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "non
 
 def rope(rope: Rope, pos, x, y) -> None:
     """Rows of x ([n_tokens, heads, head_dim], elements adjacent, other strides free) turned by their
-    positions (int32 [n_tokens]) into y; y may be x."""
+    positions (int32 [n_tokens]) into y; y may be x, and is no tensor expanded over tokens or heads."""
     if x.dtype != y.dtype or x.dtype not in _TYPE_OF or x.dim() != 3 or x.shape != y.shape:
         raise ValueError("x and y of one type and [n_tokens, heads, head_dim] expected")
     device = _current(x)

@@ -145,6 +145,7 @@ struct ColRings : ColShape<D, F8, N> {
   static constexpr int kSmem = kPAt + kPs * B::kP + 1024;
   static constexpr int kSlot = N * (D + 2);                // floats per workspace slot
   // 16 bits: 4 * 104 + 64 = 5 * 96 (launch); e4m3: 2 * 136 + 64 + 2 * 72 = 5 * 96, or 4 * 72 + 64 + 2 * 72 < 7 * 72
+  // (64 rows of e4m3 spill 8 bytes of the 72 registers)
   static constexpr int kRegsSoftmax = !F8 ? 104 : N == 32 ? 136 : 72;
   static constexpr int kRegsOther = 64, kRegsConvert = 72;
   static_assert(kK >= 2 && kV >= 2, "two tiles of each at least");

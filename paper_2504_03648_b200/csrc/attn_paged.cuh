@@ -31,7 +31,8 @@ inline uint64_t slot_bytes(int rows, int dim) {
 // the column kernel takes 123: twice the products, and registers spill).  The column kernel for requests of up to
 // 128 rows, in blocks of 32 or 64 where none has more (fewer registers, less shared memory); over e4m3, where a
 // block of 128 leaves its warps too few registers, up to 64.  The tile kernel for more: there a step costs
-// less per row (bf16, 256 rows: 236 us against 291 of two blocks; e4m3, 112 rows: 532 against 569 of two).
+// less per row (bf16, 256 rows: 236 us against 291 of two blocks; e4m3, 112 rows: 532 against 569 of two,
+// whose weights had 8 bits then).
 inline int32_t attn_plan(const aibx_kv_cache_t* c, const aibx_kv_batch_t* b,
                          const aibx_attn_params_t* p, bool tree, AttnPlan& plan) {
   PagedPool pool;

@@ -13,7 +13,11 @@
 // belong to each other, so that a pair never leaves its lane.
 // Bound: HBM for long inputs, each row being read once and written once (40,001 tokens of 32 fp16 heads: 109
 // us, 6.0 TB/s; 26,600 tokens of 28 heads of queries and 4 of K and V into an e4m3 pool: 97 us, 4.8 TB/s, where
-// the quantisation's instructions show), the chain of dependent loads for few tokens (64 tokens: 6 us).
+// the quantisation's instructions show; into a bf16 pool 92 us, 5.3 TB/s; fp32 rows 5.4 to 5.9 TB/s), the chain of
+// dependent loads for few tokens (64 tokens: 6 us).
+// 80 registers, for three CTAs an SM, are not enough for the pool's part beside two rows in flight: every rope_append
+// keeps a stack (16-bit rows 32 to 52 bytes stored and 16 to 40 loaded per thread, fp32 rows 92 to 140 and 116 to
+// 128), and so does fp32 rope alone (20 to 36 and 24 to 40); 16-bit rope keeps none.
 #pragma once
 
 #include "kv_paged.cuh"

@@ -6,7 +6,7 @@ import torch
 
 from paged_ref import DTYPE, Batch, pool_values, tolerance
 from paper_2504_03648_b200 import binding as aibx
-from steps_ref import ancestors, pack, random_tree, tree_tolerance
+from steps_ref import ancestors, pack, random_tree, tree_attention, tree_tolerance
 from test_gpu_paged import dev, make_batch, make_cache, make_pool
 from test_gpu_tree import shape_for
 
@@ -86,6 +86,28 @@ def test_an_infinite_query_beside_scores_that_grow(D, pool, n, G):
     assert np.isfinite(got[fine]).all()
     assert (np.abs(got - want) <= tree_tolerance(s, pool, want, mag, slack))[fine].all()
     assert (np.abs(gl - wl) <= slack + 2.0 ** -14 + 2.0 ** -22 * np.abs(wl))[fine].all()
+
+
+@pytest.mark.parametrize("window", [1, 5, 30])
+@pytest.mark.parametrize("G", [1, 4, 8])
+def test_a_chain_longer_than_the_window(G, window):
+    """With the bits of ancestors `window` and more nodes up cleared it is attn_paged with that window, to the
+    roundings of two orders of sums."""
+    new = [20, 4, 33]
+    lens = [n + c for n, c in zip(new, (200, 0, 131))]
+    s = shape_for(lens, H=2, D=128, T=16)
+    rng = np.random.default_rng(G + window)
+    b = Batch(rng, s, new, lens)
+    pool, _ = make_pool(rng, s)
+    sets = [[set(range(max(0, i - window + 1), i + 1)) for i in range(n)] for n in new]
+    q = torch.from_numpy(rng.normal(size=(b.n_tokens, 2 * G, 128))).bfloat16().cuda()
+    cache, batch = make_cache(s, pool, None), make_batch(b)
+    x, y = torch.empty_like(q), torch.empty_like(q)
+    aibx.attn_paged(cache, batch, q, x, window=window)
+    aibx.attn_tree(cache, batch, dev(np.concatenate([pack(t, 1) for t in sets])), q, y, window=window)
+    _, _, mag, slack = tree_attention(s, b, pool_values(s, pool, None), q.double().cpu().numpy(), 128 ** -0.5, sets, window)
+    x, y = x.double().cpu().numpy(), y.double().cpu().numpy()
+    assert (np.abs(x - y) <= 2 * tree_tolerance(s, "bf16", x, mag, slack)).all()
 
 
 # ------------------------------------------------------------------------------------------
